@@ -11,8 +11,9 @@
  * activations (Alg. 1 forward) and the nearest-subset-member projection (Eq. 2 / Eq. 5).
  * Around these: the convolution ending in the next layer's sign (1-bit activations from layer to
  * layer), the training-side lines of Alg. 1 (Eq. 3, Eq. 4, the gradient of the subset), the
- * tau-bit index storage of Sec. 4.4, the extension to 1x1 layers (appendix) and, as a yardstick, the
- * same layers as dense contractions on the matrix cores.
+ * tau-bit index storage of Sec. 4.4, the extension to 1x1 layers (appendix), the
+ * same with 16-bit activations (projections over tokens: by expert, beside low-rank adapters, with their gradients)
+ * and, as a yardstick, the 1-bit layers as dense contractions on the matrix cores.
  *
  * General rules for every entry point
  *   - Every data pointer is a DEVICE pointer owned by the caller (hipMalloc / a torch CUDA
@@ -522,6 +523,129 @@ int snn_dense_conv2d_prepared(const snn_conv_desc *desc, const void *x, const fl
 int snn_dense_conv2d_sign_prepared(const snn_conv_desc *desc, const void *x, const float *alpha,
                                    const float *beta, void *out_packed, void *workspace,
                                    size_t ws_bytes, void *stream);
+
+/* ---- projections of real-valued activations ------------------------------------------------------------------
+ *
+ * The 1x1 layer of the appendix with 16-bit activations instead of their signs (W/A = x/16), as the projections of a
+ * network over tokens use it: rows of channels in, rows of channels out,
+ *   y[t][o] = alpha[o] * sum_i W[o][i] x[t][i],   W[o][8 v + j] = element j of member idx[o][v] of the subset of {+-1}^8.
+ * One call takes several such matrices ("groups": the experts of a layer): row t belongs to the group g with
+ * offsets[g] <= t < offsets[g + 1], and is multiplied by that group's weights.  Products are exact and sums are held in fp32;
+ * the sum times alpha (with the adapter's share, below) is rounded once.
+ *
+ * Rules beside the general ones
+ *   - desc->dtype (SNN_DTYPE_*) is the type of activations, gradients of activations, alpha and adapters.
+ *   - Rows lie `ld` elements apart (ld >= the row's channels, a multiple of 8, at most 2^20); the base address is a
+ *     multiple of 16.  Channels are contiguous.  1 <= rows < 2^28; rows = 0 is allowed, and then only gradients of weights
+ *     and adapters are written (zeros).  Outputs must not overlap inputs or each other.
+ *   - offsets: device, int32 [groups + 1], non-decreasing.  A group may have no rows.  Values are read as clamped to
+ *     0 .. rows; rows before offsets[0] and from offsets[groups] on belong to no group: their outputs are not written.
+ *     NULL is allowed for groups = 1: all rows.
+ *   - A row's infinities and NaN, or those of an adapter, reach no other row and no other group's or adapter's gradient.
+ *     Sums are formed in a fixed order: a call repeated gives the same bits.
+ */
+#define SNN_DTYPE_BF16 0
+#define SNN_DTYPE_F16  1
+
+typedef struct snn_linear_desc {
+    int32_t groups;  /* weight matrices, 1 .. 1024                                     */
+    int32_t C_in;    /* input channels,  a multiple of 8, 8 .. 65536                   */
+    int32_t C_out;   /* output channels, a multiple of 8, 8 .. 65536                   */
+    int32_t K;       /* subset size 1 .. 256 (each group has a subset of its own)      */
+    int32_t dtype;   /* SNN_DTYPE_*                                                    */
+} snn_linear_desc;
+
+/*
+ * The weights as the calls below read them: one bit per weight for the outputs, one for the gradient of the inputs
+ * (laid out along the other axis), and alpha.
+ *   codebook8  device, uint16 [groups][K], 8-bit codes, element j at bit 7 - j, +1 -> 1 (a code is masked to 8 bits)
+ *   idx        device, uint16 [groups][C_out][C_in / 8] (a value >= K is read as K - 1)
+ *   alpha      device, [groups][C_out] of desc->dtype, 16-byte aligned
+ *   weights    device, >= snn_linear_weights_bytes(desc) bytes, 256-byte aligned; fully overwritten, and then read by any number of calls
+ * snn_linear_weights_bytes is host-only; 0 for an invalid desc.
+ * Errors: INVALID_ARG; WORKSPACE (weights null, misaligned or too small); LAUNCH.
+ */
+size_t snn_linear_weights_bytes(const snn_linear_desc *desc);
+int snn_linear_prepare(const snn_linear_desc *desc, const uint16_t *codebook8, const uint16_t *idx, const void *alpha,
+                       void *weights, size_t weights_bytes, void *stream);
+
+/*
+ * Outputs, and the gradient of the inputs  dx[t][i] = sum_o alpha[o] dy[t][o] W[o][i].
+ *   x, dx   device, rows of C_in;   y, dy   device, rows of C_out
+ *   weights device, as snn_linear_prepare left it
+ * Errors: INVALID_ARG; WORKSPACE (weights); LAUNCH.
+ */
+int snn_linear_forward(const snn_linear_desc *desc, const void *x, int64_t ldx, int64_t rows, const int32_t *offsets,
+                       const void *weights, size_t weights_bytes, void *y, int64_t ldy, void *stream);
+int snn_linear_input_grad(const snn_linear_desc *desc, const void *dy, int64_t lddy, int64_t rows, const int32_t *offsets,
+                          const void *weights, size_t weights_bytes, void *dx, int64_t lddx, void *stream);
+
+/*
+ * Activations kept in 8 bits for the backward pass.  The 32 consecutive channels of a chunk (the row's last may be shorter) share
+ * a power of two u, the one that makes the largest finite magnitude of the chunk 64 u <= m < 128 u (not below 2^-126):
+ *   q = x / u rounded to nearest (ties to even), limited to -127 .. 127;   kept value  q u  (|q u - x| <= u / 2, or <= u where limited)
+ * Every kept value is a value of the activations' type, so that products with it are exact.  What is not finite gets q = -128, which
+ * stands for NaN.
+ *   x   device, rows of C (a multiple of 8, 8 .. 65536) in the type `dtype`
+ *   q   device, int8 [rows][C], 16-byte aligned;   e   device, uint8 [rows][ceil(C / 32)]: u = 2^(e - 127), 1 <= e
+ * snn_checkpoint_restore writes the kept values.
+ * Errors: INVALID_ARG; LAUNCH.
+ */
+int snn_checkpoint_store(const void *x, int64_t ldx, int64_t rows, int C, int dtype, int8_t *q, uint8_t *e, void *stream);
+int snn_checkpoint_restore(const int8_t *q, const uint8_t *e, int64_t rows, int C, int dtype, void *x, int64_t ldx, void *stream);
+
+/*
+ * Gradients of the weights, with  G[o][i] = sum over the group's rows of dy[t][o] x[t][i]:
+ *   dw[g][o][i] = alpha[o] G[o][i]             the gradient of the +-1 weights (what Eq. 3 and the subset's gradient start from)
+ *   dalpha[g][o] = sum_i W[o][i] G[o][i]       the gradient of the scales
+ * The second form reads the inputs from their 8-bit form (x's kept values).
+ *   dw       device, float [groups][C_out][C_in], 16-byte aligned, fully overwritten (zeros for a group without rows)
+ *   dalpha   device, float [groups][C_out], fully overwritten; NULL: not wanted
+ *   workspace  device, >= snn_linear_weight_grad_workspace_bytes(desc, rows) bytes, 256-byte aligned
+ * Errors: INVALID_ARG; WORKSPACE (weights, workspace); LAUNCH.
+ */
+size_t snn_linear_weight_grad_workspace_bytes(const snn_linear_desc *desc, int64_t rows);
+int snn_linear_weight_grad(const snn_linear_desc *desc, const void *x, int64_t ldx, const void *dy, int64_t lddy, int64_t rows,
+                           const int32_t *offsets, const void *weights, size_t weights_bytes, float *dw, float *dalpha,
+                           void *workspace, size_t ws_bytes, void *stream);
+int snn_linear_weight_grad_checkpoint(const snn_linear_desc *desc, const int8_t *q, const uint8_t *e, const void *dy, int64_t lddy,
+                                      int64_t rows, const int32_t *offsets, const void *weights, size_t weights_bytes, float *dw,
+                                      float *dalpha, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * One projection shared by the requests of a batch, each with a low-rank adapter of its own beside it (groups = 1, else UNSUPPORTED):
+ *   y[t] = alpha * (W x[t]) + scale[a] * B[a] (A[a] x[t]),   a = adapter[t];  without the second term where a is outside 0 .. n - 1
+ *   adapter  device, int32 [rows], in any order (rows of one adapter next to each other are faster in the large calls)
+ *   A        device, [n][rank][C_in];   B   device, [n][C_out][rank];   both desc->dtype, 16-byte aligned
+ *   scale    device, float [n]
+ *   low      device, float [rows][rank], A[a] x[t] in fp32 (zeros without an adapter): what the backward call takes; NULL: not wanted
+ *   workspace  device, >= snn_adapters_workspace_bytes(desc, adapters, rows) bytes, 256-byte aligned
+ * scale[a] A[a] x[t] is held in two values of desc->dtype (twice its mantissa) in the product with B[a]: for f16 it has to be in that type's range.
+ *
+ * The backward call, with  dlow[t] = scale[a] * B[a]^T dy[t]:
+ *   dx[t] = W^T (alpha * dy[t]) + A[a]^T dlow[t];   dA[a] = sum of dlow[t] x[t]^T;   dB[a] = scale[a] * sum of dy[t] low[t]^T
+ *   dA, dB   device, as A and B, 16-byte aligned, fully overwritten (zeros for an adapter without rows); sums in fp32, rounded once
+ * The second form reads the inputs from their 8-bit form.  dlow and low are held in two values of desc->dtype in the products, as above.
+ * Errors: INVALID_ARG (n outside 1 .. 65536, rank not a multiple of 8 in 8 .. 128); UNSUPPORTED (groups != 1); WORKSPACE; LAUNCH.
+ */
+typedef struct snn_adapters {
+    int32_t n;          /* adapters                       */
+    int32_t rank;       /* a multiple of 8, 8 .. 128      */
+    const void *A, *B;
+    const float *scale;
+} snn_adapters;
+size_t snn_adapters_workspace_bytes(const snn_linear_desc *desc, const snn_adapters *adapters, int64_t rows);
+int snn_adapters_forward(const snn_linear_desc *desc, const snn_adapters *adapters, const void *x, int64_t ldx, int64_t rows,
+                         const int32_t *adapter, const void *weights, size_t weights_bytes, void *y, int64_t ldy, float *low,
+                         void *workspace, size_t ws_bytes, void *stream);
+int snn_adapters_backward(const snn_linear_desc *desc, const snn_adapters *adapters, const void *x, int64_t ldx, const float *low,
+                          const void *dy, int64_t lddy, int64_t rows, const int32_t *adapter, const void *weights,
+                          size_t weights_bytes, void *dx, int64_t lddx, void *dA, void *dB, void *workspace, size_t ws_bytes,
+                          void *stream);
+int snn_adapters_backward_checkpoint(const snn_linear_desc *desc, const snn_adapters *adapters, const int8_t *q, const uint8_t *e,
+                                     const float *low, const void *dy, int64_t lddy, int64_t rows, const int32_t *adapter,
+                                     const void *weights, size_t weights_bytes, void *dx, int64_t lddx, void *dA, void *dB,
+                                     void *workspace, size_t ws_bytes, void *stream);
 
 /* Bytes of workspace the given entry point (SNN_WS_*) needs for this layer; 0 if desc is
  * invalid or the combination is unsupported.  Host-only, no device work. */

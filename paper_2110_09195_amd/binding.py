@@ -24,6 +24,9 @@ SNN_ACT_BIN_ROWS = 0
 SNN_ACT_BIN_CHANNELS = 1
 SNN_ACT_F32 = 2
 
+SNN_DTYPE_BF16 = 0
+SNN_DTYPE_F16 = 1
+
 SNN_WS_SUBBIT = 0
 SNN_WS_BNN = 1
 SNN_WS_FORWARD = 2
@@ -40,6 +43,10 @@ EXPORTS = ("snn_pack_activations", "snn_pack_activations_many", "snn_project_ker
            "snn_project_backward_workspace_bytes", "snn_subset_update", "snn_bnn_conv2d", "snn_bnn_prepare", "snn_bnn_conv2d_prepared", "snn_bnn_conv2d_dense",
            "snn_subbit_conv2d_dense", "snn_dense_prepare", "snn_dense_conv2d_prepared",
            "snn_dense_conv2d_sign_prepared",
+           "snn_linear_weights_bytes", "snn_linear_prepare", "snn_linear_forward", "snn_linear_input_grad",
+           "snn_linear_weight_grad_workspace_bytes", "snn_linear_weight_grad", "snn_linear_weight_grad_checkpoint",
+           "snn_checkpoint_store", "snn_checkpoint_restore",
+           "snn_adapters_workspace_bytes", "snn_adapters_forward", "snn_adapters_backward", "snn_adapters_backward_checkpoint",
            "snn_workspace_bytes", "snn_packed_bytes", "snn_status_string", "snn_subbit_slots_per_channel",
            "snn_set_tuning", "snn_get_tuning")
 
@@ -70,6 +77,16 @@ class snn_layer_forward(ctypes.Structure):
     _fields_ = [("desc", snn_conv_desc), ("x_nchw", ctypes.c_void_p), ("w", ctypes.c_void_p), ("codebook", ctypes.c_void_p),
                 ("alpha", ctypes.c_void_p), ("idx_out", ctypes.c_void_p), ("y_nchw", ctypes.c_void_p),
                 ("workspace", ctypes.c_void_p), ("ws_bytes", ctypes.c_size_t)]
+
+
+class snn_linear_desc(ctypes.Structure):
+    _fields_ = [("groups", ctypes.c_int32), ("C_in", ctypes.c_int32), ("C_out", ctypes.c_int32), ("K", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class snn_adapters(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("rank", ctypes.c_int32), ("A", ctypes.c_void_p), ("B", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p)]
 
 
 class SnnError(RuntimeError):
@@ -171,6 +188,33 @@ def lib():
         L.snn_dense_conv2d_prepared.restype = i32
         L.snn_project_vectors8.argtypes = [vp, ctypes.c_int64, vp, ctypes.c_int, vp, vp]
         L.snn_project_vectors8.restype = i32
+        lp, ap = ctypes.POINTER(snn_linear_desc), ctypes.POINTER(snn_adapters)
+        L.snn_linear_weights_bytes.argtypes = [lp]
+        L.snn_linear_weights_bytes.restype = sz
+        L.snn_linear_prepare.argtypes = [lp, vp, vp, vp, vp, sz, vp]
+        L.snn_linear_prepare.restype = i32
+        L.snn_linear_forward.argtypes = [lp, vp, i64, i64, vp, vp, sz, vp, i64, vp]
+        L.snn_linear_forward.restype = i32
+        L.snn_linear_input_grad.argtypes = [lp, vp, i64, i64, vp, vp, sz, vp, i64, vp]
+        L.snn_linear_input_grad.restype = i32
+        L.snn_linear_weight_grad_workspace_bytes.argtypes = [lp, i64]
+        L.snn_linear_weight_grad_workspace_bytes.restype = sz
+        L.snn_linear_weight_grad.argtypes = [lp, vp, i64, vp, i64, i64, vp, vp, sz, vp, vp, vp, sz, vp]
+        L.snn_linear_weight_grad.restype = i32
+        L.snn_linear_weight_grad_checkpoint.argtypes = [lp, vp, vp, vp, i64, i64, vp, vp, sz, vp, vp, vp, sz, vp]
+        L.snn_linear_weight_grad_checkpoint.restype = i32
+        L.snn_checkpoint_store.argtypes = [vp, i64, i64, i32, i32, vp, vp, vp]
+        L.snn_checkpoint_store.restype = i32
+        L.snn_checkpoint_restore.argtypes = [vp, vp, i64, i32, i32, vp, i64, vp]
+        L.snn_checkpoint_restore.restype = i32
+        L.snn_adapters_workspace_bytes.argtypes = [lp, ap, i64]
+        L.snn_adapters_workspace_bytes.restype = sz
+        L.snn_adapters_forward.argtypes = [lp, ap, vp, i64, i64, vp, vp, sz, vp, i64, vp, vp, sz, vp]
+        L.snn_adapters_forward.restype = i32
+        L.snn_adapters_backward.argtypes = [lp, ap, vp, i64, vp, vp, i64, i64, vp, vp, sz, vp, i64, vp, vp, vp, sz, vp]
+        L.snn_adapters_backward.restype = i32
+        L.snn_adapters_backward_checkpoint.argtypes = [lp, ap, vp, vp, vp, vp, i64, i64, vp, vp, sz, vp, i64, vp, vp, vp, sz, vp]
+        L.snn_adapters_backward_checkpoint.restype = i32
         L.snn_dense_conv2d_sign_prepared.argtypes = [dp, vp, vp, vp, vp, vp, sz, vp]
         L.snn_dense_conv2d_sign_prepared.restype = i32
         L.snn_workspace_bytes.argtypes = [dp, i32]
@@ -748,3 +792,224 @@ def snn_project_vectors8(w, codebook8, out=None):
     _check(lib().snn_project_vectors8(_ptr(w), n, _ptr(codebook8), int(codebook8.numel()), _ptr(out), _stream()),
            "snn_project_vectors8")
     return out
+
+
+# ---- projections of real-valued activations --------------------------------------------------------------------
+
+_LINEAR_DTYPE = (torch.bfloat16, torch.float16)
+
+
+def make_linear_desc(groups, C_in, C_out, K, dtype=SNN_DTYPE_BF16):
+    return snn_linear_desc(groups, C_in, C_out, K, dtype)
+
+
+def _dtype_of(desc):
+    if not 0 <= desc.dtype < len(_LINEAR_DTYPE):
+        raise ValueError("desc.dtype is not one of SNN_DTYPE_*")
+    return _LINEAR_DTYPE[desc.dtype]
+
+
+def _rows(t, dtype, C, name):
+    """Rows of C channels on the GPU, each contiguous, any distance apart -> (pointer, distance)."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape[1] == C and t.stride(1) == 1):
+        raise TypeError("%s must be a CUDA tensor of %s, [rows][%d] with contiguous rows" % (name, dtype, C))
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(C, t.stride(0))
+
+
+def _rows_out(t, rows, C, like, name):
+    if t is None:
+        t = torch.empty((rows, C), dtype=like.dtype, device=like.device)
+    elif t.shape[0] != rows:
+        raise ValueError("%s has the wrong number of rows" % name)
+    return (t,) + _rows(t, like.dtype, C, name)
+
+
+def _whole(t, shape, dtype, name, device):
+    if t is None:
+        t = torch.empty(shape, dtype=dtype, device=device)
+    _dev(t, dtype, name)
+    if t.numel() != torch.Size(shape).numel():
+        raise ValueError("%s has the wrong size" % name)
+    return t
+
+
+def _offsets(desc, offsets):
+    if offsets is None:
+        return None
+    _dev(offsets, torch.int32, "offsets")
+    if offsets.numel() != desc.groups + 1:
+        raise ValueError("offsets must hold groups + 1 values")
+    return offsets.data_ptr()
+
+
+def _weights(weights):
+    _dev(weights, torch.uint8, "weights")
+    return weights.data_ptr(), weights.numel()
+
+
+def _scratch(t, n, device):
+    if t is None:
+        t = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+    _dev(t, torch.uint8, "workspace")
+    return t
+
+
+def _kept(x, rows, C):
+    """The 8-bit form of activations, as snn_checkpoint_store returns it, or None for a plain tensor."""
+    if isinstance(x, torch.Tensor):
+        return None
+    q, e = x
+    _dev(q, torch.int8, "q")
+    _dev(e, torch.uint8, "e")
+    if tuple(q.shape) != (rows, C) or tuple(e.shape) != (rows, (C + 31) // 32):
+        raise ValueError("the 8-bit activations have the wrong shape")
+    return q.data_ptr(), e.data_ptr()
+
+
+def snn_linear_weights_bytes(desc):
+    return int(lib().snn_linear_weights_bytes(ctypes.byref(desc)))
+
+
+def snn_linear_prepare(desc, codebook8, idx, alpha, weights=None):
+    """codebook8 int16 [groups][K], idx int16 [groups][C_out][C_in / 8], alpha [groups][C_out] of the activations' type
+    -> the prepared weights (uint8)."""
+    _dev(codebook8, torch.int16, "codebook8")
+    _dev(idx, torch.int16, "idx")
+    _dev(alpha, _dtype_of(desc), "alpha")
+    if codebook8.numel() != desc.groups * desc.K or idx.numel() * 8 != desc.groups * desc.C_out * desc.C_in or alpha.numel() != desc.groups * desc.C_out:
+        raise ValueError("codebook8, idx or alpha has the wrong size")
+    weights = _scratch(weights, snn_linear_weights_bytes(desc), idx.device)
+    _check(lib().snn_linear_prepare(ctypes.byref(desc), _ptr(codebook8), _ptr(idx), _ptr(alpha), _ptr(weights), weights.numel(),
+                                    _stream()), "snn_linear_prepare")
+    return weights
+
+
+def snn_linear_forward(desc, x, weights, offsets=None, y=None):
+    """x [rows][C_in], rows sorted by group as offsets (int32 [groups + 1]) says -> y [rows][C_out]."""
+    px, ldx = _rows(x, _dtype_of(desc), desc.C_in, "x")
+    y, py, ldy = _rows_out(y, x.shape[0], desc.C_out, x, "y")
+    _check(lib().snn_linear_forward(ctypes.byref(desc), px, ldx, x.shape[0], _offsets(desc, offsets), *_weights(weights), py, ldy,
+                                    _stream()), "snn_linear_forward")
+    return y
+
+
+def snn_linear_input_grad(desc, dy, weights, offsets=None, dx=None):
+    """dy [rows][C_out] -> dx [rows][C_in]."""
+    pdy, lddy = _rows(dy, _dtype_of(desc), desc.C_out, "dy")
+    dx, pdx, lddx = _rows_out(dx, dy.shape[0], desc.C_in, dy, "dx")
+    _check(lib().snn_linear_input_grad(ctypes.byref(desc), pdy, lddy, dy.shape[0], _offsets(desc, offsets), *_weights(weights), pdx,
+                                       lddx, _stream()), "snn_linear_input_grad")
+    return dx
+
+
+def snn_linear_weight_grad_workspace_bytes(desc, rows):
+    return int(lib().snn_linear_weight_grad_workspace_bytes(ctypes.byref(desc), rows))
+
+
+def snn_linear_weight_grad(desc, x, dy, weights, offsets=None, dw=None, dalpha=None, workspace=None):
+    """x [rows][C_in], or what snn_checkpoint_store made of it; dy [rows][C_out]
+    -> dw float32 [groups][C_out][C_in], dalpha float32 [groups][C_out]."""
+    rows = dy.shape[0]
+    pdy, lddy = _rows(dy, _dtype_of(desc), desc.C_out, "dy")
+    kept = _kept(x, rows, desc.C_in)
+    dw = _whole(dw, (desc.groups, desc.C_out, desc.C_in), torch.float32, "dw", dy.device)
+    dalpha = _whole(dalpha, (desc.groups, desc.C_out), torch.float32, "dalpha", dy.device)
+    workspace = _scratch(workspace, snn_linear_weight_grad_workspace_bytes(desc, rows), dy.device)
+    rest = (pdy, lddy, rows, _offsets(desc, offsets), *_weights(weights), _ptr(dw), _ptr(dalpha), _ptr(workspace), workspace.numel(), _stream())
+    if kept:
+        _check(lib().snn_linear_weight_grad_checkpoint(ctypes.byref(desc), *kept, *rest), "snn_linear_weight_grad_checkpoint")
+    else:
+        if x.shape[0] != rows:
+            raise ValueError("x and dy have different numbers of rows")
+        _check(lib().snn_linear_weight_grad(ctypes.byref(desc), *_rows(x, dy.dtype, desc.C_in, "x"), *rest), "snn_linear_weight_grad")
+    return dw, dalpha
+
+
+def snn_checkpoint_store(x, q=None, e=None):
+    """x [rows][C] -> (q int8 [rows][C], e uint8 [rows][ceil(C / 32)]), its 8-bit form."""
+    if not isinstance(x, torch.Tensor) or x.dtype not in _LINEAR_DTYPE or x.dim() != 2:
+        raise TypeError("x must be a CUDA tensor [rows][C] of torch.bfloat16 or torch.float16")
+    rows, C = x.shape
+    px, ldx = _rows(x, x.dtype, C, "x")
+    q = _whole(q, (rows, C), torch.int8, "q", x.device)
+    e = _whole(e, (rows, (C + 31) // 32), torch.uint8, "e", x.device)
+    _check(lib().snn_checkpoint_store(px, ldx, rows, C, _LINEAR_DTYPE.index(x.dtype), _ptr(q), _ptr(e), _stream()), "snn_checkpoint_store")
+    return q, e
+
+
+def snn_checkpoint_restore(kept, dtype, x=None):
+    """What snn_checkpoint_store returned -> the values it stands for, [rows][C] of dtype."""
+    q, e = kept
+    rows, C = q.shape
+    pq, pe = _kept(kept, rows, C)
+    if dtype not in _LINEAR_DTYPE:
+        raise TypeError("dtype must be torch.bfloat16 or torch.float16")
+    if x is None:
+        x = torch.empty((rows, C), dtype=dtype, device=q.device)
+    elif x.shape[0] != rows:
+        raise ValueError("x has the wrong number of rows")
+    px, ldx = _rows(x, dtype, C, "x")
+    _check(lib().snn_checkpoint_restore(pq, pe, rows, C, _LINEAR_DTYPE.index(dtype), px, ldx, _stream()), "snn_checkpoint_restore")
+    return x
+
+
+def _adapters(desc, A, B, scale):
+    dtype = _dtype_of(desc)
+    _dev(A, dtype, "A")
+    _dev(B, dtype, "B")
+    _dev(scale, torch.float32, "scale")
+    n, rank = A.shape[0], A.shape[1]
+    if tuple(A.shape) != (n, rank, desc.C_in) or tuple(B.shape) != (n, desc.C_out, rank) or scale.numel() != n:
+        raise ValueError("A, B or scale has the wrong shape")
+    return snn_adapters(n, rank, A.data_ptr(), B.data_ptr(), scale.data_ptr())
+
+
+def _of_row(adapter, rows):
+    _dev(adapter, torch.int32, "adapter")
+    if adapter.numel() != rows:
+        raise ValueError("adapter must hold one value a row")
+    return adapter.data_ptr()
+
+
+def snn_adapters_workspace_bytes(desc, adapters, rows):
+    return int(lib().snn_adapters_workspace_bytes(ctypes.byref(desc), ctypes.byref(adapters), rows))
+
+
+def snn_adapters_forward(desc, x, weights, adapter, A, B, scale, y=None, low=None, workspace=None):
+    """x [rows][C_in] through the shared projection and each row's adapter (int32 [rows], outside 0 .. n - 1: none);
+    A [n][rank][C_in], B [n][C_out][rank], scale float32 [n] -> y [rows][C_out], low float32 [rows][rank]."""
+    rows = x.shape[0]
+    px, ldx = _rows(x, _dtype_of(desc), desc.C_in, "x")
+    ad = _adapters(desc, A, B, scale)
+    y, py, ldy = _rows_out(y, rows, desc.C_out, x, "y")
+    low = _whole(low, (rows, ad.rank), torch.float32, "low", x.device)
+    workspace = _scratch(workspace, snn_adapters_workspace_bytes(desc, ad, rows), x.device)
+    _check(lib().snn_adapters_forward(ctypes.byref(desc), ctypes.byref(ad), px, ldx, rows, _of_row(adapter, rows), *_weights(weights),
+                                      py, ldy, _ptr(low), _ptr(workspace), workspace.numel(), _stream()), "snn_adapters_forward")
+    return y, low
+
+
+def snn_adapters_backward(desc, x, low, dy, weights, adapter, A, B, scale, dx=None, dA=None, dB=None, workspace=None):
+    """x [rows][C_in], or what snn_checkpoint_store made of it; low as the forward call returned it; dy [rows][C_out]
+    -> dx [rows][C_in], dA, dB (shapes and type of A and B)."""
+    rows = dy.shape[0]
+    pdy, lddy = _rows(dy, _dtype_of(desc), desc.C_out, "dy")
+    kept = _kept(x, rows, desc.C_in)
+    ad = _adapters(desc, A, B, scale)
+    _dev(low, torch.float32, "low")
+    if low.numel() != rows * ad.rank:
+        raise ValueError("low has the wrong size")
+    dx, pdx, lddx = _rows_out(dx, rows, desc.C_in, dy, "dx")
+    dA = _whole(dA, A.shape, A.dtype, "dA", dy.device)
+    dB = _whole(dB, B.shape, B.dtype, "dB", dy.device)
+    workspace = _scratch(workspace, snn_adapters_workspace_bytes(desc, ad, rows), dy.device)
+    rest = (_ptr(low), pdy, lddy, rows, _of_row(adapter, rows), *_weights(weights), pdx, lddx, _ptr(dA), _ptr(dB), _ptr(workspace),
+            workspace.numel(), _stream())
+    if kept:
+        _check(lib().snn_adapters_backward_checkpoint(ctypes.byref(desc), ctypes.byref(ad), *kept, *rest), "snn_adapters_backward_checkpoint")
+    else:
+        if x.shape[0] != rows:
+            raise ValueError("x and dy have different numbers of rows")
+        _check(lib().snn_adapters_backward(ctypes.byref(desc), ctypes.byref(ad), *_rows(x, dy.dtype, desc.C_in, "x"), *rest),
+               "snn_adapters_backward")
+    return dx, dA, dB

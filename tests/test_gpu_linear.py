@@ -1,0 +1,476 @@
+"""Projections of real-valued activations (snn_linear_*, snn_adapters_*, snn_checkpoint_*) against their formulas in 64 bits.
+
+Tolerances.  Products of 16-bit values are exact in fp32.  A sum of n of them in fp32, in any order, rounds n times, each time by
+at most 2^-24 of a partial sum; partial sums are about 1/sqrt(n) of the sum of magnitudes S, and the roundings add up as a
+random walk: 2^-24 S; 2^-21 S is eight times that.  A result of the activations' type is rounded once more, by at most u |y|
+(u = 2^-8 for bf16, 2^-11 for f16; below f16's normal numbers by 2^-25).  An adapter's inner product is held in two values of the
+activations' type, whose error is at most 2 u^2 of it (and, for f16, 2^-25), in the product with the adapter's other matrix."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import Guarded
+from paper_2110_09195_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"bf16": (torch.bfloat16, B.SNN_DTYPE_BF16, 2.0 ** -8, 0.0), "f16": (torch.float16, B.SNN_DTYPE_F16, 2.0 ** -11, 2.0 ** -25)}
+SUM = 2.0 ** -21
+
+
+def normal(seed, *shape):
+    return torch.from_numpy(np.random.default_rng(seed).standard_normal(shape).astype(np.float32)).cuda()
+
+
+def signs(codebook, idx):
+    """+-1 in 64 bits, [G][C_out][C_in], element by element from the codes"""
+    cb, ix = codebook.cpu().numpy(), idx.cpu().numpy()
+    G, co, V = ix.shape
+    w = np.empty((G, co, V * 8))
+    for g in range(G):
+        codes = cb[g][ix[g]]
+        for j in range(8):
+            w[g][:, j::8] = 2.0 * ((codes >> (7 - j)) & 1) - 1.0
+    return torch.from_numpy(w).cuda()
+
+
+class Layer:
+    def __init__(self, seed, groups, ci, co, K, dtype):
+        rng = np.random.default_rng(seed)
+        self.dtype, code, self.u, self.tiny = DTYPES[dtype]
+        self.ci, self.co, self.groups = ci, co, groups
+        self.desc = B.make_linear_desc(groups, ci, co, K, code)
+        self.codebook = torch.from_numpy(np.stack([rng.permutation(256)[:K] for _ in range(groups)]).astype(np.int16)).cuda()
+        self.idx = torch.from_numpy(rng.integers(0, K, (groups, co, ci // 8)).astype(np.int16)).cuda()
+        self.alpha = torch.from_numpy(rng.uniform(-1.5, 1.5, (groups, co)).astype(np.float32)).cuda().to(self.dtype)
+        buf = Guarded(B.snn_linear_weights_bytes(self.desc), torch.uint8)
+        self.weights = B.snn_linear_prepare(self.desc, self.codebook, self.idx, self.alpha, weights=buf.t)
+        buf.check("the prepared weights")
+        self.w = signs(self.codebook, self.idx)
+
+    def rows(self, seed, T, C, pad=0):
+        """T rows of C values, `pad` elements of NaN between them"""
+        wide = torch.full((T, C + pad), float("nan"), device="cuda").to(self.dtype)
+        wide[:, :C] = normal(seed, T, C)
+        return wide[:, :C]
+
+    def out(self, T, C, pad=0):
+        g = Guarded(T * (C + pad), self.dtype, fill=float("nan"))
+        return g, g.t.view(T, C + pad)[:, :C]
+
+    def close(self, got, want, S, extra=0.0, what=""):
+        tol = self.u * want.abs() * (1 + SUM) + SUM * S + extra + self.tiny
+        bad = ~((got.double() - want).abs() <= tol)
+        assert not bool(bad.any()), "%s: %d of %d differ, first at %s" % (what, int(bad.sum()), bad.numel(), bad.nonzero()[0].tolist())
+
+
+def offsets_of(counts):
+    return torch.tensor([0] + list(np.cumsum(counts)), dtype=torch.int32, device="cuda")
+
+
+# rows of each group; channels in and out; K; elements between rows
+SHAPES = [
+    ([1], 8, 8, 1, 0),
+    ([3], 64, 32, 16, 0),
+    ([0, 5, 0, 1], 72, 40, 4, 8),
+    ([33, 0, 64, 31], 136, 264, 256, 16),
+    ([1] * 40, 1032, 520, 32, 0),
+    ([127, 1, 129, 0, 300], 200, 520, 64, 8),
+    ([256, 257, 255], 320, 256, 32, 0),
+    ([700], 520, 776, 7, 8),
+    ([1000, 3, 0, 500], 1024, 512, 128, 0),
+    ([0, 0, 0], 64, 64, 2, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_forward_and_input_grad(shape, dtype):
+    counts, ci, co, K, pad = SHAPES[shape]
+    print("case", SHAPES[shape], dtype, flush=True)
+    L, T = Layer(shape, len(counts), ci, co, K, dtype), sum(counts)
+    off = offsets_of(counts)
+    x, dy = L.rows(1, T, ci, pad), L.rows(2, T, co, pad)
+    gy, y = L.out(T, co, pad)
+    gx, dx = L.out(T, ci, pad)
+    B.snn_linear_forward(L.desc, x, L.weights, offsets=off, y=y)
+    B.snn_linear_input_grad(L.desc, dy, L.weights, offsets=off, dx=dx)
+    gy.check("y")
+    gx.check("dx")
+    if pad and T:
+        assert bool(gy.t.view(T, co + pad)[:, co:].isnan().all()) and bool(gx.t.view(T, ci + pad)[:, ci:].isnan().all())
+    lo = 0
+    for g, n in enumerate(counts):
+        s = slice(lo, lo + n)
+        lo += n
+        a = L.alpha[g].double()
+        L.close(y[s], (x[s].double() @ L.w[g].t()) * a, x[s].double().abs().sum(1, keepdim=True) * a.abs(), what="y of group %d" % g)
+        d = dy[s].double() * a
+        L.close(dx[s], d @ L.w[g], d.abs().sum(1, keepdim=True), what="dx of group %d" % g)
+
+
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+def test_one_group_needs_no_offsets(dtype):
+    L = Layer(3, 1, 256, 128, 16, dtype)
+    x = L.rows(1, 50, 256)
+    y = B.snn_linear_forward(L.desc, x, L.weights)
+    assert torch.equal(y, B.snn_linear_forward(L.desc, x, L.weights, offsets=offsets_of([50])))
+    L.close(y, (x.double() @ L.w[0].t()) * L.alpha[0].double(), x.double().abs().sum(1, keepdim=True) * L.alpha[0].double().abs())
+
+
+@pytest.mark.parametrize("T", [90, 700])
+def test_rows_of_no_group_are_not_written_and_wild_offsets_stay_inside(T):
+    L = Layer(4, 3, 128, 96, 16, "bf16")
+    x, dy = L.rows(1, T, 128), L.rows(2, T, 96)
+    off = torch.tensor([7, 20, 20, T - 9], dtype=torch.int32, device="cuda")
+    g, y = L.out(T, 96)
+    B.snn_linear_forward(L.desc, x, L.weights, offsets=off, y=y)
+    g.check("y")
+    assert bool(y[:7].isnan().all()) and bool(y[T - 9:].isnan().all()) and not bool(y[7:T - 9].isnan().any())
+    for wild in ([-5, 2 ** 31 - 1, -2 ** 31, 10], [2 ** 31 - 1] * 4, [T, 5, 3, 0], [-1, -1, T + 1, T + 5]):
+        off = torch.tensor(wild, dtype=torch.int64).to(torch.int32).cuda()
+        g, y = L.out(T, 96)
+        B.snn_linear_forward(L.desc, x, L.weights, offsets=off, y=y)
+        g.check("y")
+        g, dx = L.out(T, 128)
+        B.snn_linear_input_grad(L.desc, dy, L.weights, offsets=off, dx=dx)
+        g.check("dx")
+        g = Guarded(3 * 96 * 128, torch.float32)
+        B.snn_linear_weight_grad(L.desc, x, dy, L.weights, offsets=off, dw=g.t.view(3, 96, 128))
+        g.check("dw")
+
+
+@pytest.mark.parametrize("T", [40, 600])
+def test_what_is_not_finite_stays_in_its_row_and_group(T):
+    L = Layer(5, 2, 192, 160, 32, "bf16")
+    n = T // 2 + 3
+    off = offsets_of([n, T - n])
+    x, dy = L.rows(1, T, 192), L.rows(2, T, 160)
+    bad_x, bad_dy = x.clone(), dy.clone()
+    bad_x[5, 3], bad_x[n - 1, 191], bad_dy[n - 1, 0], bad_dy[2, 159] = float("inf"), float("nan"), float("-inf"), float("nan")
+    y, by = (B.snn_linear_forward(L.desc, v, L.weights, offsets=off) for v in (x, bad_x))
+    keep = torch.ones(T, dtype=torch.bool, device="cuda")
+    keep[5] = keep[n - 1] = False
+    assert torch.equal(y[keep], by[keep]) and not bool(by[~keep].isfinite().any())
+    dx, bdx = (B.snn_linear_input_grad(L.desc, v, L.weights, offsets=off) for v in (dy, bad_dy))
+    keep[5], keep[2] = True, False
+    assert torch.equal(dx[keep], bdx[keep]) and not bool(bdx[~keep].isfinite().any())
+    (dw, da), (bdw, bda) = (B.snn_linear_weight_grad(L.desc, v, d, L.weights, offsets=off) for v, d in ((x, dy), (bad_x, bad_dy)))
+    assert torch.equal(dw[1], bdw[1]) and torch.equal(da[1], bda[1])
+    assert not bool(bdw[0, :, 3].isfinite().any()) and not bool(bdw[0, 159].isfinite().any()) and not bool(bda[0].isfinite().any())
+    k, bk = (B.snn_linear_weight_grad(L.desc, B.snn_checkpoint_store(v), dy, L.weights, offsets=off)[0] for v in (x, bad_x))
+    assert torch.equal(k[1], bk[1]) and bool(bk[0, :, 3].isnan().all()) and bool(bk[0, :, 191].isnan().all())
+    assert torch.equal(k[0, :, 40:160], bk[0, :, 40:160])
+
+
+# ---- the 8-bit form --------------------------------------------------------------------------------------------
+
+def kept_in_f64(x):
+    x = x.double().cpu()
+    out = torch.empty_like(x)
+    for c in range(0, x.shape[1], 32):
+        part = x[:, c:c + 32]
+        ok = part.isfinite()
+        top = torch.where(ok, part, torch.zeros_like(part)).abs().amax(1, keepdim=True)
+        _, e = torch.frexp(top)
+        u = torch.where(top > 0, torch.ldexp(torch.ones_like(top), e - 7), torch.zeros_like(top)).clamp(min=2.0 ** -126)
+        out[:, c:c + 32] = torch.where(ok, (part / u).round().clamp(-127, 127) * u, torch.full_like(part, float("nan")))
+    return out.cuda()
+
+
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+@pytest.mark.parametrize("T, C, pad", [(1, 8, 0), (3, 40, 8), (7, 32, 0), (64, 1000, 0), (33, 264, 16), (5, 4096, 0), (130, 72, 0)])
+def test_checkpoint_values(T, C, pad, dtype):
+    tdtype = DTYPES[dtype][0]
+    wide = torch.full((T, C + pad), float("nan"), device="cuda").to(tdtype)
+    wide[:, :C] = normal(T, T, C) * torch.exp2(4 * normal(C, T, C))
+    x = wide[:, :C]
+    x[0, :8] = torch.tensor([0.0, -0.0, float("inf"), float("-inf"), float("nan"), 1.0, -1.9921875, 1.9921875]).to(tdtype)
+    if T > 2:
+        x[1] = 0.0
+        x[2] = torch.finfo(tdtype).max * torch.where(normal(9, C) < 0, -1.0, 0.25)
+    if T > 4:
+        x[3] = torch.finfo(tdtype).tiny * normal(3, C)       # some of these are below the normal numbers
+        x[4] = float("nan")
+    gq, ge = Guarded(T * C, torch.int8), Guarded(T * ((C + 31) // 32), torch.uint8)
+    kept = B.snn_checkpoint_store(x, q=gq.t.view(T, C), e=ge.t.view(T, -1))
+    gq.check("q")
+    ge.check("e")
+    assert bool((kept[1] >= 1).all()) and bool((kept[1] <= 254).all())
+    g = Guarded(T * (C + pad), tdtype, fill=7.0)
+    got = B.snn_checkpoint_restore(kept, tdtype, x=g.t.view(T, C + pad)[:, :C])
+    g.check("x")
+    want = kept_in_f64(x)
+    same = (got.double() == want) | (got.isnan() & want.isnan())
+    assert bool(same.all()), (same == False).nonzero()[:4].tolist()  # noqa: E712
+    if pad:
+        assert bool((g.t.view(T, C + pad)[:, C:] == 7).all())
+
+
+# ---- gradients of the weights ----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kept", [False, True])
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_weight_grad(shape, dtype, kept):
+    counts, ci, co, K, pad = SHAPES[shape]
+    print("case", SHAPES[shape], dtype, kept, flush=True)
+    L, T, G = Layer(shape, len(counts), ci, co, K, dtype), sum(counts), len(counts)
+    off = offsets_of(counts)
+    x, dy = L.rows(1, T, ci, pad), L.rows(2, T, co, pad)
+    gw, ga = Guarded(G * co * ci, torch.float32, fill=float("nan")), Guarded(G * co, torch.float32, fill=float("nan"))
+    gs = Guarded(max(B.snn_linear_weight_grad_workspace_bytes(L.desc, T), 256), torch.uint8)
+    arg = B.snn_checkpoint_store(x) if kept else x
+    dw, da = B.snn_linear_weight_grad(L.desc, arg, dy, L.weights, offsets=off, dw=gw.t.view(G, co, ci), dalpha=ga.t.view(G, co), workspace=gs.t)
+    gw.check("dw")
+    ga.check("dalpha")
+    gs.check("the workspace")
+    xv = B.snn_checkpoint_restore(arg, L.dtype) if kept else x
+    lo = 0
+    for g, n in enumerate(counts):
+        s = slice(lo, lo + n)
+        lo += n
+        want = dy[s].double().t() @ xv[s].double()
+        S = dy[s].double().abs().t() @ xv[s].double().abs()
+        a = L.alpha[g].double()[:, None]
+        # (the product with alpha rounds once more)
+        assert bool(((dw[g].double() - want * a).abs() <= (SUM * S + 2.0 ** -24 * want.abs()) * a.abs()).all()), g
+        assert bool(((da[g].double() - (L.w[g] * want).sum(1)).abs() <= 2 * SUM * S.sum(1)).all()), g
+    again, _ = B.snn_linear_weight_grad(L.desc, arg, dy, L.weights, offsets=off)
+    assert torch.equal(again, dw)
+
+
+def test_weight_grad_without_dalpha_and_without_rows():
+    L = Layer(9, 2, 72, 48, 8, "bf16")
+    x, dy = L.rows(1, 30, 72), L.rows(2, 30, 48)
+    off = offsets_of([10, 20])
+    dw, _ = B.snn_linear_weight_grad(L.desc, x, dy, L.weights, offsets=off)
+    other = torch.full_like(dw, float("nan"))
+    import ctypes
+    ws = torch.empty(max(B.snn_linear_weight_grad_workspace_bytes(L.desc, 30), 256), dtype=torch.uint8, device="cuda")
+    rc = B.lib().snn_linear_weight_grad(ctypes.byref(L.desc), x.data_ptr(), 72, dy.data_ptr(), 48, 30, off.data_ptr(), L.weights.data_ptr(),
+                                        L.weights.numel(), other.data_ptr(), None, ws.data_ptr(), ws.numel(),
+                                        torch.cuda.current_stream().cuda_stream)
+    assert rc == 0 and torch.equal(other, dw)
+    for arg in (x[:0], B.snn_checkpoint_store(x[:0])):
+        dw, da = B.snn_linear_weight_grad(L.desc, arg, dy[:0], L.weights, offsets=offsets_of([0, 0]))
+        assert not bool(dw.any()) and not bool(da.any())
+    assert B.snn_linear_forward(L.desc, x[:0], L.weights, offsets=offsets_of([0, 0])).shape == (0, 48)
+
+
+# ---- adapters --------------------------------------------------------------------------------------------------
+
+def ids_of(kind, T, n, seed):
+    rng = np.random.default_rng(seed)
+    if kind == "each":                                       # single tokens, any order, some without
+        ids = rng.integers(-1, n, T)
+    elif kind == "runs":                                     # prompts of some dozen tokens
+        ids = np.repeat(rng.integers(-1, n, T // 20 + 1), 20)[:T]
+    elif kind == "sorted":
+        ids = np.sort(rng.integers(0, n, T))
+    elif kind == "none":
+        ids = np.full(T, -1)
+    else:                                                    # values outside the range: no adapter
+        ids = rng.choice([-2 ** 31, -1, 0, n - 1, n, 2 ** 31 - 1], T)
+    return torch.from_numpy(ids.astype(np.int32)).cuda()
+
+
+ADAPTED = [
+    (1, 64, 64, 3, 8, "each"), (5, 72, 40, 4, 8, "each"), (16, 512, 264, 40, 16, "each"), (48, 136, 1032, 9, 128, "each"),
+    (70, 1024, 512, 5, 24, "wild"), (100, 200, 96, 3, 64, "runs"), (333, 320, 256, 6, 40, "runs"), (300, 64, 72, 2, 16, "none"),
+    (513, 256, 520, 4, 32, "sorted"), (1000, 776, 1032, 7, 72, "runs"), (700, 512, 512, 1, 128, "sorted"), (300, 128, 128, 90, 8, "each"),
+]
+
+
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+@pytest.mark.parametrize("case", range(len(ADAPTED)))
+def test_adapters(case, dtype):
+    T, ci, co, n, r, kind = ADAPTED[case]
+    print("case", ADAPTED[case], dtype, flush=True)
+    L = Layer(case, 1, ci, co, 32, dtype)
+    ids = ids_of(kind, T, n, case)
+    pad = 8 * (case % 3)
+    x, dy = L.rows(1, T, ci, pad), L.rows(2, T, co, pad)
+    A, Bm = (normal(3, n, r, ci) / ci ** 0.5).to(L.dtype), (0.5 * normal(4, n, co, r)).to(L.dtype)
+    scale = 0.5 + normal(5, n).abs()
+    low_err, tiny = 2 * L.u * L.u, L.tiny
+
+    gy, y = L.out(T, co, pad)
+    gl = Guarded(T * r, torch.float32, fill=float("nan"))
+    need = B.snn_adapters_workspace_bytes(L.desc, B._adapters(L.desc, A, Bm, scale), T)
+    gs = Guarded(need, torch.uint8)
+    _, low = B.snn_adapters_forward(L.desc, x, L.weights, ids, A, Bm, scale, y=y, low=gl.t.view(T, r), workspace=gs.t)
+    for g, what in ((gy, "y"), (gl, "low"), (gs, "the workspace")):
+        g.check(what)
+
+    has = (ids >= 0) & (ids < n)
+    a = torch.where(has, ids, torch.zeros_like(ids)).long()
+    c = torch.where(has, scale[a], torch.zeros_like(scale[a])).double()[:, None]
+    xd, dyd, w, alpha = x.double(), dy.double(), L.w[0], L.alpha[0].double()
+    Ad, Bd = A.double(), Bm.double()
+    want_low, S_low = torch.zeros(T, r, dtype=torch.float64, device="cuda"), torch.zeros(T, r, dtype=torch.float64, device="cuda")
+    want, S, extra = (xd @ w.t()) * alpha, xd.abs().sum(1, keepdim=True) * alpha.abs(), torch.zeros(T, co, dtype=torch.float64, device="cuda")
+    dlow, S_dlow = torch.zeros_like(want_low), torch.zeros_like(want_low)
+    dx, S_dx = (dyd * alpha) @ w, ((dyd * alpha).abs().sum(1, keepdim=True)).expand(T, ci).clone()
+    extra_dx = torch.zeros(T, ci, dtype=torch.float64, device="cuda")
+    members = [(k, (has & (ids == k)).nonzero().flatten()) for k in range(n)]
+    for k, rows in members:
+        if not rows.numel():
+            continue
+        s = c[rows]
+        want_low[rows], S_low[rows] = xd[rows] @ Ad[k].t(), xd[rows].abs() @ Ad[k].abs().t()
+        z = s * want_low[rows]
+        want[rows] += z @ Bd[k].t()
+        S[rows] += (s * S_low[rows]) @ Bd[k].abs().t()
+        extra[rows] = (low_err * z.abs() + tiny) @ Bd[k].abs().t()
+        dlow[rows], S_dlow[rows] = s * (dyd[rows] @ Bd[k]), s * (dyd[rows].abs() @ Bd[k].abs())
+        dx[rows] += dlow[rows] @ Ad[k]
+        S_dx[rows] += S_dlow[rows] @ Ad[k].abs()
+        extra_dx[rows] = (low_err * dlow[rows].abs() + tiny) @ Ad[k].abs()
+    assert bool(((low.double() - want_low).abs() <= SUM * S_low).all())
+    L.close(y, want, S, extra, "y")
+
+    for kept in (False, True):
+        arg = B.snn_checkpoint_store(x) if kept else x
+        xv = B.snn_checkpoint_restore(arg, L.dtype).double() if kept else xd
+        gx, out = L.out(T, ci, pad)
+        ga, gb = Guarded(A.numel(), L.dtype, fill=float("nan")), Guarded(Bm.numel(), L.dtype, fill=float("nan"))
+        gs = Guarded(need, torch.uint8)
+        _, dA, dB = B.snn_adapters_backward(L.desc, arg, low, dy, L.weights, ids, A, Bm, scale, dx=out, dA=ga.t.view(A.shape), dB=gb.t.view(Bm.shape),
+                                            workspace=gs.t)
+        for g, what in ((gx, "dx"), (ga, "dA"), (gb, "dB"), (gs, "the workspace")):
+            g.check(what)
+        L.close(out, dx, S_dx, extra_dx, "dx")
+        for k, rows in members:
+            ax, ady = xv[rows].abs(), dyd[rows].abs()
+            L.close(dA[k], dlow[rows].t() @ xv[rows], S_dlow[rows].t() @ ax, (low_err * dlow[rows].abs() + tiny).t() @ ax, "dA of %d" % k)
+            s = c[rows]
+            L.close(dB[k], dyd[rows].t() @ (s * want_low[rows]), ady.t() @ (s * S_low[rows]),
+                    scale[k].double() * (ady.t() @ (low_err * want_low[rows].abs() + tiny)), "dB of %d" % k)
+
+
+@pytest.mark.parametrize("T, kind", [(24, "each"), (400, "runs")])
+def test_a_broken_adapter_reaches_its_own_rows_only(T, kind):
+    L, n, r = Layer(6, 1, 128, 96, 16, "bf16"), 5, 16
+    ids = ids_of(kind, T, n, 1)
+    ids[0] = 2
+    x, dy = L.rows(1, T, 128), L.rows(2, T, 96)
+    A, Bm, scale = (normal(3, n, r, 128)).to(L.dtype), normal(4, n, 96, r).to(L.dtype), normal(5, n)
+    badA, badB, bad_scale = A.clone(), Bm.clone(), scale.clone()
+    badA[2], badB[2], bad_scale[2] = float("nan"), float("inf"), float("nan")
+    bad_x, bad_dy = x.clone(), dy.clone()
+    bad_x[ids == 2], bad_dy[ids == 2] = float("inf"), float("nan")
+    y, low = B.snn_adapters_forward(L.desc, x, L.weights, ids, A, Bm, scale)
+    by, blow = B.snn_adapters_forward(L.desc, bad_x, L.weights, ids, badA, badB, bad_scale)
+    other = ids != 2
+    assert torch.equal(y[other], by[other]) and torch.equal(low[other], blow[other]) and not bool(by[~other].isfinite().any())
+    for keep in (lambda v: v, B.snn_checkpoint_store):
+        dx, dA, dB = B.snn_adapters_backward(L.desc, keep(x), low, dy, L.weights, ids, A, Bm, scale)
+        bdx, bdA, bdB = B.snn_adapters_backward(L.desc, keep(bad_x), blow, bad_dy, L.weights, ids, badA, badB, bad_scale)
+        assert torch.equal(dx[other], bdx[other])
+        rest = [k for k in range(n) if k != 2]
+        assert torch.equal(dA[rest], bdA[rest]) and torch.equal(dB[rest], bdB[rest])
+
+
+def test_no_rows_give_zero_adapter_gradients():
+    L, n, r = Layer(6, 1, 64, 96, 16, "f16"), 3, 8
+    A, Bm, scale = normal(3, n, r, 64).to(L.dtype), normal(4, n, 96, r).to(L.dtype), normal(5, n)
+    x, dy, ids = L.rows(1, 0, 64), L.rows(2, 0, 96), torch.zeros(0, dtype=torch.int32, device="cuda")
+    y, low = B.snn_adapters_forward(L.desc, x, L.weights, ids, A, Bm, scale)
+    dx, dA, dB = B.snn_adapters_backward(L.desc, x, low, dy, L.weights, ids, A, Bm, scale)
+    assert y.shape == (0, 96) and dx.shape == (0, 64) and not bool(dA.any()) and not bool(dB.any())
+
+
+# ---- gradients against differences -----------------------------------------------------------------------------
+# Small whole numbers and powers of two: every output is exact, and so is a difference of two of them.
+
+def whole(seed, shape, lo, hi, dtype):
+    return torch.from_numpy(np.random.default_rng(seed).integers(lo, hi + 1, shape).astype(np.float32)).cuda().to(dtype)
+
+
+def loss(y, c):
+    return float((y.double() * c.double()).sum())
+
+
+@pytest.mark.parametrize("T", [12, 300])
+def test_gradients_are_differences(T):
+    L = Layer(8, 2, 32, 24, 256, "f16")
+    L.alpha = torch.tensor(np.random.default_rng(1).choice([0.5, 1.0, 2.0], (2, 24)).astype(np.float32)).cuda().half()
+    L.weights = B.snn_linear_prepare(L.desc, L.codebook, L.idx, L.alpha)
+    counts = [T // 3, T - T // 3]
+    off = offsets_of(counts)
+    x, c, step = whole(1, (T, 32), -3, 3, L.dtype), whole(2, (T, 24), -2, 2, L.dtype), whole(3, (T, 32), -1, 1, L.dtype)
+    base = loss(B.snn_linear_forward(L.desc, x, L.weights, offsets=off), c)
+    dx = B.snn_linear_input_grad(L.desc, c, L.weights, offsets=off)
+    assert loss(B.snn_linear_forward(L.desc, x + step, L.weights, offsets=off), c) - base == loss(dx, step)
+    dw, da = B.snn_linear_weight_grad(L.desc, x, c, L.weights, offsets=off)
+    for g, o in ((0, 0), (1, 23), (0, 11)):
+        alpha = L.alpha.clone()
+        alpha[g, o] += 1
+        moved = B.snn_linear_prepare(L.desc, L.codebook, L.idx, alpha)
+        assert loss(B.snn_linear_forward(L.desc, x, moved, offsets=off), c) - base == float(da[g, o])
+        for v, j in ((0, 0), (3, 7), (2, 4)):                # one weight changes its sign
+            idx, code = L.idx.clone(), int(L.codebook[g, int(L.idx[g, o, v])])
+            flipped = code ^ (1 << (7 - j))
+            idx[g, o, v] = int((L.codebook[g] == flipped).nonzero()[0])
+            moved = B.snn_linear_prepare(L.desc, L.codebook, idx, L.alpha)
+            change = 2.0 if (flipped >> (7 - j)) & 1 else -2.0
+            assert loss(B.snn_linear_forward(L.desc, x, moved, offsets=off), c) - base == change * float(dw[g, o, 8 * v + j])
+
+
+@pytest.mark.parametrize("T", [12, 150])
+def test_adapter_gradients_are_differences(T):
+    n, r = 3, 8
+    L = Layer(8, 1, 16, 24, 256, "f16")
+    L.alpha = torch.ones(1, 24, device="cuda").half()
+    L.weights = B.snn_linear_prepare(L.desc, L.codebook, L.idx, L.alpha)
+    ids = ids_of("each", T, n, 2)
+    x, c = whole(1, (T, 16), -1, 1, L.dtype), whole(2, (T, 24), -1, 1, L.dtype)
+    A, Bm = whole(3, (n, r, 16), -1, 1, L.dtype), whole(4, (n, 24, r), -1, 1, L.dtype)
+    scale = torch.tensor([1.0, 2.0, 0.5], device="cuda")
+
+    def f(x, A, Bm):
+        return loss(B.snn_adapters_forward(L.desc, x, L.weights, ids, A, Bm, scale)[0], c)
+
+    _, low = B.snn_adapters_forward(L.desc, x, L.weights, ids, A, Bm, scale)
+    dx, dA, dB = B.snn_adapters_backward(L.desc, x, low, c, L.weights, ids, A, Bm, scale)
+    base = f(x, A, Bm)
+    step = whole(5, (T, 16), -1, 1, L.dtype)
+    assert f(x + step, A, Bm) - base == loss(dx, step)
+    step = whole(6, (n, r, 16), -1, 1, L.dtype)
+    assert f(x, A + step, Bm) - base == loss(dA, step)
+    step = whole(7, (n, 24, r), -1, 1, L.dtype)
+    assert f(x, A, Bm + step) - base == loss(dB, step)
+
+
+# ---- streams and graphs ----------------------------------------------------------------------------------------
+
+def test_on_another_stream_and_in_a_graph():
+    L, n, r, T = Layer(7, 1, 256, 192, 16, "bf16"), 4, 16, 200
+    ids = ids_of("runs", T, n, 1)
+    A, Bm, scale = (0.1 * normal(3, n, r, 256)).to(L.dtype), normal(4, n, 192, r).to(L.dtype), normal(5, n)
+    x, dy = L.rows(1, T, 256), L.rows(2, T, 192)
+
+    def step():
+        kept = B.snn_checkpoint_store(x)
+        y, low = B.snn_adapters_forward(L.desc, x, L.weights, ids, A, Bm, scale)
+        grads = B.snn_adapters_backward(L.desc, kept, low, dy, L.weights, ids, A, Bm, scale)
+        return (y, low) + grads + B.snn_linear_weight_grad(L.desc, kept, dy, L.weights)
+
+    want = step()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = step()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for seed in range(4):
+        x.copy_(normal(10 + seed, T, 256))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), seed
