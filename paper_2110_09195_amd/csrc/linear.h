@@ -49,16 +49,16 @@ struct Adapters {
 
 int launch_linear_prepare(const LinearGeom &g, const uint16_t *codebook, const uint16_t *idx, const void *alpha, void *weights, hipStream_t s);
 
-// rows through the F image (grad = false: x -> y) or the D image (grad = true: dy -> dx); ad != nullptr: with the adapters' share,
-// from `low` (fp32 [rows][rank], scale applied)
+// rows through the F image (grad = false: x -> y) or the D image (grad = true: dy -> dx); ad != nullptr: with the adapters' share, from
+// `low` (fp32 [rows][rank], scale applied) and `up`, [n][columns of the output][rank]
 int launch_linear_rows(const LinearGeom &g, bool grad, const void *in, int64_t ld_in, int64_t rows, const int32_t *offsets,
-                       const void *weights, void *out, int64_t ld_out, const Adapters *ad, const float *low, hipStream_t s);
+                       const void *weights, void *out, int64_t ld_out, const Adapters *ad, const void *up, const float *low, hipStream_t s);
 
 size_t linear_weight_grad_workspace_bytes(const LinearGeom &g, int64_t rows);
 int launch_linear_weight_grad(const LinearGeom &g, const RowsIn &x, const void *dy, int64_t lddy, int64_t rows, const int32_t *offsets,
                               const void *weights, float *dw, float *dalpha, void *ws, hipStream_t s);
 
-size_t adapters_workspace_bytes(const LinearGeom &g, int rank, int64_t rows);
+size_t adapters_workspace_bytes(const LinearGeom &g, int n, int rank, int64_t rows);
 int launch_adapters_forward(const LinearGeom &g, const Adapters &ad, const void *x, int64_t ldx, int64_t rows, const void *weights,
                             void *y, int64_t ldy, float *low, void *ws, hipStream_t s);
 int launch_adapters_backward(const LinearGeom &g, const Adapters &ad, const RowsIn &x, const float *low, const void *dy, int64_t lddy,

@@ -1,0 +1,68 @@
+// Device pieces of the projections' kernels: 16-bit operands of the matrix cores, loads from memory into LDS.
+#pragma once
+
+#include "linear.h"
+
+namespace snn {
+
+using s32x4 = __attribute__((ext_vector_type(4))) int;
+using u32x4 = __attribute__((ext_vector_type(4))) uint32_t;
+using u32x2 = __attribute__((ext_vector_type(2))) uint32_t;
+using f32x4 = __attribute__((ext_vector_type(4))) float;
+using f32x16 = __attribute__((ext_vector_type(16))) float;
+
+template <class T> struct Half;
+template <> struct Half<__bf16> {
+    using v8 = __attribute__((ext_vector_type(8))) __bf16;
+    using v4 = __attribute__((ext_vector_type(4))) __bf16;
+    using v2 = __attribute__((ext_vector_type(2))) __bf16;
+    static constexpr uint32_t ONES = 0x3f803f80u;              // (1, 1)
+    static __device__ f32x16 mfma(v8 a, v8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Half<_Float16> {
+    using v8 = __attribute__((ext_vector_type(8))) _Float16;
+    using v4 = __attribute__((ext_vector_type(4))) _Float16;
+    using v2 = __attribute__((ext_vector_type(2))) _Float16;
+    static constexpr uint32_t ONES = 0x3c003c00u;
+    static __device__ f32x16 mfma(v8 a, v8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+
+// A buffer resource: loads past `bytes` give zeros.
+__device__ inline s32x4 resource(const void *p, uint32_t bytes)
+{
+    const uint64_t a = (uint64_t)p;
+    s32x4 r;
+    r[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)a);
+    r[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32));
+    r[2] = __builtin_amdgcn_readfirstlane((int)bytes);
+    r[3] = 0x00020000;
+    return r;
+}
+
+__device__ inline uint32_t lds_address(const void *p) { return (uint32_t)(uint64_t)(__attribute__((address_space(3))) const void *)p; }
+
+// Memory to LDS without registers: lane l's 16 (4) bytes go to lds + 16 l (4 l); `lds` is the wave's.  Not counted by the compiler: the
+// kernel waits for them itself.
+__device__ inline void load_lds16(uint32_t lds, uint32_t offset, s32x4 from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(from) : "memory");
+}
+__device__ inline void load_lds4(uint32_t lds, uint32_t offset, s32x4 from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(from) : "memory");
+}
+
+constexpr uint32_t NOWHERE = 0x80000000u;                      // an offset past every resource
+
+// Two values of the activations' type that together hold v with twice its mantissa.
+template <class T>
+__device__ inline void split8(const float *v, typename Half<T>::v8 &hi, typename Half<T>::v8 &lo)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        hi[j] = (T)v[j];
+        lo[j] = (T)(v[j] - (float)hi[j]);
+    }
+}
+
+}  // namespace snn
