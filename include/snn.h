@@ -587,7 +587,8 @@ int snn_linear_input_grad(const snn_linear_desc *desc, const void *dy, int64_t l
  * Every kept value is a value of the activations' type, so that products with it are exact.  What is not finite gets q = -128, which
  * stands for NaN.
  *   x   device, rows of C (a multiple of 8, 8 .. 65536) in the type `dtype`
- *   q   device, int8 [rows][C], 16-byte aligned;   e   device, uint8 [rows][ceil(C / 32)]: u = 2^(e - 127), 1 <= e
+ *   q   device, int8 [rows][C], 16-byte aligned
+ *   e   device, uint8 [rows][4 ceil(C / 128)] (a row's chunks in whole words), 4-byte aligned: u = 2^(e - 127), 1 <= e
  * snn_checkpoint_restore writes the kept values.
  * Errors: INVALID_ARG; LAUNCH.
  */

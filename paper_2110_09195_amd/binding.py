@@ -854,6 +854,10 @@ def _scratch(t, n, device):
     return t
 
 
+def _words(C):
+    return (C + 127) // 128 * 4          # exponents of a row: one a chunk of 32 channels, in whole words
+
+
 def _kept(x, rows, C):
     """The 8-bit form of activations, as snn_checkpoint_store returns it, or None for a plain tensor."""
     if isinstance(x, torch.Tensor):
@@ -861,7 +865,7 @@ def _kept(x, rows, C):
     q, e = x
     _dev(q, torch.int8, "q")
     _dev(e, torch.uint8, "e")
-    if tuple(q.shape) != (rows, C) or tuple(e.shape) != (rows, (C + 31) // 32):
+    if tuple(q.shape) != (rows, C) or tuple(e.shape) != (rows, _words(C)):
         raise ValueError("the 8-bit activations have the wrong shape")
     return q.data_ptr(), e.data_ptr()
 
@@ -926,13 +930,13 @@ def snn_linear_weight_grad(desc, x, dy, weights, offsets=None, dw=None, dalpha=N
 
 
 def snn_checkpoint_store(x, q=None, e=None):
-    """x [rows][C] -> (q int8 [rows][C], e uint8 [rows][ceil(C / 32)]), its 8-bit form."""
+    """x [rows][C] -> (q int8 [rows][C], e uint8 [rows][4 ceil(C / 128)]), its 8-bit form."""
     if not isinstance(x, torch.Tensor) or x.dtype not in _LINEAR_DTYPE or x.dim() != 2:
         raise TypeError("x must be a CUDA tensor [rows][C] of torch.bfloat16 or torch.float16")
     rows, C = x.shape
     px, ldx = _rows(x, x.dtype, C, "x")
     q = _whole(q, (rows, C), torch.int8, "q", x.device)
-    e = _whole(e, (rows, (C + 31) // 32), torch.uint8, "e", x.device)
+    e = _whole(e, (rows, _words(C)), torch.uint8, "e", x.device)
     _check(lib().snn_checkpoint_store(px, ldx, rows, C, _LINEAR_DTYPE.index(x.dtype), _ptr(q), _ptr(e), _stream()), "snn_checkpoint_store")
     return q, e
 

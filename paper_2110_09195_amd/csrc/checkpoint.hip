@@ -1,11 +1,18 @@
-// Activations kept in 8 bits: chunks of 32 channels of a row share a power of two.
-#include "linear.h"
+// Activations kept in 8 bits: chunks of 32 channels of a row share a power of two.  Both directions move memory and nothing else counts:
+// a thread takes 8 channels (16 bytes one side, 8 the other), four neighbouring lanes a chunk.
+#include "linear_device.h"
 
 namespace snn {
 
 namespace {
 
-constexpr int CHUNK = 32;
+// Where a thread's pieces of 8 channels lie: rows of `pieces` (whole words of exponents: 16 pieces each), a grid's stride apart.
+struct Walk {
+    int64_t rows;
+    int pieces;
+    int64_t step_rows;
+    int step_pieces;
+};
 
 // The unit's biased exponent: that of the largest finite magnitude less 6, not below 2^-126.
 __device__ inline uint32_t unit_exponent(float top)
@@ -15,57 +22,102 @@ __device__ inline uint32_t unit_exponent(float top)
 
 template <class T>
 __global__ __launch_bounds__(256)
-void checkpoint_store_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int C, int8_t *__restrict__ q, uint8_t *__restrict__ e)
+void checkpoint_store_kernel(const T *__restrict__ x, int64_t ldx, Walk w, int C, int8_t *__restrict__ q, uint8_t *__restrict__ e)
 {
-    const int chunks = (C + CHUNK - 1) / CHUNK;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows * chunks) return;
-    const int64_t t = i / chunks;
-    const int c0 = (int)(i % chunks) * CHUNK, c1 = min(c0 + CHUNK, C);
-    float top = 0.0f;
-    for (int c = c0; c < c1; ++c) {
-        const float v = fabsf((float)x[t * ldx + c]);
-        if (v < INFINITY) top = fmaxf(top, v);
+    using v8 = typename Half<T>::v8;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    int64_t t = id / w.pieces;
+    int p = (int)(id - t * w.pieces);
+    for (; t < w.rows; t += w.step_rows) {
+        const bool in = p * 8 < C;
+        u32x4 raw = {0, 0, 0, 0};
+        if (in) raw = *(const u32x4 *)(x + t * ldx + p * 8);
+        const v8 v = __builtin_bit_cast(v8, raw);
+        float f[8], top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            f[i] = (float)v[i];
+            const float m = fabsf(f[i]);
+            top = fmaxf(top, m < INFINITY ? m : 0.0f);
+        }
+        // (lanes of a chunk are in step: pieces is a multiple of 4, and so is the stride)
+        top = fmaxf(top, __shfl_xor(top, 1));
+        top = fmaxf(top, __shfl_xor(top, 2));
+        const uint32_t ue = unit_exponent(top);
+        const float inv = unit_of(254 - ue);
+        uint32_t out[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int k = fabsf(f[i]) < INFINITY ? (int)fminf(fmaxf(rintf(f[i] * inv), -127.0f), 127.0f) : -128;
+            out[i >> 2] |= (uint32_t)(k & 255) << (8 * (i & 3));
+        }
+        if (in) *(uint2 *)(q + t * C + p * 8) = make_uint2(out[0], out[1]);
+        if ((p & 3) == 0) e[t * (w.pieces >> 2) + (p >> 2)] = (uint8_t)ue;
+        p += w.step_pieces;
+        if (p >= w.pieces) {
+            p -= w.pieces;
+            ++t;
+        }
     }
-    const uint32_t ue = unit_exponent(top);
-    const float inv = unit_of(254 - ue);
-    for (int c = c0; c < c1; ++c) {
-        const float v = (float)x[t * ldx + c];
-        q[t * C + c] = fabsf(v) < INFINITY ? (int8_t)fminf(fmaxf(rintf(v * inv), -127.0f), 127.0f) : (int8_t)-128;
-    }
-    e[i] = (uint8_t)ue;
 }
 
 template <class T>
 __global__ __launch_bounds__(256)
-void checkpoint_restore_kernel(const int8_t *__restrict__ q, const uint8_t *__restrict__ e, int64_t rows, int C, T *__restrict__ x, int64_t ldx)
+void checkpoint_restore_kernel(const int8_t *__restrict__ q, const uint8_t *__restrict__ e, Walk w, int C, T *__restrict__ x, int64_t ldx)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows * C) return;
-    const int64_t t = i / C;
-    const int c = (int)(i % C);
-    x[t * ldx + c] = (T)kept_value(q[i], unit_of(e[t * ((C + CHUNK - 1) / CHUNK) + c / CHUNK]));
+    using v8 = typename Half<T>::v8;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    int64_t t = id / w.pieces;
+    int p = (int)(id - t * w.pieces);
+    for (; t < w.rows; t += w.step_rows) {
+        if (p * 8 < C) {
+            const uint2 raw = *(const uint2 *)(q + t * C + p * 8);
+            const float u = unit_of(e[t * (w.pieces >> 2) + (p >> 2)]);
+            v8 v;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = (T)kept_value((int)(int8_t)((i < 4 ? raw.x : raw.y) >> (8 * (i & 3))), u);
+            *(u32x4 *)(x + t * ldx + p * 8) = __builtin_bit_cast(u32x4, v);
+        }
+        p += w.step_pieces;
+        if (p >= w.pieces) {
+            p -= w.pieces;
+            ++t;
+        }
+    }
+}
+
+// a grid of at most 8192 workgroups, and the walk of its threads
+unsigned walk_of(int64_t rows, int C, Walk &w)
+{
+    w.rows = rows;
+    w.pieces = (C + 127) / 128 * 16;
+    const int64_t blocks = (rows * w.pieces + 255) / 256, grid = blocks < 8192 ? blocks : 8192;
+    w.step_rows = grid * 256 / w.pieces;
+    w.step_pieces = (int)(grid * 256 % w.pieces);
+    return (unsigned)grid;
 }
 
 }  // namespace
 
 int launch_checkpoint_store(const void *x, int64_t ldx, int64_t rows, int C, int dtype, int8_t *q, uint8_t *e, hipStream_t s)
 {
-    const unsigned blocks = (unsigned)((rows * ((C + CHUNK - 1) / CHUNK) + 255) / 256);
+    Walk w;
+    const unsigned grid = walk_of(rows, C, w);
     if (dtype == SNN_DTYPE_BF16)
-        checkpoint_store_kernel<__bf16><<<blocks, 256, 0, s>>>((const __bf16 *)x, ldx, rows, C, q, e);
+        checkpoint_store_kernel<__bf16><<<grid, 256, 0, s>>>((const __bf16 *)x, ldx, w, C, q, e);
     else
-        checkpoint_store_kernel<_Float16><<<blocks, 256, 0, s>>>((const _Float16 *)x, ldx, rows, C, q, e);
+        checkpoint_store_kernel<_Float16><<<grid, 256, 0, s>>>((const _Float16 *)x, ldx, w, C, q, e);
     return check_launch();
 }
 
 int launch_checkpoint_restore(const int8_t *q, const uint8_t *e, int64_t rows, int C, int dtype, void *x, int64_t ldx, hipStream_t s)
 {
-    const unsigned blocks = (unsigned)((rows * C + 255) / 256);
+    Walk w;
+    const unsigned grid = walk_of(rows, C, w);
     if (dtype == SNN_DTYPE_BF16)
-        checkpoint_restore_kernel<__bf16><<<blocks, 256, 0, s>>>(q, e, rows, C, (__bf16 *)x, ldx);
+        checkpoint_restore_kernel<__bf16><<<grid, 256, 0, s>>>(q, e, w, C, (__bf16 *)x, ldx);
     else
-        checkpoint_restore_kernel<_Float16><<<blocks, 256, 0, s>>>(q, e, rows, C, (_Float16 *)x, ldx);
+        checkpoint_restore_kernel<_Float16><<<grid, 256, 0, s>>>(q, e, w, C, (_Float16 *)x, ldx);
     return check_launch();
 }
 

@@ -33,7 +33,7 @@ inline LinearGeom make_linear_geom(const snn_linear_desc &d)
     return g;
 }
 
-// Rows of one kind of activations: 16-bit values `ld` elements apart, or (e != nullptr) their 8-bit form.
+// Rows of one kind of activations: 16-bit values `ld` elements apart, or (e != nullptr) their 8-bit form, `ld` = the channels.
 struct RowsIn {
     const void *p;
     const uint8_t *e;
@@ -84,6 +84,9 @@ __device__ inline bool weight_negative(const uint32_t *image, int kbs, int n, in
     const int j = k & 7;
     return (w >> (15 - (4 * ((k >> 4) & 3) + (j >> 1)) + 16 * (j & 1))) & 1;
 }
+
+// exponents of a row, in whole words
+__host__ __device__ inline int exponent_words(int C) { return (C + 127) / 128; }
 
 // 2^(e - 127); the stored exponents are 1 .. 254
 __device__ inline float unit_of(uint32_t e) { return __uint_as_float(e << 23); }

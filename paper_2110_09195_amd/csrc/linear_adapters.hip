@@ -9,7 +9,7 @@ template <class T>
 __device__ inline float row_value(const RowsIn &x, int C, int64_t t, int c)
 {
     if (!x.e) return (float)((const T *)x.p)[t * x.ld + c];
-    return kept_value(((const int8_t *)x.p)[t * x.ld + c], unit_of(x.e[t * ((C + 31) / 32) + c / 32]));
+    return kept_value(((const int8_t *)x.p)[t * x.ld + c], unit_of(x.e[t * (4 * exponent_words(C)) + c / 32]));
 }
 
 // low[t][r] = down[a][r] . x[t] and scaled[t][r] = scale[a] times it, a = the row's adapter; down [n][rank][C].

@@ -46,7 +46,7 @@ int rows_call(const snn_linear_desc *desc, bool grad, const void *in, int64_t ld
 }
 
 // the 8-bit form of activations: q rows lie C apart
-bool kept_ok(const int8_t *q, const uint8_t *e, int64_t rows) { return rows == 0 || (q && e && aligned(q, 16)); }
+bool kept_ok(const int8_t *q, const uint8_t *e, int64_t rows) { return rows == 0 || (q && e && aligned(q, 16) && aligned(e, 4)); }
 
 int weight_grad_call(const snn_linear_desc *desc, const RowsIn &x, const void *dy, int64_t lddy, int64_t rows, const int32_t *offsets,
                      const void *weights, size_t weights_bytes, float *dw, float *dalpha, void *workspace, size_t ws_bytes,

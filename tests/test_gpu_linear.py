@@ -192,7 +192,7 @@ def test_checkpoint_values(T, C, pad, dtype):
     if T > 4:
         x[3] = torch.finfo(tdtype).tiny * normal(3, C)       # some of these are below the normal numbers
         x[4] = float("nan")
-    gq, ge = Guarded(T * C, torch.int8), Guarded(T * ((C + 31) // 32), torch.uint8)
+    gq, ge = Guarded(T * C, torch.int8), Guarded(T * ((C + 127) // 128 * 4), torch.uint8)
     kept = B.snn_checkpoint_store(x, q=gq.t.view(T, C), e=ge.t.view(T, -1))
     gq.check("q")
     ge.check("e")
