@@ -65,4 +65,35 @@ __device__ inline void split8(const float *v, typename Half<T>::v8 &hi, typename
     }
 }
 
+// Eight values along the rows (the contracted axis) of a lane's channel, out of a tile of rows in LDS: two reads that exchange the axes
+// of 4 x 16 values within 16 lanes.  `next` bytes further on lie the other four rows.
+template <class T>
+__device__ inline typename Half<T>::v8 read_turned(const char *at, int next)
+{
+    using v4s = __attribute__((ext_vector_type(4))) short;
+    using v8s = __attribute__((ext_vector_type(8))) short;
+    using lds_v4s = __attribute__((address_space(3))) v4s;
+    const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(at));
+    const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(at + next));
+    return __builtin_bit_cast(typename Half<T>::v8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// 16 kept values out of their bytes
+template <class T>
+__device__ inline void widen16(u32x4 raw, float u, typename Half<T>::v8 out[2])
+{
+    bool odd = false;                                          // some byte is -128: not a number
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t z = raw[i] ^ 0x80808080u;
+        odd |= ((z - 0x01010101u) & ~z & 0x80808080u) != 0;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) out[i >> 3][i & 7] = (T)((float)(int8_t)(raw[i >> 2] >> (8 * (i & 3))) * u);
+    if (__builtin_expect(odd, 0)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) out[i >> 3][i & 7] = (T)kept_value((int)(int8_t)(raw[i >> 2] >> (8 * (i & 3))), u);
+    }
+}
+
 }  // namespace snn
