@@ -5,12 +5,21 @@ namespace snn {
 
 namespace {
 
+// v in two values of the activations' type, in planes of their own
+template <class T>
+__device__ inline void split1(float v, T *to, int64_t plane)
+{
+    const T hi = (T)v;
+    to[0] = hi;
+    to[plane] = (T)(v - (float)hi);
+}
+
 // low[t][r] = down[a][r] . x[t] and scaled[t][r] = scale[a] times it, a = the row's adapter; down [n][rank][C].
 // Few rows: a wave an inner product, so that the adapters' matrices, of which nearly every row has its own, are read by many CUs.
 template <class T>
 __global__ __launch_bounds__(256)
 void low_few_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__restrict__ x, int64_t ldx, float *__restrict__ low,
-                    float *__restrict__ scaled)
+                    float *__restrict__ scaled, T *__restrict__ pair, int64_t plane)
 {
     using v8 = typename Half<T>::v8;
     const int t = blockIdx.x, lane = threadIdx.x & 63, r = blockIdx.y * 4 + (threadIdx.x >> 6);
@@ -31,91 +40,186 @@ void low_few_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__r
     if (lane == 0) {
         if (low) low[(int64_t)t * ad.rank + r] = acc;
         scaled[(int64_t)t * ad.rank + r] = acc * c;
+        if (pair) split1(acc * c, pair + (int64_t)t * ad.rank + r, plane);
     }
 }
 
-// Many rows: 32 rows by 32 of the rank on the matrix cores, for each adapter of the 32 rows in turn; the eight waves take the channels
-// in turn and are joined in LDS.
-template <class T>
-__global__ __launch_bounds__(512)
+// Many rows: 32 rows by 32 RB of the rank on the matrix cores, for each adapter of the 32 rows in turn.  The waves take the channels in
+// turn (blocks of 64), rows and matrix both by way of LDS, a wave's own part of it, STAGES in flight without registers; then
+// their sums are joined there.
+template <class T, int RB, int STAGES>
+__global__ __launch_bounds__(256)
 void low_tile_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__restrict__ x, int64_t ldx, int rows,
-                     float *__restrict__ low, float *__restrict__ scaled)
+                     float *__restrict__ low, float *__restrict__ scaled, T *__restrict__ pair, int64_t plane)
 {
     using H = Half<T>;
     using v8 = typename H::v8;
-    constexpr int WAVES = 8;
-    __shared__ float part[WAVES][32][33];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5, ln = lane & 31;
-    const int t0 = blockIdx.x * 32, r0 = blockIdx.y * 32;
+    constexpr int WAVES = 4, STAGE = 4096 * (1 + RB), LOADS = 4 * (1 + RB), PITCH = 32 * RB + 1;
+    extern __shared__ __align__(16) char lds[];
+    float *part = (float *)lds;                                // [WAVES][32][PITCH], when the loads are done
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, ln = lane & 31;
+    const int t0 = blockIdx.x * 32, r0 = blockIdx.y * 32 * RB, here = min(rows - t0, 32), ranks = min(ad.rank - r0, 32 * RB);
     const int t = t0 + ln;
     const int id = t < rows ? ad.of_row[t] : -1;
-    const bool some = id >= 0 && id < ad.n;
-    uint64_t left = __ballot(some);
-    const int rr = tid >> 4, rc = r0 + (tid & 15) * 2;         // what this thread joins and writes
-    const int rid = __shfl(id, rr & 31);
-    const bool rsome = rid >= 0 && rid < ad.n;
-    float v0 = 0.0f, v1 = 0.0f;
-    const T *xr = x + (int64_t)min(t, rows - 1) * ldx + 8 * h;
+    uint64_t left = __ballot(id >= 0 && id < ad.n);
+    const int rr = tid >> 3, rc = (tid & 7) * 4 * RB, rid = __shfl(id, rr);      // what this thread joins and writes: 4 RB sums of a row
+    float sum[4 * RB] = {};
+
+    // a load: 8 rows of 128 bytes, 16-byte pieces xor-ed by half the row's number
+    const int lr = lane >> 3, lp = (lane & 7) ^ (lr >> 1);
+    char *mine = lds + wave * STAGES * STAGE;
+    const uint32_t mine0 = __builtin_amdgcn_readfirstlane(lds_address(mine));
+    const s32x4 rx = resource(x + (int64_t)t0 * ldx, (uint32_t)(here - 1) * (uint32_t)ldx * 2 + C * 2);
+    uint32_t xo[4], piece[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) piece[s] = ln * 128 + (((2 * s + h) ^ ((ln >> 1) & 7)) << 4);
+    const int blocks = (C + 63) / 64;
     while (left) {
         const int a = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
-        left &= ~__ballot(id == a);
-        const T *dr = down + ((int64_t)a * ad.rank + min(r0 + ln, ad.rank - 1)) * C + 8 * h;
-        f32x16 acc = {};
-#pragma unroll 4
-        for (int k = wave * 16; k < C; k += WAVES * 16) {
-            u32x4 u = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-            if (k + 8 * h < C) {
-                u = *(const u32x4 *)(dr + k);
-                if (id == a) v = *(const u32x4 *)(xr + k);
-            }
-            acc = H::mfma(__builtin_bit_cast(v8, u), __builtin_bit_cast(v8, v), acc);
-        }
+        const uint64_t own = __ballot(id == a);
+        left &= ~own;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) part[wave][ln][8 * (i >> 2) + 4 * h + (i & 3)] = acc[i];
+        for (int i = 0; i < 4; ++i) {                          // (rows 8 i + lr: their half's number ends in 4 i + lr / 2)
+            const int r = 8 * i + lr;
+            xo[i] = (own >> r) & 1 ? (uint32_t)r * (uint32_t)ldx * 2 + ((lp ^ ((4 * i) & 7)) << 4) : NOWHERE;
+        }
+        const s32x4 rd = resource(down + ((int64_t)a * ad.rank + r0) * C, (uint32_t)ranks * C * 2);
+        auto issue = [&](int k, int slot) {
+            const uint32_t at = __builtin_amdgcn_readfirstlane(mine0 + slot * STAGE);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int c = lp ^ ((4 * i) & 7);
+                load_lds16(at + i * 1024, k * 64 + c * 8 < C ? xo[i] + k * 128 : NOWHERE, rx);
+            }
+#pragma unroll
+            for (int i = 0; i < 4 * RB; ++i) {
+                const int c = lp ^ ((4 * i) & 7), r = 8 * i + lr;
+                load_lds16(at + 4096 + i * 1024, k * 64 + c * 8 < C && r < ranks ? (uint32_t)r * C * 2 + (c << 4) + k * 128 : NOWHERE, rd);
+            }
+        };
+        f32x16 acc[RB] = {};
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s) issue(wave + s * WAVES, s);
+        int slot = 0;
+        for (int k = wave; k < blocks; k += WAVES) {
+            issue(k + (STAGES - 1) * WAVES, slot == 0 ? STAGES - 1 : slot - 1);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS * (STAGES - 1)) : "memory");
+            const char *at = mine + slot * STAGE;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const v8 v = *(const v8 *)(at + piece[s]);
+#pragma unroll
+                for (int i = 0; i < RB; ++i) acc[i] = H::mfma(*(const v8 *)(at + 4096 + i * 4096 + piece[s]), v, acc[i]);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            slot = slot == STAGES - 1 ? 0 : slot + 1;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < RB; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) part[(wave * 32 + ln) * PITCH + j * 32 + 8 * (i >> 2) + 4 * h + (i & 3)] = acc[j][i];
         __syncthreads();
         if (rid == a) {
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) {
-                v0 += part[w][rr][(tid & 15) * 2];
-                v1 += part[w][rr][(tid & 15) * 2 + 1];
-            }
+            for (int w = 0; w < WAVES; ++w)
+#pragma unroll
+                for (int i = 0; i < 4 * RB; ++i) sum[i] += part[(w * 32 + rr) * PITCH + rc + i];
         }
         __syncthreads();
     }
-    if (t0 + rr >= rows || rc >= ad.rank) return;
-    const float c = rsome ? ad.scale[rid] : 0.0f;
-    const int64_t at = (int64_t)(t0 + rr) * ad.rank + rc;
-    if (low) *(float2 *)(low + at) = make_float2(v0, v1);
-    *(float2 *)(scaled + at) = rsome ? make_float2(v0 * c, v1 * c) : make_float2(0.0f, 0.0f);
+    if (rr >= here) return;
+    const bool some = rid >= 0 && rid < ad.n;
+    const float c = some ? ad.scale[rid] : 0.0f;
+    const int64_t at = (int64_t)(t0 + rr) * ad.rank + r0 + rc;
+#pragma unroll
+    for (int i = 0; i < 4 * RB; i += 4) {
+        if (rc + i >= ranks) break;
+        const f32x4 v = {sum[i], sum[i + 1], sum[i + 2], sum[i + 3]};
+        if (low) *(f32x4 *)(low + at + i) = v;
+        const f32x4 z = some ? v * c : v;
+        *(f32x4 *)(scaled + at + i) = z;
+        if (pair) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) split1(z[k], pair + at + i + k, plane);
+        }
+    }
 }
 
-// [n][R][C] -> [n][C][R], 16-bit values
-__global__ __launch_bounds__(256)
-void transpose_kernel(const uint16_t *__restrict__ in, uint16_t *__restrict__ out, int R, int C)
+// What the backward call needs laid out otherwise, in one launch: A and B with their last two axes exchanged (tiles of 64 x 64), and low in two values
+// of the activations' type.
+struct Exchange {
+    const uint16_t *in;
+    uint16_t *out;
+    int R, C, tiles_r, tiles_c;       // [n][R][C] -> [n][C][R]
+};
+
+__device__ inline void exchange_tile(const Exchange &e, int id, uint16_t (*s)[72])
 {
-    __shared__ uint16_t s[64][66];
-    const int tid = threadIdx.x, c0 = blockIdx.x * 64, r0 = blockIdx.y * 64;
-    const size_t base = (size_t)blockIdx.z * R * C;
-    for (int i = tid; i < 64 * 64; i += 256) {
-        const int r = r0 + i / 64, c = c0 + i % 64;
-        if (r < R && c < C) s[i / 64][i % 64] = in[base + (size_t)r * C + c];
+    const int tid = threadIdx.x, per = e.tiles_r * e.tiles_c, n = id / per, r0 = id % per / e.tiles_c * 64, c0 = id % e.tiles_c * 64;
+    const size_t base = (size_t)n * e.R * e.C;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {                              // (R and C are multiples of 8)
+        const int k = i * 256 + tid, r = k >> 3, c = (k & 7) * 8;
+        if (r0 + r < e.R && c0 + c < e.C) *(u32x4 *)&s[r][c] = *(const u32x4 *)(e.in + base + (size_t)(r0 + r) * e.C + c0 + c);
     }
     __syncthreads();
-    for (int i = tid; i < 64 * 64; i += 256) {
-        const int c = c0 + i / 64, r = r0 + i % 64;
-        if (r < R && c < C) out[base + (size_t)c * R + r] = s[i % 64][i / 64];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int k = i * 256 + tid, c = k >> 3, r = (k & 7) * 8;
+        if (r0 + r >= e.R || c0 + c >= e.C) continue;
+        u32x4 v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = s[r + 2 * j][c] | (uint32_t)s[r + 2 * j + 1][c] << 16;
+        *(u32x4 *)(e.out + base + (size_t)(c0 + c) * e.R + r0 + r) = v;
     }
 }
 
 template <class T>
-int launch_low(int C, const Adapters &ad, const void *down, const void *x, int64_t ldx, int64_t rows, float *low, float *scaled, hipStream_t s)
+__global__ __launch_bounds__(256)
+void adapters_lay_out_kernel(Exchange A, Exchange B, int tiles_a, int tiles_ab, const float *__restrict__ low, T *__restrict__ pair, int64_t values)
 {
-    if (rows <= 64)
-        low_few_kernel<T><<<dim3((unsigned)rows, ad.rank / 4), 256, 0, s>>>(C, ad, (const T *)down, (const T *)x, ldx, low, scaled);
-    else
-        low_tile_kernel<T><<<dim3((unsigned)((rows + 31) / 32), (ad.rank + 31) / 32), 512, 0, s>>>(C, ad, (const T *)down, (const T *)x, ldx,
-                                                                                                 (int)rows, low, scaled);
+    __shared__ __align__(16) uint16_t s[64][72];
+    const int id = blockIdx.x;
+    if (id < tiles_a) exchange_tile(A, id, s);
+    else if (id < tiles_ab) exchange_tile(B, id - tiles_a, s);
+    else {
+        for (int64_t i = ((int64_t)(id - tiles_ab) * 256 + threadIdx.x) * 8; i < values; i += (int64_t)(gridDim.x - tiles_ab) * 2048) {
+            float v[8];
+            *(f32x4 *)v = *(const f32x4 *)(low + i);
+            *(f32x4 *)(v + 4) = *(const f32x4 *)(low + i + 4);
+            typename Half<T>::v8 hi, lo;
+            split8<T>(v, hi, lo);
+            *(typename Half<T>::v8 *)(pair + i) = hi;
+            *(typename Half<T>::v8 *)(pair + values + i) = lo;
+        }
+    }
+}
+
+template <class T, int RB, int STAGES>
+int launch_low_tile(int C, const Adapters &ad, const T *down, const T *x, int64_t ldx, int64_t rows, float *low, float *scaled, T *pair, hipStream_t s)
+{
+    constexpr size_t LDS = (size_t)4 * STAGES * 4096 * (1 + RB);
+    static_assert(LDS >= 4 * 32 * (32 * RB + 1) * sizeof(float) && LDS <= 160 * 1024, "LDS");
+    static LdsGrant grant;
+    const auto kernel = low_tile_kernel<T, RB, STAGES>;
+    const int rc = grant_dynamic_lds((const void *)kernel, LDS, grant);
+    if (rc != SNN_OK) return rc;
+    kernel<<<dim3((unsigned)((rows + 31) / 32), (ad.rank + 32 * RB - 1) / (32 * RB)), 256, LDS, s>>>(C, ad, down, x, ldx, (int)rows, low, scaled,
+                                                                                                  pair, rows * ad.rank);
     return check_launch();
+}
+
+template <class T>
+int launch_low(int C, const Adapters &ad, const void *down, const void *x, int64_t ldx, int64_t rows, float *low, float *scaled, T *pair, hipStream_t s)
+{
+    if (rows <= 64) {
+        low_few_kernel<T><<<dim3((unsigned)rows, ad.rank / 4), 256, 0, s>>>(C, ad, (const T *)down, (const T *)x, ldx, low, scaled, pair, rows * ad.rank);
+        return check_launch();
+    }
+    if (ad.rank <= 32) return launch_low_tile<T, 1, 4>(C, ad, (const T *)down, (const T *)x, ldx, rows, low, scaled, pair, s);
+    return launch_low_tile<T, 2, 3>(C, ad, (const T *)down, (const T *)x, ldx, rows, low, scaled, pair, s);
 }
 
 // Gradients of an adapter: D[c][r] = sum over its rows of x[t][c] low[t][r], for A (x the inputs, low = dlow) and B (x = dy, low as the
@@ -123,73 +227,79 @@ int launch_low(int C, const Adapters &ad, const void *down, const void *x, int64
 //   - Rows come in chunks of 32.  Lanes look 64 chunks over at once for the adapter's rows, and the waves take the chunks that
 //     have some in turn, each with its own double buffer in LDS, filled without registers; no wave waits for another until the sums are joined.
 //   - Rows of other adapters inside a chunk are not loaded (zeros in LDS, and zeros for their inner products).
-//   - The inner products are held in two values of the activations' type.
+//   - The inner products come in two values of the activations' type, and are turned by the reads of their fragments as the rows are.
 struct AdapterGradArgs {
     RowsIn x;
-    const float *low;
+    const void *pair;                 // the inner products: [2][rows][rank]
     int C;
     void *out;
     bool is_b;                        // out [C][rank] times scale, else [rank][C]
 };
 
-template <int CH, int RB, int W>
+template <int CH, int RB>
 struct AdapterGrad {
-    static constexpr int WAVES = W, X_BYTES = 32 * CH * 2, STAGE = X_BYTES + 32 * RB * 32 * 4 + 256;
-    static constexpr int JOIN = WAVES * 32 * 33 * 4;
-    static constexpr size_t LDS = (size_t)WAVES * 2 * STAGE > JOIN ? (size_t)WAVES * 2 * STAGE : JOIN;
+    static constexpr int WAVES = 4, X_BYTES = 32 * CH * 2, P_BYTES = 32 * RB * 64, STAGE = X_BYTES + 2 * P_BYTES + 256;
+    static constexpr size_t LDS = WAVES * 2 * STAGE;
+    static_assert(LDS >= WAVES * 32 * 33 * 4 && LDS <= 160 * 1024, "LDS");
 };
 
-template <class T, bool KEPT, int CH, int RB, int WAVES>
-__device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradArgs &g, int a, int c0, int r0, int rows, char *lds)
+// How 32-byte pieces of a row of `bytes` bytes are exchanged in LDS, so that those of rows 0 .. 3 lie in different banks.
+__device__ constexpr int piece_turn(int bytes, int row) { return bytes >= 256 ? (row & 3) << 1 : bytes == 128 ? row & 2 : 0; }
+
+template <class T, bool KEPT, int CH, int RB>
+__device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradArgs &g, int a, int c0, int r0, int rows, int chunk0, int chunks, float *part_out,
+                                          uint32_t *flag, char *lds)
 {
     using H = Half<T>;
     using v8 = typename H::v8;
-    using S = AdapterGrad<CH, RB, WAVES>;
-    constexpr int CB = CH / 32;
-    constexpr int PX = KEPT ? CH / 16 : CH / 8, XL = 32 * PX / 64;     // pieces of a row, loads of a lane for a chunk
-    constexpr int LL = RB * 4;                                         // loads of a lane for the inner products of a chunk
-    constexpr int LOADS = XL + LL + (KEPT ? 1 : 0);
+    using S = AdapterGrad<CH, RB>;
+    constexpr int WAVES = S::WAVES, CB = CH / 32;
+    constexpr int PX = KEPT ? CH / 16 : CH / 8, XL = 32 * PX / 64;     // 16-byte pieces of a row, loads of a lane for a chunk
+    constexpr int PP = RB * 4, PL = 32 * PP / 64;                      // the same for a plane of the inner products
+    constexpr int LOADS = XL + 2 * PL + (KEPT ? 1 : 0);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, ln = lane & 31;
     const int x_size = KEPT ? 1 : 2, ew = 4 * exponent_words(g.C);
-    // rows of 64 channels are half of the banks wide: what keeps rows 0 .. 3 apart is their second bit
-    const auto turn = [](int r) { return CH >= 128 ? (r & 3) << 1 : (r & 2); };
     char *mine = lds + wave * 2 * S::STAGE;
     const uint32_t mine0 = lds_address(mine);
 
-    uint32_t xo[XL];
-    int xrow[XL];
+    uint32_t xo[XL], po[PL];
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
         const int r = (i * 64 + lane) / PX, c = lane % PX;
-        xrow[i] = r;
-        xo[i] = (uint32_t)r * (uint32_t)(g.x.ld * x_size) + (KEPT ? c * 16 : ((((c >> 1) ^ turn(r)) << 1) | (c & 1)) * 16);
+        xo[i] = (uint32_t)r * (uint32_t)(g.x.ld * x_size) + (KEPT ? c * 16 : ((((c >> 1) ^ piece_turn(CH * 2, r)) << 1) | (c & 1)) * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < PL; ++i) {
+        const int r = (i * 64 + lane) / PP, c = lane % PP, from = (((c >> 1) ^ piece_turn(RB * 64, r)) << 1) | (c & 1);
+        po[i] = r0 + from * 8 < ad.rank ? (uint32_t)(r * ad.rank + from * 8) * 2 : NOWHERE;
     }
     auto issue = [&](int chunk, uint32_t own, int slot) {
         const int64_t t = (int64_t)chunk * 32;
         const int left = min(rows - (int)t, 32);
         const uint32_t at = __builtin_amdgcn_readfirstlane(mine0 + slot * S::STAGE);
         const s32x4 rx = resource((const char *)g.x.p + (t * g.x.ld + c0) * x_size, (uint32_t)(((left - 1) * g.x.ld + g.C - c0) * x_size));
-        const s32x4 rl = resource(g.low + t * ad.rank + r0, (uint32_t)(left * ad.rank - r0) * 4);
 #pragma unroll
-        for (int i = 0; i < XL; ++i) load_lds16(at + i * 1024, (own >> xrow[i]) & 1 ? xo[i] : NOWHERE, rx);
-        // inner products: rows of RB * 32 in LDS
+        for (int i = 0; i < XL; ++i) load_lds16(at + i * 1024, (own >> ((i * 64 + lane) / PX)) & 1 ? xo[i] : NOWHERE, rx);
 #pragma unroll
-        for (int i = 0; i < LL; ++i) {
-            const int r = (i * 64 + lane) / (RB * 8), c = lane % (RB * 8) * 4;
-            load_lds16(at + S::X_BYTES + i * 1024, ((own >> r) & 1) && r0 + c < ad.rank ? (uint32_t)(r * ad.rank + c) * 4 : NOWHERE, rl);
+        for (int k = 0; k < 2; ++k) {
+            const s32x4 rp = resource((const T *)g.pair + (k * (int64_t)rows + t) * ad.rank + r0, (uint32_t)(left * ad.rank - r0) * 2);
+#pragma unroll
+            for (int i = 0; i < PL; ++i)
+                load_lds16(at + S::X_BYTES + k * S::P_BYTES + i * 1024, (own >> ((i * 64 + lane) / PP)) & 1 ? po[i] : NOWHERE, rp);
         }
         if constexpr (KEPT) {
-            constexpr int EW = CH >= 128 ? CH / 128 : 1;
             const s32x4 re = resource(g.x.e + t * ew + c0 / 128 * 4, (uint32_t)((left - 1) * ew + ew - c0 / 128 * 4));
-            load_lds4(at + S::X_BYTES + 32 * RB * 32 * 4, lane < 32 * EW ? (uint32_t)(lane / EW) * ew + lane % EW * 4 : NOWHERE, re);
+            load_lds4(at + S::X_BYTES + 2 * S::P_BYTES, lane < 32 ? (uint32_t)lane * ew : NOWHERE, re);
         }
     };
 
     f32x16 acc[CB][RB] = {};
     const int q = lane >> 4, rr = (lane & 15) >> 2;
-    uint32_t xa[CB];
+    uint32_t xa[CB], pa[RB];                                   // this lane's place in a tile of rows, and in a plane
 #pragma unroll
-    for (int i = 0; i < CB; ++i) xa[i] = (8 * h + rr) * (CH * 2) + (((2 * i + (q & 1)) ^ turn(rr)) * 32) + (lane & 3) * 8;
+    for (int i = 0; i < CB; ++i) xa[i] = (8 * h + rr) * (CH * 2) + (((2 * i + (q & 1)) ^ piece_turn(CH * 2, rr)) * 32) + (lane & 3) * 8;
+#pragma unroll
+    for (int i = 0; i < RB; ++i) pa[i] = (8 * h + rr) * (RB * 64) + (((2 * i + (q & 1)) ^ piece_turn(RB * 64, rr)) * 32) + (lane & 3) * 8;
 
     auto compute = [&](uint32_t own, int slot) {
         char *at = mine + slot * S::STAGE;
@@ -199,16 +309,18 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
             float u[XL];
 #pragma unroll
             for (int i = 0; i < XL; ++i) {
-                constexpr int EB = CH >= 128 ? CH / 32 : 4;
+                const int r = (i * 64 + lane) / PX;
                 raw[i] = *(const u32x4 *)(at + (i * 64 + lane) * 16);
-                u[i] = unit_of(*(const uint8_t *)(at + S::X_BYTES + 32 * RB * 32 * 4 + xrow[i] * EB + ((c0 & 127) >> 5) + (lane % PX >> 1)));
+                u[i] = unit_of(*(const uint8_t *)(at + S::X_BYTES + 2 * S::P_BYTES + r * 4 + ((c0 & 127) >> 5) + (lane % PX >> 1)));
+                if (!((own >> r) & 1)) u[i] = 0.0f;
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
             for (int i = 0; i < XL; ++i) {
+                const int r = (i * 64 + lane) / PX;
                 v8 v[2];
-                widen16<T>(raw[i], (own >> xrow[i]) & 1 ? u[i] : 0.0f, v);
-                char *to = at + xrow[i] * (CH * 2) + ((lane % PX) ^ turn(xrow[i])) * 32;
+                widen16<T>(raw[i], u[i], v);
+                char *to = at + r * (CH * 2) + ((lane % PX) ^ piece_turn(CH * 2, r)) * 32;
                 *(v8 *)to = v[0];
                 *(v8 *)(to + 16) = v[1];
             }
@@ -216,33 +328,36 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            v8 x[CB];
+            v8 x[CB], z[RB];
 #pragma unroll
             for (int i = 0; i < CB; ++i) x[i] = read_turned<T>(at + xa[i] + s * 16 * (CH * 2), 4 * (CH * 2));
 #pragma unroll
-            for (int j = 0; j < RB; ++j) {
-                float z[8];
+            for (int k = 0; k < 2; ++k) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    z[k] = *(const float *)(at + S::X_BYTES + ((16 * s + 8 * h + k) * (RB * 32) + j * 32 + ln) * 4);
-                v8 hi, lo;
-                split8<T>(z, hi, lo);
+                for (int j = 0; j < RB; ++j)
+                    z[j] = read_turned<T>(at + S::X_BYTES + k * S::P_BYTES + pa[j] + s * 16 * (RB * 64), 4 * (RB * 64));
 #pragma unroll
-                for (int i = 0; i < CB; ++i) {
-                    acc[i][j] = H::mfma(x[i], hi, acc[i][j]);
-                    acc[i][j] = H::mfma(x[i], lo, acc[i][j]);
-                }
+                for (int i = 0; i < CB; ++i)
+#pragma unroll
+                    for (int j = 0; j < RB; ++j) acc[i][j] = H::mfma(x[i], z[j], acc[i][j]);
             }
         }
     };
 
-    const int chunks = (rows + 31) / 32;
-    for (int base = 0; base < chunks; base += 64) {
+    const __amdgpu_buffer_rsrc_t r_ids = buffer(ad.of_row, (uint32_t)rows * 4);
+    bool any = false;
+    for (int base = chunk0; base < chunks; base += 64) {
         uint32_t match = 0;
         const int t = (base + lane) * 32;
-        if (base + lane < chunks)
-            for (int i = 0; i < 32 && t + i < rows; ++i) match |= (ad.of_row[t + i] == a ? 1u : 0u) << i;
+        u32x4 ids[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ids[i] = __builtin_amdgcn_raw_buffer_load_b128(r_ids, (uint32_t)(t + 4 * i) * 4, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) match |= ((int)ids[i >> 2][i & 3] == a ? 1u : 0u) << i;
+        if (t + 32 > rows) match &= t < rows ? (1u << (rows - t)) - 1 : 0u;
+        if (base + lane >= chunks) match = 0;
         uint64_t some = __ballot(match != 0);
+        any |= some != 0;
         // every WAVES-th of the chunks that have rows of this adapter, from the wave's own on
         int skip = wave;
         auto next = [&](int &chunk, uint32_t &own) {
@@ -278,6 +393,10 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
         }
     }
 
+    if (part_out) {
+        if (tid == 0 && flag) *flag = any;
+        if (!any) return;
+    }
     // the waves' sums, 32 x 32 at a time, in their order
     const float scale = g.is_b ? ad.scale[a] : 1.0f;
     float(*part)[32][33] = (float(*)[32][33])lds;
@@ -297,64 +416,104 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
                 for (int w = 0; w < WAVES; ++w) v += part[w][r][c];
                 const int cc = c0 + i * 32 + c, rank = r0 + j * 32 + r;
                 if (cc < g.C && rank < ad.rank) {
-                    const int64_t at = g.is_b ? ((int64_t)a * g.C + cc) * ad.rank + rank : ((int64_t)a * ad.rank + rank) * g.C + cc;
+                    const int64_t at = g.is_b ? (int64_t)cc * ad.rank + rank : (int64_t)rank * g.C + cc;
                     // (an adapter without rows has a gradient of zero, whatever its scale)
-                    ((T *)g.out)[at] = (T)(v == 0.0f ? 0.0f : v * scale);
+                    if (part_out) part_out[at] = v;
+                    else ((T *)g.out)[(int64_t)a * g.C * ad.rank + at] = (T)(v == 0.0f ? 0.0f : v * scale);
                 }
             }
         }
 }
 
-template <class T, bool KEPT, int CH, int RB, int WAVES>
-__global__ __launch_bounds__(64 * WAVES)
-void adapters_grad_kernel(Adapters ad, AdapterGradArgs A, AdapterGradArgs B, int rows, int tiles_a, int tiles)
+template <class T, bool KEPT, int CH, int RB>
+__global__ __launch_bounds__(256)
+void adapters_grad_kernel(Adapters ad, AdapterGradArgs A, AdapterGradArgs B, int rows, int tiles_a, int tiles, float *part, uint32_t *flags)
 {
     extern __shared__ __align__(16) char lds[];
     const int a = blockIdx.x / tiles, tile = blockIdx.x % tiles, r0 = blockIdx.y * RB * 32;
-    if (tile < tiles_a) adapters_grad_tile<T, KEPT, CH, RB, WAVES>(ad, A, a, tile * CH, r0, rows, lds);
-    else adapters_grad_tile<T, false, CH, RB, WAVES>(ad, B, a, (tile - tiles_a) * CH, r0, rows, lds);
+    // part z of the rows, in whole chunks
+    const int all = (rows + 31) / 32, each = (all + (int)gridDim.z - 1) / (int)gridDim.z, chunk0 = blockIdx.z * each, chunks = min(all, chunk0 + each);
+    const int at = blockIdx.z * ad.n + a;
+    if (part) part += (int64_t)at * ad.rank * (A.C + B.C);
+    uint32_t *flag = part && tile == 0 && r0 == 0 ? flags + at : nullptr;
+    if (tile < tiles_a) adapters_grad_tile<T, KEPT, CH, RB>(ad, A, a, tile * CH, r0, rows, chunk0, chunks, part, flag, lds);
+    else adapters_grad_tile<T, false, CH, RB>(ad, B, a, (tile - tiles_a) * CH, r0, rows, chunk0, chunks, part ? part + (int64_t)ad.rank * A.C : nullptr, flag, lds);
 }
 
-template <class T, bool KEPT, int CH, int RB, int WAVES>
-int launch_adapters_grad(const Adapters &ad, const AdapterGradArgs &A, const AdapterGradArgs &B, int64_t rows, hipStream_t s)
+// The parts of the rows in their order, those that had some of the adapter's.
+template <class T>
+__global__ __launch_bounds__(256)
+void adapters_join_kernel(Adapters ad, AdapterGradArgs A, AdapterGradArgs B, const float *__restrict__ part, const uint32_t *__restrict__ flags, int parts)
 {
-    constexpr size_t LDS = AdapterGrad<CH, RB, WAVES>::LDS;
-    static_assert(LDS <= 160 * 1024, "LDS");
+    const int64_t per = (int64_t)ad.rank * (A.C + B.C), in_a = (int64_t)ad.rank * A.C;
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    const int a = blockIdx.y;
+    if (i >= per) return;
+    f32x4 v = {0, 0, 0, 0};
+    for (int s = 0; s < parts; ++s)
+        if (flags[s * ad.n + a]) v += *(const f32x4 *)(part + ((int64_t)s * ad.n + a) * per + i);
+    const bool is_b = i >= in_a;
+    const float scale = is_b ? ad.scale[a] : 1.0f;
+    typename Half<T>::v4 out;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) out[k] = (T)(v[k] == 0.0f ? 0.0f : v[k] * scale);
+    T *to = is_b ? (T *)B.out + (int64_t)a * ad.rank * B.C + (i - in_a) : (T *)A.out + (int64_t)a * in_a + i;
+    *(typename Half<T>::v4 *)to = out;
+}
+
+template <class T, bool KEPT, int RB>
+int launch_adapters_grad(const Adapters &ad, const AdapterGradArgs &A, const AdapterGradArgs &B, int64_t rows, int parts, float *part, uint32_t *flags,
+                         hipStream_t s)
+{
+    constexpr int CH = 128;
+    constexpr size_t LDS = AdapterGrad<CH, RB>::LDS;
     static LdsGrant grant;
-    const auto kernel = adapters_grad_kernel<T, KEPT, CH, RB, WAVES>;
-    const int rc = grant_dynamic_lds((const void *)kernel, LDS, grant);
+    const auto kernel = adapters_grad_kernel<T, KEPT, CH, RB>;
+    int rc = grant_dynamic_lds((const void *)kernel, LDS, grant);
     if (rc != SNN_OK) return rc;
     const int tiles_a = (A.C + CH - 1) / CH, tiles = tiles_a + (B.C + CH - 1) / CH;
-    kernel<<<dim3((unsigned)tiles * ad.n, (ad.rank + RB * 32 - 1) / (RB * 32)), 64 * WAVES, LDS, s>>>(ad, A, B, (int)rows, tiles_a, tiles);
+    kernel<<<dim3((unsigned)tiles * ad.n, (ad.rank + RB * 32 - 1) / (RB * 32), parts), 256, LDS, s>>>(ad, A, B, (int)rows, tiles_a, tiles, parts > 1 ? part : nullptr, flags);
+    rc = check_launch();
+    if (rc != SNN_OK || parts == 1) return rc;
+    adapters_join_kernel<T><<<dim3((unsigned)(((int64_t)ad.rank * (A.C + B.C) / 4 + 255) / 256), ad.n), 256, 0, s>>>(ad, A, B, part, flags, parts);
     return check_launch();
 }
 
-template <class T, bool KEPT>
-int launch_adapters_grad(const Adapters &ad, const AdapterGradArgs &A, const AdapterGradArgs &B, int64_t rows, hipStream_t s)
+// Parts of the rows, joined by another launch: an adapter can have nearly all of them, and then its tiles alone would occupy a
+// fraction of the CUs.  Parts of at least 1024 rows, while the workgroups (most of which find no rows of theirs, and end) stay few.
+int grad_parts(const LinearGeom &g, int n, int64_t rows)
 {
-    if (ad.rank <= 32) return launch_adapters_grad<T, KEPT, 64, 1, 8>(ad, A, B, rows, s);
-    return launch_adapters_grad<T, KEPT, 64, 2, 4>(ad, A, B, rows, s);
+    const int64_t tiles = (int64_t)n * ((g.C_in + 127) / 128 + (g.C_out + 127) / 128);
+    int parts = 1;
+    while (parts < 16 && rows / (2 * parts) >= 1024 && tiles * 2 * parts <= 4096) parts *= 2;
+    return parts;
 }
 
-// the workspace: scaled inner products, A and B with their last two axes exchanged
+// The workspace: scaled inner products (for the backward call also in two values of the activations' type, and low so), A and B with
+// their last two axes exchanged.
 struct Scratch {
     float *scaled;
-    void *At, *Bt;
+    char *pair, *low_pair, *At, *Bt;
+    float *part;                      // sums of parts of the rows, and which parts have some of an adapter's
+    uint32_t *flags;
+    int parts;
     size_t bytes;
 };
 
 Scratch scratch(const LinearGeom &g, int n, int rank, int64_t rows, void *ws)
 {
-    const size_t a = align_up((size_t)rows * rank * 4, 256), b = align_up((size_t)n * rank * g.C_in * 2, 256);
-    char *w = (char *)ws;
-    return {(float *)w, w + a, w + a + b, a + b + align_up((size_t)n * rank * g.C_out * 2, 256)};
+    const int parts = grad_parts(g, n, rows);
+    const size_t z = align_up((size_t)rows * rank * 4, 256), a = align_up((size_t)n * rank * g.C_in * 2, 256), b = align_up((size_t)n * rank * g.C_out * 2, 256);
+    const size_t sums = parts > 1 ? align_up((size_t)parts * n * rank * (g.C_in + g.C_out) * 4, 256) : 0, flags = align_up((size_t)parts * n * 4, 256);
+    char *w = (char *)ws, *e = w + 3 * z + a + b;
+    return {(float *)w, w + z, w + 2 * z, w + 3 * z, w + 3 * z + a, (float *)e, (uint32_t *)(e + sums), parts, 3 * z + a + b + sums + flags};
 }
 
 template <class T>
 int forward(const LinearGeom &g, const Adapters &ad, const void *x, int64_t ldx, int64_t rows, const void *weights, void *y, int64_t ldy,
             float *low, const Scratch &w, hipStream_t s)
 {
-    const int rc = launch_low<T>(g.C_in, ad, ad.A, x, ldx, rows, low, w.scaled, s);
+    const int rc = launch_low<T>(g.C_in, ad, ad.A, x, ldx, rows, low, w.scaled, nullptr, s);
     if (rc != SNN_OK) return rc;
     return launch_linear_rows(g, false, x, ldx, rows, nullptr, weights, y, ldy, &ad, ad.B, w.scaled, s);
 }
@@ -364,15 +523,23 @@ int backward(const LinearGeom &g, const Adapters &ad, const RowsIn &x, const flo
              const void *weights, void *dx, int64_t lddx, void *dA, void *dB, const Scratch &w, hipStream_t s)
 {
     if (rows) {
-        transpose_kernel<<<dim3((g.C_in + 63) / 64, (ad.rank + 63) / 64, ad.n), 256, 0, s>>>((const uint16_t *)ad.A, (uint16_t *)w.At, ad.rank, g.C_in);
-        transpose_kernel<<<dim3((ad.rank + 63) / 64, (g.C_out + 63) / 64, ad.n), 256, 0, s>>>((const uint16_t *)ad.B, (uint16_t *)w.Bt, g.C_out, ad.rank);
-        int rc = launch_low<T>(g.C_out, ad, w.Bt, dy, lddy, rows, nullptr, w.scaled, s);
+        const int rt = (ad.rank + 63) / 64, ct = (g.C_in + 63) / 64, ot = (g.C_out + 63) / 64;
+        const Exchange A = {(const uint16_t *)ad.A, (uint16_t *)w.At, ad.rank, g.C_in, rt, ct};
+        const Exchange B = {(const uint16_t *)ad.B, (uint16_t *)w.Bt, g.C_out, ad.rank, ot, rt};
+        const int64_t values = rows * ad.rank, blocks = (values / 8 + 255) / 256;
+        const int tiles_a = ad.n * rt * ct, tiles_ab = tiles_a + ad.n * rt * ot;
+        adapters_lay_out_kernel<T><<<(unsigned)(tiles_ab + (blocks < 512 ? blocks : 512)), 256, 0, s>>>(A, B, tiles_a, tiles_ab, low, (T *)w.low_pair, values);
+        int rc = check_launch();
+        if (rc != SNN_OK) return rc;
+        rc = launch_low<T>(g.C_out, ad, w.Bt, dy, lddy, rows, nullptr, w.scaled, (T *)w.pair, s);
         if (rc != SNN_OK) return rc;
         rc = launch_linear_rows(g, true, dy, lddy, rows, nullptr, weights, dx, lddx, &ad, w.At, w.scaled, s);
         if (rc != SNN_OK) return rc;
     }
-    const AdapterGradArgs A = {x, w.scaled, g.C_in, dA, false}, B = {{dy, nullptr, lddy}, low, g.C_out, dB, true};
-    return x.e ? launch_adapters_grad<T, true>(ad, A, B, rows, s) : launch_adapters_grad<T, false>(ad, A, B, rows, s);
+    const AdapterGradArgs A = {x, w.pair, g.C_in, dA, false}, B = {{dy, nullptr, lddy}, w.low_pair, g.C_out, dB, true};
+    if (ad.rank <= 32)
+        return x.e ? launch_adapters_grad<T, true, 1>(ad, A, B, rows, w.parts, w.part, w.flags, s) : launch_adapters_grad<T, false, 1>(ad, A, B, rows, w.parts, w.part, w.flags, s);
+    return x.e ? launch_adapters_grad<T, true, 2>(ad, A, B, rows, w.parts, w.part, w.flags, s) : launch_adapters_grad<T, false, 2>(ad, A, B, rows, w.parts, w.part, w.flags, s);
 }
 
 }  // namespace

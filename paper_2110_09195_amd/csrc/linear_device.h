@@ -18,6 +18,7 @@ template <> struct Half<__bf16> {
     using v2 = __attribute__((ext_vector_type(2))) __bf16;
     static constexpr uint32_t ONES = 0x3f803f80u;              // (1, 1)
     static __device__ f32x16 mfma(v8 a, v8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    static __device__ f32x4 mfma16(v8 a, v8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct Half<_Float16> {
     using v8 = __attribute__((ext_vector_type(8))) _Float16;
@@ -25,6 +26,7 @@ template <> struct Half<_Float16> {
     using v2 = __attribute__((ext_vector_type(2))) _Float16;
     static constexpr uint32_t ONES = 0x3c003c00u;
     static __device__ f32x16 mfma(v8 a, v8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+    static __device__ f32x4 mfma16(v8 a, v8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 
 // A buffer resource: loads past `bytes` give zeros.
@@ -37,6 +39,12 @@ __device__ inline s32x4 resource(const void *p, uint32_t bytes)
     r[2] = __builtin_amdgcn_readfirstlane((int)bytes);
     r[3] = 0x00020000;
     return r;
+}
+
+__device__ inline __amdgpu_buffer_rsrc_t buffer(const void *p, uint32_t bytes)
+{
+    const s32x4 r = resource(p, bytes);
+    return __builtin_amdgcn_make_buffer_rsrc((void *)((uint64_t)(uint32_t)r[0] | (uint64_t)(uint32_t)r[1] << 32), 0, r[2], 0x00020000);
 }
 
 __device__ inline uint32_t lds_address(const void *p) { return (uint32_t)(uint64_t)(__attribute__((address_space(3))) const void *)p; }

@@ -1,6 +1,8 @@
 // Rows through sub-bit weights: outputs and the gradient of the inputs (see linear.h for the bits' layout).
 #include "linear_device.h"
 
+#include <math.h>
+
 namespace snn {
 
 namespace {
@@ -82,7 +84,7 @@ struct RowTile {
 };
 
 template <int BT>
-__device__ inline bool find_tile(const int32_t *offsets, int groups, int rows, int col_tiles, RowTile &tile)
+__device__ inline bool find_tile(const int32_t *offsets, int groups, int rows, int col_tiles, const Divisor &col_div, RowTile &tile)
 {
     const int lane = threadIdx.x & 63;
     int total = 0;
@@ -96,12 +98,12 @@ __device__ inline bool find_tile(const int32_t *offsets, int groups, int rows, i
             for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
             total += n;
         }
-    const int64_t tiles = (int64_t)total * col_tiles;
-    const int64_t share = (tiles + 7) / 8, at = blockIdx.x / 8;
-    const int64_t id = (int64_t)(blockIdx.x % 8) * share + at;
+    const uint32_t tiles = (uint32_t)total * col_tiles;        // (no more than the grid has workgroups, whatever the offsets hold: see tile_grid)
+    const uint32_t share = (tiles + 7) / 8, at = blockIdx.x / 8;
+    const uint32_t id = (blockIdx.x % 8) * share + at;
     if (at >= share || id >= tiles) return false;
-    int m = (int)(id / col_tiles);
-    tile.col = (int)(id - (int64_t)m * col_tiles);
+    int m = (int)fast_div(id, col_div);
+    tile.col = (int)id - m * col_tiles;
     if (!offsets) {
         tile.group = 0;
         tile.t0 = m * BT;
@@ -153,12 +155,13 @@ struct RowsArgs {
     void *out;
     int64_t ld_out;
     int N, K, col_tiles;
+    Divisor col_div;                 // by col_tiles
     AdapterShare ad;
 };
 
 // out tile = rows x signs on the matrix cores (D[n][t]: n from the bits, t the rows).
-//   - Rows go to LDS 64 channels at a time (128 bytes a row, 16-byte pieces xor-ed by the row so that a fragment's reads meet no bank
-//     twice), with the 64-channel blocks of the bits; STAGES of these in flight, loaded without registers.
+//   - Rows go to LDS 64 channels at a time (128 bytes a row, 16-byte pieces xor-ed by half the row's number, so that the sixteen
+//     rows that are read at once lie in sixteen different places of the 256 bytes of banks), with the 64-channel blocks of the bits; STAGES of these in flight, loaded without registers.
 //   - Bits become operand registers by a shift and a masked xor (two VALU instructions for 128 weights): the weights cost LDS a
 //     sixteenth of what the rows cost, and HBM as well.
 //   - GRAD: the contracted axis is the output channels, and alpha, on that axis, is what the signs are put on: exact, and free.
@@ -179,7 +182,7 @@ void linear_rows_kernel(RowsArgs p)
     extern __shared__ __align__(16) char lds[];
 
     RowTile tile;
-    if (!find_tile<BT>(p.offsets, p.groups, p.rows, p.col_tiles, tile)) return;
+    if (!find_tile<BT>(p.offsets, p.groups, p.rows, p.col_tiles, p.col_div, tile)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wt = wave % (BT / WT), wn = wave / (BT / WT);
     const int n0 = tile.col * BN, rows = tile.t1 - tile.t0;
@@ -192,58 +195,97 @@ void linear_rows_kernel(RowsArgs p)
 
     // where this thread's pieces come from
     uint32_t xo[XL];
-    const int xr = tid >> 3, xc = (tid & 7) ^ (xr & 7);        // (THREADS / 8 rows further on the row's low three bits are the same)
+    const int xr = tid >> 3, xc = (tid & 7) ^ ((xr >> 1) & 7); // (THREADS / 8 rows further on these bits of the row are the same)
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
         const int r = xr + i * (THREADS / 8);
         xo[i] = r < rows ? (uint32_t)r * row_bytes + xc * 16 : NOWHERE;
     }
     const uint32_t lds0 = lds_address(lds);
-    auto issue = [&](int kb, int slot) {
+    // a quarter of a step's loads
+    auto issue = [&](int kb, int slot, int part) {
         const uint32_t at = __builtin_amdgcn_readfirstlane(lds0 + slot * STAGE);
         const bool in = kb * 64 + xc * 8 < p.K;                // (past the last channel: zeros, whatever the row holds there)
 #pragma unroll
-        for (int i = 0; i < XL; ++i)
+        for (int i = part * XL / 4; i < (part + 1) * XL / 4; ++i)
             load_lds16(at + i * THREADS * 16 + wave * 1024, in ? xo[i] + (uint32_t)kb * 128 : NOWHERE, rx);
+        if (part == 0) {
 #pragma unroll
-        for (int i = 0; i < BL; ++i) {
-            const int nb = n0 / 32 + wave * BL + i;
-            load_lds4(at + X_BYTES + (wave * BL + i) * 256, kb < p.kbs ? (uint32_t)((nb * p.kbs + kb) * 64 + lane) * 4 : NOWHERE, rb);
+            for (int i = 0; i < BL; ++i) {
+                const int nb = n0 / 32 + wave * BL + i;
+                load_lds4(at + X_BYTES + (wave * BL + i) * 256, kb < p.kbs ? (uint32_t)((nb * p.kbs + kb) * 64 + lane) * 4 : NOWHERE, rb);
+            }
+            if constexpr (GRAD) load_lds4(at + X_BYTES + BIT_BYTES + wave * 256, kb < p.kbs ? (uint32_t)kb * 128 + lane * 4 : NOWHERE, ra);
         }
-        if constexpr (GRAD) load_lds4(at + X_BYTES + BIT_BYTES + wave * 256, kb < p.kbs ? (uint32_t)kb * 128 + lane * 4 : NOWHERE, ra);
     };
 
     f32x16 acc[NB][TB] = {};
-    for (int s = 0; s < STAGES - 1; ++s) issue(s, s);
+    for (int s = 0; s < STAGES - 1; ++s)
+        for (int q = 0; q < 4; ++q) issue(s, s, q);
     const int h = lane >> 5, ln = lane & 31;
     uint32_t piece[4];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) piece[s] = (uint32_t)(wt * WT + ln) * 128 + (((2 * s + h) ^ (ln & 7)) << 4);
+    for (int s = 0; s < 4; ++s) piece[s] = (uint32_t)(wt * WT + ln) * 128 + (((2 * s + h) ^ ((ln >> 1) & 7)) << 4);
 
+    // While the products of 16 channels run, the operands of the next 16 are made: fragments are read from LDS, bits turned into registers.  The
+    // instructions are dealt out between the matrix instructions, in whose shadow they issue.
+    v8 x[2][TB], w[2][NB];
+    uint32_t ones = H::ONES;
+    asm("" : "+v"(ones));                                      // (known to be constant, the masked xor would take two instructions)
+    uint32_t word[NB];
+    auto read_x = [&](int slot, int s, int to) {
+#pragma unroll
+        for (int i = 0; i < TB; ++i) x[to][i] = *(const v8 *)(lds + slot * STAGE + piece[s] + i * 4096);
+    };
+    auto read_word = [&](int slot) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i) word[i] = *(const uint32_t *)(lds + slot * STAGE + X_BYTES + ((wn * NB + i) * 64 + lane) * 4);
+    };
+    uint32_t word_next[NB];
+    auto read_word_next = [&](int slot) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i) word_next[i] = *(const uint32_t *)(lds + slot * STAGE + X_BYTES + ((wn * NB + i) * 64 + lane) * 4);
+    };
+    auto make_w = [&](int slot, int s, int to) {
+        u32x4 one = {ones, ones, ones, ones};
+        if constexpr (GRAD) one = *(const u32x4 *)(lds + slot * STAGE + X_BYTES + BIT_BYTES + wave * 256 + (2 * s + h) * 16);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) w[to][i] = signed_operand<T>(word[i], s, one);
+    };
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LOADS * (STAGES - 2)) : "memory");
+    read_word(0);
+    read_x(0, 0, 0);
+    make_w(0, 0, 0);
     int slot = 0;
     for (int kb = 0; kb < p.kbs; ++kb) {
-        // this stage has landed (the ones behind it may be in flight), and everyone is done with the slot that is loaded next
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS * (STAGES - 2)) : "memory");
-        issue(kb + STAGES - 1, slot == 0 ? STAGES - 1 : slot - 1);
-        const char *at = lds + slot * STAGE;
-        uint32_t word[NB];
-#pragma unroll
-        for (int i = 0; i < NB; ++i) word[i] = *(const uint32_t *)(at + X_BYTES + ((wn * NB + i) * 64 + lane) * 4);
+        // the next step's loads have landed (the ones behind it may be in flight), and everyone is done with the slot that is loaded next
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS * (STAGES - 3)) : "memory");
+        const int free = slot == 0 ? STAGES - 1 : slot - 1, next = slot == STAGES - 1 ? 0 : slot + 1;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            u32x4 one = {H::ONES, H::ONES, H::ONES, H::ONES};
-            if constexpr (GRAD) one = *(const u32x4 *)(at + X_BYTES + BIT_BYTES + wave * 256 + (2 * s + h) * 16);
-            v8 x[TB], w[NB];
+            issue(kb + STAGES - 1, free, s);
+            if (s == 2) read_word_next(next);
+            if (s < 3) {
+                read_x(slot, s + 1, (s + 1) & 1);
+                make_w(slot, s + 1, (s + 1) & 1);
+            } else {
+                read_x(next, 0, 0);
 #pragma unroll
-            for (int i = 0; i < TB; ++i) x[i] = *(const v8 *)(at + piece[s] + i * 4096);
-#pragma unroll
-            for (int i = 0; i < NB; ++i) w[i] = signed_operand<T>(word[i], s, one);
+                for (int i = 0; i < NB; ++i) word[i] = word_next[i];
+                make_w(next, 0, 0);
+            }
 #pragma unroll
             for (int i = 0; i < NB; ++i)
 #pragma unroll
-                for (int j = 0; j < TB; ++j) acc[i][j] = H::mfma(w[i], x[j], acc[i][j]);
+                for (int j = 0; j < TB; ++j) acc[i][j] = H::mfma(w[s & 1][i], x[s & 1][j], acc[i][j]);
+#pragma unroll
+            for (int i = 0; i < NB * TB; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);           // a matrix instruction
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);           // an LDS read
+                __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);           // VALU
+            }
         }
-        slot = slot == STAGES - 1 ? 0 : slot + 1;
+        slot = next;
     }
     // nothing of this workgroup writes to LDS any more, and every wave is done reading
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -323,47 +365,76 @@ void linear_rows_kernel(RowsArgs p)
 }
 
 // ---- few rows ----------------------------------------------------------------------------------------------------
-// 32 rows by 32 columns a workgroup: its eight waves take the contracted channels in turn (blocks of 64), straight from memory (the
-// weights are read once, one bit each, and the rows stay in L2), and their sums are joined in LDS in the order of the waves.
-template <class T, bool GRAD, bool ADAPT>
+// 16 rows by 16 NB columns a workgroup: its eight waves take the contracted channels in turn (blocks of 64) and their sums are joined in
+// LDS in the order of the waves.  The weights are read once, one bit each; what counts is how fast a CU gets at the rows, which every
+// workgroup reads (they stay in L2): neighbouring lanes have to load neighbouring bytes (150 GB/s a CU; with a row a lane, as the operand
+// wants them, 38), so the rows go through LDS, without registers, a wave's own part of it, AHEAD blocks at once.
+template <class T, bool GRAD, bool ADAPT, int NB, int AHEAD>
 __global__ __launch_bounds__(512)
 void linear_few_kernel(RowsArgs p)
 {
     using H = Half<T>;
     using v8 = typename H::v8;
     constexpr int WAVES = 8;
-    __shared__ float part[WAVES][32][33];
+    __shared__ __align__(16) char rows_in[WAVES][AHEAD * 2048];
+    __shared__ float part[WAVES][16][16 * NB + 1];
     RowTile tile;
-    if (!find_tile<32>(p.offsets, p.groups, p.rows, p.col_tiles, tile)) return;
+    if (!find_tile<16>(p.offsets, p.groups, p.rows, p.col_tiles, p.col_div, tile)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int h = lane >> 5, ln = lane & 31;
-    const bool in_rows = tile.t0 + ln < tile.t1;
-    const T *x = (const T *)p.in + (int64_t)(tile.t0 + (in_rows ? ln : 0)) * p.ld_in + 8 * h;
-    const uint32_t *bits = p.image + (size_t)tile.group * p.words + (size_t)tile.col * p.kbs * 64 + lane;
+    const int q = lane >> 4, ln = lane & 15, n0 = tile.col * 16 * NB;
+    const s32x4 rx = resource((const T *)p.in + (int64_t)tile.t0 * p.ld_in, (uint32_t)(tile.t1 - tile.t0 - 1) * (uint32_t)p.ld_in * 2 + p.K * 2);
+    // a load: 16 rows of 64 bytes, four lanes a row, their 16-byte pieces xor-ed by a quarter of the row's number against bank conflicts
+    const int lr = lane >> 2, lp = (lane & 3) ^ ((lane >> 4) & 3);
+    const uint32_t xo = tile.t0 + lr < tile.t1 ? (uint32_t)lr * (uint32_t)p.ld_in * 2 + lp * 16 : NOWHERE;
+    char *mine = rows_in[wave];
+    const uint32_t mine0 = __builtin_amdgcn_readfirstlane(lds_address(mine));
+    const char *from = mine + (4 * ln + (q ^ (ln >> 2))) * 16;
+    // Channels 64 kb + 32 m + 8 q + j of a lane: the half q % 2 of the block's words, steps 2 m + q / 2.
+    const __amdgpu_buffer_rsrc_t rb = buffer(p.image + (size_t)tile.group * p.words, p.words * 4);
+    uint32_t bo[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        const int n = n0 + 16 * i;
+        bo[i] = ((uint32_t)(n >> 5) * p.kbs * 64 + (q & 1) * 32 + (n & 16) + ln) * 4;
+    }
     const T *alpha = (const T *)p.alpha + (size_t)tile.group * p.alpha_stride;
+    const __amdgpu_buffer_rsrc_t ra = buffer(alpha, p.alpha_stride * 2);
 
-    f32x16 acc = {};
-#pragma unroll 2
-    for (int kb = wave; kb < p.kbs; kb += WAVES) {
-        const uint32_t word = bits[kb * 64];
-        u32x4 xs[4], one[4];
+    f32x4 acc[NB] = {};
+    for (int k0 = wave; k0 < p.kbs; k0 += WAVES * AHEAD) {
+        uint32_t word[AHEAD][NB];
+        u32x4 one[AHEAD][2];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int k = kb * 64 + 16 * s;
-            xs[s] = u32x4{0, 0, 0, 0};
-            if (in_rows && k + 8 * h < p.K) xs[s] = *(const u32x4 *)(x + k);
-            one[s] = u32x4{H::ONES, H::ONES, H::ONES, H::ONES};
-            if constexpr (GRAD) one[s] = *(const u32x4 *)(alpha + k + 8 * h);
+        for (int a = 0; a < AHEAD; ++a) {
+            const int kb = k0 + a * WAVES;                     // (blocks past the last: zeros for rows)
+#pragma unroll
+            for (int i = 0; i < NB; ++i) word[a][i] = __builtin_amdgcn_raw_buffer_load_b32(rb, bo[i] + kb * 256, 0, 0);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                one[a][m] = u32x4{H::ONES, H::ONES, H::ONES, H::ONES};
+                if constexpr (GRAD) one[a][m] = __builtin_amdgcn_raw_buffer_load_b128(ra, kb * 128 + m * 64 + 16 * q, 0, 0);
+                load_lds16(mine0 + (a * 2 + m) * 1024, kb * 64 + 32 * m + 8 * lp < p.K ? xo + kb * 128 + m * 64 : NOWHERE, rx);
+            }
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-            acc = H::mfma(signed_operand<T>(word, s, one[s]), __builtin_bit_cast(v8, xs[s]), acc);
+        for (int a = 0; a < AHEAD; ++a)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                const v8 x = *(const v8 *)(from + (a * 2 + m) * 1024);
+#pragma unroll
+                for (int i = 0; i < NB; ++i) acc[i] = H::mfma16(signed_operand<T>(word[a][i] << (4 * (q >> 1)), 2 * m, one[a][m]), x, acc[i]);
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 #pragma unroll
-    for (int r = 0; r < 16; ++r) part[wave][ln][8 * (r >> 2) + 4 * h + (r & 3)] = acc[r];
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) part[wave][ln][16 * i + 4 * q + r] = acc[i][r];
     __syncthreads();
 
-    const int r = tid >> 4, c = (tid & 15) * 2, t = tile.t0 + r, n = tile.col * 32 + c;
+    if (tid >= 128 * NB) return;
+    const int r = tid / (8 * NB), c = tid % (8 * NB) * 2, t = tile.t0 + r, n = n0 + c;
     if (t >= tile.t1 || n >= p.N) return;
     float v0 = 0.0f, v1 = 0.0f;
 #pragma unroll
@@ -380,12 +451,12 @@ void linear_few_kernel(RowsArgs p)
         if (a >= 0 && a < p.ad.n) {
             const T *u = (const T *)p.ad.up + ((int64_t)a * p.N + n) * p.ad.rank;
             const float *z = p.ad.low + (int64_t)t * p.ad.rank;
-            for (int q = 0; q < p.ad.rank; q += 8) {
-                const v8 u0 = *(const v8 *)(u + q), u1 = *(const v8 *)(u + p.ad.rank + q);
+            for (int k = 0; k < p.ad.rank; k += 8) {
+                const v8 u0 = *(const v8 *)(u + k), u1 = *(const v8 *)(u + p.ad.rank + k);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    v0 = fmaf(z[q + i], (float)u0[i], v0);
-                    v1 = fmaf(z[q + i], (float)u1[i], v1);
+                    v0 = fmaf(z[k + i], (float)u0[i], v0);
+                    v1 = fmaf(z[k + i], (float)u1[i], v1);
                 }
             }
         }
@@ -425,25 +496,76 @@ int launch_tiles(RowsArgs p, hipStream_t s)
     const int rc = grant_dynamic_lds((const void *)kernel, LDS, grant);
     if (rc != SNN_OK) return rc;
     p.col_tiles = (p.N + BN - 1) / BN;
+    p.col_div = make_divisor(p.col_tiles);
     const int64_t grid = tile_grid(p.rows, p.groups, BT, p.col_tiles);
     if (grid >= ((int64_t)1 << 31)) return SNN_ERR_UNSUPPORTED;
     kernel<<<dim3((unsigned)grid), 64 * WAVES, LDS, s>>>(p);
     return check_launch();
 }
 
+template <class T, bool GRAD, bool ADAPT, int NB, int AHEAD>
+int launch_few(RowsArgs p, hipStream_t s)
+{
+    p.col_tiles = (p.N + 16 * NB - 1) / (16 * NB);
+    p.col_div = make_divisor(p.col_tiles);
+    const int64_t grid = tile_grid(p.rows, p.groups, 16, p.col_tiles);
+    if (grid >= ((int64_t)1 << 31)) return SNN_ERR_UNSUPPORTED;
+    linear_few_kernel<T, GRAD, ADAPT, NB, AHEAD><<<dim3((unsigned)grid), 512, 0, s>>>(p);
+    return check_launch();
+}
+
+// Which tile a call of many rows takes.  Measured for each, in microseconds for 64 contracted channels (4096 -> 4096 bf16, 128 to 8192
+// rows): a tile alone on its CU with most CUs idle, and its share of a CU when all are busy (then the clock is down to 1.8 - 1.9 GHz: such calls are
+// bound by power, and what moves fewer bytes for a product is faster).  A tile is small to spread few rows over the chip and large
+// to be fed with fewer reads: 4096 rows 106 us in 256 x 256, 111 in 128 x 256, 118 in 128 x 128, 127 in 64 x 128, 151 in 32 x 128; 512 rows 67,
+// 38, 25, 24, 25; 128 rows 67, 38, 24, 22, 18.
+struct TileForm {
+    int rows, cols;
+    float alone, share;
+};
+constexpr TileForm TILE_FORMS[] = {{256, 256, 1.05f, 1.57f}, {128, 256, 0.60f, 0.87f}, {128, 128, 0.38f, 0.48f}, {64, 128, 0.33f, 0.27f}, {32, 128, 0.28f, 0.19f}};
+
+int tile_form(int64_t rows, int groups, int N)
+{
+    int best = 0;
+    float least = 0.0f;
+    for (int i = 0; i < (int)(sizeof(TILE_FORMS) / sizeof(TILE_FORMS[0])); ++i) {
+        const TileForm &f = TILE_FORMS[i];
+        // (of several groups, the last tile of each is half full on average)
+        const float used = (float)(rows < groups ? rows : groups);
+        const float down = groups > 1 ? (float)rows / f.rows + 0.5f * used : (float)((rows + f.rows - 1) / f.rows);
+        const float tiles = down * (float)((N + f.cols - 1) / f.cols);
+        const float turns = ceilf(tiles / 256.0f), full = turns * f.share > f.alone ? turns * f.share : f.alone;
+        const float time = f.alone + (full - f.alone) * tiles / (256.0f * turns);
+        if (i == 0 || time < least) {
+            best = i;
+            least = time;
+        }
+    }
+    return best;
+}
+
 template <class T, bool GRAD, bool ADAPT>
 int launch_rows(RowsArgs p, hipStream_t s)
 {
-    const int64_t per_group = (p.rows + p.groups - 1) / p.groups;
-    if (per_group <= 64) {
-        p.col_tiles = (p.N + 31) / 32;
-        const int64_t grid = tile_grid(p.rows, p.groups, 32, p.col_tiles);
-        linear_few_kernel<T, GRAD, ADAPT><<<dim3((unsigned)grid), 512, 0, s>>>(p);
-        return check_launch();
+    // Few rows: up to 1024 workgroups of 16 rows x 64 columns (4096 -> 4096: 256 rows 18 us either way, 64 rows 7.6 against 18; 2048 -> 2048:
+    // 256 rows 7.5 against 11, 512 rows 12 either way; 60 groups 1032 -> 1416: 64 rows 9 either way, 1537 rows 53 against 17).
+    // Narrower ones where they would leave CUs idle: 4096 columns, 16 rows 4.7 us in 16, 5.3 in 32, 7.1 in 64; 64 rows 10.1, 7.5, 7.6;
+    // 100 rows 13.8, 11.6, 11.1.
+    const int64_t used = p.rows < p.groups ? p.rows : p.groups, tiles = (p.rows + used * 15) / 16;
+    if (tiles * ((p.N + 63) / 64) <= 1024) {
+        const int64_t narrow = tiles * ((p.N + 15) / 16);
+        if (narrow <= 256) return launch_few<T, GRAD, ADAPT, 1, 2>(p, s);
+        if (narrow <= 1024) return launch_few<T, GRAD, ADAPT, 2, 2>(p, s);
+        return launch_few<T, GRAD, ADAPT, 4, 1>(p, s);
     }
-    const int64_t large = (int64_t)((p.rows + 255) / 256) * ((p.N + 255) / 256);
-    if (per_group >= 256 && large >= 200) return launch_tiles<T, GRAD, ADAPT, 256, 256, 128, 64, 4>(p, s);
-    return launch_tiles<T, GRAD, ADAPT, 128, 128, 64, 64, 4>(p, s);
+    switch (tile_form(p.rows, p.groups, p.N)) {
+    case 0: return launch_tiles<T, GRAD, ADAPT, 256, 256, 128, 64, 4>(p, s);
+    case 1: return launch_tiles<T, GRAD, ADAPT, 128, 256, 128, 64, 4>(p, s);
+    case 2: return launch_tiles<T, GRAD, ADAPT, 128, 128, 128, 32, 4>(p, s);
+    case 3: return launch_tiles<T, GRAD, ADAPT, 64, 128, 64, 32, 4>(p, s);
+    default: return launch_tiles<T, GRAD, ADAPT, 32, 128, 32, 32, 4>(p, s);
+    }
 }
 
 template <class T>

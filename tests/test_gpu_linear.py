@@ -283,7 +283,7 @@ ADAPTED = [
     (1, 64, 64, 3, 8, "each"), (5, 72, 40, 4, 8, "each"), (16, 512, 264, 40, 16, "each"), (48, 136, 1032, 9, 128, "each"),
     (70, 1024, 512, 5, 24, "wild"), (100, 200, 96, 3, 64, "runs"), (333, 320, 256, 6, 40, "runs"), (300, 64, 72, 2, 16, "none"),
     (513, 256, 520, 4, 32, "sorted"), (1000, 776, 1032, 7, 72, "runs"), (700, 512, 512, 1, 128, "sorted"), (300, 128, 128, 90, 8, "each"),
-    (4000, 136, 4104, 5, 24, "runs"), (4000, 4104, 136, 3, 40, "wild"),
+    (4500, 136, 4104, 5, 24, "runs"), (4000, 4104, 136, 3, 40, "wild"), (500, 1032, 1416, 12, 72, "runs"), (400, 1416, 1032, 12, 24, "wild"),
 ]
 
 
