@@ -112,6 +112,9 @@ def _use(L):
     names = ("snn_subbit_conv2d", "snn_subbit_conv2d_prepared", "snn_subbit_conv2d_sign_prepared", "snn_subbit_conv1x1_prepared",
              "snn_bnn_conv2d_prepared", "snn_pack_activations", "snn_packed_bytes", "snn_project_backward", "snn_subset_update")
     _marshal.use(snn_conv_desc, SnnError, tuple(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in names))
+    linear = ("snn_linear_forward", "snn_linear_input_grad", "snn_checkpoint_store", "snn_checkpoint_restore", "snn_adapters_workspace_bytes",
+              "snn_adapters_forward")
+    _marshal.use_linear(snn_linear_desc, tuple(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in linear))
     _lib, _fast = L, _marshal
 
 
@@ -207,7 +210,7 @@ def lib():
         L.snn_checkpoint_store.restype = i32
         L.snn_checkpoint_restore.argtypes = [vp, vp, i64, i32, i32, vp, i64, vp]
         L.snn_checkpoint_restore.restype = i32
-        L.snn_adapters_workspace_bytes.argtypes = [lp, ap, i64]
+        L.snn_adapters_workspace_bytes.argtypes = [lp, ap, i64, i32]
         L.snn_adapters_workspace_bytes.restype = sz
         L.snn_adapters_forward.argtypes = [lp, ap, vp, i64, i64, vp, vp, sz, vp, i64, vp, vp, sz, vp]
         L.snn_adapters_forward.restype = i32
@@ -890,6 +893,8 @@ def snn_linear_prepare(desc, codebook8, idx, alpha, weights=None):
 
 def snn_linear_forward(desc, x, weights, offsets=None, y=None):
     """x [rows][C_in], rows sorted by group as offsets (int32 [groups + 1]) says -> y [rows][C_out]."""
+    if _fast and (r := _fast.linear_forward(desc, x, weights, offsets, y)) is not False:
+        return r
     px, ldx = _rows(x, _dtype_of(desc), desc.C_in, "x")
     y, py, ldy = _rows_out(y, x.shape[0], desc.C_out, x, "y")
     _check(lib().snn_linear_forward(ctypes.byref(desc), px, ldx, x.shape[0], _offsets(desc, offsets), *_weights(weights), py, ldy,
@@ -899,6 +904,8 @@ def snn_linear_forward(desc, x, weights, offsets=None, y=None):
 
 def snn_linear_input_grad(desc, dy, weights, offsets=None, dx=None):
     """dy [rows][C_out] -> dx [rows][C_in]."""
+    if _fast and (r := _fast.linear_input_grad(desc, dy, weights, offsets, dx)) is not False:
+        return r
     pdy, lddy = _rows(dy, _dtype_of(desc), desc.C_out, "dy")
     dx, pdx, lddx = _rows_out(dx, dy.shape[0], desc.C_in, dy, "dx")
     _check(lib().snn_linear_input_grad(ctypes.byref(desc), pdy, lddy, dy.shape[0], _offsets(desc, offsets), *_weights(weights), pdx,
@@ -931,6 +938,8 @@ def snn_linear_weight_grad(desc, x, dy, weights, offsets=None, dw=None, dalpha=N
 
 def snn_checkpoint_store(x, q=None, e=None):
     """x [rows][C] -> (q int8 [rows][C], e uint8 [rows][4 ceil(C / 128)]), its 8-bit form."""
+    if _fast and (r := _fast.checkpoint_store(x, q, e)) is not False:
+        return r
     if not isinstance(x, torch.Tensor) or x.dtype not in _LINEAR_DTYPE or x.dim() != 2:
         raise TypeError("x must be a CUDA tensor [rows][C] of torch.bfloat16 or torch.float16")
     rows, C = x.shape
@@ -944,10 +953,12 @@ def snn_checkpoint_store(x, q=None, e=None):
 def snn_checkpoint_restore(kept, dtype, x=None):
     """What snn_checkpoint_store returned -> the values it stands for, [rows][C] of dtype."""
     q, e = kept
-    rows, C = q.shape
-    pq, pe = _kept(kept, rows, C)
     if dtype not in _LINEAR_DTYPE:
         raise TypeError("dtype must be torch.bfloat16 or torch.float16")
+    if _fast and (r := _fast.checkpoint_restore(q, e, _LINEAR_DTYPE.index(dtype), x)) is not False:
+        return r
+    rows, C = q.shape
+    pq, pe = _kept(kept, rows, C)
     if x is None:
         x = torch.empty((rows, C), dtype=dtype, device=q.device)
     elif x.shape[0] != rows:
@@ -975,13 +986,15 @@ def _of_row(adapter, rows):
     return adapter.data_ptr()
 
 
-def snn_adapters_workspace_bytes(desc, adapters, rows):
-    return int(lib().snn_adapters_workspace_bytes(ctypes.byref(desc), ctypes.byref(adapters), rows))
+def snn_adapters_workspace_bytes(desc, adapters, rows, backward=False):
+    return int(lib().snn_adapters_workspace_bytes(ctypes.byref(desc), ctypes.byref(adapters), rows, int(backward)))
 
 
 def snn_adapters_forward(desc, x, weights, adapter, A, B, scale, y=None, low=None, workspace=None):
     """x [rows][C_in] through the shared projection and each row's adapter (int32 [rows], outside 0 .. n - 1: none);
     A [n][rank][C_in], B [n][C_out][rank], scale float32 [n] -> y [rows][C_out], low float32 [rows][rank]."""
+    if _fast and (r := _fast.adapters_forward(desc, x, weights, adapter, A, B, scale, y, low, workspace)) is not False:
+        return r
     rows = x.shape[0]
     px, ldx = _rows(x, _dtype_of(desc), desc.C_in, "x")
     ad = _adapters(desc, A, B, scale)
@@ -1006,7 +1019,7 @@ def snn_adapters_backward(desc, x, low, dy, weights, adapter, A, B, scale, dx=No
     dx, pdx, lddx = _rows_out(dx, rows, desc.C_in, dy, "dx")
     dA = _whole(dA, A.shape, A.dtype, "dA", dy.device)
     dB = _whole(dB, B.shape, B.dtype, "dB", dy.device)
-    workspace = _scratch(workspace, snn_adapters_workspace_bytes(desc, ad, rows), dy.device)
+    workspace = _scratch(workspace, snn_adapters_workspace_bytes(desc, ad, rows, True), dy.device)
     rest = (_ptr(low), pdy, lddy, rows, _of_row(adapter, rows), *_weights(weights), pdx, lddx, _ptr(dA), _ptr(dB), _ptr(workspace),
             workspace.numel(), _stream())
     if kept:

@@ -489,8 +489,8 @@ int grad_parts(const LinearGeom &g, int n, int64_t rows)
     return parts;
 }
 
-// The workspace: scaled inner products (for the backward call also in two values of the activations' type, and low so), A and B with
-// their last two axes exchanged.
+// The backward call's workspace: scaled inner products, also in two values of the activations' type, and low so; A and B with
+// their last two axes exchanged.  (The forward call's: scaled inner products.)
 struct Scratch {
     float *scaled;
     char *pair, *low_pair, *At, *Bt;
@@ -511,11 +511,11 @@ Scratch scratch(const LinearGeom &g, int n, int rank, int64_t rows, void *ws)
 
 template <class T>
 int forward(const LinearGeom &g, const Adapters &ad, const void *x, int64_t ldx, int64_t rows, const void *weights, void *y, int64_t ldy,
-            float *low, const Scratch &w, hipStream_t s)
+            float *low, float *scaled, hipStream_t s)
 {
-    const int rc = launch_low<T>(g.C_in, ad, ad.A, x, ldx, rows, low, w.scaled, nullptr, s);
+    const int rc = launch_low<T>(g.C_in, ad, ad.A, x, ldx, rows, low, scaled, nullptr, s);
     if (rc != SNN_OK) return rc;
-    return launch_linear_rows(g, false, x, ldx, rows, nullptr, weights, y, ldy, &ad, ad.B, w.scaled, s);
+    return launch_linear_rows(g, false, x, ldx, rows, nullptr, weights, y, ldy, &ad, ad.B, scaled, s);
 }
 
 template <class T>
@@ -544,14 +544,16 @@ int backward(const LinearGeom &g, const Adapters &ad, const RowsIn &x, const flo
 
 }  // namespace
 
-size_t adapters_workspace_bytes(const LinearGeom &g, int n, int rank, int64_t rows) { return scratch(g, n, rank, rows, nullptr).bytes; }
+size_t adapters_workspace_bytes(const LinearGeom &g, int n, int rank, int64_t rows, bool backward)
+{
+    return backward ? scratch(g, n, rank, rows, nullptr).bytes : align_up((size_t)rows * rank * 4 + 256, 256);
+}
 
 int launch_adapters_forward(const LinearGeom &g, const Adapters &ad, const void *x, int64_t ldx, int64_t rows, const void *weights,
                             void *y, int64_t ldy, float *low, void *ws, hipStream_t s)
 {
-    const Scratch w = scratch(g, ad.n, ad.rank, rows, ws);
-    return g.dtype == SNN_DTYPE_BF16 ? forward<__bf16>(g, ad, x, ldx, rows, weights, y, ldy, low, w, s)
-                                     : forward<_Float16>(g, ad, x, ldx, rows, weights, y, ldy, low, w, s);
+    return g.dtype == SNN_DTYPE_BF16 ? forward<__bf16>(g, ad, x, ldx, rows, weights, y, ldy, low, (float *)ws, s)
+                                     : forward<_Float16>(g, ad, x, ldx, rows, weights, y, ldy, low, (float *)ws, s);
 }
 
 int launch_adapters_backward(const LinearGeom &g, const Adapters &ad, const RowsIn &x, const float *low, const void *dy, int64_t lddy,

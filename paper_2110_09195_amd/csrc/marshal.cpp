@@ -4,7 +4,7 @@
 // descriptor, pointers, the stream's handle and the conversion of nine arguments were the rest.  Here they take 0.3 us.
 //
 // A function here takes the ordinary case alone: plain torch.Tensor objects of the right type and size, on the GPU and contiguous, outputs and
-// workspace given.  It returns true if it has enqueued the call.  For anything else, and where the library has refused the arguments (nothing
+// workspace given (those of projections make what is not given).  It returns true, or the outputs, if it has enqueued the call.  For anything else, and where the library has refused the arguments (nothing
 // is enqueued then), it returns false, and the caller goes on with its own checks, which say what is wrong.  Any other status raises here and
 // now: after SNN_ERR_LAUNCH some of the call's work may be on the stream (the error can be that of a second launch, or of some earlier
 // call on the thread), and a second call would do it twice.  Nothing is kept between calls.
@@ -34,7 +34,15 @@ struct Library {
     decltype(&snn_subset_update) subset_update;
 };
 Library lib;
-PyTypeObject *desc_type = nullptr;
+struct LinearLibrary {
+    decltype(&snn_linear_forward) forward, input_grad;
+    decltype(&snn_checkpoint_store) checkpoint_store;
+    decltype(&snn_checkpoint_restore) checkpoint_restore;
+    decltype(&snn_adapters_workspace_bytes) adapters_workspace_bytes;
+    decltype(&snn_adapters_forward) adapters_forward;
+};
+LinearLibrary linear;
+PyTypeObject *desc_type = nullptr, *linear_desc_type = nullptr;
 PyObject *error_type = nullptr;              // called with the status and the function's name
 
 // Plain tensors only: subclasses have their own say in Python.
@@ -227,6 +235,162 @@ PyObject *subset_update(PyObject *const *a)
     return both;
 }
 
+// ---- projections of real-valued activations: rows of contiguous channels, any distance apart ----
+
+bool linear_descriptor(PyObject *o, snn_linear_desc &d)
+{
+    if (Py_TYPE(o) != linear_desc_type) return false;
+    Py_buffer view;
+    if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) {
+        PyErr_Clear();
+        return false;
+    }
+    const bool ok = view.len == (Py_ssize_t)sizeof d;
+    if (ok) std::memcpy(&d, view.buf, sizeof d);
+    PyBuffer_Release(&view);
+    return ok && (d.dtype == SNN_DTYPE_BF16 || d.dtype == SNN_DTYPE_F16);
+}
+
+at::ScalarType type_of(int dtype) { return dtype == SNN_DTYPE_BF16 ? at::kBFloat16 : at::kHalf; }
+
+const at::Tensor *rows_of(PyObject *o, at::ScalarType type, int64_t C)
+{
+    const at::Tensor *const t = tensor(o);
+    return t && t->is_cuda() && t->scalar_type() == type && t->dim() == 2 && t->size(1) == C && t->stride(1) == 1 ? t : nullptr;
+}
+
+int64_t distance(const at::Tensor &t) { return t.size(0) > 1 ? t.stride(0) : std::max(t.size(1), t.stride(0)); }
+
+// The output that the caller gave, or a new one; undefined if what was given is not of the right kind.
+at::Tensor rows_out(PyObject *o, const at::Tensor &like, int64_t rows, int64_t C)
+{
+    if (o == Py_None) return at::empty({rows, C}, like.options().requires_grad(false));
+    const at::Tensor *const t = rows_of(o, like.scalar_type(), C);
+    return t && t->size(0) == rows ? *t : at::Tensor();
+}
+
+// `ok` was true: the outputs in its place
+PyObject *outputs(PyObject *ok, at::Tensor &&a)
+{
+    if (ok != Py_True) return ok;
+    Py_DECREF(ok);
+    return THPVariable_Wrap(std::move(a));
+}
+
+PyObject *outputs(PyObject *ok, at::Tensor &&a, at::Tensor &&b)
+{
+    if (ok != Py_True) return ok;
+    Py_DECREF(ok);
+    PyObject *const pa = THPVariable_Wrap(std::move(a)), *const pb = THPVariable_Wrap(std::move(b));
+    PyObject *const both = pa && pb ? PyTuple_Pack(2, pa, pb) : nullptr;
+    Py_XDECREF(pa);
+    Py_XDECREF(pb);
+    return both;
+}
+
+// desc, rows in, weights, offsets or None, rows out or None
+template <bool GRAD>
+PyObject *linear_rows(PyObject *const *a)
+{
+    snn_linear_desc d;
+    const at::Tensor *x, *w, *off = nullptr;
+    if (!linear_descriptor(a[0], d) || !(x = rows_of(a[1], type_of(d.dtype), GRAD ? d.C_out : d.C_in)) || !(w = checked(a[2], at::kByte))) Py_RETURN_FALSE;
+    if (a[3] != Py_None && (!(off = checked(a[3], at::kInt)) || off->numel() != (int64_t)d.groups + 1)) Py_RETURN_FALSE;
+    const int64_t rows = x->size(0);
+    at::Tensor y = rows_out(a[4], *x, rows, GRAD ? d.C_in : d.C_out);
+    if (!y.defined()) Py_RETURN_FALSE;
+    const void *const px = x->data_ptr(), *const pw = w->data_ptr();
+    const int32_t *const po = off ? (const int32_t *)off->data_ptr() : nullptr;
+    void *const py = y.data_ptr(), *const s = stream();
+    const int64_t ldx = distance(*x), ldy = distance(y);
+    const size_t bytes = (size_t)w->numel();
+    return outputs(enqueued(GRAD ? "snn_linear_input_grad" : "snn_linear_forward", [&] {
+        return (GRAD ? linear.input_grad : linear.forward)(&d, px, ldx, rows, po, pw, bytes, py, ldy, s);
+    }), std::move(y));
+}
+
+// rows in, q or None, e or None
+PyObject *checkpoint_store(PyObject *const *a)
+{
+    const at::Tensor *const x = tensor(a[0]);
+    if (!x || !x->is_cuda() || x->dim() != 2 || x->stride(1) != 1 || (x->scalar_type() != at::kBFloat16 && x->scalar_type() != at::kHalf) ||
+        a[1] != Py_None || a[2] != Py_None)
+        Py_RETURN_FALSE;
+    const int64_t rows = x->size(0), C = x->size(1);
+    if (C > 65536) Py_RETURN_FALSE;
+    at::Tensor q = at::empty({rows, C}, x->options().dtype(at::kChar).requires_grad(false));
+    at::Tensor e = at::empty({rows, (C + 127) / 128 * 4}, x->options().dtype(at::kByte).requires_grad(false));
+    const void *const px = x->data_ptr();
+    void *const pq = q.data_ptr(), *const pe = e.data_ptr(), *const s = stream();
+    const int64_t ldx = distance(*x);
+    const int dtype = x->scalar_type() == at::kBFloat16 ? SNN_DTYPE_BF16 : SNN_DTYPE_F16;
+    return outputs(enqueued("snn_checkpoint_store", [&] {
+        return linear.checkpoint_store(px, ldx, rows, (int)C, dtype, (int8_t *)pq, (uint8_t *)pe, s);
+    }), std::move(q), std::move(e));
+}
+
+// q, e, code of the type, rows out or None
+PyObject *checkpoint_restore(PyObject *const *a)
+{
+    const at::Tensor *const q = checked(a[0], at::kChar), *const e = checked(a[1], at::kByte);
+    if (!q || !e || q->dim() != 2 || e->dim() != 2 || !PyLong_CheckExact(a[2]) || a[3] != Py_None) Py_RETURN_FALSE;
+    const int64_t rows = q->size(0), C = q->size(1);
+    const long dtype = PyLong_AsLong(a[2]);
+    if (C > 65536 || e->size(0) != rows || e->size(1) != (C + 127) / 128 * 4 || (dtype != SNN_DTYPE_BF16 && dtype != SNN_DTYPE_F16)) {
+        PyErr_Clear();
+        Py_RETURN_FALSE;
+    }
+    at::Tensor x = at::empty({rows, C}, q->options().dtype(type_of((int)dtype)));
+    const void *const pq = q->data_ptr(), *const pe = e->data_ptr();
+    void *const px = x.data_ptr(), *const s = stream();
+    return outputs(enqueued("snn_checkpoint_restore", [&] {
+        return linear.checkpoint_restore((const int8_t *)pq, (const uint8_t *)pe, rows, (int)C, (int)dtype, px, C, s);
+    }), std::move(x));
+}
+
+// desc, x, weights, adapter, A, B, scale, y or None, low or None, workspace or None
+PyObject *adapters_forward(PyObject *const *a)
+{
+    snn_linear_desc d;
+    const at::Tensor *x, *w, *ids, *A, *B, *scale;
+    if (!linear_descriptor(a[0], d) || !(x = rows_of(a[1], type_of(d.dtype), d.C_in)) || !(w = checked(a[2], at::kByte)) ||
+        !(ids = checked(a[3], at::kInt)) || !(A = checked(a[4], type_of(d.dtype))) || !(B = checked(a[5], type_of(d.dtype))) ||
+        !(scale = checked(a[6], at::kFloat)) || A->dim() != 3 || B->dim() != 3 || a[8] != Py_None || a[9] != Py_None)
+        Py_RETURN_FALSE;
+    const int64_t rows = x->size(0), n = A->size(0), rank = A->size(1);
+    if (ids->numel() != rows || n > 65536 || rank > 128 || A->size(2) != d.C_in || B->size(0) != n || B->size(1) != d.C_out || B->size(2) != rank ||
+        scale->numel() != n)
+        Py_RETURN_FALSE;
+    snn_adapters ad = {(int32_t)n, (int32_t)rank, A->data_ptr(), B->data_ptr(), (const float *)scale->data_ptr()};
+    at::Tensor y = rows_out(a[7], *x, rows, d.C_out);
+    const size_t need = linear.adapters_workspace_bytes(&d, &ad, rows, 0);
+    if (!y.defined() || !need) Py_RETURN_FALSE;
+    at::Tensor low = at::empty({rows, rank}, scale->options().requires_grad(false));
+    const at::Tensor ws = at::empty({(int64_t)need}, w->options());
+    const void *const px = x->data_ptr(), *const pw = w->data_ptr();
+    const int32_t *const pi = (const int32_t *)ids->data_ptr();
+    void *const py = y.data_ptr(), *const pl = low.data_ptr(), *const pws = ws.data_ptr(), *const s = stream();
+    const int64_t ldx = distance(*x), ldy = distance(y);
+    const size_t bytes = (size_t)w->numel();
+    return outputs(enqueued("snn_adapters_forward", [&] {
+        return linear.adapters_forward(&d, &ad, px, ldx, rows, pi, pw, bytes, py, ldy, (float *)pl, pws, need, s);
+    }), std::move(y), std::move(low));
+}
+
+// use_linear(descriptor type, addresses of the library's functions in the order of LinearLibrary); after use
+PyObject *use_linear(PyObject *, PyObject *args)
+{
+    PyObject *type;
+    unsigned long long f[6];
+    if (!PyArg_ParseTuple(args, "O!(KKKKKK)", &PyType_Type, &type, f, f + 1, f + 2, f + 3, f + 4, f + 5)) return nullptr;
+    static_assert(sizeof(LinearLibrary) == sizeof f, "one address each");
+    std::memcpy(&linear, f, sizeof f);
+    Py_INCREF(type);
+    Py_XDECREF(linear_desc_type);
+    linear_desc_type = (PyTypeObject *)type;
+    Py_RETURN_NONE;
+}
+
 // use(descriptor type, type of the errors, addresses of the library's functions in the order of Library)
 PyObject *use(PyObject *, PyObject *args)
 {
@@ -256,6 +420,12 @@ PyMethodDef methods[] = {
     SNN_FAST(pack_activations, 3),
     SNN_FAST(project_backward, 7),
     SNN_FAST(subset_update, 3),
+    {"use_linear", use_linear, METH_VARARGS, nullptr},
+    {"linear_forward", (PyCFunction)(void (*)(void))guarded<linear_rows<false>, 5>, METH_FASTCALL, nullptr},
+    {"linear_input_grad", (PyCFunction)(void (*)(void))guarded<linear_rows<true>, 5>, METH_FASTCALL, nullptr},
+    SNN_FAST(checkpoint_store, 3),
+    SNN_FAST(checkpoint_restore, 4),
+    SNN_FAST(adapters_forward, 10),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
