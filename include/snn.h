@@ -602,10 +602,11 @@ int snn_checkpoint_restore(const int8_t *q, const uint8_t *e, int64_t rows, int 
  * The second form reads the inputs from their 8-bit form (x's kept values).
  *   dw       device, float [groups][C_out][C_in], 16-byte aligned, fully overwritten (zeros for a group without rows)
  *   dalpha   device, float [groups][C_out], fully overwritten; NULL: not wanted
- *   workspace  device, >= snn_linear_weight_grad_workspace_bytes(desc, rows) bytes, 256-byte aligned
+ *   workspace  device, >= snn_linear_weight_grad_workspace_bytes(desc, rows, 0) bytes (the second form: 1; it holds the kept values
+ *              while the call runs, 2 C_in bytes a row), 256-byte aligned
  * Errors: INVALID_ARG; WORKSPACE (weights, workspace); LAUNCH.
  */
-size_t snn_linear_weight_grad_workspace_bytes(const snn_linear_desc *desc, int64_t rows);
+size_t snn_linear_weight_grad_workspace_bytes(const snn_linear_desc *desc, int64_t rows, int checkpoint);
 int snn_linear_weight_grad(const snn_linear_desc *desc, const void *x, int64_t ldx, const void *dy, int64_t lddy, int64_t rows,
                            const int32_t *offsets, const void *weights, size_t weights_bytes, float *dw, float *dalpha,
                            void *workspace, size_t ws_bytes, void *stream);

@@ -200,7 +200,7 @@ def lib():
         L.snn_linear_forward.restype = i32
         L.snn_linear_input_grad.argtypes = [lp, vp, i64, i64, vp, vp, sz, vp, i64, vp]
         L.snn_linear_input_grad.restype = i32
-        L.snn_linear_weight_grad_workspace_bytes.argtypes = [lp, i64]
+        L.snn_linear_weight_grad_workspace_bytes.argtypes = [lp, i64, i32]
         L.snn_linear_weight_grad_workspace_bytes.restype = sz
         L.snn_linear_weight_grad.argtypes = [lp, vp, i64, vp, i64, i64, vp, vp, sz, vp, vp, vp, sz, vp]
         L.snn_linear_weight_grad.restype = i32
@@ -913,8 +913,8 @@ def snn_linear_input_grad(desc, dy, weights, offsets=None, dx=None):
     return dx
 
 
-def snn_linear_weight_grad_workspace_bytes(desc, rows):
-    return int(lib().snn_linear_weight_grad_workspace_bytes(ctypes.byref(desc), rows))
+def snn_linear_weight_grad_workspace_bytes(desc, rows, checkpoint=False):
+    return int(lib().snn_linear_weight_grad_workspace_bytes(ctypes.byref(desc), rows, int(checkpoint)))
 
 
 def snn_linear_weight_grad(desc, x, dy, weights, offsets=None, dw=None, dalpha=None, workspace=None):
@@ -925,7 +925,7 @@ def snn_linear_weight_grad(desc, x, dy, weights, offsets=None, dw=None, dalpha=N
     kept = _kept(x, rows, desc.C_in)
     dw = _whole(dw, (desc.groups, desc.C_out, desc.C_in), torch.float32, "dw", dy.device)
     dalpha = _whole(dalpha, (desc.groups, desc.C_out), torch.float32, "dalpha", dy.device)
-    workspace = _scratch(workspace, snn_linear_weight_grad_workspace_bytes(desc, rows), dy.device)
+    workspace = _scratch(workspace, snn_linear_weight_grad_workspace_bytes(desc, rows, kept is not None), dy.device)
     rest = (pdy, lddy, rows, _offsets(desc, offsets), *_weights(weights), _ptr(dw), _ptr(dalpha), _ptr(workspace), workspace.numel(), _stream())
     if kept:
         _check(lib().snn_linear_weight_grad_checkpoint(ctypes.byref(desc), *kept, *rest), "snn_linear_weight_grad_checkpoint")

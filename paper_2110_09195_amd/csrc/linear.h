@@ -54,7 +54,7 @@ int launch_linear_prepare(const LinearGeom &g, const uint16_t *codebook, const u
 int launch_linear_rows(const LinearGeom &g, bool grad, const void *in, int64_t ld_in, int64_t rows, const int32_t *offsets,
                        const void *weights, void *out, int64_t ld_out, const Adapters *ad, const void *up, const float *low, hipStream_t s);
 
-size_t linear_weight_grad_workspace_bytes(const LinearGeom &g, int64_t rows);
+size_t linear_weight_grad_workspace_bytes(const LinearGeom &g, int64_t rows, bool kept);
 int launch_linear_weight_grad(const LinearGeom &g, const RowsIn &x, const void *dy, int64_t lddy, int64_t rows, const int32_t *offsets,
                               const void *weights, float *dw, float *dalpha, void *ws, hipStream_t s);
 

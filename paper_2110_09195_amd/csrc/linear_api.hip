@@ -56,7 +56,7 @@ int weight_grad_call(const snn_linear_desc *desc, const RowsIn &x, const void *d
     if (!rows_ok(dy, lddy, desc->C_out, rows) || !dw || !aligned(dw, 16)) return SNN_ERR_INVALID_ARG;
     const LinearGeom g = make_linear_geom(*desc);
     if (!weights_ok(g, weights, weights_bytes)) return SNN_ERR_WORKSPACE;
-    if (!workspace || !aligned(workspace, 256) || ws_bytes < linear_weight_grad_workspace_bytes(g, rows)) return SNN_ERR_WORKSPACE;
+    if (!workspace || !aligned(workspace, 256) || ws_bytes < linear_weight_grad_workspace_bytes(g, rows, x.e != nullptr)) return SNN_ERR_WORKSPACE;
     return launch_linear_weight_grad(g, x, dy, lddy, rows, offsets, weights, dw, dalpha, workspace, (hipStream_t)stream);
 }
 
@@ -117,9 +117,9 @@ int snn_checkpoint_restore(const int8_t *q, const uint8_t *e, int64_t rows, int 
     return launch_checkpoint_restore(q, e, rows, C, dtype, x, ldx, (hipStream_t)stream);
 }
 
-size_t snn_linear_weight_grad_workspace_bytes(const snn_linear_desc *desc, int64_t rows)
+size_t snn_linear_weight_grad_workspace_bytes(const snn_linear_desc *desc, int64_t rows, int checkpoint)
 {
-    return desc_ok(desc) && count_ok(rows) ? linear_weight_grad_workspace_bytes(make_linear_geom(*desc), rows) : 0;
+    return desc_ok(desc) && count_ok(rows) ? linear_weight_grad_workspace_bytes(make_linear_geom(*desc), rows, checkpoint != 0) : 0;
 }
 
 int snn_linear_weight_grad(const snn_linear_desc *desc, const void *x, int64_t ldx, const void *dy, int64_t lddy, int64_t rows,

@@ -223,7 +223,7 @@ def test_weight_grad(shape, dtype, kept):
     off = offsets_of(counts)
     x, dy = L.rows(1, T, ci, pad), L.rows(2, T, co, pad)
     gw, ga = Guarded(G * co * ci, torch.float32, fill=float("nan")), Guarded(G * co, torch.float32, fill=float("nan"))
-    gs = Guarded(max(B.snn_linear_weight_grad_workspace_bytes(L.desc, T), 256), torch.uint8)
+    gs = Guarded(max(B.snn_linear_weight_grad_workspace_bytes(L.desc, T, kept), 256), torch.uint8)
     arg = B.snn_checkpoint_store(x) if kept else x
     dw, da = B.snn_linear_weight_grad(L.desc, arg, dy, L.weights, offsets=off, dw=gw.t.view(G, co, ci), dalpha=ga.t.view(G, co), workspace=gs.t)
     gw.check("dw")
