@@ -7,58 +7,109 @@ namespace snn {
 
 namespace {
 
-// The member bits of a block of 64 output channels by 64 vectors (512 input channels), turned into the words of both images.
+// ---- the images of the weights ---------------------------------------------------------------------------------
+// A block of 64 output channels by 64 vectors (512 input channels).  A member's byte is kept with the bits of its odd elements (1, 3, 5, 7 from the top) in the
+// high nibble and those of its even ones in the low one, set for -1: in that order four bytes make a word by their nibbles alone (linear.h).
+// F takes the bytes as they are; for D, 8 x 8 bits (the members of 8 outputs) are turned by three exchanges of bits.
 constexpr int PREP_O = 64, PREP_V = 64, PREP_THREADS = 256;
+
+// The word of four bytes B0 .. B3, given with B0 at the top: low nibbles to the low half, high ones to the high half.
+__device__ inline uint32_t word_of_nibbles(uint32_t b)
+{
+    uint32_t even = b & 0x0f0f0f0fu, odd = (b >> 4) & 0x0f0f0f0fu;
+    even = (even | even >> 4) & 0x00ff00ffu;
+    odd = (odd | odd >> 4) & 0x00ff00ffu;
+    even = (even | even >> 8) & 0xffffu;
+    odd = (odd | odd >> 8) & 0xffffu;
+    return even | odd << 16;
+}
+
+// Bit c of byte r <-> bit r of byte c, of the eight bytes lo (0 .. 3), hi (4 .. 7): 2 x 2 bits, then 2 x 2 such blocks, then those.
+__device__ inline void turn_8x8(uint32_t &lo, uint32_t &hi)
+{
+    uint32_t t = (lo ^ lo >> 7) & 0x00aa00aau;
+    lo ^= t ^ t << 7;
+    t = (hi ^ hi >> 7) & 0x00aa00aau;
+    hi ^= t ^ t << 7;
+    t = (lo ^ lo >> 14) & 0x0000ccccu;
+    lo ^= t ^ t << 14;
+    t = (hi ^ hi >> 14) & 0x0000ccccu;
+    hi ^= t ^ t << 14;
+    t = (lo ^ hi << 4) & 0xf0f0f0f0u;
+    lo ^= t;
+    hi ^= t >> 4;
+}
 
 __global__ __launch_bounds__(PREP_THREADS)
 void linear_prepare_kernel(LinearGeom g, const uint16_t *__restrict__ codebook, const uint16_t *__restrict__ idx,
                            const uint16_t *__restrict__ alpha, uint32_t *__restrict__ image_f, uint32_t *__restrict__ image_d,
                            uint16_t *__restrict__ alpha_out)
 {
-    __shared__ uint8_t code[PREP_O][PREP_V + 4];       // inverted: bit 7 - j set where element j is -1
+    __shared__ __align__(16) uint8_t by_o[PREP_O][PREP_V + 8], by_v[PREP_V][PREP_O + 8];
     __shared__ uint8_t member[256];
     const int tid = threadIdx.x, grp = blockIdx.z;
     const int ob = blockIdx.y, o0 = ob * PREP_O, v0 = blockIdx.x * PREP_V;
     const int V = g.C_in / 8;
     codebook += (size_t)grp * g.K;
     idx += (size_t)grp * g.C_out * V;
-    if (tid < g.K) member[tid] = (uint8_t)~codebook[tid];
-    __syncthreads();
-    for (int i = tid; i < PREP_O * PREP_V; i += PREP_THREADS) {
-        const int o = i / PREP_V, v = i % PREP_V;
-        uint8_t c = 0;
-        if (o0 + o < g.C_out && v0 + v < V) c = member[min((int)idx[(size_t)(o0 + o) * V + v0 + v], g.K - 1)];
-        code[o][v] = c;
+    int k[PREP_O * PREP_V / PREP_THREADS];                     // this thread's indices: all loads before the first use
+#pragma unroll
+    for (int i = 0; i < PREP_O * PREP_V / PREP_THREADS; ++i) {
+        const int n = i * PREP_THREADS + tid, o = o0 + n / PREP_V, v = v0 + n % PREP_V;
+        k[i] = o < g.C_out && v < V ? idx[(size_t)o * V + v] : -1;
+    }
+    if (tid < g.K) {
+        const uint32_t c = ~(uint32_t)codebook[tid];           // element j at bit 7 - j, set for -1
+        uint32_t m = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m |= ((c >> (7 - 2 * r)) & 1u) << (3 - r) | ((c >> (6 - 2 * r)) & 1u) << (7 - r);
+        member[tid] = (uint8_t)m;
     }
     __syncthreads();
-    // F: 2 blocks of 32 outputs x 8 blocks of 64 inputs
-    image_f += (size_t)grp * g.words_f;
-    for (int i = tid; i < 2 * 8 * 64; i += PREP_THREADS) {
-        const int l = i & 63, kbl = (i >> 6) & 7, nbl = i >> 9, h = l >> 5;
-        const int nb = 2 * ob + nbl, kb = v0 / 8 + kbl;
-        if (nb >= g.nb_f || kb >= g.kb_f) continue;
-        uint32_t w = 0;
-        for (int s = 0; s < 4; ++s) {
-            const uint32_t c = code[nbl * 32 + (l & 31)][kbl * 8 + 2 * s + h];
-            for (int r = 0; r < 4; ++r)
-                w |= ((c >> (7 - 2 * r)) & 1u) << (15 - 4 * s - r) | ((c >> (6 - 2 * r)) & 1u) << (31 - 4 * s - r);
-        }
-        image_f[((size_t)nb * g.kb_f + kb) * 64 + l] = w;
+#pragma unroll
+    for (int i = 0; i < PREP_O * PREP_V / PREP_THREADS; ++i) {
+        const int n = i * PREP_THREADS + tid, o = n / PREP_V, v = n % PREP_V;
+        const uint8_t c = k[i] < 0 ? (uint8_t)0 : member[min(k[i], g.K - 1)];
+        by_o[o][v] = c;
+        by_v[v][o] = c;
     }
-    // D: 16 blocks of 32 inputs x this block of 64 outputs
-    image_d += (size_t)grp * g.words_d;
-    for (int i = tid; i < 16 * 64; i += PREP_THREADS) {
-        const int l = i & 63, nbl = i >> 6, h = l >> 5;
-        const int nb = v0 / 4 + nbl;
-        if (nb >= g.nb_d) continue;
-        const int v = nbl * 4 + ((l & 31) >> 3), bit = 7 - (l & 7);
-        uint32_t w = 0;
-        for (int s = 0; s < 4; ++s)
-            for (int r = 0; r < 4; ++r) {
-                const int o = 16 * s + 8 * h + 2 * r;
-                w |= (((uint32_t)code[o][v] >> bit) & 1u) << (15 - 4 * s - r) | (((uint32_t)code[o + 1][v] >> bit) & 1u) << (31 - 4 * s - r);
+    __syncthreads();
+    if (tid < 128) {
+        // F, half h of the words of an output: bytes 2 s + h of its eight of a block of 64 inputs
+        const int h = tid >> 6, o = tid & 63, nb = 2 * ob + (o >> 5);
+        if (nb < g.nb_f) {
+            uint32_t *to = image_f + (size_t)grp * g.words_f + ((size_t)nb * g.kb_f + v0 / 8) * 64 + h * 32 + (o & 31);
+#pragma unroll
+            for (int kb = 0; kb < PREP_V / 8; ++kb) {
+                const u32x2 b = *(const u32x2 *)&by_o[o][kb * 8];
+                const uint32_t four = h ? __builtin_amdgcn_perm(b[0], b[1], 0x05070103u) : __builtin_amdgcn_perm(b[0], b[1], 0x04060002u);
+                if (v0 / 8 + kb < g.kb_f) to[kb * 64] = word_of_nibbles(four);
             }
-        image_d[((size_t)nb * g.kb_d + ob) * 64 + l] = w;
+        }
+    } else {
+        // D, half h of the words of the eight inputs of a vector: outputs 16 s + 8 h + j, turned, then input by input
+        const int h = (tid >> 6) & 1, v = tid & 63, nb = (v0 + v) / 4;
+        if (nb < g.nb_d) {
+            uint32_t lo[4], hi[4];                             // [s]: bytes 0 .. 3 and 4 .. 7 of the turned eight, that is by bit of a member
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const u32x2 b = *(const u32x2 *)&by_v[v][16 * s + 8 * h];
+                lo[s] = __builtin_amdgcn_perm(b[1], b[0], 0x00020406u);       // outputs 6, 4, 2, 0: bits 0 .. 3 of a byte of the word
+                hi[s] = __builtin_amdgcn_perm(b[1], b[0], 0x01030507u);       // 7, 5, 3, 1
+                turn_8x8(lo[s], hi[s]);
+            }
+            uint32_t word[8];                                  // by input j: odd ones from bit 7 - j / 2, even ones from bit 3 - j / 2
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const uint32_t *from = c < 4 ? lo : hi;
+                const uint32_t sel = 0x0c0c0000u | (uint32_t)(c & 3) | (uint32_t)(4 + (c & 3)) << 8;
+                const uint32_t top = __builtin_amdgcn_perm(from[0], from[1], sel), low = __builtin_amdgcn_perm(from[2], from[3], sel);
+                word[c >= 4 ? 2 * (7 - c) + 1 : 2 * (3 - c)] = word_of_nibbles(top << 16 | low);
+            }
+            uint32_t *to = image_d + (size_t)grp * g.words_d + ((size_t)nb * g.kb_d + ob) * 64 + h * 32 + ((v0 + v) & 3) * 8;
+            *(u32x4 *)to = u32x4{word[0], word[1], word[2], word[3]};
+            *(u32x4 *)(to + 4) = u32x4{word[4], word[5], word[6], word[7]};
+        }
     }
     if (blockIdx.x == 0 && tid < PREP_O)
         alpha_out[(size_t)grp * g.alpha_stride + o0 + tid] = o0 + tid < g.C_out ? alpha[(size_t)grp * g.C_out + o0 + tid] : (uint16_t)0;
