@@ -621,7 +621,8 @@ int snn_linear_weight_grad_checkpoint(const snn_linear_desc *desc, const int8_t 
  *   A        device, [n][rank][C_in];   B   device, [n][C_out][rank];   both desc->dtype, 16-byte aligned
  *   scale    device, float [n]
  *   low      device, float [rows][rank], A[a] x[t] in fp32 (zeros without an adapter): what the backward call takes; NULL: not wanted
- *   workspace  device, >= snn_adapters_workspace_bytes(desc, adapters, rows, 0) bytes (the backward call: 1), 256-byte aligned
+ *   workspace  device, >= snn_adapters_workspace_bytes(desc, adapters, rows, call) bytes, `call` the SNN_ADAPTERS_* of the entry point,
+ *              256-byte aligned (A and B of *adapters are not looked at)
  * scale[a] A[a] x[t] is held in two values of desc->dtype (twice its mantissa) in the product with B[a]: for f16 it has to be in that type's range.
  *
  * The backward call, with  dlow[t] = scale[a] * B[a]^T dy[t]:
@@ -636,7 +637,10 @@ typedef struct snn_adapters {
     const void *A, *B;
     const float *scale;
 } snn_adapters;
-size_t snn_adapters_workspace_bytes(const snn_linear_desc *desc, const snn_adapters *adapters, int64_t rows, int backward);
+#define SNN_ADAPTERS_FORWARD             0
+#define SNN_ADAPTERS_BACKWARD            1
+#define SNN_ADAPTERS_BACKWARD_CHECKPOINT 2
+size_t snn_adapters_workspace_bytes(const snn_linear_desc *desc, const snn_adapters *adapters, int64_t rows, int call);
 int snn_adapters_forward(const snn_linear_desc *desc, const snn_adapters *adapters, const void *x, int64_t ldx, int64_t rows,
                          const int32_t *adapter, const void *weights, size_t weights_bytes, void *y, int64_t ldy, float *low,
                          void *workspace, size_t ws_bytes, void *stream);

@@ -986,8 +986,11 @@ def _of_row(adapter, rows):
     return adapter.data_ptr()
 
 
-def snn_adapters_workspace_bytes(desc, adapters, rows, backward=False):
-    return int(lib().snn_adapters_workspace_bytes(ctypes.byref(desc), ctypes.byref(adapters), rows, int(backward)))
+SNN_ADAPTERS_FORWARD, SNN_ADAPTERS_BACKWARD, SNN_ADAPTERS_BACKWARD_CHECKPOINT = range(3)
+
+
+def snn_adapters_workspace_bytes(desc, adapters, rows, call=SNN_ADAPTERS_FORWARD):
+    return int(lib().snn_adapters_workspace_bytes(ctypes.byref(desc), ctypes.byref(adapters), rows, call))
 
 
 def snn_adapters_forward(desc, x, weights, adapter, A, B, scale, y=None, low=None, workspace=None):
@@ -1019,7 +1022,8 @@ def snn_adapters_backward(desc, x, low, dy, weights, adapter, A, B, scale, dx=No
     dx, pdx, lddx = _rows_out(dx, rows, desc.C_in, dy, "dx")
     dA = _whole(dA, A.shape, A.dtype, "dA", dy.device)
     dB = _whole(dB, B.shape, B.dtype, "dB", dy.device)
-    workspace = _scratch(workspace, snn_adapters_workspace_bytes(desc, ad, rows, True), dy.device)
+    workspace = _scratch(workspace, snn_adapters_workspace_bytes(
+        desc, ad, rows, SNN_ADAPTERS_BACKWARD_CHECKPOINT if kept else SNN_ADAPTERS_BACKWARD), dy.device)
     rest = (_ptr(low), pdy, lddy, rows, _of_row(adapter, rows), *_weights(weights), pdx, lddx, _ptr(dA), _ptr(dB), _ptr(workspace),
             workspace.numel(), _stream())
     if kept:

@@ -58,7 +58,7 @@ size_t linear_weight_grad_workspace_bytes(const LinearGeom &g, int64_t rows, boo
 int launch_linear_weight_grad(const LinearGeom &g, const RowsIn &x, const void *dy, int64_t lddy, int64_t rows, const int32_t *offsets,
                               const void *weights, float *dw, float *dalpha, void *ws, hipStream_t s);
 
-size_t adapters_workspace_bytes(const LinearGeom &g, int n, int rank, int64_t rows, bool backward);
+size_t adapters_workspace_bytes(const LinearGeom &g, int n, int rank, int64_t rows, bool backward, bool kept);
 int launch_adapters_forward(const LinearGeom &g, const Adapters &ad, const void *x, int64_t ldx, int64_t rows, const void *weights,
                             void *y, int64_t ldy, float *low, void *ws, hipStream_t s);
 int launch_adapters_backward(const LinearGeom &g, const Adapters &ad, const RowsIn &x, const float *low, const void *dy, int64_t lddy,

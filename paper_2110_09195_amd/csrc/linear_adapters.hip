@@ -222,74 +222,73 @@ int launch_low(int C, const Adapters &ad, const void *down, const void *x, int64
     return launch_low_tile<T, 2, 3>(C, ad, (const T *)down, (const T *)x, ldx, rows, low, scaled, pair, s);
 }
 
-// Gradients of an adapter: D[c][r] = sum over its rows of x[t][c] low[t][r], for A (x the inputs, low = dlow) and B (x = dy, low as the
-// forward call left it, times scale).  A workgroup takes one adapter and CH channels and the whole rank.
-//   - Rows come in chunks of 32.  Lanes look 64 chunks over at once for the adapter's rows, and the waves take the chunks that
-//     have some in turn, each with its own double buffer in LDS, filled without registers; no wave waits for another until the sums are joined.
-//   - Rows of other adapters inside a chunk are not loaded (zeros in LDS, and zeros for their inner products).
-//   - The inner products come in two values of the activations' type, and are turned by the reads of their fragments as the rows are.
+// Gradients of an adapter: the sum over its rows of x[t][c] low[t][r], for A (x the inputs, low = dlow) and B (x = dy, low as the forward
+// call left it, times scale).  A workgroup takes one adapter, 256 channels (64 a wave) and 32 RB of the rank.
+//   - Rows come in chunks of 32.  Lanes look 64 chunks over at once for the adapter's rows, and the chunks that have some are gone through, the loads
+//     of two of them in flight, without registers.  Rows of other adapters inside a chunk are not loaded: zeros in LDS.
+//   - Rows and inner products (in two values of the activations' type) have the contracted axis across memory, and are turned by the reads of their
+//     fragments.
 struct AdapterGradArgs {
-    RowsIn x;
+    const void *x;
+    int64_t ld;
     const void *pair;                 // the inner products: [2][rows][rank]
     int C;
-    void *out;
-    bool is_b;                        // out [C][rank] times scale, else [rank][C]
+    void *out;                        // A: [n][rank][C]; B: [n][C][rank], times scale
 };
 
-template <int CH, int RB>
+template <int RB>
 struct AdapterGrad {
-    static constexpr int WAVES = 4, X_BYTES = 32 * CH * 2, P_BYTES = 32 * RB * 64, STAGE = X_BYTES + 2 * P_BYTES + 256;
-    static constexpr size_t LDS = WAVES * 2 * STAGE;
-    static_assert(LDS >= WAVES * 32 * 33 * 4 && LDS <= 160 * 1024, "LDS");
+    static constexpr int CH = 256, WAVES = 4, STAGES = 3;
+    static constexpr int X_BYTES = 32 * CH * 2, P_BYTES = 32 * RB * 64, STAGE = X_BYTES + 2 * P_BYTES;
+    static constexpr size_t LDS = STAGES * STAGE;
+    static_assert(LDS <= 80 * 1024, "two workgroups a CU");
 };
 
 // How 32-byte pieces of a row of `bytes` bytes are exchanged in LDS, so that those of rows 0 .. 3 lie in different banks.
 __device__ constexpr int piece_turn(int bytes, int row) { return bytes >= 256 ? (row & 3) << 1 : bytes == 128 ? row & 2 : 0; }
 
-template <class T, bool KEPT, int CH, int RB>
+template <class T, bool IS_B, int RB>
 __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradArgs &g, int a, int c0, int r0, int rows, int chunk0, int chunks, float *part_out,
                                           uint32_t *flag, char *lds)
 {
     using H = Half<T>;
     using v8 = typename H::v8;
-    using S = AdapterGrad<CH, RB>;
-    constexpr int WAVES = S::WAVES, CB = CH / 32;
-    constexpr int PX = KEPT ? CH / 16 : CH / 8, XL = 32 * PX / 64;     // 16-byte pieces of a row, loads of a lane for a chunk
-    constexpr int PP = RB * 4, PL = 32 * PP / 64;                      // the same for a plane of the inner products
-    constexpr int LOADS = XL + 2 * PL + (KEPT ? 1 : 0);
+    using S = AdapterGrad<RB>;
+    constexpr int CH = S::CH, STAGES = S::STAGES, THREADS = 64 * S::WAVES, CB = CH / 32 / S::WAVES;
+    constexpr int PX = CH / 8, XL = 32 * PX / THREADS;                      // 16-byte pieces of a row, loads of a thread for a chunk
+    constexpr int PP = RB * 4, PL = 64 * PP / THREADS;                      // the same for the inner products' planes, one after the other
+    constexpr int LOADS = XL + PL;
+    static_assert(XL * THREADS == 32 * PX && PL * THREADS == 64 * PP, "whole loads");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, ln = lane & 31;
-    const int x_size = KEPT ? 1 : 2, ew = 4 * exponent_words(g.C);
-    char *mine = lds + wave * 2 * S::STAGE;
-    const uint32_t mine0 = lds_address(mine);
+    const uint32_t lds0 = lds_address(lds);
 
     uint32_t xo[XL], po[PL];
+    int xr[XL], pr[PL];
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
-        const int r = (i * 64 + lane) / PX, c = lane % PX;
-        xo[i] = (uint32_t)r * (uint32_t)(g.x.ld * x_size) + (KEPT ? c * 16 : ((((c >> 1) ^ piece_turn(CH * 2, r)) << 1) | (c & 1)) * 16);
+        const int r = (i * THREADS + tid) / PX, c = tid % PX;
+        xr[i] = r;
+        xo[i] = (uint32_t)r * (uint32_t)(g.ld * 2) + ((((c >> 1) ^ piece_turn(CH * 2, r)) << 1) | (c & 1)) * 16;
     }
 #pragma unroll
     for (int i = 0; i < PL; ++i) {
-        const int r = (i * 64 + lane) / PP, c = lane % PP, from = (((c >> 1) ^ piece_turn(RB * 64, r)) << 1) | (c & 1);
+        const int r = (i * THREADS + tid) / PP % 32, c = tid % PP, from = (((c >> 1) ^ piece_turn(RB * 64, r)) << 1) | (c & 1);
+        pr[i] = r;
         po[i] = r0 + from * 8 < ad.rank ? (uint32_t)(r * ad.rank + from * 8) * 2 : NOWHERE;
     }
+    // (a chunk that is none: zeros)
     auto issue = [&](int chunk, uint32_t own, int slot) {
         const int64_t t = (int64_t)chunk * 32;
         const int left = min(rows - (int)t, 32);
-        const uint32_t at = __builtin_amdgcn_readfirstlane(mine0 + slot * S::STAGE);
-        const s32x4 rx = resource((const char *)g.x.p + (t * g.x.ld + c0) * x_size, (uint32_t)(((left - 1) * g.x.ld + g.C - c0) * x_size));
+        const uint32_t at = __builtin_amdgcn_readfirstlane(lds0 + slot * S::STAGE);
+        const s32x4 rx = resource((const T *)g.x + t * g.ld + c0, (uint32_t)((left - 1) * (int)g.ld + g.C - c0) * 2);
 #pragma unroll
-        for (int i = 0; i < XL; ++i) load_lds16(at + i * 1024, (own >> ((i * 64 + lane) / PX)) & 1 ? xo[i] : NOWHERE, rx);
+        for (int i = 0; i < XL; ++i) load_lds16(at + i * THREADS * 16 + wave * 1024, (own >> xr[i]) & 1 ? xo[i] : NOWHERE, rx);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const s32x4 rp = resource((const T *)g.pair + (k * (int64_t)rows + t) * ad.rank + r0, (uint32_t)(left * ad.rank - r0) * 2);
-#pragma unroll
-            for (int i = 0; i < PL; ++i)
-                load_lds16(at + S::X_BYTES + k * S::P_BYTES + i * 1024, (own >> ((i * 64 + lane) / PP)) & 1 ? po[i] : NOWHERE, rp);
-        }
-        if constexpr (KEPT) {
-            const s32x4 re = resource(g.x.e + t * ew + c0 / 128 * 4, (uint32_t)((left - 1) * ew + ew - c0 / 128 * 4));
-            load_lds4(at + S::X_BYTES + 2 * S::P_BYTES, lane < 32 ? (uint32_t)lane * ew : NOWHERE, re);
+        for (int i = 0; i < PL; ++i) {
+            const int plane = (i * THREADS + wave * 64) / (32 * PP);         // (whole waves load from one)
+            const s32x4 rp = resource((const T *)g.pair + (plane * (int64_t)rows + t) * ad.rank + r0, (uint32_t)(left * ad.rank - r0) * 2);
+            load_lds16(at + S::X_BYTES + i * THREADS * 16 + wave * 1024, (own >> pr[i]) & 1 ? po[i] : NOWHERE, rp);
         }
     };
 
@@ -297,52 +296,9 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
     const int q = lane >> 4, rr = (lane & 15) >> 2;
     uint32_t xa[CB], pa[RB];                                   // this lane's place in a tile of rows, and in a plane
 #pragma unroll
-    for (int i = 0; i < CB; ++i) xa[i] = (8 * h + rr) * (CH * 2) + (((2 * i + (q & 1)) ^ piece_turn(CH * 2, rr)) * 32) + (lane & 3) * 8;
+    for (int i = 0; i < CB; ++i) xa[i] = (8 * h + rr) * (CH * 2) + (((2 * (wave * CB + i) + (q & 1)) ^ piece_turn(CH * 2, rr)) * 32) + (lane & 3) * 8;
 #pragma unroll
     for (int i = 0; i < RB; ++i) pa[i] = (8 * h + rr) * (RB * 64) + (((2 * i + (q & 1)) ^ piece_turn(RB * 64, rr)) * 32) + (lane & 3) * 8;
-
-    auto compute = [&](uint32_t own, int slot) {
-        char *at = mine + slot * S::STAGE;
-        if constexpr (KEPT) {
-            // a lane's own pieces, widened in place: all of them are read before the first is written
-            u32x4 raw[XL];
-            float u[XL];
-#pragma unroll
-            for (int i = 0; i < XL; ++i) {
-                const int r = (i * 64 + lane) / PX;
-                raw[i] = *(const u32x4 *)(at + (i * 64 + lane) * 16);
-                u[i] = unit_of(*(const uint8_t *)(at + S::X_BYTES + 2 * S::P_BYTES + r * 4 + ((c0 & 127) >> 5) + (lane % PX >> 1)));
-                if (!((own >> r) & 1)) u[i] = 0.0f;
-            }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-            for (int i = 0; i < XL; ++i) {
-                const int r = (i * 64 + lane) / PX;
-                v8 v[2];
-                widen16<T>(raw[i], u[i], v);
-                char *to = at + r * (CH * 2) + ((lane % PX) ^ piece_turn(CH * 2, r)) * 32;
-                *(v8 *)to = v[0];
-                *(v8 *)(to + 16) = v[1];
-            }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        }
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            v8 x[CB], z[RB];
-#pragma unroll
-            for (int i = 0; i < CB; ++i) x[i] = read_turned<T>(at + xa[i] + s * 16 * (CH * 2), 4 * (CH * 2));
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-#pragma unroll
-                for (int j = 0; j < RB; ++j)
-                    z[j] = read_turned<T>(at + S::X_BYTES + k * S::P_BYTES + pa[j] + s * 16 * (RB * 64), 4 * (RB * 64));
-#pragma unroll
-                for (int i = 0; i < CB; ++i)
-#pragma unroll
-                    for (int j = 0; j < RB; ++j) acc[i][j] = H::mfma(x[i], z[j], acc[i][j]);
-            }
-        }
-    };
 
     const __amdgpu_buffer_rsrc_t r_ids = buffer(ad.of_row, (uint32_t)rows * 4);
     bool any = false;
@@ -356,77 +312,82 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
         for (int i = 0; i < 32; ++i) match |= ((int)ids[i >> 2][i & 3] == a ? 1u : 0u) << i;
         if (t + 32 > rows) match &= t < rows ? (1u << (rows - t)) - 1 : 0u;
         if (base + lane >= chunks) match = 0;
-        uint64_t some = __ballot(match != 0);
+        uint64_t some = __ballot(match != 0);                  // (the same in every wave)
         any |= some != 0;
-        // every WAVES-th of the chunks that have rows of this adapter, from the wave's own on
-        int skip = wave;
-        auto next = [&](int &chunk, uint32_t &own) {
-            while (some && skip) {
-                some &= some - 1;
-                --skip;
-            }
-            if (!some) return false;
+        uint32_t own0 = 0, own1 = 0, own2 = 0;                 // this chunk's rows of the adapter, the next one's, and of the one after
+        int chunk = base;
+        auto next = [&]() {
+            if (!some) return 0u;
             const int l = __builtin_ctzll(some);
             some &= some - 1;
-            skip = WAVES - 1;
             chunk = base + l;
-            own = (uint32_t)__builtin_amdgcn_readlane((int)match, l);
-            return true;
+            return (uint32_t)__builtin_amdgcn_readlane((int)match, l);
         };
-        int chunk, slot = 0;
-        uint32_t own, own2;
-        // (the look-over's loads are done: what is waited for below are the chunk's)
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        bool more = next(chunk, own);
-        if (more) issue(chunk, own, 0);
-        while (more) {
-            const bool more2 = next(chunk, own2);
-            if (more2) {
-                issue(chunk, own2, slot ^ 1);
-                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
-            } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            compute(own, slot);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            own = own2;
-            slot ^= 1;
-            more = more2;
+        // (the look-over's loads are done, and the last chunks' fragments read: what is waited for below are loads of chunks)
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        own0 = next();
+        issue(chunk, own0, 0);
+        own1 = next();
+        issue(chunk, own1, 1);
+        int slot = 0;
+        while (own0) {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+            own2 = next();
+            issue(chunk, own2, slot == 0 ? STAGES - 1 : slot - 1);
+            const char *at = lds + slot * S::STAGE;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                v8 x[CB], z[2][RB];
+#pragma unroll
+                for (int i = 0; i < CB; ++i) x[i] = read_turned<T>(at + xa[i] + s * 16 * (CH * 2), 4 * (CH * 2));
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int j = 0; j < RB; ++j)
+                        z[k][j] = read_turned<T>(at + S::X_BYTES + k * S::P_BYTES + pa[j] + s * 16 * (RB * 64), 4 * (RB * 64));
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int i = 0; i < CB; ++i)
+#pragma unroll
+                        for (int j = 0; j < RB; ++j) acc[i][j] = IS_B ? H::mfma(x[i], z[k][j], acc[i][j]) : H::mfma(z[k][j], x[i], acc[i][j]);
+            }
+            own0 = own1;
+            own1 = own2;
+            slot = slot == STAGES - 1 ? 0 : slot + 1;
         }
     }
-
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (part_out) {
         if (tid == 0 && flag) *flag = any;
         if (!any) return;
     }
-    // the waves' sums, 32 x 32 at a time, in their order
-    const float scale = g.is_b ? ad.scale[a] : 1.0f;
-    float(*part)[32][33] = (float(*)[32][33])lds;
+    // The lane's column is what is contiguous in the result: the channel of A, the rank of B.  Stores that lie outside are sent past the end.
+    const float scale = IS_B ? ad.scale[a] : 1.0f;
+    const uint32_t size = part_out ? 4 : 2, whole = (uint32_t)g.C * ad.rank;
+    const __amdgpu_buffer_rsrc_t to = part_out ? buffer(part_out, whole * 4) : buffer((T *)g.out + (int64_t)a * whole, whole * 2);
 #pragma unroll
     for (int i = 0; i < CB; ++i)
 #pragma unroll
-        for (int j = 0; j < RB; ++j) {
-            __syncthreads();
+        for (int j = 0; j < RB; ++j)
 #pragma unroll
-            for (int k = 0; k < 16; ++k) part[wave][ln][8 * (k >> 2) + 4 * h + (k & 3)] = acc[i][j][k];     // [r][c]
-            __syncthreads();
+            for (int m = 0; m < 4; ++m) {
+                const int row = 8 * m + 4 * h, c = c0 + (wave * CB + i) * 32 + (IS_B ? row : ln), r = r0 + j * 32 + (IS_B ? ln : row);
+                // (C and rank are multiples of 8: the four rows exist together)
+                const uint32_t step = (uint32_t)(IS_B ? ad.rank : g.C) * size;
+                const uint32_t at = c < g.C && r < ad.rank ? (IS_B ? (uint32_t)c * ad.rank + r : (uint32_t)r * g.C + c) * size : NOWHERE;
 #pragma unroll
-            for (int k = 0; k < 16 / WAVES; ++k) {
-                const int m = k * 64 * WAVES + tid, r = g.is_b ? m & 31 : m >> 5, c = g.is_b ? m >> 5 : m & 31;
-                float v = 0.0f;
-#pragma unroll
-                for (int w = 0; w < WAVES; ++w) v += part[w][r][c];
-                const int cc = c0 + i * 32 + c, rank = r0 + j * 32 + r;
-                if (cc < g.C && rank < ad.rank) {
-                    const int64_t at = g.is_b ? (int64_t)cc * ad.rank + rank : (int64_t)rank * g.C + cc;
+                for (int k = 0; k < 4; ++k) {
+                    const float v = acc[i][j][4 * m + k];
+                    if (part_out) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), to, at + k * step, 0, 0);
                     // (an adapter without rows has a gradient of zero, whatever its scale)
-                    if (part_out) part_out[at] = v;
-                    else ((T *)g.out)[(int64_t)a * g.C * ad.rank + at] = (T)(v == 0.0f ? 0.0f : v * scale);
+                    else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (T)(v == 0.0f ? 0.0f : v * scale)), to, at + k * step, 0, 0);
                 }
             }
-        }
 }
 
-template <class T, bool KEPT, int CH, int RB>
-__global__ __launch_bounds__(256)
+template <class T, int RB>
+__global__ __launch_bounds__(256, 2)
 void adapters_grad_kernel(Adapters ad, AdapterGradArgs A, AdapterGradArgs B, int rows, int tiles_a, int tiles, float *part, uint32_t *flags)
 {
     extern __shared__ __align__(16) char lds[];
@@ -436,8 +397,8 @@ void adapters_grad_kernel(Adapters ad, AdapterGradArgs A, AdapterGradArgs B, int
     const int at = blockIdx.z * ad.n + a;
     if (part) part += (int64_t)at * ad.rank * (A.C + B.C);
     uint32_t *flag = part && tile == 0 && r0 == 0 ? flags + at : nullptr;
-    if (tile < tiles_a) adapters_grad_tile<T, KEPT, CH, RB>(ad, A, a, tile * CH, r0, rows, chunk0, chunks, part, flag, lds);
-    else adapters_grad_tile<T, false, CH, RB>(ad, B, a, (tile - tiles_a) * CH, r0, rows, chunk0, chunks, part ? part + (int64_t)ad.rank * A.C : nullptr, flag, lds);
+    if (tile < tiles_a) adapters_grad_tile<T, false, RB>(ad, A, a, tile * 256, r0, rows, chunk0, chunks, part, flag, lds);
+    else adapters_grad_tile<T, true, RB>(ad, B, a, (tile - tiles_a) * 256, r0, rows, chunk0, chunks, part ? part + (int64_t)ad.rank * A.C : nullptr, flag, lds);
 }
 
 // The parts of the rows in their order, those that had some of the adapter's.
@@ -461,14 +422,14 @@ void adapters_join_kernel(Adapters ad, AdapterGradArgs A, AdapterGradArgs B, con
     *(typename Half<T>::v4 *)to = out;
 }
 
-template <class T, bool KEPT, int RB>
+template <class T, int RB>
 int launch_adapters_grad(const Adapters &ad, const AdapterGradArgs &A, const AdapterGradArgs &B, int64_t rows, int parts, float *part, uint32_t *flags,
                          hipStream_t s)
 {
-    constexpr int CH = 128;
-    constexpr size_t LDS = AdapterGrad<CH, RB>::LDS;
+    constexpr int CH = AdapterGrad<RB>::CH;
+    constexpr size_t LDS = AdapterGrad<RB>::LDS;
     static LdsGrant grant;
-    const auto kernel = adapters_grad_kernel<T, KEPT, CH, RB>;
+    const auto kernel = adapters_grad_kernel<T, RB>;
     int rc = grant_dynamic_lds((const void *)kernel, LDS, grant);
     if (rc != SNN_OK) return rc;
     const int tiles_a = (A.C + CH - 1) / CH, tiles = tiles_a + (B.C + CH - 1) / CH;
@@ -483,30 +444,32 @@ int launch_adapters_grad(const Adapters &ad, const AdapterGradArgs &A, const Ada
 // fraction of the CUs.  Parts of at least 1024 rows, while the workgroups (most of which find no rows of theirs, and end) stay few.
 int grad_parts(const LinearGeom &g, int n, int64_t rows)
 {
-    const int64_t tiles = (int64_t)n * ((g.C_in + 127) / 128 + (g.C_out + 127) / 128);
+    const int64_t tiles = (int64_t)n * ((g.C_in + 255) / 256 + (g.C_out + 255) / 256);
     int parts = 1;
     while (parts < 16 && rows / (2 * parts) >= 1024 && tiles * 2 * parts <= 4096) parts *= 2;
     return parts;
 }
 
 // The backward call's workspace: scaled inner products, also in two values of the activations' type, and low so; A and B with
-// their last two axes exchanged.  (The forward call's: scaled inner products.)
+// their last two axes exchanged; inputs in 8 bits as the values that they stand for.  (The forward call's: scaled inner products.)
 struct Scratch {
     float *scaled;
-    char *pair, *low_pair, *At, *Bt;
+    char *pair, *low_pair, *At, *Bt, *kept;
     float *part;                      // sums of parts of the rows, and which parts have some of an adapter's
     uint32_t *flags;
     int parts;
     size_t bytes;
 };
 
-Scratch scratch(const LinearGeom &g, int n, int rank, int64_t rows, void *ws)
+Scratch scratch(const LinearGeom &g, int n, int rank, int64_t rows, bool kept, void *ws)
 {
     const int parts = grad_parts(g, n, rows);
     const size_t z = align_up((size_t)rows * rank * 4, 256), a = align_up((size_t)n * rank * g.C_in * 2, 256), b = align_up((size_t)n * rank * g.C_out * 2, 256);
     const size_t sums = parts > 1 ? align_up((size_t)parts * n * rank * (g.C_in + g.C_out) * 4, 256) : 0, flags = align_up((size_t)parts * n * 4, 256);
+    const size_t x = kept ? align_up((size_t)rows * g.C_in * 2, 256) : 0;
     char *w = (char *)ws, *e = w + 3 * z + a + b;
-    return {(float *)w, w + z, w + 2 * z, w + 3 * z, w + 3 * z + a, (float *)e, (uint32_t *)(e + sums), parts, 3 * z + a + b + sums + flags};
+    return {(float *)w, w + z, w + 2 * z, w + 3 * z, w + 3 * z + a, e + sums + flags, (float *)e, (uint32_t *)(e + sums), parts,
+            3 * z + a + b + sums + flags + x};
 }
 
 template <class T>
@@ -536,17 +499,24 @@ int backward(const LinearGeom &g, const Adapters &ad, const RowsIn &x, const flo
         rc = launch_linear_rows(g, true, dy, lddy, rows, nullptr, weights, dx, lddx, &ad, w.At, w.scaled, s);
         if (rc != SNN_OK) return rc;
     }
-    const AdapterGradArgs A = {x, w.pair, g.C_in, dA, false}, B = {{dy, nullptr, lddy}, w.low_pair, g.C_out, dB, true};
-    if (ad.rank <= 32)
-        return x.e ? launch_adapters_grad<T, true, 1>(ad, A, B, rows, w.parts, w.part, w.flags, s) : launch_adapters_grad<T, false, 1>(ad, A, B, rows, w.parts, w.part, w.flags, s);
-    return x.e ? launch_adapters_grad<T, true, 2>(ad, A, B, rows, w.parts, w.part, w.flags, s) : launch_adapters_grad<T, false, 2>(ad, A, B, rows, w.parts, w.part, w.flags, s);
+    AdapterGradArgs A = {x.p, x.ld, w.pair, g.C_in, dA};
+    const AdapterGradArgs B = {dy, lddy, w.low_pair, g.C_out, dB};
+    if (x.e && rows) {
+        // (16-bit values once, not bytes widened by every tile: see launch_linear_weight_grad)
+        A.x = w.kept;
+        A.ld = g.C_in;
+        const int rc = launch_checkpoint_restore((const int8_t *)x.p, x.e, rows, g.C_in, g.dtype, w.kept, A.ld, s);
+        if (rc != SNN_OK) return rc;
+    }
+    return ad.rank <= 32 ? launch_adapters_grad<T, 1>(ad, A, B, rows, w.parts, w.part, w.flags, s)
+                         : launch_adapters_grad<T, 2>(ad, A, B, rows, w.parts, w.part, w.flags, s);
 }
 
 }  // namespace
 
-size_t adapters_workspace_bytes(const LinearGeom &g, int n, int rank, int64_t rows, bool backward)
+size_t adapters_workspace_bytes(const LinearGeom &g, int n, int rank, int64_t rows, bool backward, bool kept)
 {
-    return backward ? scratch(g, n, rank, rows, nullptr).bytes : align_up((size_t)rows * rank * 4 + 256, 256);
+    return backward ? scratch(g, n, rank, rows, kept, nullptr).bytes : align_up((size_t)rows * rank * 4 + 256, 256);
 }
 
 int launch_adapters_forward(const LinearGeom &g, const Adapters &ad, const void *x, int64_t ldx, int64_t rows, const void *weights,
@@ -559,7 +529,7 @@ int launch_adapters_forward(const LinearGeom &g, const Adapters &ad, const void 
 int launch_adapters_backward(const LinearGeom &g, const Adapters &ad, const RowsIn &x, const float *low, const void *dy, int64_t lddy,
                              int64_t rows, const void *weights, void *dx, int64_t lddx, void *dA, void *dB, void *ws, hipStream_t s)
 {
-    const Scratch w = scratch(g, ad.n, ad.rank, rows, ws);
+    const Scratch w = scratch(g, ad.n, ad.rank, rows, x.e != nullptr, ws);
     return g.dtype == SNN_DTYPE_BF16 ? backward<__bf16>(g, ad, x, low, dy, lddy, rows, weights, dx, lddx, dA, dB, w, s)
                                      : backward<_Float16>(g, ad, x, low, dy, lddy, rows, weights, dx, lddx, dA, dB, w, s);
 }

@@ -69,7 +69,7 @@ int adapters_backward_call(const snn_linear_desc *desc, const snn_adapters *a, c
     if (desc->groups != 1) return SNN_ERR_UNSUPPORTED;
     const LinearGeom g = make_linear_geom(*desc);
     if (!weights_ok(g, weights, weights_bytes)) return SNN_ERR_WORKSPACE;
-    if (!workspace || !aligned(workspace, 256) || ws_bytes < adapters_workspace_bytes(g, a->n, a->rank, rows, true)) return SNN_ERR_WORKSPACE;
+    if (!workspace || !aligned(workspace, 256) || ws_bytes < adapters_workspace_bytes(g, a->n, a->rank, rows, true, x.e != nullptr)) return SNN_ERR_WORKSPACE;
     const Adapters ad = {a->n, a->rank, a->A, a->B, a->scale, adapter};
     return launch_adapters_backward(g, ad, x, low, dy, lddy, rows, weights, dx, lddx, dA, dB, workspace, (hipStream_t)stream);
 }
@@ -141,10 +141,12 @@ int snn_linear_weight_grad_checkpoint(const snn_linear_desc *desc, const int8_t 
                             ws_bytes, stream);
 }
 
-size_t snn_adapters_workspace_bytes(const snn_linear_desc *desc, const snn_adapters *adapters, int64_t rows, int backward)
+size_t snn_adapters_workspace_bytes(const snn_linear_desc *desc, const snn_adapters *adapters, int64_t rows, int call)
 {
     if (!desc_ok(desc) || desc->groups != 1 || !adapters_ok(adapters) || !count_ok(rows)) return 0;
-    return adapters_workspace_bytes(make_linear_geom(*desc), adapters->n, adapters->rank, rows, backward != 0);
+    if (call < SNN_ADAPTERS_FORWARD || call > SNN_ADAPTERS_BACKWARD_CHECKPOINT) return 0;
+    return adapters_workspace_bytes(make_linear_geom(*desc), adapters->n, adapters->rank, rows, call != SNN_ADAPTERS_FORWARD,
+                                    call == SNN_ADAPTERS_BACKWARD_CHECKPOINT);
 }
 
 int snn_adapters_forward(const snn_linear_desc *desc, const snn_adapters *a, const void *x, int64_t ldx, int64_t rows,
@@ -157,7 +159,7 @@ int snn_adapters_forward(const snn_linear_desc *desc, const snn_adapters *a, con
     if (desc->groups != 1) return SNN_ERR_UNSUPPORTED;
     const LinearGeom g = make_linear_geom(*desc);
     if (!weights_ok(g, weights, weights_bytes)) return SNN_ERR_WORKSPACE;
-    if (!workspace || !aligned(workspace, 256) || ws_bytes < adapters_workspace_bytes(g, a->n, a->rank, rows, false)) return SNN_ERR_WORKSPACE;
+    if (!workspace || !aligned(workspace, 256) || ws_bytes < adapters_workspace_bytes(g, a->n, a->rank, rows, false, false)) return SNN_ERR_WORKSPACE;
     if (rows == 0) return SNN_OK;
     const Adapters ad = {a->n, a->rank, a->A, a->B, a->scale, adapter};
     return launch_adapters_forward(g, ad, x, ldx, rows, weights, y, ldy, low, workspace, (hipStream_t)stream);

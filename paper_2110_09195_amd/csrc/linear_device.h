@@ -86,24 +86,4 @@ __device__ inline typename Half<T>::v8 read_turned(const char *at, int next)
     return __builtin_bit_cast(typename Half<T>::v8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// 16 kept values out of their bytes: q u = (q + 128) u - 128 u, exact in one fused multiply-add (u is a power of two), q + 128 out of an
-// unsigned byte.  -128 stands for NaN; kept values hardly ever hold one.
-template <class T>
-__device__ inline void widen16(u32x4 raw, float u, typename Half<T>::v8 out[2])
-{
-    uint32_t odd = 0;
-    const float back = -128.0f * u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t z = raw[i] ^ 0x80808080u;
-        odd |= (z - 0x01010101u) & ~z & 0x80808080u;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) out[i >> 1][(i & 1) * 4 + k] = (T)fmaf((float)((z >> (8 * k)) & 255u), u, back);
-    }
-    if (__any(odd != 0)) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) out[i >> 3][i & 7] = (T)kept_value((int)(int8_t)(raw[i >> 2] >> (8 * (i & 3))), u);
-    }
-}
-
 }  // namespace snn

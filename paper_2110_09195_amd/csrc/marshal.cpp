@@ -363,7 +363,7 @@ PyObject *adapters_forward(PyObject *const *a)
         Py_RETURN_FALSE;
     snn_adapters ad = {(int32_t)n, (int32_t)rank, A->data_ptr(), B->data_ptr(), (const float *)scale->data_ptr()};
     at::Tensor y = rows_out(a[7], *x, rows, d.C_out);
-    const size_t need = linear.adapters_workspace_bytes(&d, &ad, rows, 0);
+    const size_t need = linear.adapters_workspace_bytes(&d, &ad, rows, SNN_ADAPTERS_FORWARD);
     if (!y.defined() || !need) Py_RETURN_FALSE;
     at::Tensor low = at::empty({rows, rank}, scale->options().requires_grad(false));
     const at::Tensor ws = at::empty({(int64_t)need}, w->options());

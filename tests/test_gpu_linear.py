@@ -302,7 +302,7 @@ def test_adapters(case, dtype):
 
     gy, y = L.out(T, co, pad)
     gl = Guarded(T * r, torch.float32, fill=float("nan"))
-    need = [B.snn_adapters_workspace_bytes(L.desc, B._adapters(L.desc, A, Bm, scale), T, back) for back in (False, True)]
+    need = [B.snn_adapters_workspace_bytes(L.desc, B._adapters(L.desc, A, Bm, scale), T, call) for call in range(3)]
     gs = Guarded(need[0], torch.uint8)
     _, low = B.snn_adapters_forward(L.desc, x, L.weights, ids, A, Bm, scale, y=y, low=gl.t.view(T, r), workspace=gs.t)
     for g, what in ((gy, "y"), (gl, "low"), (gs, "the workspace")):
@@ -340,7 +340,7 @@ def test_adapters(case, dtype):
         xv = B.snn_checkpoint_restore(arg, L.dtype).double() if kept else xd
         gx, out = L.out(T, ci, pad)
         ga, gb = Guarded(A.numel(), L.dtype, fill=float("nan")), Guarded(Bm.numel(), L.dtype, fill=float("nan"))
-        gs = Guarded(need[1], torch.uint8)
+        gs = Guarded(need[2 if kept else 1], torch.uint8)
         _, dA, dB = B.snn_adapters_backward(L.desc, arg, low, dy, L.weights, ids, A, Bm, scale, dx=out, dA=ga.t.view(A.shape), dB=gb.t.view(Bm.shape),
                                             workspace=gs.t)
         for g, what in ((gx, "dx"), (ga, "dA"), (gb, "dB"), (gs, "the workspace")):

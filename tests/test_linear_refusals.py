@@ -58,6 +58,7 @@ def test_descriptors(name):
         assert call(name, CALLS[name], desc=desc(**bad)) == BAD, bad
     assert B.lib().snn_linear_weights_bytes(desc(C_in=60)) == 0 and B.lib().snn_linear_weights_bytes(None) == 0
     assert B.lib().snn_linear_weight_grad_workspace_bytes(desc(K=0), 8, 0) == 0 and B.lib().snn_linear_weight_grad_workspace_bytes(desc(), -1, 1) == 0
+    assert B.lib().snn_adapters_workspace_bytes(desc(groups=1), adapters(), 8, 3) == 0 and B.lib().snn_adapters_workspace_bytes(desc(groups=1), adapters(), 8, 2) > 0
     assert B.lib().snn_adapters_workspace_bytes(desc(), adapters(), 8, 1) == 0            # two groups
 
 
