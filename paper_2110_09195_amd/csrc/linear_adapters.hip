@@ -441,12 +441,13 @@ int launch_adapters_grad(const Adapters &ad, const AdapterGradArgs &A, const Ada
 }
 
 // Parts of the rows, joined by another launch: an adapter can have nearly all of them, and then its tiles alone would occupy a
-// fraction of the CUs.  Parts of at least 1024 rows, while the workgroups (most of which find no rows of theirs, and end) stay few.
+// fraction of the CUs (8192 rows of one adapter of rank 64, 4096 -> 4096: 64 chunks take 45 us, and eight parts of 32 chunks 33 with 5 for the join).  Parts of
+// at least 384 rows, while the workgroups (most of which find no rows of theirs, and end) stay few.
 int grad_parts(const LinearGeom &g, int n, int64_t rows)
 {
-    const int64_t tiles = (int64_t)n * ((g.C_in + 255) / 256 + (g.C_out + 255) / 256);
+    const int64_t tiles = (g.C_in + 255) / 256 + (g.C_out + 255) / 256;
     int parts = 1;
-    while (parts < 16 && rows / (2 * parts) >= 1024 && tiles * 2 * parts <= 4096) parts *= 2;
+    while (parts < 16 && tiles * parts < 256 && rows / (2 * parts) >= 384 && n * tiles * 2 * parts <= 4096) parts *= 2;
     return parts;
 }
 

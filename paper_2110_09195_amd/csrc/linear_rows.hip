@@ -368,24 +368,35 @@ void linear_rows_kernel(RowsArgs p)
                 const int a = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
                 const bool own = id == a;
                 left &= ~__ballot(own);
+                const __amdgpu_buffer_rsrc_t ru = buffer((const T *)p.ad.up + (int64_t)a * p.N * p.ad.rank, (uint32_t)p.N * p.ad.rank * 2);
+                const __amdgpu_buffer_rsrc_t rz = buffer(p.ad.low + (int64_t)tj * p.ad.rank, 32u * p.ad.rank * 4);
                 f32x16 d[NB] = {};
-                for (int r0 = 0; r0 < p.ad.rank; r0 += 16) {
-                    const int r = r0 + 8 * h;
-                    const bool in = r < p.ad.rank;
-                    float z[8] = {};
-                    if (in && own) {
-                        *(f32x4 *)z = *(const f32x4 *)(p.ad.low + (int64_t)t * p.ad.rank + r);
-                        *(f32x4 *)(z + 4) = *(const f32x4 *)(p.ad.low + (int64_t)t * p.ad.rank + r + 4);
-                    }
-                    v8 hi, lo;
-                    split8<T>(z, hi, lo);
+                for (int r0 = 0; r0 < p.ad.rank; r0 += 64) {
+                    // 64 of the rank: all loads before the first product
+                    u32x4 u[4][NB], z[4][2];
 #pragma unroll
-                    for (int i = 0; i < NB; ++i) {
-                        const int n = min(nw + i * 32 + ln, p.N - 1);
-                        v8 u = {};
-                        if (in) u = *(const v8 *)((const T *)p.ad.up + ((int64_t)a * p.N + n) * p.ad.rank + r);
-                        d[i] = H::mfma(u, hi, d[i]);
-                        d[i] = H::mfma(u, lo, d[i]);
+                    for (int s = 0; s < 4; ++s) {
+                        const int r = r0 + 16 * s + 8 * h;
+#pragma unroll
+                        for (int i = 0; i < NB; ++i)
+                            u[s][i] = __builtin_amdgcn_raw_buffer_load_b128(ru, r < p.ad.rank ? (uint32_t)((nw + i * 32 + ln) * p.ad.rank + r) * 2 : NOWHERE, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            z[s][i] = __builtin_amdgcn_raw_buffer_load_b128(rz, own && r < p.ad.rank ? (uint32_t)(ln * p.ad.rank + r + 4 * i) * 4 : NOWHERE, 0, 0);
+                    }
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        if (r0 + 16 * s >= p.ad.rank) break;
+                        float zf[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) zf[i] = __uint_as_float(z[s][i >> 2][i & 3]);
+                        v8 hi, lo;
+                        split8<T>(zf, hi, lo);
+#pragma unroll
+                        for (int i = 0; i < NB; ++i) {
+                            d[i] = H::mfma(__builtin_bit_cast(v8, u[s][i]), hi, d[i]);
+                            d[i] = H::mfma(__builtin_bit_cast(v8, u[s][i]), lo, d[i]);
+                        }
                     }
                 }
 #pragma unroll
