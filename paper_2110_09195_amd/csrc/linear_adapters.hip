@@ -15,32 +15,43 @@ __device__ inline void split1(float v, T *to, int64_t plane)
 }
 
 // low[t][r] = down[a][r] . x[t] and scaled[t][r] = scale[a] times it, a = the row's adapter; down [n][rank][C].
-// Few rows: a wave an inner product, so that the adapters' matrices, of which nearly every row has its own, are read by many CUs.
-template <class T>
+// Few rows: a wave takes NR inner products of a row, so that the adapters' matrices, of which nearly every row has its own, are read by many CUs.
+template <class T, int NR>
 __global__ __launch_bounds__(256)
 void low_few_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__restrict__ x, int64_t ldx, float *__restrict__ low,
                     float *__restrict__ scaled, T *__restrict__ pair, int64_t plane)
 {
     using v8 = typename Half<T>::v8;
-    const int t = blockIdx.x, lane = threadIdx.x & 63, r = blockIdx.y * 4 + (threadIdx.x >> 6);
-    const int a = ad.of_row[t];                                // (rank is a multiple of 4: every wave has an r)
-    float acc = 0.0f, c = 0.0f;
+    const int t = blockIdx.x, lane = threadIdx.x & 63, r = (blockIdx.y * 4 + (threadIdx.x >> 6)) * NR;
+    if (r >= ad.rank) return;                                  // (rank is a multiple of NR)
+    const int a = ad.of_row[t];
+    float acc[NR] = {}, c = 0.0f;
     if (a >= 0 && a < ad.n) {
         c = ad.scale[a];
         const T *xr = x + t * ldx, *dr = down + ((int64_t)a * ad.rank + r) * C;
-#pragma unroll 4
+#pragma unroll(NR == 1 ? 4 : 2)
         for (int k = lane * 8; k < C; k += 512) {
-            const v8 u = *(const v8 *)(xr + k), v = *(const v8 *)(dr + k);
+            const v8 u = *(const v8 *)(xr + k);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) acc = fmaf((float)u[i], (float)v[i], acc);
+            for (int j = 0; j < NR; ++j) {
+                const v8 v = *(const v8 *)(dr + (int64_t)j * C + k);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[j] = fmaf((float)u[i], (float)v[i], acc[j]);
+            }
         }
 #pragma unroll
-        for (int d = 32; d; d >>= 1) acc += __shfl_xor(acc, d);
+        for (int d = 32; d; d >>= 1)
+#pragma unroll
+            for (int j = 0; j < NR; ++j) acc[j] += __shfl_xor(acc[j], d);
     }
     if (lane == 0) {
-        if (low) low[(int64_t)t * ad.rank + r] = acc;
-        scaled[(int64_t)t * ad.rank + r] = acc * c;
-        if (pair) split1(acc * c, pair + (int64_t)t * ad.rank + r, plane);
+        const int64_t at = (int64_t)t * ad.rank + r;
+#pragma unroll
+        for (int j = 0; j < NR; ++j) {
+            if (low) low[at + j] = acc[j];
+            scaled[at + j] = acc[j] * c;
+            if (pair) split1(acc[j] * c, pair + at + j, plane);
+        }
     }
 }
 
@@ -197,6 +208,10 @@ void adapters_lay_out_kernel(Exchange A, Exchange B, int tiles_a, int tiles_ab, 
     }
 }
 
+// Up to so many products (rows x rank x channels) a wave takes four inner products of a row, and the matrices come from L2 again for every row: 512 rows,
+// rank 16, 4096 channels 5.4 us against 13.3 by tiles; 1000 rows, rank 32, 2048 channels (62 M) 9.3 against 9.5; 1000 rows, rank 64, 4096 channels 29 against 22.
+constexpr int64_t LOW_FEW_PRODUCTS = (int64_t)64 << 20;
+
 template <class T, int RB, int STAGES>
 int launch_low_tile(int C, const Adapters &ad, const T *down, const T *x, int64_t ldx, int64_t rows, float *low, float *scaled, T *pair, hipStream_t s)
 {
@@ -215,7 +230,11 @@ template <class T>
 int launch_low(int C, const Adapters &ad, const void *down, const void *x, int64_t ldx, int64_t rows, float *low, float *scaled, T *pair, hipStream_t s)
 {
     if (rows <= 64) {
-        low_few_kernel<T><<<dim3((unsigned)rows, ad.rank / 4), 256, 0, s>>>(C, ad, (const T *)down, (const T *)x, ldx, low, scaled, pair, rows * ad.rank);
+        low_few_kernel<T, 1><<<dim3((unsigned)rows, ad.rank / 4), 256, 0, s>>>(C, ad, (const T *)down, (const T *)x, ldx, low, scaled, pair, rows * ad.rank);
+        return check_launch();
+    }
+    if (rows * ad.rank * C <= LOW_FEW_PRODUCTS) {
+        low_few_kernel<T, 4><<<dim3((unsigned)rows, (ad.rank + 15) / 16), 256, 0, s>>>(C, ad, (const T *)down, (const T *)x, ldx, low, scaled, pair, rows * ad.rank);
         return check_launch();
     }
     if (ad.rank <= 32) return launch_low_tile<T, 1, 4>(C, ad, (const T *)down, (const T *)x, ldx, rows, low, scaled, pair, s);
