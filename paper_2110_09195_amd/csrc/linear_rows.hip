@@ -138,17 +138,28 @@ template <int BT>
 __device__ inline bool find_tile(const int32_t *offsets, int groups, int rows, int col_tiles, const Divisor &col_div, RowTile &tile)
 {
     const int lane = threadIdx.x & 63;
-    int total = 0;
-    if (!offsets) total = (rows + BT - 1) / BT;
-    else
-        for (int g0 = 0; g0 < groups; g0 += 64) {
-            int lo = 0, hi = 0;
-            if (g0 + lane < groups) group_rows(offsets, g0 + lane, rows, lo, hi);
-            int n = (hi - lo + BT - 1) / BT;
+    // (groups g0 .. g0 + 63, a lane each: their rows, and the tiles of those up to it)
+    auto look = [&](int g0, int &lo, int &hi) {
+        lo = hi = 0;
+        if (g0 + lane < groups) group_rows(offsets, g0 + lane, rows, lo, hi);
+        int upto = (hi - lo + BT - 1) / BT;
 #pragma unroll
-            for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
-            total += n;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int v = __shfl_up(upto, d);
+            if (lane >= d) upto += v;
         }
+        return upto;
+    };
+    int total, lo = 0, hi = 0, upto = 0;
+    if (!offsets) total = (rows + BT - 1) / BT;
+    else {
+        upto = look(0, lo, hi);
+        total = __builtin_amdgcn_readlane(upto, 63);
+        for (int g0 = 64; g0 < groups; g0 += 64) {
+            int l, h;
+            total += __builtin_amdgcn_readlane(look(g0, l, h), 63);
+        }
+    }
     const uint32_t tiles = (uint32_t)total * col_tiles;        // (no more than the grid has workgroups, whatever the offsets hold: see tile_grid)
     const uint32_t share = (tiles + 7) / 8, at = blockIdx.x / 8;
     const uint32_t id = (blockIdx.x % 8) * share + at;
@@ -161,28 +172,21 @@ __device__ inline bool find_tile(const int32_t *offsets, int groups, int rows, i
         tile.t1 = min(tile.t0 + BT, rows);
         return true;
     }
-    for (int g0 = 0; g0 < groups; g0 += 64) {
-        int lo = 0, hi = 0;
-        if (g0 + lane < groups) group_rows(offsets, g0 + lane, rows, lo, hi);
-        const int n = (hi - lo + BT - 1) / BT;
-        int upto = n;                                          // tiles of this group and those before it
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int v = __shfl_up(upto, d);
-            if (lane >= d) upto += v;
-        }
+    for (int g0 = 0;;) {
         const uint64_t past = __ballot(upto > m);
         if (past) {
             const int l = __builtin_ctzll(past);
-            m -= __builtin_amdgcn_readlane(upto - n, l);
+            m -= l ? __builtin_amdgcn_readlane(upto, l - 1) : 0;
             tile.group = g0 + l;
             tile.t0 = __builtin_amdgcn_readlane(lo, l) + m * BT;
             tile.t1 = min(tile.t0 + BT, __builtin_amdgcn_readlane(hi, l));
             return true;
         }
         m -= __builtin_amdgcn_readlane(upto, 63);
+        g0 += 64;
+        if (g0 >= groups) return false;
+        upto = look(g0, lo, hi);
     }
-    return false;
 }
 
 // The adapters' share as the rows kernels add it: up [n][N][rank] and the scaled inner products, fp32 [rows][rank].
@@ -217,7 +221,7 @@ struct RowsArgs {
 //     sixteenth of what the rows cost, and HBM as well.
 //   - GRAD: the contracted axis is the output channels, and alpha, on that axis, is what the signs are put on: exact, and free.
 template <class T, bool GRAD, bool ADAPT, int BT, int BN, int WT, int WN, int STAGES>
-__global__ __launch_bounds__(64 * (BT / WT) * (BN / WN))
+__global__ __launch_bounds__(64 * (BT / WT) * (BN / WN), 2)
 void linear_rows_kernel(RowsArgs p)
 {
     using H = Half<T>;
@@ -438,8 +442,10 @@ void linear_few_kernel(RowsArgs p)
     using H = Half<T>;
     using v8 = typename H::v8;
     constexpr int WAVES = 8;
-    __shared__ __align__(16) char rows_in[WAVES][AHEAD * 2048];
-    __shared__ float part[WAVES][16][16 * NB + 1];
+    // the rows on their way; then the sums
+    constexpr int IN = WAVES * AHEAD * 2048, SUMS = WAVES * 16 * (16 * NB + 1) * 4;
+    __shared__ __align__(16) char lds[IN > SUMS ? IN : SUMS];
+    float(*const part)[16][16 * NB + 1] = (float(*)[16][16 * NB + 1])lds;
     RowTile tile;
     if (!find_tile<16>(p.offsets, p.groups, p.rows, p.col_tiles, p.col_div, tile)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -448,7 +454,7 @@ void linear_few_kernel(RowsArgs p)
     // a load: 16 rows of 64 bytes, four lanes a row, their 16-byte pieces xor-ed by a quarter of the row's number against bank conflicts
     const int lr = lane >> 2, lp = (lane & 3) ^ ((lane >> 4) & 3);
     const uint32_t xo = tile.t0 + lr < tile.t1 ? (uint32_t)lr * (uint32_t)p.ld_in * 2 + lp * 16 : NOWHERE;
-    char *mine = rows_in[wave];
+    char *mine = lds + wave * AHEAD * 2048;
     const uint32_t mine0 = __builtin_amdgcn_readfirstlane(lds_address(mine));
     const char *from = mine + (4 * ln + (q ^ (ln >> 2))) * 16;
     // Channels 64 kb + 32 m + 8 q + j of a lane: the half q % 2 of the block's words, steps 2 m + q / 2.
@@ -489,6 +495,7 @@ void linear_few_kernel(RowsArgs p)
             }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
@@ -576,30 +583,41 @@ int launch_few(RowsArgs p, hipStream_t s)
     return check_launch();
 }
 
-// Which tile a call of many rows takes.  Measured for each, in microseconds for 64 contracted channels (4096 -> 4096 bf16, 128 to 8192
-// rows): a tile alone on its CU with most CUs idle, and its share of a CU when all are busy (then the clock is down to 1.8 - 1.9 GHz: such calls are
-// bound by power, and what moves fewer bytes for a product is faster).  A tile is small to spread few rows over the chip and large
-// to be fed with fewer reads: 4096 rows 106 us in 256 x 256, 111 in 128 x 256, 118 in 128 x 128, 127 in 64 x 128, 151 in 32 x 128; 512 rows 67,
-// 38, 25, 24, 25; 128 rows 67, 38, 24, 22, 18.
+// Which tile a call of many rows takes.  Costs for 64 contracted channels in microseconds, fitted to calls of 512 to 16384 rows, of 1, 8 and 60
+// groups, 1032 to 4096 channels wide: a tile alone on its CU with most CUs idle, and its share of a CU when all are busy (then the clock is down
+// to 1.8 - 1.9 GHz: such calls are bound by power, and what moves fewer bytes for a product is faster).  The input's gradient also
+// scales its weights, which makes the tiles of few rows dearer.  A tile is small to spread few rows over the chip and large to be fed with
+// fewer reads; two of 128 x 256 stay on a CU and fill each other's waits.  One group, 4096 -> 4096, outputs / input gradients in us:
+//   rows    256 x 256   128 x 256   128 x 128   64 x 128   32 x 128
+//    512       72 / 71     42 / 55     28 / 38    25 / 32    25 / 28
+//   1024       69 / 72     44 / 57     33 / 41    36 / 41    42 / 46
+//   4096      100 / 104   100 / 110   111 / 122  121 / 133  141 / 156
+//  16384      381 / 388   367 / 398   417 / 461  450 / 492  524 / 587
 struct TileForm {
     int rows, cols;
-    float alone, share;
+    float alone[2], share[2];                                  // [input's gradient]
 };
-constexpr TileForm TILE_FORMS[] = {{256, 256, 1.05f, 1.57f}, {128, 256, 0.60f, 0.87f}, {128, 128, 0.38f, 0.48f}, {64, 128, 0.33f, 0.27f}, {32, 128, 0.28f, 0.19f}};
+constexpr TileForm TILE_FORMS[] = {{256, 256, {0.0f, 0.93f}, {0.0f, 1.62f}},
+                                   {128, 256, {0.53f, 0.95f}, {0.80f, 0.83f}},
+                                   {128, 128, {0.34f, 0.57f}, {0.44f, 0.48f}},
+                                   {64, 128, {0.35f, 0.46f}, {0.24f, 0.26f}},
+                                   {32, 128, {0.35f, 0.39f}, {0.14f, 0.153f}}};
 
-int tile_form(int64_t rows, int groups, int N)
+int tile_form(int64_t rows, int groups, int N, bool grad)
 {
     int best = 0;
     float least = 0.0f;
-    for (int i = 0; i < (int)(sizeof(TILE_FORMS) / sizeof(TILE_FORMS[0])); ++i) {
+    const int first = grad ? 0 : 1;                            // (outputs: two tiles of 128 x 256 on a CU beat one of 256 x 256 everywhere)
+    for (int i = first; i < (int)(sizeof(TILE_FORMS) / sizeof(TILE_FORMS[0])); ++i) {
         const TileForm &f = TILE_FORMS[i];
+        const float alone = f.alone[grad], share = f.share[grad];
         // (of several groups, the last tile of each is half full on average)
         const float used = (float)(rows < groups ? rows : groups);
         const float down = groups > 1 ? (float)rows / f.rows + 0.5f * used : (float)((rows + f.rows - 1) / f.rows);
         const float tiles = down * (float)((N + f.cols - 1) / f.cols);
-        const float turns = ceilf(tiles / 256.0f), full = turns * f.share > f.alone ? turns * f.share : f.alone;
-        const float time = f.alone + (full - f.alone) * tiles / (256.0f * turns);
-        if (i == 0 || time < least) {
+        const float turns = ceilf(tiles / 256.0f), full = turns * share > alone ? turns * share : alone;
+        const float time = alone + (full - alone) * tiles / (256.0f * turns);
+        if (i == first || time < least) {
             best = i;
             least = time;
         }
@@ -619,10 +637,12 @@ int launch_rows(RowsArgs p, hipStream_t s)
         const int64_t narrow = tiles * ((p.N + 15) / 16);
         if (narrow <= 256) return launch_few<T, GRAD, ADAPT, 1, 2>(p, s);
         if (narrow <= 1024) return launch_few<T, GRAD, ADAPT, 2, 2>(p, s);
-        return launch_few<T, GRAD, ADAPT, 4, 1>(p, s);
+        return launch_few<T, GRAD, ADAPT, 4, 2>(p, s);
     }
-    switch (tile_form(p.rows, p.groups, p.N)) {
-    case 0: return launch_tiles<T, GRAD, ADAPT, 256, 256, 128, 64, 4>(p, s);
+    switch (tile_form(p.rows, p.groups, p.N, GRAD)) {
+    case 0:
+        if constexpr (GRAD) return launch_tiles<T, GRAD, ADAPT, 256, 256, 128, 64, 4>(p, s);
+        return SNN_ERR_UNSUPPORTED;                            // (never: see tile_form)
     case 1: return launch_tiles<T, GRAD, ADAPT, 128, 256, 128, 64, 4>(p, s);
     case 2: return launch_tiles<T, GRAD, ADAPT, 128, 128, 128, 32, 4>(p, s);
     case 3: return launch_tiles<T, GRAD, ADAPT, 64, 128, 64, 32, 4>(p, s);
