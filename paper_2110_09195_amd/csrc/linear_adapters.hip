@@ -49,7 +49,7 @@ void low_few_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__r
 #pragma unroll
         for (int j = 0; j < NR; ++j) {
             if (low) low[at + j] = acc[j];
-            scaled[at + j] = acc[j] * c;
+            scaled[scaled_at(t, r + j, ad.rank)] = acc[j] * c;
             if (pair) split1(acc[j] * c, pair + at + j, plane);
         }
     }
@@ -150,7 +150,7 @@ void low_tile_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__
         const f32x4 v = {sum[i], sum[i + 1], sum[i + 2], sum[i + 3]};
         if (low) *(f32x4 *)(low + at + i) = v;
         const f32x4 z = some ? v * c : v;
-        *(f32x4 *)(scaled + at + i) = z;
+        *(f32x4 *)(scaled + scaled_at(t0 + rr, r0 + rc + i, ad.rank)) = z;
         if (pair) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) split1(z[k], pair + at + i + k, plane);
@@ -481,10 +481,12 @@ struct Scratch {
     size_t bytes;
 };
 
+size_t scaled_bytes(int64_t rows, int rank) { return align_up((size_t)((rows + 31) / 32) * 32 * rank * 4, 256); }
+
 Scratch scratch(const LinearGeom &g, int n, int rank, int64_t rows, bool kept, void *ws)
 {
     const int parts = grad_parts(g, n, rows);
-    const size_t z = align_up((size_t)rows * rank * 4, 256), a = align_up((size_t)n * rank * g.C_in * 2, 256), b = align_up((size_t)n * rank * g.C_out * 2, 256);
+    const size_t z = scaled_bytes(rows, rank), a = align_up((size_t)n * rank * g.C_in * 2, 256), b = align_up((size_t)n * rank * g.C_out * 2, 256);
     const size_t sums = parts > 1 ? align_up((size_t)parts * n * rank * (g.C_in + g.C_out) * 4, 256) : 0, flags = align_up((size_t)parts * n * 4, 256);
     const size_t x = kept ? align_up((size_t)rows * g.C_in * 2, 256) : 0;
     char *w = (char *)ws, *e = w + 3 * z + a + b;
@@ -536,7 +538,7 @@ int backward(const LinearGeom &g, const Adapters &ad, const RowsIn &x, const flo
 
 size_t adapters_workspace_bytes(const LinearGeom &g, int n, int rank, int64_t rows, bool backward, bool kept)
 {
-    return backward ? scratch(g, n, rank, rows, kept, nullptr).bytes : align_up((size_t)rows * rank * 4 + 256, 256);
+    return backward ? scratch(g, n, rank, rows, kept, nullptr).bytes : scaled_bytes(rows, rank) + 256;
 }
 
 int launch_adapters_forward(const LinearGeom &g, const Adapters &ad, const void *x, int64_t ldx, int64_t rows, const void *weights,

@@ -60,6 +60,10 @@ __device__ inline void load_lds4(uint32_t lds, uint32_t offset, s32x4 from)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(from) : "memory");
 }
 
+// The adapters' scaled inner products as the rows kernels read them: blocks of 32 rows, of those pieces of 4 of the rank, so that the rows of a
+// block lie next to each other (a load of a wave's operand is 512 bytes in a row then; read with a row a lane, they took half the adapters' share).
+__device__ inline int64_t scaled_at(int t, int r, int rank) { return ((int64_t)(t >> 5) * rank + (r & ~3)) * 32 + (t & 31) * 4 + (r & 3); }
+
 constexpr uint32_t NOWHERE = 0x80000000u;                      // an offset past every resource
 
 // Two values of the activations' type that together hold v with twice its mantissa.

@@ -342,6 +342,14 @@ void linear_rows_kernel(RowsArgs p)
         }
         slot = next;
     }
+    int ids[TB];                                               // the adapters of the rows 32 j + ln
+    if constexpr (ADAPT) {
+#pragma unroll
+        for (int j = 0; j < TB; ++j) {
+            const int t = tile.t0 + wt * WT + j * 32 + ln;
+            ids[j] = t < tile.t1 ? p.ad.of_row[t] : -1;
+        }
+    }
     // nothing of this workgroup writes to LDS any more, and every wave is done reading
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
@@ -349,6 +357,8 @@ void linear_rows_kernel(RowsArgs p)
     constexpr int PITCH = WN * 2 + 16;
     char *mine = lds + wave * 32 * PITCH;
     const int nw = n0 + wn * WN;
+    u32x4 u[4][NB] = {};
+    int held = -1;
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
         const int tj = tile.t0 + wt * WT + j * 32;
@@ -364,29 +374,31 @@ void linear_rows_kernel(RowsArgs p)
                 }
         }
         if constexpr (ADAPT) {
-            // For each adapter of these 32 rows in turn: its product with the rows' inner products, added where the row is its own.
-            const int t = tj + ln;
-            const int id = t < tile.t1 ? p.ad.of_row[t] : -1;
+            // For each adapter of these 32 rows in turn: its product with the rows' inner products, added where the row is its own.  (Tiles start at
+            // multiples of 32; a matrix of the rank 64 or less stays for the next rows when they have the same adapter.)
+            const int id = ids[j];
             uint64_t left = __ballot(id >= 0 && id < p.ad.n);
             while (left) {
                 const int a = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
                 const bool own = id == a;
                 left &= ~__ballot(own);
                 const __amdgpu_buffer_rsrc_t ru = buffer((const T *)p.ad.up + (int64_t)a * p.N * p.ad.rank, (uint32_t)p.N * p.ad.rank * 2);
-                const __amdgpu_buffer_rsrc_t rz = buffer(p.ad.low + (int64_t)tj * p.ad.rank, 32u * p.ad.rank * 4);
+                const __amdgpu_buffer_rsrc_t rz = buffer(p.ad.low + scaled_at(tj, 0, p.ad.rank), 32u * p.ad.rank * 4);
                 f32x16 d[NB] = {};
                 for (int r0 = 0; r0 < p.ad.rank; r0 += 64) {
                     // 64 of the rank: all loads before the first product
-                    u32x4 u[4][NB], z[4][2];
+                    u32x4 z[4][2];
+                    const bool load_u = a != held;
 #pragma unroll
                     for (int s = 0; s < 4; ++s) {
                         const int r = r0 + 16 * s + 8 * h;
+                        if (load_u)
 #pragma unroll
-                        for (int i = 0; i < NB; ++i)
-                            u[s][i] = __builtin_amdgcn_raw_buffer_load_b128(ru, r < p.ad.rank ? (uint32_t)((nw + i * 32 + ln) * p.ad.rank + r) * 2 : NOWHERE, 0, 0);
+                            for (int i = 0; i < NB; ++i)
+                                u[s][i] = __builtin_amdgcn_raw_buffer_load_b128(ru, r < p.ad.rank ? (uint32_t)((nw + i * 32 + ln) * p.ad.rank + r) * 2 : NOWHERE, 0, 0);
 #pragma unroll
                         for (int i = 0; i < 2; ++i)
-                            z[s][i] = __builtin_amdgcn_raw_buffer_load_b128(rz, own && r < p.ad.rank ? (uint32_t)(ln * p.ad.rank + r + 4 * i) * 4 : NOWHERE, 0, 0);
+                            z[s][i] = __builtin_amdgcn_raw_buffer_load_b128(rz, own && r < p.ad.rank ? (uint32_t)((r + 4 * i) * 32 + ln * 4) * 4 : NOWHERE, 0, 0);
                     }
 #pragma unroll
                     for (int s = 0; s < 4; ++s) {
@@ -403,6 +415,7 @@ void linear_rows_kernel(RowsArgs p)
                         }
                     }
                 }
+                held = p.ad.rank <= 64 ? a : -1;
 #pragma unroll
                 for (int i = 0; i < NB; ++i)
 #pragma unroll
@@ -519,13 +532,15 @@ void linear_few_kernel(RowsArgs p)
         const int a = p.ad.of_row[t];
         if (a >= 0 && a < p.ad.n) {
             const T *u = (const T *)p.ad.up + ((int64_t)a * p.N + n) * p.ad.rank;
-            const float *z = p.ad.low + (int64_t)t * p.ad.rank;
             for (int k = 0; k < p.ad.rank; k += 8) {
                 const v8 u0 = *(const v8 *)(u + k), u1 = *(const v8 *)(u + p.ad.rank + k);
+                float z[8];
+#pragma unroll
+                for (int i = 0; i < 8; i += 4) *(f32x4 *)(z + i) = *(const f32x4 *)(p.ad.low + scaled_at(t, k + i, p.ad.rank));
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    v0 = fmaf(z[k + i], (float)u0[i], v0);
-                    v1 = fmaf(z[k + i], (float)u1[i], v1);
+                    v0 = fmaf(z[i], (float)u0[i], v0);
+                    v1 = fmaf(z[i], (float)u1[i], v1);
                 }
             }
         }
