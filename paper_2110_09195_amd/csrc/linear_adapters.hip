@@ -84,7 +84,7 @@ void low_tile_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__
     uint32_t xo[4], piece[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s) piece[s] = ln * 128 + (((2 * s + h) ^ ((ln >> 1) & 7)) << 4);
-    const int blocks = (C + 63) / 64;
+    const int blocks = (C + 63) / 64, each = (blocks + WAVES - 1) / WAVES, first = wave * each, last = min(first + each, blocks);
     while (left) {
         const int a = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
         const uint64_t own = __ballot(id == a);
@@ -110,10 +110,10 @@ void low_tile_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__
         };
         f32x16 acc[RB] = {};
 #pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s) issue(wave + s * WAVES, s);
+        for (int s = 0; s < STAGES - 1; ++s) issue(first + s, s);
         int slot = 0;
-        for (int k = wave; k < blocks; k += WAVES) {
-            issue(k + (STAGES - 1) * WAVES, slot == 0 ? STAGES - 1 : slot - 1);
+        for (int k = first; k < last; ++k) {
+            issue(k + STAGES - 1, slot == 0 ? STAGES - 1 : slot - 1);
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS * (STAGES - 1)) : "memory");
             const char *at = mine + slot * STAGE;
 #pragma unroll
