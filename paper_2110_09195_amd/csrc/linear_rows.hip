@@ -258,7 +258,13 @@ void linear_rows_kernel(RowsArgs p)
     }
     const uint32_t lds0 = lds_address(lds);
     // a quarter of a step's loads
-    auto issue = [&](int kb, int slot, int part) {
+    // Input gradients in tiles of 128 x 256 start each row of tiles at another channel: 2048 rows of 4096 -> 4096 68.7 -> 61.2 us, 8 experts of
+    // 8192 rows 236 -> 230 (others lose by it: tiles of 32 x 128 14.2 -> 15.4, outputs 2 %).
+    constexpr bool TURNED = GRAD && BT == 128 && BN == 256;
+    const int turn = TURNED ? tile.t0 / BT * 5 % p.kbs : 0;
+    auto issue = [&](int step, int slot, int part) {
+        int kb = step;
+        if constexpr (TURNED) kb = step >= p.kbs ? step : step + turn >= p.kbs ? step + turn - p.kbs : step + turn;
         const uint32_t at = __builtin_amdgcn_readfirstlane(lds0 + slot * STAGE);
         const bool in = kb * 64 + xc * 8 < p.K;                // (past the last channel: zeros, whatever the row holds there)
 #pragma unroll
@@ -599,31 +605,30 @@ int launch_few(RowsArgs p, hipStream_t s)
 }
 
 // Which tile a call of many rows takes.  Costs for 64 contracted channels in microseconds, fitted to calls of 512 to 16384 rows, of 1, 8 and 60
-// groups, 1032 to 4096 channels wide: a tile alone on its CU with most CUs idle, and its share of a CU when all are busy (then the clock is down
-// to 1.8 - 1.9 GHz: such calls are bound by power, and what moves fewer bytes for a product is faster).  The input's gradient also
-// scales its weights, which makes the tiles of few rows dearer.  A tile is small to spread few rows over the chip and large to be fed with
-// fewer reads; two of 128 x 256 stay on a CU and fill each other's waits.  One group, 4096 -> 4096, outputs / input gradients in us:
-//   rows    256 x 256   128 x 256   128 x 128   64 x 128   32 x 128
-//    512       72 / 71     42 / 55     28 / 38    25 / 32    25 / 28
-//   1024       69 / 72     44 / 57     33 / 41    36 / 41    42 / 46
-//   4096      100 / 104   100 / 110   111 / 122  121 / 133  141 / 156
-//  16384      381 / 388   367 / 398   417 / 461  450 / 492  524 / 587
+// groups, 1024 to 4096 channels wide (the rule takes the fastest form in all 47): a tile alone on its CU with most CUs idle, and its share of a CU
+// when all are busy (then the clock is down to 1.8 - 1.9 GHz: such calls are bound by power, and what moves fewer bytes for a product is
+// faster).  The input's gradient also scales its weights, which makes small tiles dearer.  A tile is small to spread few rows over the chip
+// and large to be fed with fewer reads; two of 128 x 256 stay on a CU and fill each other's waits (one of 256 x 256 instead: 72 / 69 us,
+// 69 / 69, 100 / 104, 381 / 385).  One group, 4096 -> 4096, outputs / input gradients in us:
+//   rows    128 x 256   128 x 128   64 x 128   32 x 128
+//    512      42 / 47     28 / 36    25 / 30    25 / 26
+//   1024      44 / 49     33 / 41    36 / 39    42 / 44
+//   4096     100 / 103   111 / 119  121 / 128  141 / 152
+//  16384     367 / 383   417 / 450  450 / 479  524 / 576
 struct TileForm {
     int rows, cols;
     float alone[2], share[2];                                  // [input's gradient]
 };
-constexpr TileForm TILE_FORMS[] = {{256, 256, {0.0f, 0.93f}, {0.0f, 1.62f}},
-                                   {128, 256, {0.53f, 0.95f}, {0.80f, 0.83f}},
-                                   {128, 128, {0.34f, 0.57f}, {0.44f, 0.48f}},
-                                   {64, 128, {0.35f, 0.46f}, {0.24f, 0.26f}},
-                                   {32, 128, {0.35f, 0.39f}, {0.14f, 0.153f}}};
+constexpr TileForm TILE_FORMS[] = {{128, 256, {0.53f, 0.64f}, {0.80f, 0.825f}},
+                                   {128, 128, {0.34f, 0.54f}, {0.44f, 0.47f}},
+                                   {64, 128, {0.35f, 0.42f}, {0.24f, 0.25f}},
+                                   {32, 128, {0.35f, 0.36f}, {0.14f, 0.15f}}};
 
 int tile_form(int64_t rows, int groups, int N, bool grad)
 {
     int best = 0;
     float least = 0.0f;
-    const int first = grad ? 0 : 1;                            // (outputs: two tiles of 128 x 256 on a CU beat one of 256 x 256 everywhere)
-    for (int i = first; i < (int)(sizeof(TILE_FORMS) / sizeof(TILE_FORMS[0])); ++i) {
+    for (int i = 0; i < (int)(sizeof(TILE_FORMS) / sizeof(TILE_FORMS[0])); ++i) {
         const TileForm &f = TILE_FORMS[i];
         const float alone = f.alone[grad], share = f.share[grad];
         // (of several groups, the last tile of each is half full on average)
@@ -632,7 +637,7 @@ int tile_form(int64_t rows, int groups, int N, bool grad)
         const float tiles = down * (float)((N + f.cols - 1) / f.cols);
         const float turns = ceilf(tiles / 256.0f), full = turns * share > alone ? turns * share : alone;
         const float time = alone + (full - alone) * tiles / (256.0f * turns);
-        if (i == first || time < least) {
+        if (i == 0 || time < least) {
             best = i;
             least = time;
         }
@@ -655,12 +660,9 @@ int launch_rows(RowsArgs p, hipStream_t s)
         return launch_few<T, GRAD, ADAPT, 4, 2>(p, s);
     }
     switch (tile_form(p.rows, p.groups, p.N, GRAD)) {
-    case 0:
-        if constexpr (GRAD) return launch_tiles<T, GRAD, ADAPT, 256, 256, 128, 64, 4>(p, s);
-        return SNN_ERR_UNSUPPORTED;                            // (never: see tile_form)
-    case 1: return launch_tiles<T, GRAD, ADAPT, 128, 256, 128, 64, 4>(p, s);
-    case 2: return launch_tiles<T, GRAD, ADAPT, 128, 128, 128, 32, 4>(p, s);
-    case 3: return launch_tiles<T, GRAD, ADAPT, 64, 128, 64, 32, 4>(p, s);
+    case 0: return launch_tiles<T, GRAD, ADAPT, 128, 256, 128, 64, 4>(p, s);
+    case 1: return launch_tiles<T, GRAD, ADAPT, 128, 128, 128, 32, 4>(p, s);
+    case 2: return launch_tiles<T, GRAD, ADAPT, 64, 128, 64, 32, 4>(p, s);
     default: return launch_tiles<T, GRAD, ADAPT, 32, 128, 32, 32, 4>(p, s);
     }
 }
