@@ -54,6 +54,11 @@ int launch_linear_prepare(const LinearGeom &g, const uint16_t *codebook, const u
 int launch_linear_rows(const LinearGeom &g, bool grad, const void *in, int64_t ld_in, int64_t rows, const int32_t *offsets,
                        const void *weights, void *out, int64_t ld_out, const Adapters *ad, const void *up, const float *low, hipStream_t s);
 
+// few rows with the adapters' inner products made by the same launch: whether a call is one of these, and it
+bool adapters_in_one_launch(const LinearGeom &g, int64_t rows, int rank);
+int launch_adapters_in_one(const LinearGeom &g, const Adapters &ad, const void *x, int64_t ldx, int64_t rows, const void *weights, void *y, int64_t ldy,
+                           float *low, hipStream_t s);
+
 size_t linear_weight_grad_workspace_bytes(const LinearGeom &g, int64_t rows, bool kept);
 int launch_linear_weight_grad(const LinearGeom &g, const RowsIn &x, const void *dy, int64_t lddy, int64_t rows, const int32_t *offsets,
                               const void *weights, float *dw, float *dalpha, void *ws, hipStream_t s);

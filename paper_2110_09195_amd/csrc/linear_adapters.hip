@@ -498,6 +498,7 @@ template <class T>
 int forward(const LinearGeom &g, const Adapters &ad, const void *x, int64_t ldx, int64_t rows, const void *weights, void *y, int64_t ldy,
             float *low, float *scaled, hipStream_t s)
 {
+    if (adapters_in_one_launch(g, rows, ad.rank)) return launch_adapters_in_one(g, ad, x, ldx, rows, weights, y, ldy, low, s);
     const int rc = launch_low<T>(g.C_in, ad, ad.A, x, ldx, rows, low, scaled, nullptr, s);
     if (rc != SNN_OK) return rc;
     return launch_linear_rows(g, false, x, ldx, rows, nullptr, weights, y, ldy, &ad, ad.B, scaled, s);

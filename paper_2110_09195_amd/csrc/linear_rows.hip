@@ -195,7 +195,13 @@ struct AdapterShare {
     const float *low;
     const int32_t *of_row;
     int n, rank;
+    const void *down;                // OWN: the adapters' other matrix [n][rank][K], their scales, and where the unscaled inner products go
+    const float *scale;
+    float *low_out;
 };
+
+// How the adapters' share gets its inner products: not at all, from another launch, or by the kernel itself.
+enum { NONE, GIVEN, OWN };
 
 struct RowsArgs {
     const void *in;
@@ -220,7 +226,7 @@ struct RowsArgs {
 //   - Bits become operand registers by a shift and a masked xor (two VALU instructions for 128 weights): the weights cost LDS a
 //     sixteenth of what the rows cost, and HBM as well.
 //   - GRAD: the contracted axis is the output channels, and alpha, on that axis, is what the signs are put on: exact, and free.
-template <class T, bool GRAD, bool ADAPT, int BT, int BN, int WT, int WN, int STAGES>
+template <class T, bool GRAD, int ADAPT, int BT, int BN, int WT, int WN, int STAGES>
 __global__ __launch_bounds__(64 * (BT / WT) * (BN / WN), 2)
 void linear_rows_kernel(RowsArgs p)
 {
@@ -450,12 +456,55 @@ void linear_rows_kernel(RowsArgs p)
 }
 
 // ---- few rows ----------------------------------------------------------------------------------------------------
+// Few rows of small adapters need one launch, not two: eight more waves make the inner products beside the others, in every workgroup again, which is
+// little as long as there are few of them (rows x rank x channels up to 64 K: 2048 -> 2048, one row of rank 8 4.3 us against 5.8, of rank 32 5.8 against 6.8,
+// 64 (128 K) 8.0 against 7.9; 4096 -> 4096, two rows of rank 8 6.7 against 6.9, of rank 16 8.0 against 7.3).
+constexpr int64_t OWN_PRODUCTS = 64 * 1024;
+// OWN: wave `first` of eight takes NR inner products of a row at a time, to LDS with the adapter's scale and, from one workgroup, to memory without.
+constexpr int OWN_DOTS = 256;
+template <class T, int NR>
+__device__ inline void own_dots(const RowsArgs &p, int first, int lane, bool out, float *own)
+{
+    using v8 = typename Half<T>::v8;
+    const int rank = p.ad.rank;
+    for (int i = first * NR; i < p.rows * rank; i += 8 * NR) { // (rank is a multiple of NR)
+        const int t = i / rank, r = i - t * rank, a = p.ad.of_row[t];
+        const bool some = a >= 0 && a < p.ad.n;
+        float sum[NR] = {}, scale = 0.0f;
+        if (some) {
+            scale = p.ad.scale[a];
+            const T *x = (const T *)p.in + t * p.ld_in, *down = (const T *)p.ad.down + ((int64_t)a * rank + r) * p.K;
+#pragma unroll(NR == 1 ? 4 : 2)
+            for (int k = lane * 8; k < p.K; k += 512) {
+                const v8 u = *(const v8 *)(x + k);
+#pragma unroll
+                for (int j = 0; j < NR; ++j) {
+                    const v8 v = *(const v8 *)(down + (int64_t)j * p.K + k);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[j] = fmaf((float)u[e], (float)v[e], sum[j]);
+                }
+            }
+#pragma unroll
+            for (int d = 32; d; d >>= 1)
+#pragma unroll
+                for (int j = 0; j < NR; ++j) sum[j] += __shfl_xor(sum[j], d);
+        }
+        if (lane == 0) {
+#pragma unroll
+            for (int j = 0; j < NR; ++j) {
+                own[i + j] = sum[j] * scale;
+                if (out && p.ad.low_out) p.ad.low_out[i + j] = sum[j];
+            }
+        }
+    }
+}
+
 // 16 rows by 16 NB columns a workgroup: its eight waves take the contracted channels in turn (blocks of 64) and their sums are joined in
 // LDS in the order of the waves.  The weights are read once, one bit each; what counts is how fast a CU gets at the rows, which every
 // workgroup reads (they stay in L2): neighbouring lanes have to load neighbouring bytes (150 GB/s a CU; with a row a lane, as the operand
 // wants them, 38), so the rows go through LDS, without registers, a wave's own part of it, AHEAD blocks at once.
-template <class T, bool GRAD, bool ADAPT, int NB, int AHEAD>
-__global__ __launch_bounds__(512)
+template <class T, bool GRAD, int ADAPT, int NB, int AHEAD>
+__global__ __launch_bounds__(ADAPT == OWN ? 1024 : 512)
 void linear_few_kernel(RowsArgs p)
 {
     using H = Half<T>;
@@ -465,6 +514,7 @@ void linear_few_kernel(RowsArgs p)
     constexpr int IN = WAVES * AHEAD * 2048, SUMS = WAVES * 16 * (16 * NB + 1) * 4;
     __shared__ __align__(16) char lds[IN > SUMS ? IN : SUMS];
     float(*const part)[16][16 * NB + 1] = (float(*)[16][16 * NB + 1])lds;
+    __shared__ __align__(16) float own[ADAPT == OWN ? OWN_DOTS : 1];         // scaled inner products [rows][rank]
     RowTile tile;
     if (!find_tile<16>(p.offsets, p.groups, p.rows, p.col_tiles, p.col_div, tile)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -488,7 +538,14 @@ void linear_few_kernel(RowsArgs p)
     const __amdgpu_buffer_rsrc_t ra = buffer(alpha, p.alpha_stride * 2);
 
     f32x4 acc[NB] = {};
-    for (int k0 = wave; k0 < p.kbs; k0 += WAVES * AHEAD) {
+    if constexpr (ADAPT == OWN) {
+        // the upper eight waves: inner products with the adapters' matrices
+        if (wave >= WAVES) {
+            if (p.rows * p.ad.rank <= 2 * WAVES) own_dots<T, 1>(p, wave - WAVES, lane, tile.col == 0, own);
+            else own_dots<T, 4>(p, wave - WAVES, lane, tile.col == 0, own);
+        }
+    }
+    for (int k0 = wave; k0 < (ADAPT == OWN && wave >= WAVES ? 0 : p.kbs); k0 += WAVES * AHEAD) {
         uint32_t word[AHEAD][NB];
         u32x4 one[AHEAD][2];
 #pragma unroll
@@ -515,10 +572,11 @@ void linear_few_kernel(RowsArgs p)
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
     __syncthreads();
+    if (ADAPT != OWN || wave < WAVES)
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+        for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) part[wave][ln][16 * i + 4 * q + r] = acc[i][r];
+            for (int r = 0; r < 4; ++r) part[wave][ln][16 * i + 4 * q + r] = acc[i][r];
     __syncthreads();
 
     if (tid >= 128 * NB) return;
@@ -542,7 +600,8 @@ void linear_few_kernel(RowsArgs p)
                 const v8 u0 = *(const v8 *)(u + k), u1 = *(const v8 *)(u + p.ad.rank + k);
                 float z[8];
 #pragma unroll
-                for (int i = 0; i < 8; i += 4) *(f32x4 *)(z + i) = *(const f32x4 *)(p.ad.low + scaled_at(t, k + i, p.ad.rank));
+                for (int i = 0; i < 8; i += 4)
+                    *(f32x4 *)(z + i) = ADAPT == OWN ? *(const f32x4 *)(own + t * p.ad.rank + k + i) : *(const f32x4 *)(p.ad.low + scaled_at(t, k + i, p.ad.rank));
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     v0 = fmaf(z[i], (float)u0[i], v0);
@@ -575,7 +634,7 @@ int64_t tile_grid(int64_t rows, int groups, int BT, int col_tiles)
     return ((rows + used * (BT - 1)) / BT * col_tiles + 7) / 8 * 8;
 }
 
-template <class T, bool GRAD, bool ADAPT, int BT, int BN, int WT, int WN, int STAGES>
+template <class T, bool GRAD, int ADAPT, int BT, int BN, int WT, int WN, int STAGES>
 int launch_tiles(RowsArgs p, hipStream_t s)
 {
     constexpr int WAVES = (BT / WT) * (BN / WN);
@@ -593,14 +652,14 @@ int launch_tiles(RowsArgs p, hipStream_t s)
     return check_launch();
 }
 
-template <class T, bool GRAD, bool ADAPT, int NB, int AHEAD>
+template <class T, bool GRAD, int ADAPT, int NB, int AHEAD>
 int launch_few(RowsArgs p, hipStream_t s)
 {
     p.col_tiles = (p.N + 16 * NB - 1) / (16 * NB);
     p.col_div = make_divisor(p.col_tiles);
     const int64_t grid = tile_grid(p.rows, p.groups, 16, p.col_tiles);
     if (grid >= ((int64_t)1 << 31)) return SNN_ERR_UNSUPPORTED;
-    linear_few_kernel<T, GRAD, ADAPT, NB, AHEAD><<<dim3((unsigned)grid), 512, 0, s>>>(p);
+    linear_few_kernel<T, GRAD, ADAPT, NB, AHEAD><<<dim3((unsigned)grid), ADAPT == OWN ? 1024 : 512, 0, s>>>(p);
     return check_launch();
 }
 
@@ -645,7 +704,7 @@ int tile_form(int64_t rows, int groups, int N, bool grad)
     return best;
 }
 
-template <class T, bool GRAD, bool ADAPT>
+template <class T, bool GRAD, int ADAPT>
 int launch_rows(RowsArgs p, hipStream_t s)
 {
     // Few rows: up to 1024 workgroups of 16 rows x 64 columns (4096 -> 4096: 256 rows 18 us either way, 64 rows 7.6 against 18; 2048 -> 2048:
@@ -670,14 +729,12 @@ int launch_rows(RowsArgs p, hipStream_t s)
 template <class T>
 int launch_typed(const RowsArgs &p, bool grad, hipStream_t s)
 {
-    if (p.ad.up) return grad ? launch_rows<T, true, true>(p, s) : launch_rows<T, false, true>(p, s);
-    return grad ? launch_rows<T, true, false>(p, s) : launch_rows<T, false, false>(p, s);
+    if (p.ad.up) return grad ? launch_rows<T, true, GIVEN>(p, s) : launch_rows<T, false, GIVEN>(p, s);
+    return grad ? launch_rows<T, true, NONE>(p, s) : launch_rows<T, false, NONE>(p, s);
 }
 
-}  // namespace
-
-int launch_linear_rows(const LinearGeom &g, bool grad, const void *in, int64_t ld_in, int64_t rows, const int32_t *offsets,
-                       const void *weights, void *out, int64_t ld_out, const Adapters *ad, const void *up, const float *low, hipStream_t s)
+RowsArgs rows_args(const LinearGeom &g, bool grad, const void *in, int64_t ld_in, int64_t rows, const int32_t *offsets, const void *weights, void *out,
+                   int64_t ld_out)
 {
     const char *w = (const char *)weights;
     RowsArgs p = {};
@@ -689,8 +746,30 @@ int launch_linear_rows(const LinearGeom &g, bool grad, const void *in, int64_t l
     p.out = out; p.ld_out = ld_out;
     p.N = grad ? g.C_in : g.C_out;
     p.K = grad ? g.C_out : g.C_in;
-    if (ad) p.ad = {up, low, ad->of_row, ad->n, ad->rank};
+    return p;
+}
+
+}  // namespace
+
+int launch_linear_rows(const LinearGeom &g, bool grad, const void *in, int64_t ld_in, int64_t rows, const int32_t *offsets,
+                       const void *weights, void *out, int64_t ld_out, const Adapters *ad, const void *up, const float *low, hipStream_t s)
+{
+    RowsArgs p = rows_args(g, grad, in, ld_in, rows, offsets, weights, out, ld_out);
+    if (ad) p.ad = {up, low, ad->of_row, ad->n, ad->rank, nullptr, nullptr, nullptr};
     return g.dtype == SNN_DTYPE_BF16 ? launch_typed<__bf16>(p, grad, s) : launch_typed<_Float16>(p, grad, s);
+}
+
+bool adapters_in_one_launch(const LinearGeom &g, int64_t rows, int rank)
+{
+    return rows > 0 && rows <= 16 && g.C_out <= 4096 && rows * rank <= OWN_DOTS && rows * rank * g.C_in <= OWN_PRODUCTS;
+}
+
+int launch_adapters_in_one(const LinearGeom &g, const Adapters &ad, const void *x, int64_t ldx, int64_t rows, const void *weights, void *y, int64_t ldy,
+                           float *low, hipStream_t s)
+{
+    RowsArgs p = rows_args(g, false, x, ldx, rows, nullptr, weights, y, ldy);
+    p.ad = {ad.B, nullptr, ad.of_row, ad.n, ad.rank, ad.A, ad.scale, low};
+    return g.dtype == SNN_DTYPE_BF16 ? launch_few<__bf16, false, OWN, 1, 2>(p, s) : launch_few<_Float16, false, OWN, 1, 2>(p, s);
 }
 
 }  // namespace snn

@@ -284,6 +284,7 @@ ADAPTED = [
     (70, 1024, 512, 5, 24, "wild"), (100, 200, 96, 3, 64, "runs"), (333, 320, 256, 6, 40, "runs"), (300, 64, 72, 2, 16, "none"),
     (513, 256, 520, 4, 32, "sorted"), (1000, 776, 1032, 7, 72, "runs"), (700, 512, 512, 1, 128, "sorted"), (300, 128, 128, 90, 8, "each"),
     (4500, 136, 4104, 5, 24, "runs"), (4000, 4104, 136, 3, 40, "wild"), (500, 1032, 1416, 12, 72, "runs"), (400, 1416, 1032, 12, 24, "wild"),
+    (1, 2048, 2056, 3, 32, "each"), (7, 520, 72, 4, 16, "wild"), (16, 264, 4096, 20, 8, "each"), (2, 4096, 4104, 2, 8, "each"),
 ]
 
 
@@ -354,7 +355,7 @@ def test_adapters(case, dtype):
                     scale[k].double() * (ady.t() @ (low_err * want_low[rows].abs() + tiny)), "dB of %d" % k)
 
 
-@pytest.mark.parametrize("T, kind", [(24, "each"), (400, "runs")])
+@pytest.mark.parametrize("T, kind", [(7, "each"), (24, "each"), (400, "runs")])
 def test_a_broken_adapter_reaches_its_own_rows_only(T, kind):
     L, n, r = Layer(6, 1, 128, 96, 16, "bf16"), 5, 16
     ids = ids_of(kind, T, n, 1)
