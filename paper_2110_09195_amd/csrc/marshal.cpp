@@ -269,6 +269,14 @@ at::Tensor rows_out(PyObject *o, const at::Tensor &like, int64_t rows, int64_t C
     return t && t->size(0) == rows ? *t : at::Tensor();
 }
 
+// The same for an output or a workspace whose elements lie next to each other, `sizes` of them along its axes.
+at::Tensor whole_out(PyObject *o, at::IntArrayRef sizes, const at::TensorOptions &options)
+{
+    if (o == Py_None) return at::empty(sizes, options);
+    const at::Tensor *const t = checked(o, c10::typeMetaToScalarType(options.dtype()));
+    return t && t->sizes() == sizes ? *t : at::Tensor();
+}
+
 // `ok` was true: the outputs in its place
 PyObject *outputs(PyObject *ok, at::Tensor &&a)
 {
@@ -313,13 +321,13 @@ PyObject *linear_rows(PyObject *const *a)
 PyObject *checkpoint_store(PyObject *const *a)
 {
     const at::Tensor *const x = tensor(a[0]);
-    if (!x || !x->is_cuda() || x->dim() != 2 || x->stride(1) != 1 || (x->scalar_type() != at::kBFloat16 && x->scalar_type() != at::kHalf) ||
-        a[1] != Py_None || a[2] != Py_None)
+    if (!x || !x->is_cuda() || x->dim() != 2 || x->stride(1) != 1 || (x->scalar_type() != at::kBFloat16 && x->scalar_type() != at::kHalf))
         Py_RETURN_FALSE;
     const int64_t rows = x->size(0), C = x->size(1);
     if (C > 65536) Py_RETURN_FALSE;
-    at::Tensor q = at::empty({rows, C}, x->options().dtype(at::kChar).requires_grad(false));
-    at::Tensor e = at::empty({rows, (C + 127) / 128 * 4}, x->options().dtype(at::kByte).requires_grad(false));
+    at::Tensor q = whole_out(a[1], {rows, C}, x->options().dtype(at::kChar).requires_grad(false));
+    at::Tensor e = whole_out(a[2], {rows, (C + 127) / 128 * 4}, x->options().dtype(at::kByte).requires_grad(false));
+    if (!q.defined() || !e.defined()) Py_RETURN_FALSE;
     const void *const px = x->data_ptr();
     void *const pq = q.data_ptr(), *const pe = e.data_ptr(), *const s = stream();
     const int64_t ldx = distance(*x);
@@ -333,18 +341,21 @@ PyObject *checkpoint_store(PyObject *const *a)
 PyObject *checkpoint_restore(PyObject *const *a)
 {
     const at::Tensor *const q = checked(a[0], at::kChar), *const e = checked(a[1], at::kByte);
-    if (!q || !e || q->dim() != 2 || e->dim() != 2 || !PyLong_CheckExact(a[2]) || a[3] != Py_None) Py_RETURN_FALSE;
+    if (!q || !e || q->dim() != 2 || e->dim() != 2 || !PyLong_CheckExact(a[2])) Py_RETURN_FALSE;
     const int64_t rows = q->size(0), C = q->size(1);
     const long dtype = PyLong_AsLong(a[2]);
     if (C > 65536 || e->size(0) != rows || e->size(1) != (C + 127) / 128 * 4 || (dtype != SNN_DTYPE_BF16 && dtype != SNN_DTYPE_F16)) {
         PyErr_Clear();
         Py_RETURN_FALSE;
     }
-    at::Tensor x = at::empty({rows, C}, q->options().dtype(type_of((int)dtype)));
+    const at::Tensor *const given = a[3] == Py_None ? nullptr : rows_of(a[3], type_of((int)dtype), C);
+    if (a[3] != Py_None && (!given || given->size(0) != rows)) Py_RETURN_FALSE;
+    at::Tensor x = given ? *given : at::empty({rows, C}, q->options().dtype(type_of((int)dtype)));
     const void *const pq = q->data_ptr(), *const pe = e->data_ptr();
     void *const px = x.data_ptr(), *const s = stream();
+    const int64_t ldx = distance(x);
     return outputs(enqueued("snn_checkpoint_restore", [&] {
-        return linear.checkpoint_restore((const int8_t *)pq, (const uint8_t *)pe, rows, (int)C, (int)dtype, px, C, s);
+        return linear.checkpoint_restore((const int8_t *)pq, (const uint8_t *)pe, rows, (int)C, (int)dtype, px, ldx, s);
     }), std::move(x));
 }
 
@@ -355,7 +366,7 @@ PyObject *adapters_forward(PyObject *const *a)
     const at::Tensor *x, *w, *ids, *A, *B, *scale;
     if (!linear_descriptor(a[0], d) || !(x = rows_of(a[1], type_of(d.dtype), d.C_in)) || !(w = checked(a[2], at::kByte)) ||
         !(ids = checked(a[3], at::kInt)) || !(A = checked(a[4], type_of(d.dtype))) || !(B = checked(a[5], type_of(d.dtype))) ||
-        !(scale = checked(a[6], at::kFloat)) || A->dim() != 3 || B->dim() != 3 || a[8] != Py_None || a[9] != Py_None)
+        !(scale = checked(a[6], at::kFloat)) || A->dim() != 3 || B->dim() != 3)
         Py_RETURN_FALSE;
     const int64_t rows = x->size(0), n = A->size(0), rank = A->size(1);
     if (ids->numel() != rows || n > 65536 || rank > 128 || A->size(2) != d.C_in || B->size(0) != n || B->size(1) != d.C_out || B->size(2) != rank ||
@@ -364,16 +375,17 @@ PyObject *adapters_forward(PyObject *const *a)
     snn_adapters ad = {(int32_t)n, (int32_t)rank, A->data_ptr(), B->data_ptr(), (const float *)scale->data_ptr()};
     at::Tensor y = rows_out(a[7], *x, rows, d.C_out);
     const size_t need = linear.adapters_workspace_bytes(&d, &ad, rows, SNN_ADAPTERS_FORWARD);
-    if (!y.defined() || !need) Py_RETURN_FALSE;
-    at::Tensor low = at::empty({rows, rank}, scale->options().requires_grad(false));
-    const at::Tensor ws = at::empty({(int64_t)need}, w->options());
+    at::Tensor low = whole_out(a[8], {rows, rank}, scale->options().requires_grad(false));
+    const at::Tensor *const given = a[9] == Py_None ? nullptr : checked(a[9], at::kByte);
+    if (!y.defined() || !need || !low.defined() || (a[9] != Py_None && (!given || (size_t)given->numel() < need))) Py_RETURN_FALSE;
+    const at::Tensor ws = given ? *given : at::empty({(int64_t)need}, w->options());
     const void *const px = x->data_ptr(), *const pw = w->data_ptr();
     const int32_t *const pi = (const int32_t *)ids->data_ptr();
     void *const py = y.data_ptr(), *const pl = low.data_ptr(), *const pws = ws.data_ptr(), *const s = stream();
     const int64_t ldx = distance(*x), ldy = distance(y);
     const size_t bytes = (size_t)w->numel();
     return outputs(enqueued("snn_adapters_forward", [&] {
-        return linear.adapters_forward(&d, &ad, px, ldx, rows, pi, pw, bytes, py, ldy, (float *)pl, pws, need, s);
+        return linear.adapters_forward(&d, &ad, px, ldx, rows, pi, pw, bytes, py, ldy, (float *)pl, pws, (size_t)ws.numel(), s);
     }), std::move(y), std::move(low));
 }
 

@@ -81,3 +81,23 @@ def test_given_outputs_and_rows_apart():
         y = B.snn_linear_forward(d, x, w, off)
     side.synchronize()
     assert torch.equal(y, want)
+
+
+def test_given_outputs_are_taken_natively_or_refused():
+    calls = {name: args for name, args, _ in _calls()}
+    x = calls["snn_checkpoint_store"][0]
+    q, e = B.snn_checkpoint_store(x)
+    q1, e1 = torch.empty_like(q), torch.empty_like(e)
+    assert B._fast.checkpoint_store(x, q1, e1) is not False and torch.equal(q, q1) and torch.equal(e, e1)
+    wide = torch.zeros(20, 88, device="cuda").half()
+    assert B._fast.checkpoint_restore(q, e, B.SNN_DTYPE_F16, wide[:, 8:80]) is not False
+    assert torch.equal(wide[:, 8:80], B.snn_checkpoint_restore((q, e), torch.float16)) and not bool(wide[:, :8].any()) and not bool(wide[:, 80:].any())
+    args = calls["snn_adapters_forward"]
+    y, low = B.snn_adapters_forward(*args)
+    y1, low1, ws = torch.zeros_like(y), torch.zeros_like(low), torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    assert B._fast.adapters_forward(*args, y1, low1, ws) is not False and torch.equal(y, y1) and torch.equal(low, low1)
+    for name, a, kw in (("snn_checkpoint_store", [x], {"q": q1[:3].contiguous()}), ("snn_checkpoint_store", [x], {"e": e1.short()}),
+                        ("snn_checkpoint_restore", [(q, e), torch.float16], {"x": wide[:7, :72]}), ("snn_adapters_forward", args, {"low": low1.double()}),
+                        ("snn_adapters_forward", args, {"workspace": ws[:16]}), ("snn_adapters_forward", args, {"workspace": ws.cpu()})):
+        with pytest.raises(Exception):
+            getattr(B, name)(*a, **kw)
