@@ -1,6 +1,8 @@
 // Rows through sub-bit weights: outputs and the gradient of the inputs (see linear.h for the bits' layout).
 #include "linear_device.h"
 
+#include <type_traits>
+
 #include <math.h>
 
 namespace snn {
@@ -226,7 +228,7 @@ struct RowsArgs {
 //   - Bits become operand registers by a shift and a masked xor (two VALU instructions for 128 weights): the weights cost LDS a
 //     sixteenth of what the rows cost, and HBM as well.
 //   - GRAD: the contracted axis is the output channels, and alpha, on that axis, is what the signs are put on: exact, and free.
-template <class T, bool GRAD, int ADAPT, int BT, int BN, int WT, int WN, int STAGES>
+template <class T, bool GRAD, int ADAPT, int BT, int BN, int WT, int WN, int STAGES, bool DEEP>
 __global__ __launch_bounds__(64 * (BT / WT) * (BN / WN), 2)
 void linear_rows_kernel(RowsArgs p)
 {
@@ -287,72 +289,118 @@ void linear_rows_kernel(RowsArgs p)
     };
 
     f32x16 acc[NB][TB] = {};
-    for (int s = 0; s < STAGES - 1; ++s)
+    for (int s = 0; s < (DEEP ? STAGES : STAGES - 1); ++s)
         for (int q = 0; q < 4; ++q) issue(s, s, q);
     const int h = lane >> 5, ln = lane & 31;
     uint32_t piece[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s) piece[s] = (uint32_t)(wt * WT + ln) * 128 + (((2 * s + h) ^ ((ln >> 1) & 7)) << 4);
 
-    // While the products of 16 channels run, the operands of the next 16 are made: fragments are read from LDS, bits turned into registers.  The
-    // instructions are dealt out between the matrix instructions, in whose shadow they issue.
-    v8 x[2][TB], w[2][NB];
     uint32_t ones = H::ONES;
     asm("" : "+v"(ones));                                      // (known to be constant, the masked xor would take two instructions)
-    uint32_t word[NB];
-    auto read_x = [&](int slot, int s, int to) {
+    if constexpr (DEEP) {
+        // Small tiles: a wave has too few products to hide LDS behind 16 channels at a time, and there may be no other wave on its SIMD.  All
+        // fragments of the next 64 channels are read while these are multiplied; a slot is free as soon as it has been read.  512 rows, 4096 -> 4096 in
+        // 64 x 128: outputs 22.6 -> 19.7 us, input gradients 29.5 -> 21.0.  (128 x 128 loses by it: 26.3 -> 30.7.)
+        v8 x[2][4][TB];
+        uint32_t word[2][NB];
+        u32x4 one[2][4];
+        auto fetch = [&](int slot, int to) {
+            const char *at = lds + slot * STAGE;
 #pragma unroll
-        for (int i = 0; i < TB; ++i) x[to][i] = *(const v8 *)(lds + slot * STAGE + piece[s] + i * 4096);
-    };
-    auto read_word = [&](int slot) {
+            for (int i = 0; i < NB; ++i) word[to][i] = *(const uint32_t *)(at + X_BYTES + ((wn * NB + i) * 64 + lane) * 4);
 #pragma unroll
-        for (int i = 0; i < NB; ++i) word[i] = *(const uint32_t *)(lds + slot * STAGE + X_BYTES + ((wn * NB + i) * 64 + lane) * 4);
-    };
-    uint32_t word_next[NB];
-    auto read_word_next = [&](int slot) {
+            for (int s = 0; s < 4; ++s) {
+                one[to][s] = u32x4{ones, ones, ones, ones};
+                if constexpr (GRAD) one[to][s] = *(const u32x4 *)(at + X_BYTES + BIT_BYTES + wave * 256 + (2 * s + h) * 16);
 #pragma unroll
-        for (int i = 0; i < NB; ++i) word_next[i] = *(const uint32_t *)(lds + slot * STAGE + X_BYTES + ((wn * NB + i) * 64 + lane) * 4);
-    };
-    auto make_w = [&](int slot, int s, int to) {
-        u32x4 one = {ones, ones, ones, ones};
-        if constexpr (GRAD) one = *(const u32x4 *)(lds + slot * STAGE + X_BYTES + BIT_BYTES + wave * 256 + (2 * s + h) * 16);
-#pragma unroll
-        for (int i = 0; i < NB; ++i) w[to][i] = signed_operand<T>(word[i], s, one);
-    };
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LOADS * (STAGES - 2)) : "memory");
-    read_word(0);
-    read_x(0, 0, 0);
-    make_w(0, 0, 0);
-    int slot = 0;
-    for (int kb = 0; kb < p.kbs; ++kb) {
-        // the next step's loads have landed (the ones behind it may be in flight), and everyone is done with the slot that is loaded next
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS * (STAGES - 3)) : "memory");
-        const int free = slot == 0 ? STAGES - 1 : slot - 1, next = slot == STAGES - 1 ? 0 : slot + 1;
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            issue(kb + STAGES - 1, free, s);
-            if (s == 2) read_word_next(next);
-            if (s < 3) {
-                read_x(slot, s + 1, (s + 1) & 1);
-                make_w(slot, s + 1, (s + 1) & 1);
-            } else {
-                read_x(next, 0, 0);
-#pragma unroll
-                for (int i = 0; i < NB; ++i) word[i] = word_next[i];
-                make_w(next, 0, 0);
+                for (int i = 0; i < TB; ++i) x[to][s][i] = *(const v8 *)(at + piece[s] + i * 4096);
             }
+        };
+        int slot = 0;
+        auto step = [&](int kb, auto which) {
+            constexpr int from = decltype(which)::value;
+            // the next step's loads have landed, and everyone has read this step's
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS * (STAGES - 2)) : "memory");
+            const int next = slot == STAGES - 1 ? 0 : slot + 1;
+            fetch(next, from ^ 1);
 #pragma unroll
-            for (int i = 0; i < NB; ++i)
+            for (int q = 0; q < 4; ++q) issue(kb + STAGES, slot, q);
 #pragma unroll
-                for (int j = 0; j < TB; ++j) acc[i][j] = H::mfma(w[s & 1][i], x[s & 1][j], acc[i][j]);
+            for (int s = 0; s < 4; ++s)
 #pragma unroll
-            for (int i = 0; i < NB * TB; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);           // a matrix instruction
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);           // an LDS read
-                __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);           // VALU
-            }
+                for (int i = 0; i < NB; ++i) {
+                    const v8 w = signed_operand<T>(word[from][i], s, one[from][s]);
+#pragma unroll
+                    for (int j = 0; j < TB; ++j) acc[i][j] = H::mfma(w, x[from][s][j], acc[i][j]);
+                }
+            slot = next;
+        };
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LOADS * (STAGES - 1)) : "memory");
+        fetch(0, 0);
+        for (int kb = 0; kb < p.kbs; kb += 2) {                // (a step past the last: zeros)
+            step(kb, std::integral_constant<int, 0>{});
+            step(kb + 1, std::integral_constant<int, 1>{});
         }
-        slot = next;
+    } else {
+        // While the products of 16 channels run, the operands of the next 16 are made: fragments are read from LDS, bits turned into registers.  The
+        // instructions are dealt out between the matrix instructions, in whose shadow they issue.
+        v8 x[2][TB], w[2][NB];
+        uint32_t word[NB];
+        auto read_x = [&](int slot, int s, int to) {
+#pragma unroll
+            for (int i = 0; i < TB; ++i) x[to][i] = *(const v8 *)(lds + slot * STAGE + piece[s] + i * 4096);
+        };
+        auto read_word = [&](int slot) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) word[i] = *(const uint32_t *)(lds + slot * STAGE + X_BYTES + ((wn * NB + i) * 64 + lane) * 4);
+        };
+        uint32_t word_next[NB];
+        auto read_word_next = [&](int slot) {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) word_next[i] = *(const uint32_t *)(lds + slot * STAGE + X_BYTES + ((wn * NB + i) * 64 + lane) * 4);
+        };
+        auto make_w = [&](int slot, int s, int to) {
+            u32x4 one = {ones, ones, ones, ones};
+            if constexpr (GRAD) one = *(const u32x4 *)(lds + slot * STAGE + X_BYTES + BIT_BYTES + wave * 256 + (2 * s + h) * 16);
+#pragma unroll
+            for (int i = 0; i < NB; ++i) w[to][i] = signed_operand<T>(word[i], s, one);
+        };
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LOADS * (STAGES - 2)) : "memory");
+        read_word(0);
+        read_x(0, 0, 0);
+        make_w(0, 0, 0);
+        int slot = 0;
+        for (int kb = 0; kb < p.kbs; ++kb) {
+            // the next step's loads have landed (the ones behind it may be in flight), and everyone is done with the slot that is loaded next
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS * (STAGES - 3)) : "memory");
+            const int free = slot == 0 ? STAGES - 1 : slot - 1, next = slot == STAGES - 1 ? 0 : slot + 1;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                issue(kb + STAGES - 1, free, s);
+                if (s == 2) read_word_next(next);
+                if (s < 3) {
+                    read_x(slot, s + 1, (s + 1) & 1);
+                    make_w(slot, s + 1, (s + 1) & 1);
+                } else {
+                    read_x(next, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < NB; ++i) word[i] = word_next[i];
+                    make_w(next, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < NB; ++i)
+#pragma unroll
+                    for (int j = 0; j < TB; ++j) acc[i][j] = H::mfma(w[s & 1][i], x[s & 1][j], acc[i][j]);
+#pragma unroll
+                for (int i = 0; i < NB * TB; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);           // a matrix instruction
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);           // an LDS read
+                    __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);           // VALU
+                }
+            }
+            slot = next;
+        }
     }
     int ids[TB];                                               // the adapters of the rows 32 j + ln
     if constexpr (ADAPT) {
@@ -634,14 +682,14 @@ int64_t tile_grid(int64_t rows, int groups, int BT, int col_tiles)
     return ((rows + used * (BT - 1)) / BT * col_tiles + 7) / 8 * 8;
 }
 
-template <class T, bool GRAD, int ADAPT, int BT, int BN, int WT, int WN, int STAGES>
+template <class T, bool GRAD, int ADAPT, int BT, int BN, int WT, int WN, int STAGES, bool DEEP>
 int launch_tiles(RowsArgs p, hipStream_t s)
 {
     constexpr int WAVES = (BT / WT) * (BN / WN);
     constexpr size_t LDS = (size_t)STAGES * (BT * 128 + BN * 8 + (GRAD ? 256 * WAVES : 0));
     static_assert(LDS >= (size_t)WAVES * 32 * (WN * 2 + 16) && LDS <= 160 * 1024, "LDS");
     static LdsGrant grant;
-    const auto kernel = linear_rows_kernel<T, GRAD, ADAPT, BT, BN, WT, WN, STAGES>;
+    const auto kernel = linear_rows_kernel<T, GRAD, ADAPT, BT, BN, WT, WN, STAGES, DEEP>;
     const int rc = grant_dynamic_lds((const void *)kernel, LDS, grant);
     if (rc != SNN_OK) return rc;
     p.col_tiles = (p.N + BN - 1) / BN;
@@ -663,33 +711,34 @@ int launch_few(RowsArgs p, hipStream_t s)
     return check_launch();
 }
 
-// Which tile a call of many rows takes.  Costs for 64 contracted channels in microseconds, fitted to calls of 512 to 16384 rows, of 1, 8 and 60
-// groups, 1024 to 4096 channels wide (the rule takes the fastest form in all 47): a tile alone on its CU with most CUs idle, and its share of a CU
-// when all are busy (then the clock is down to 1.8 - 1.9 GHz: such calls are bound by power, and what moves fewer bytes for a product is
-// faster).  The input's gradient also scales its weights, which makes small tiles dearer.  A tile is small to spread few rows over the chip
-// and large to be fed with fewer reads; two of 128 x 256 stay on a CU and fill each other's waits (one of 256 x 256 instead: 72 / 69 us,
-// 69 / 69, 100 / 104, 381 / 385).  One group, 4096 -> 4096, outputs / input gradients in us:
+// Which tile a call of many rows takes.  Costs in microseconds, fitted to 65 calls and their gradients of 320 to 16384 rows, of 1 to 60 groups of
+// even, random and skewed sizes, 776 to 4096 channels wide (the rule's choice is more than 5 % slower than the best form in nine of 130): for
+// 64 contracted channels a tile alone on its CU with most CUs idle, and its share of a CU when all are busy (then the clock is down to
+// 1.8 - 1.9 GHz: such calls are bound by power, and what moves fewer bytes for a product is faster); and once for a tile.  The input's gradient also
+// scales its weights, which makes small tiles dearer.  A tile is small to spread few rows over the chip and large to be fed with fewer
+// reads; two of 128 x 256 stay on a CU and fill each other's waits (one of 256 x 256 instead: 72 / 69 us, 69 / 69, 100 / 104, 381 / 385).
+// One group, 4096 -> 4096, outputs / input gradients in us:
 //   rows    128 x 256   128 x 128   64 x 128   32 x 128
-//    512      42 / 47     28 / 36    25 / 30    25 / 26
-//   1024      44 / 49     33 / 41    36 / 39    42 / 44
-//   4096     100 / 103   111 / 119  121 / 128  141 / 152
-//  16384     367 / 383   417 / 450  450 / 479  524 / 576
+//    512      38 / 46     26 / 36    20 / 23    22 / 26
+//   1024      41 / 47     32 / 39    33 / 36    39 / 45
+//   4096     100 / 104   110 / 121  116 / 126  136 / 155
+//  16384     376 / 390   418 / 461  441 / 478  521 / 590
 struct TileForm {
     int rows, cols;
-    float alone[2], share[2];                                  // [input's gradient]
+    float alone[2], share[2], once[2];                         // [input's gradient]
 };
-constexpr TileForm TILE_FORMS[] = {{128, 256, {0.53f, 0.64f}, {0.80f, 0.825f}},
-                                   {128, 128, {0.34f, 0.54f}, {0.44f, 0.47f}},
-                                   {64, 128, {0.35f, 0.42f}, {0.24f, 0.25f}},
-                                   {32, 128, {0.35f, 0.36f}, {0.14f, 0.15f}}};
+constexpr TileForm TILE_FORMS[] = {{128, 256, {0.44f, 0.66f}, {0.718f, 0.819f}, {4.3f, 1.8f}},
+                                   {128, 128, {0.30f, 0.52f}, {0.412f, 0.449f}, {1.4f, 2.2f}},
+                                   {64, 128, {0.28f, 0.29f}, {0.209f, 0.223f}, {1.2f, 1.5f}},
+                                   {32, 128, {0.29f, 0.37f}, {0.134f, 0.142f}, {0.8f, 0.9f}}};
 
-int tile_form(int64_t rows, int groups, int N, bool grad)
+int tile_form(int64_t rows, int groups, int N, int blocks, bool grad)
 {
     int best = 0;
     float least = 0.0f;
     for (int i = 0; i < (int)(sizeof(TILE_FORMS) / sizeof(TILE_FORMS[0])); ++i) {
         const TileForm &f = TILE_FORMS[i];
-        const float alone = f.alone[grad], share = f.share[grad];
+        const float alone = f.alone[grad] * blocks + f.once[grad], share = f.share[grad] * blocks + f.once[grad];
         // (of several groups, the last tile of each is half full on average)
         const float used = (float)(rows < groups ? rows : groups);
         const float down = groups > 1 ? (float)rows / f.rows + 0.5f * used : (float)((rows + f.rows - 1) / f.rows);
@@ -718,11 +767,11 @@ int launch_rows(RowsArgs p, hipStream_t s)
         if (narrow <= 1024) return launch_few<T, GRAD, ADAPT, 2, 2>(p, s);
         return launch_few<T, GRAD, ADAPT, 4, 2>(p, s);
     }
-    switch (tile_form(p.rows, p.groups, p.N, GRAD)) {
-    case 0: return launch_tiles<T, GRAD, ADAPT, 128, 256, 128, 64, 4>(p, s);
-    case 1: return launch_tiles<T, GRAD, ADAPT, 128, 128, 128, 32, 4>(p, s);
-    case 2: return launch_tiles<T, GRAD, ADAPT, 64, 128, 64, 32, 4>(p, s);
-    default: return launch_tiles<T, GRAD, ADAPT, 32, 128, 32, 32, 4>(p, s);
+    switch (tile_form(p.rows, p.groups, p.N, p.kbs, GRAD)) {
+    case 0: return launch_tiles<T, GRAD, ADAPT, 128, 256, 128, 64, 4, false>(p, s);
+    case 1: return launch_tiles<T, GRAD, ADAPT, 128, 128, 128, 32, 4, false>(p, s);
+    case 2: return launch_tiles<T, GRAD, ADAPT, 64, 128, 64, 32, 4, true>(p, s);
+    default: return launch_tiles<T, GRAD, ADAPT, 32, 128, 32, 32, 4, !GRAD>(p, s);
     }
 }
 
