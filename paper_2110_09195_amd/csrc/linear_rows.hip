@@ -714,7 +714,9 @@ int launch_few(RowsArgs p, hipStream_t s)
 // Which tile a call of many rows takes.  Costs in microseconds, fitted to 65 calls and their gradients of 320 to 16384 rows, of 1 to 60 groups of
 // even, random and skewed sizes, 776 to 4096 channels wide (the rule's choice is more than 5 % slower than the best form in nine of 130): for
 // 64 contracted channels a tile alone on its CU with most CUs idle, and its share of a CU when all are busy (then the clock is down to
-// 1.8 - 1.9 GHz: such calls are bound by power, and what moves fewer bytes for a product is faster); and once for a tile.  The input's gradient also
+// 1.8 - 1.9 GHz: such calls are bound by power, and what moves fewer bytes for a product is faster); and once for a tile.  Adapters add 0.9 us for every
+// 32 rows of a tile, whose loads wait for each other, and 0.3 when other tiles fill the wait (rank 64 or less): 1111 rows of rank 24, 1352 ->
+// 2056, 22.8 us in 128 x 128, 20.2 in 32 x 128; 3636 rows, 880 -> 4096, 44 and 46, and 40 in 128 x 256.  The input's gradient also
 // scales its weights, which makes small tiles dearer.  A tile is small to spread few rows over the chip and large to be fed with fewer
 // reads; two of 128 x 256 stay on a CU and fill each other's waits (one of 256 x 256 instead: 72 / 69 us, 69 / 69, 100 / 104, 381 / 385).
 // One group, 4096 -> 4096, outputs / input gradients in us:
@@ -732,13 +734,14 @@ constexpr TileForm TILE_FORMS[] = {{128, 256, {0.44f, 0.66f}, {0.718f, 0.819f}, 
                                    {64, 128, {0.28f, 0.29f}, {0.209f, 0.223f}, {1.2f, 1.5f}},
                                    {32, 128, {0.29f, 0.37f}, {0.134f, 0.142f}, {0.8f, 0.9f}}};
 
-int tile_form(int64_t rows, int groups, int N, int blocks, bool grad)
+int tile_form(int64_t rows, int groups, int N, int blocks, bool grad, int adapter_rank)
 {
     int best = 0;
     float least = 0.0f;
     for (int i = 0; i < (int)(sizeof(TILE_FORMS) / sizeof(TILE_FORMS[0])); ++i) {
         const TileForm &f = TILE_FORMS[i];
-        const float alone = f.alone[grad] * blocks + f.once[grad], share = f.share[grad] * blocks + f.once[grad];
+        const float adapters = (float)(f.rows / 32 * ((adapter_rank + 63) / 64));
+        const float alone = f.alone[grad] * blocks + f.once[grad] + 0.9f * adapters, share = f.share[grad] * blocks + f.once[grad] + 0.3f * adapters;
         // (of several groups, the last tile of each is half full on average)
         const float used = (float)(rows < groups ? rows : groups);
         const float down = groups > 1 ? (float)rows / f.rows + 0.5f * used : (float)((rows + f.rows - 1) / f.rows);
@@ -767,7 +770,7 @@ int launch_rows(RowsArgs p, hipStream_t s)
         if (narrow <= 1024) return launch_few<T, GRAD, ADAPT, 2, 2>(p, s);
         return launch_few<T, GRAD, ADAPT, 4, 2>(p, s);
     }
-    switch (tile_form(p.rows, p.groups, p.N, p.kbs, GRAD)) {
+    switch (tile_form(p.rows, p.groups, p.N, p.kbs, GRAD, ADAPT ? p.ad.rank : 0)) {
     case 0: return launch_tiles<T, GRAD, ADAPT, 128, 256, 128, 64, 4, false>(p, s);
     case 1: return launch_tiles<T, GRAD, ADAPT, 128, 128, 128, 32, 4, false>(p, s);
     case 2: return launch_tiles<T, GRAD, ADAPT, 64, 128, 64, 32, 4, true>(p, s);
