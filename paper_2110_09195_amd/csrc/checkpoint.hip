@@ -1,5 +1,6 @@
 // Activations kept in 8 bits: chunks of 32 channels of a row share a power of two.  Both directions move memory and nothing else counts:
-// a thread takes 8 channels (16 bytes one side, 8 the other), four neighbouring lanes a chunk.
+// a thread takes 8 channels (16 bytes one side, 8 the other), four neighbouring lanes a chunk.  16384 rows of 8192 channels: 73 - 88 us to
+// store, 66 to restore, 407 MB each: 5.1 TB/s and 6.1, a copy's rate (5.05) and, where some is still in the last cache, more.
 #include "linear_device.h"
 
 namespace snn {

@@ -61,7 +61,8 @@ __device__ inline void load_lds4(uint32_t lds, uint32_t offset, s32x4 from)
 }
 
 // The adapters' scaled inner products as the rows kernels read them: blocks of 32 rows, of those pieces of 4 of the rank, so that the rows of a
-// block lie next to each other (a load of a wave's operand is 512 bytes in a row then; read with a row a lane, they took half the adapters' share).
+// block lie next to each other (a load of a wave's operand is 512 bytes in a row then; with a row a lane, and the matrix read again for every 32 rows,
+// the backward call of 8192 rows of rank 64, 4096 -> 4096 took 305 us, and takes 294).
 __device__ inline int64_t scaled_at(int t, int r, int rank) { return ((int64_t)(t >> 5) * rank + (r & ~3)) * 32 + (t & 31) * 4 + (r & 3); }
 
 constexpr uint32_t NOWHERE = 0x80000000u;                      // an offset past every resource

@@ -13,6 +13,7 @@ namespace {
 // A block of 64 output channels by 64 vectors (512 input channels).  A member's byte is kept with the bits of its odd elements (1, 3, 5, 7 from the top) in the
 // high nibble and those of its even ones in the low one, set for -1: in that order four bytes make a word by their nibbles alone (linear.h).
 // F takes the bytes as they are; for D, 8 x 8 bits (the members of 8 outputs) are turned by three exchanges of bits.
+// Bound by memory and the members' look-up: 8 matrices of 4096 x 4096 (34 MB of indices in, 34 MB of images out) 18.3 us, 3.7 TB/s.
 constexpr int PREP_O = 64, PREP_V = 64, PREP_THREADS = 256;
 
 // The word of four bytes B0 .. B3, given with B0 at the top: low nibbles to the low half, high ones to the high half.
@@ -228,6 +229,9 @@ struct RowsArgs {
 //   - Bits become operand registers by a shift and a masked xor (two VALU instructions for 128 weights): the weights cost LDS a
 //     sixteenth of what the rows cost, and HBM as well.
 //   - GRAD: the contracted axis is the output channels, and alpha, on that axis, is what the signs are put on: exact, and free.
+// Bound: many rows by the matrix pipes at the clock that the chip's power leaves them (77 % busy; 16384 rows in 8 groups of uneven sizes, 4096 ->
+// 4096, 413 us = 1.33 PFLOP/s, 16384 rows 8192 -> 8192 in one 1427 us = 1.54; input gradients 434 and 1490), few rows by a step's latency, 0.3 us:
+// 1537 rows of 60 groups, 1032 -> 1416, 13.7 us.
 template <class T, bool GRAD, int ADAPT, int BT, int BN, int WT, int WN, int STAGES, bool DEEP>
 __global__ __launch_bounds__(64 * (BT / WT) * (BN / WN), 2)
 void linear_rows_kernel(RowsArgs p)
@@ -550,7 +554,8 @@ __device__ inline void own_dots(const RowsArgs &p, int first, int lane, bool out
 // 16 rows by 16 NB columns a workgroup: its eight waves take the contracted channels in turn (blocks of 64) and their sums are joined in
 // LDS in the order of the waves.  The weights are read once, one bit each; what counts is how fast a CU gets at the rows, which every
 // workgroup reads (they stay in L2): neighbouring lanes have to load neighbouring bytes (150 GB/s a CU; with a row a lane, as the operand
-// wants them, 38), so the rows go through LDS, without registers, a wave's own part of it, AHEAD blocks at once.
+// wants them, 38), so the rows go through LDS, without registers, a wave's own part of it, AHEAD blocks at once.  Bound by latency: 16 rows
+// 4096 -> 4096 4.7 us, of which the 2 MB of weights are 0.4 at the memory's rate; 32 rows of 32 groups 2048 -> 1024 (5 MB) 6.7 with its launch.
 template <class T, bool GRAD, int ADAPT, int NB, int AHEAD>
 __global__ __launch_bounds__(ADAPT == OWN ? 1024 : 512)
 void linear_few_kernel(RowsArgs p)
@@ -711,8 +716,8 @@ int launch_few(RowsArgs p, hipStream_t s)
     return check_launch();
 }
 
-// Which tile a call of many rows takes.  Costs in microseconds, fitted to 65 calls and their gradients of 320 to 16384 rows, of 1 to 60 groups of
-// even, random and skewed sizes, 776 to 4096 channels wide (the rule's choice is more than 5 % slower than the best form in nine of 130): for
+// Which tile a call of many rows takes.  Costs in microseconds, fitted to 59 calls and their gradients of 320 to 16384 rows, of 1 to 60 groups of
+// even, random and skewed sizes, 776 to 4096 channels wide (its choice is more than 5 % slower than the best form in five of 118): for
 // 64 contracted channels a tile alone on its CU with most CUs idle, and its share of a CU when all are busy (then the clock is down to
 // 1.8 - 1.9 GHz: such calls are bound by power, and what moves fewer bytes for a product is faster); and once for a tile.  Adapters add 0.9 us for every
 // 32 rows of a tile, whose loads wait for each other, and 0.3 when other tiles fill the wait (rank 64 or less): 1111 rows of rank 24, 1352 ->
@@ -759,12 +764,13 @@ int tile_form(int64_t rows, int groups, int N, int blocks, bool grad, int adapte
 template <class T, bool GRAD, int ADAPT>
 int launch_rows(RowsArgs p, hipStream_t s)
 {
-    // Few rows: up to 1024 workgroups of 16 rows x 64 columns (4096 -> 4096: 256 rows 18 us either way, 64 rows 7.6 against 18; 2048 -> 2048:
-    // 256 rows 7.5 against 11, 512 rows 12 either way; 60 groups 1032 -> 1416: 64 rows 9 either way, 1537 rows 53 against 17).
+    // Few rows: as long as there are not many workgroups of 16 rows x 64 columns.  Outputs / input gradients in us, so and in tiles: 4096 -> 4096, 64
+    // rows 8.1 / 8.6 and 18.5 / 19.9, 256 rows (1024 workgroups) 19.2 / 17.1 and 18.9 / 20.2, 320 rows 21.5 / 19.9 and 18.8 / 20.2; 2048 -> 2048, 384 rows
+    // (768) 9.7 / 9.1 and 9.9 / 11.8, 640 rows (1280) 13.4 / 12.2 and 12.3 / 11.9; 60 groups 1032 -> 1416, 1537 rows 20.1 / 19.7 and 11.5 / 14.4.
     // Narrower ones where they would leave CUs idle: 4096 columns, 16 rows 4.7 us in 16, 5.3 in 32, 7.1 in 64; 64 rows 10.1, 7.5, 7.6;
     // 100 rows 13.8, 11.6, 11.1.
     const int64_t used = p.rows < p.groups ? p.rows : p.groups, tiles = (p.rows + used * 15) / 16;
-    if (tiles * ((p.N + 63) / 64) <= 1024) {
+    if (tiles * ((p.N + 63) / 64) <= (GRAD ? 1280 : 896)) {
         const int64_t narrow = tiles * ((p.N + 15) / 16);
         if (narrow <= 256) return launch_few<T, GRAD, ADAPT, 1, 2>(p, s);
         if (narrow <= 1024) return launch_few<T, GRAD, ADAPT, 2, 2>(p, s);
