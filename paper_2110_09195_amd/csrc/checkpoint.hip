@@ -7,14 +7,6 @@ namespace snn {
 
 namespace {
 
-// Where a thread's pieces of 8 channels lie: rows of `pieces` (whole words of exponents: 16 pieces each), a grid's stride apart.
-struct Walk {
-    int64_t rows;
-    int pieces;
-    int64_t step_rows;
-    int step_pieces;
-};
-
 // The unit's biased exponent: that of the largest finite magnitude less 6, not below 2^-126.
 __device__ inline uint32_t unit_exponent(float top)
 {
@@ -66,36 +58,7 @@ template <class T>
 __global__ __launch_bounds__(256)
 void checkpoint_restore_kernel(const int8_t *__restrict__ q, const uint8_t *__restrict__ e, Walk w, int C, T *__restrict__ x, int64_t ldx)
 {
-    using v8 = typename Half<T>::v8;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    int64_t t = id / w.pieces;
-    int p = (int)(id - t * w.pieces);
-    for (; t < w.rows; t += w.step_rows) {
-        if (p * 8 < C) {
-            const uint2 raw = *(const uint2 *)(q + t * C + p * 8);
-            const float u = unit_of(e[t * (w.pieces >> 2) + (p >> 2)]);
-            v8 v;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = (T)kept_value((int)(int8_t)((i < 4 ? raw.x : raw.y) >> (8 * (i & 3))), u);
-            *(u32x4 *)(x + t * ldx + p * 8) = __builtin_bit_cast(u32x4, v);
-        }
-        p += w.step_pieces;
-        if (p >= w.pieces) {
-            p -= w.pieces;
-            ++t;
-        }
-    }
-}
-
-// a grid of at most 8192 workgroups, and the walk of its threads
-unsigned walk_of(int64_t rows, int C, Walk &w)
-{
-    w.rows = rows;
-    w.pieces = (C + 127) / 128 * 16;
-    const int64_t blocks = (rows * w.pieces + 255) / 256, grid = blocks < 8192 ? blocks : 8192;
-    w.step_rows = grid * 256 / w.pieces;
-    w.step_pieces = (int)(grid * 256 % w.pieces);
-    return (unsigned)grid;
+    restore_rows(q, e, w, C, x, ldx, blockIdx.x);
 }
 
 }  // namespace

@@ -161,8 +161,16 @@ void low_tile_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__
     }
 }
 
-// What the backward call needs laid out otherwise, in one launch: A and B with their last two axes exchanged (tiles of 64 x 64), and low in two values
-// of the activations' type.
+// What the backward call needs laid out otherwise, in one launch: A and B with their last two axes exchanged (tiles of 64 x 64), low in two values
+// of the activations' type, and the inputs from their 8-bit form.  Bound by memory, and in small calls by the launch.
+struct KeptRows {
+    const int8_t *q;
+    const uint8_t *e;
+    Walk walk;
+    int C;
+    void *x;                          // [rows][C]
+};
+
 struct Exchange {
     const uint16_t *in;
     uint16_t *out;
@@ -192,14 +200,16 @@ __device__ inline void exchange_tile(const Exchange &e, int id, uint16_t (*s)[72
 
 template <class T>
 __global__ __launch_bounds__(256)
-void adapters_lay_out_kernel(Exchange A, Exchange B, int tiles_a, int tiles_ab, const float *__restrict__ low, T *__restrict__ pair, int64_t values)
+void adapters_lay_out_kernel(Exchange A, Exchange B, int tiles_a, int tiles_ab, const float *__restrict__ low, T *__restrict__ pair, int64_t values,
+                             int low_blocks, KeptRows kept)
 {
     __shared__ __align__(16) uint16_t s[64][72];
     const int id = blockIdx.x;
     if (id < tiles_a) exchange_tile(A, id, s);
     else if (id < tiles_ab) exchange_tile(B, id - tiles_a, s);
+    else if (id >= tiles_ab + low_blocks) restore_rows(kept.q, kept.e, kept.walk, kept.C, (T *)kept.x, kept.C, id - tiles_ab - low_blocks);
     else {
-        for (int64_t i = ((int64_t)(id - tiles_ab) * 256 + threadIdx.x) * 8; i < values; i += (int64_t)(gridDim.x - tiles_ab) * 2048) {
+        for (int64_t i = ((int64_t)(id - tiles_ab) * 256 + threadIdx.x) * 8; i < values; i += (int64_t)low_blocks * 2048) {
             float v[8];
             *(f32x4 *)v = *(const f32x4 *)(low + i);
             *(f32x4 *)(v + 4) = *(const f32x4 *)(low + i + 4);
@@ -517,8 +527,16 @@ int backward(const LinearGeom &g, const Adapters &ad, const RowsIn &x, const flo
         const Exchange A = {(const uint16_t *)ad.A, (uint16_t *)w.At, ad.rank, g.C_in, rt, ct};
         const Exchange B = {(const uint16_t *)ad.B, (uint16_t *)w.Bt, g.C_out, ad.rank, ot, rt};
         const int64_t values = rows * ad.rank, blocks = (values / 8 + 255) / 256;
-        const int tiles_a = ad.n * rt * ct, tiles_ab = tiles_a + ad.n * rt * ot;
-        adapters_lay_out_kernel<T><<<(unsigned)(tiles_ab + (blocks < 512 ? blocks : 512)), 256, 0, s>>>(A, B, tiles_a, tiles_ab, low, (T *)w.low_pair, values);
+        const int tiles_a = ad.n * rt * ct, tiles_ab = tiles_a + ad.n * rt * ot, low_blocks = (int)(blocks < 512 ? blocks : 512);
+        // (the inputs as 16-bit values once, not bytes widened by every tile: see launch_linear_weight_grad)
+        KeptRows kept = {};
+        unsigned kept_blocks = 0;
+        if (x.e) {
+            kept = {(const int8_t *)x.p, x.e, {}, g.C_in, w.kept};
+            kept_blocks = walk_of(rows, g.C_in, kept.walk);
+        }
+        adapters_lay_out_kernel<T><<<(unsigned)(tiles_ab + low_blocks) + kept_blocks, 256, 0, s>>>(A, B, tiles_a, tiles_ab, low, (T *)w.low_pair, values,
+                                                                                              low_blocks, kept);
         int rc = check_launch();
         if (rc != SNN_OK) return rc;
         rc = launch_low<T>(g.C_out, ad, w.Bt, dy, lddy, rows, nullptr, w.scaled, (T *)w.pair, s);
@@ -528,12 +546,9 @@ int backward(const LinearGeom &g, const Adapters &ad, const RowsIn &x, const flo
     }
     AdapterGradArgs A = {x.p, x.ld, w.pair, g.C_in, dA};
     const AdapterGradArgs B = {dy, lddy, w.low_pair, g.C_out, dB};
-    if (x.e && rows) {
-        // (16-bit values once, not bytes widened by every tile: see launch_linear_weight_grad)
+    if (x.e) {
         A.x = w.kept;
         A.ld = g.C_in;
-        const int rc = launch_checkpoint_restore((const int8_t *)x.p, x.e, rows, g.C_in, g.dtype, w.kept, A.ld, s);
-        if (rc != SNN_OK) return rc;
     }
     return ad.rank <= 32 ? launch_adapters_grad<T, 1>(ad, A, B, rows, w.parts, w.part, w.flags, s)
                          : launch_adapters_grad<T, 2>(ad, A, B, rows, w.parts, w.part, w.flags, s);

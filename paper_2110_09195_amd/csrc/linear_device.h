@@ -91,4 +91,50 @@ __device__ inline typename Half<T>::v8 read_turned(const char *at, int next)
     return __builtin_bit_cast(typename Half<T>::v8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// ---- 8-bit activations ---------------------------------------------------------------------------------------
+
+// Where a thread's pieces of 8 channels lie: rows of `pieces` (whole words of exponents: 16 pieces each), a grid's stride apart.
+struct Walk {
+    int64_t rows;
+    int pieces;
+    int64_t step_rows;
+    int step_pieces;
+};
+
+// a grid of at most 8192 workgroups, and the walk of its threads
+inline unsigned walk_of(int64_t rows, int C, Walk &w)
+{
+    w.rows = rows;
+    w.pieces = (C + 127) / 128 * 16;
+    const int64_t blocks = (rows * w.pieces + 255) / 256, grid = blocks < 8192 ? blocks : 8192;
+    w.step_rows = grid * 256 / w.pieces;
+    w.step_pieces = (int)(grid * 256 % w.pieces);
+    return (unsigned)grid;
+}
+
+// Values from their 8-bit form, by workgroup `block` of the walk's grid.
+template <class T>
+__device__ inline void restore_rows(const int8_t *__restrict__ q, const uint8_t *__restrict__ e, const Walk &w, int C, T *__restrict__ x, int64_t ldx, int64_t block)
+{
+    using v8 = typename Half<T>::v8;
+    const int64_t id = block * 256 + threadIdx.x;
+    int64_t t = id / w.pieces;
+    int p = (int)(id - t * w.pieces);
+    for (; t < w.rows; t += w.step_rows) {
+        if (p * 8 < C) {
+            const uint2 raw = *(const uint2 *)(q + t * C + p * 8);
+            const float u = unit_of(e[t * (w.pieces >> 2) + (p >> 2)]);
+            v8 v;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = (T)kept_value((int)(int8_t)((i < 4 ? raw.x : raw.y) >> (8 * (i & 3))), u);
+            *(u32x4 *)(x + t * ldx + p * 8) = __builtin_bit_cast(u32x4, v);
+        }
+        p += w.step_pieces;
+        if (p >= w.pieces) {
+            p -= w.pieces;
+            ++t;
+        }
+    }
+}
+
 }  // namespace snn
