@@ -705,14 +705,18 @@ int launch_tiles(RowsArgs p, hipStream_t s)
     return check_launch();
 }
 
-template <class T, bool GRAD, int ADAPT, int NB, int AHEAD>
+template <class T, bool GRAD, int ADAPT, int NB>
 int launch_few(RowsArgs p, hipStream_t s)
 {
     p.col_tiles = (p.N + 16 * NB - 1) / (16 * NB);
     p.col_div = make_divisor(p.col_tiles);
     const int64_t grid = tile_grid(p.rows, p.groups, 16, p.col_tiles);
     if (grid >= ((int64_t)1 << 31)) return SNN_ERR_UNSUPPORTED;
-    linear_few_kernel<T, GRAD, ADAPT, NB, AHEAD><<<dim3((unsigned)grid), ADAPT == OWN ? 1024 : 512, 0, s>>>(p);
+    // (up to eight blocks of 64 channels a wave has one: 98 rows of 14 groups 512 -> 2800 6.1 us, 7.3 with loads for two)
+    if (p.kbs <= 8)
+        linear_few_kernel<T, GRAD, ADAPT, NB, 1><<<dim3((unsigned)grid), ADAPT == OWN ? 1024 : 512, 0, s>>>(p);
+    else
+        linear_few_kernel<T, GRAD, ADAPT, NB, 2><<<dim3((unsigned)grid), ADAPT == OWN ? 1024 : 512, 0, s>>>(p);
     return check_launch();
 }
 
@@ -767,14 +771,16 @@ int launch_rows(RowsArgs p, hipStream_t s)
     // Few rows: as long as there are not many workgroups of 16 rows x 64 columns.  Outputs / input gradients in us, so and in tiles: 4096 -> 4096, 64
     // rows 8.1 / 8.6 and 18.5 / 19.9, 256 rows (1024 workgroups) 19.2 / 17.1 and 18.9 / 20.2, 320 rows 21.5 / 19.9 and 18.8 / 20.2; 2048 -> 2048, 384 rows
     // (768) 9.7 / 9.1 and 9.9 / 11.8, 640 rows (1280) 13.4 / 12.2 and 12.3 / 11.9; 60 groups 1032 -> 1416, 1537 rows 20.1 / 19.7 and 11.5 / 14.4.
-    // Narrower ones where they would leave CUs idle: 4096 columns, 16 rows 4.7 us in 16, 5.3 in 32, 7.1 in 64; 64 rows 10.1, 7.5, 7.6;
-    // 100 rows 13.8, 11.6, 11.1.
     const int64_t used = p.rows < p.groups ? p.rows : p.groups, tiles = (p.rows + used * 15) / 16;
     if (tiles * ((p.N + 63) / 64) <= (GRAD ? 1280 : 896)) {
-        const int64_t narrow = tiles * ((p.N + 15) / 16);
-        if (narrow <= 256) return launch_few<T, GRAD, ADAPT, 1, 2>(p, s);
-        if (narrow <= 1024) return launch_few<T, GRAD, ADAPT, 2, 2>(p, s);
-        return launch_few<T, GRAD, ADAPT, 4, 2>(p, s);
+        // Narrower ones where they would leave CUs idle (of several groups, some 0.6 tiles end in each).  Outputs / input gradients in workgroups of 16, 32 and
+        // 64 columns: 4096 -> 4096, 16 rows 5.0 / 5.1, 5.4 / 5.3, 7.2 / 7.1; 48 rows (768 of the narrowest) 8.5 / 9.5, 7.5 / 7.9, 7.3 / 7.1; 100 rows
+        // (1792) 14.1 / 16.8, 10.9 / 11.7, 10.6 / 9.9; 32 rows of 32 groups 2048 -> 1024 7.7, 6.5, 7.0.
+        const float ends = p.groups > 1 ? p.rows / 16.0f + 0.6f * (float)used : (float)tiles;
+        const float narrow = ends * (float)((p.N + 15) / 16);
+        if (narrow <= 256.0f) return launch_few<T, GRAD, ADAPT, 1>(p, s);
+        if (narrow <= (GRAD ? 640.0f : 1500.0f)) return launch_few<T, GRAD, ADAPT, 2>(p, s);
+        return launch_few<T, GRAD, ADAPT, 4>(p, s);
     }
     switch (tile_form(p.rows, p.groups, p.N, p.kbs, GRAD, ADAPT ? p.ad.rank : 0)) {
     case 0: return launch_tiles<T, GRAD, ADAPT, 128, 256, 128, 64, 4, false>(p, s);
@@ -827,7 +833,7 @@ int launch_adapters_in_one(const LinearGeom &g, const Adapters &ad, const void *
 {
     RowsArgs p = rows_args(g, false, x, ldx, rows, nullptr, weights, y, ldy);
     p.ad = {ad.B, nullptr, ad.of_row, ad.n, ad.rank, ad.A, ad.scale, low};
-    return g.dtype == SNN_DTYPE_BF16 ? launch_few<__bf16, false, OWN, 1, 2>(p, s) : launch_few<_Float16, false, OWN, 1, 2>(p, s);
+    return g.dtype == SNN_DTYPE_BF16 ? launch_few<__bf16, false, OWN, 1>(p, s) : launch_few<_Float16, false, OWN, 1>(p, s);
 }
 
 }  // namespace snn
