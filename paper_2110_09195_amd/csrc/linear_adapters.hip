@@ -258,7 +258,8 @@ int launch_low(int C, const Adapters &ad, const void *down, const void *x, int64
 // call left it, times scale).  A workgroup takes one adapter, 256 channels (64 a wave) and 32 RB of the rank.
 //   - Rows come in chunks of 32.  Lanes look 64 chunks over at once for the adapter's rows, and the chunks that have some are gone through, the loads
 //     of two of them in flight, without registers.  Rows of other adapters inside a chunk are not loaded: zeros in LDS.
-//   - Bound by memory: 8192 rows of rank 64, 4096 -> 4096 (134 MB) 41 - 45 us and 6 for the join; 27 at a copy's rate.
+//   - Bound by memory: 8192 rows of rank 64, 4096 -> 4096 (134 MB) 42 - 49 us (less where the inputs are still in the last cache) and 7 for the join; 27 at a copy's
+//     rate.
 //   - Rows and inner products (in two values of the activations' type) have the contracted axis across memory, and are turned by the reads of their
 //     fragments.
 struct AdapterGradArgs {

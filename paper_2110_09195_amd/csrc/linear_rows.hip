@@ -231,7 +231,7 @@ struct RowsArgs {
 //   - GRAD: the contracted axis is the output channels, and alpha, on that axis, is what the signs are put on: exact, and free.
 // Bound: many rows by the matrix pipes at the clock that the chip's power leaves them (77 % busy; 16384 rows in 8 groups of uneven sizes, 4096 ->
 // 4096, 413 us = 1.33 PFLOP/s, 16384 rows 8192 -> 8192 in one 1427 us = 1.54; input gradients 434 and 1490), few rows by a step's latency, 0.3 us:
-// 1537 rows of 60 groups, 1032 -> 1416, 13.7 us.
+// 1537 rows of 60 groups, 1032 -> 1416, 13.3 us.
 template <class T, bool GRAD, int ADAPT, int BT, int BN, int WT, int WN, int STAGES, bool DEEP>
 __global__ __launch_bounds__(64 * (BT / WT) * (BN / WN), 2)
 void linear_rows_kernel(RowsArgs p)
@@ -555,7 +555,7 @@ __device__ inline void own_dots(const RowsArgs &p, int first, int lane, bool out
 // LDS in the order of the waves.  The weights are read once, one bit each; what counts is how fast a CU gets at the rows, which every
 // workgroup reads (they stay in L2): neighbouring lanes have to load neighbouring bytes (150 GB/s a CU; with a row a lane, as the operand
 // wants them, 38), so the rows go through LDS, without registers, a wave's own part of it, AHEAD blocks at once.  Bound by latency: 16 rows
-// 4096 -> 4096 4.7 us, of which the 2 MB of weights are 0.4 at the memory's rate; 32 rows of 32 groups 2048 -> 1024 (5 MB) 6.7 with its launch.
+// 4096 -> 4096 4.7 us, of which the 2 MB of weights are 0.4 at the memory's rate; 32 rows of 32 groups 2048 -> 1024 (5 MB) 6.1 with its launch.
 template <class T, bool GRAD, int ADAPT, int NB, int AHEAD>
 __global__ __launch_bounds__(ADAPT == OWN ? 1024 : 512)
 void linear_few_kernel(RowsArgs p)
