@@ -84,6 +84,11 @@ SHAPES = [
     ([2100, 0, 1811], 264, 4104, 32, 0),
     ([2100, 0, 1811], 4104, 264, 32, 8),
     ([301, 0, 77], 2056, 2064, 64, 0),
+    # every form of tiles: outputs in 64 x 128, 32 x 128, 128 x 128, 128 x 256; the gradient of inputs likewise
+    ([13] * 20, 136, 2056, 32, 0), ([65] * 20, 136, 520, 16, 8), ([150] * 19 + [151], 136, 520, 64, 0), ([195] * 18 + [1, 396], 1032, 1416, 32, 0),
+    ([65] * 20, 776, 136, 8, 8), ([13] * 20, 2904, 136, 32, 0), ([150] * 19 + [151], 776, 136, 64, 0), ([26] * 20, 4104, 136, 32, 0),
+    # weights' gradients: rows in eight parts, in two, in one, of tiles dealt out in blocks
+    ([2100], 136, 1416, 32, 0), ([1101, 1100], 1416, 1416, 16, 0), ([2050, 2150], 1416, 1416, 32, 8), ([3100, 3001, 3200], 776, 4104, 32, 0),
 ]
 
 
@@ -285,6 +290,9 @@ ADAPTED = [
     (513, 256, 520, 4, 32, "sorted"), (1000, 776, 1032, 7, 72, "runs"), (700, 512, 512, 1, 128, "sorted"), (300, 128, 128, 90, 8, "each"),
     (4500, 136, 4104, 5, 24, "runs"), (4000, 4104, 136, 3, 40, "wild"), (500, 1032, 1416, 12, 72, "runs"), (400, 1416, 1032, 12, 24, "wild"),
     (1, 2048, 2056, 3, 32, "each"), (7, 520, 72, 4, 16, "wild"), (16, 264, 4096, 20, 8, "each"), (2, 4096, 4104, 2, 8, "each"),
+    # every form of tiles with adapters, outputs and the gradient of inputs
+    (5003, 520, 1416, 4, 24, "runs"), (8003, 136, 136, 30, 24, "wild"), (5003, 520, 136, 5, 24, "runs"), (5003, 136, 520, 7, 40, "sorted"),
+    (3001, 136, 4104, 3, 72, "wild"), (3907, 2904, 4104, 3, 24, "runs"),
 ]
 
 
