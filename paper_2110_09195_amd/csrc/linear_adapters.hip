@@ -476,13 +476,17 @@ int launch_adapters_grad(const Adapters &ad, const AdapterGradArgs &A, const Ada
 
 // Parts of the rows, joined by another launch: an adapter can have nearly all of them, and then its tiles alone would occupy a
 // fraction of the CUs (8192 rows of one adapter of rank 64, 4096 -> 4096: 64 chunks take 45 us, and eight parts of 32 chunks 33 with 5 for the join).  Parts of
-// at least 384 rows, while the workgroups (most of which find no rows of theirs, and end) stay few.
+// at least 384 rows, while the workgroups (most of which find no rows of theirs, and end) stay few; of 96, and 75 an adapter, where
+// there are not even as many of them as CUs (the call of 1274 rows of two adapters of rank 32, 1440 -> 608: two parts 36.7 us, eight 32.4; one
+// of 400 rows of eight adapters, 2048 -> 2048, 36.0 whole and 39 in two).
 int grad_parts(const LinearGeom &g, int n, int64_t rows)
 {
     const int64_t tiles = (g.C_in + 255) / 256 + (g.C_out + 255) / 256;
-    int parts = 1;
-    while (parts < 16 && tiles * parts < 256 && rows / (2 * parts) >= 384 && n * tiles * 2 * parts <= 4096) parts *= 2;
-    return parts;
+    for (int parts = 1;; parts *= 2) {
+        const int64_t of = rows / (2 * parts), workgroups = n * tiles * 2 * parts;
+        const bool more = tiles * parts < 256 && ((of >= 384 && workgroups <= 4096) || (of >= 96 && of / n >= 75 && workgroups <= 256));
+        if (parts == 16 || !more) return parts;
+    }
 }
 
 // The backward call's workspace: scaled inner products, also in two values of the activations' type, and low so; A and B with
