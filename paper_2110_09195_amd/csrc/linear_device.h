@@ -29,7 +29,9 @@ template <> struct Half<_Float16> {
     static __device__ f32x4 mfma16(v8 a, v8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 
-// A buffer resource: loads past `bytes` give zeros.
+// A buffer resource for the loads below: what they load past `bytes` is zeros.  The vector unit writes its registers (readfirstlane), and a vector memory
+// instruction may read such a register five wait states later at the earliest.  The compiler knows of its own loads, not of those in
+// assembly text, so the wait is part of the resource: nobody gets at the registers before it is over.
 __device__ inline s32x4 resource(const void *p, uint32_t bytes)
 {
     const uint64_t a = (uint64_t)p;
@@ -38,13 +40,16 @@ __device__ inline s32x4 resource(const void *p, uint32_t bytes)
     r[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32));
     r[2] = __builtin_amdgcn_readfirstlane((int)bytes);
     r[3] = 0x00020000;
+    asm("s_nop 4" : "+s"(r));
     return r;
 }
 
+// The same for the compiler's own loads.
 __device__ inline __amdgpu_buffer_rsrc_t buffer(const void *p, uint32_t bytes)
 {
-    const s32x4 r = resource(p, bytes);
-    return __builtin_amdgcn_make_buffer_rsrc((void *)((uint64_t)(uint32_t)r[0] | (uint64_t)(uint32_t)r[1] << 32), 0, r[2], 0x00020000);
+    const uint64_t a = (uint64_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)a), hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc((void *)((uint64_t)lo | (uint64_t)hi << 32), 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000);
 }
 
 __device__ inline uint32_t lds_address(const void *p) { return (uint32_t)(uint64_t)(__attribute__((address_space(3))) const void *)p; }
