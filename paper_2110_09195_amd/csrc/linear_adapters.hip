@@ -5,22 +5,13 @@ namespace snn {
 
 namespace {
 
-// v in two values of the activations' type, in planes of their own
-template <class T>
-__device__ inline void split1(float v, T *to, int64_t plane)
-{
-    const T hi = (T)v;
-    to[0] = hi;
-    to[plane] = (T)(v - (float)hi);
-}
-
 // low[t][r] = down[a][r] . x[t] and scaled[t][r] = scale[a] times it, a = the row's adapter; down [n][rank][C].
 // Few rows: a wave takes NR inner products of a row, so that the adapters' matrices, of which nearly every row has its own, are read by many CUs.
 // Bound by latency: 48 rows of rank 16, 4096 channels (6 MB) 3.4 us.
 template <class T, int NR>
 __global__ __launch_bounds__(256)
 void low_few_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__restrict__ x, int64_t ldx, float *__restrict__ low,
-                    float *__restrict__ scaled, T *__restrict__ pair, int64_t plane)
+                    float *__restrict__ scaled)
 {
     using v8 = typename Half<T>::v8;
     const int t = blockIdx.x, lane = threadIdx.x & 63, r = (blockIdx.y * 4 + (threadIdx.x >> 6)) * NR;
@@ -51,7 +42,6 @@ void low_few_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__r
         for (int j = 0; j < NR; ++j) {
             if (low) low[at + j] = acc[j];
             scaled[scaled_at(t, r + j, ad.rank)] = acc[j] * c;
-            if (pair) split1(acc[j] * c, pair + at + j, plane);
         }
     }
 }
@@ -64,7 +54,7 @@ void low_few_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__r
 template <class T, int RB, int STAGES>
 __global__ __launch_bounds__(256)
 void low_tile_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__restrict__ x, int64_t ldx, int rows,
-                     float *__restrict__ low, float *__restrict__ scaled, T *__restrict__ pair, int64_t plane)
+                     float *__restrict__ low, float *__restrict__ scaled)
 {
     using H = Half<T>;
     using v8 = typename H::v8;
@@ -154,15 +144,11 @@ void low_tile_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__
         if (low) *(f32x4 *)(low + at + i) = v;
         const f32x4 z = some ? v * c : v;
         *(f32x4 *)(scaled + scaled_at(t0 + rr, r0 + rc + i, ad.rank)) = z;
-        if (pair) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) split1(z[k], pair + at + i + k, plane);
-        }
     }
 }
 
-// What the backward call needs laid out otherwise, in one launch: A and B with their last two axes exchanged (tiles of 64 x 64), low in two values
-// of the activations' type, and the inputs from their 8-bit form.  Bound by memory, and in small calls by the launch.
+// What the backward call needs laid out otherwise, in one launch: A and B with their last two axes exchanged (tiles of 64 x 64), and the inputs
+// from their 8-bit form.  Bound by memory, and in small calls by the launch.
 struct KeptRows {
     const int8_t *q;
     const uint8_t *e;
@@ -200,25 +186,13 @@ __device__ inline void exchange_tile(const Exchange &e, int id, uint16_t (*s)[72
 
 template <class T>
 __global__ __launch_bounds__(256)
-void adapters_lay_out_kernel(Exchange A, Exchange B, int tiles_a, int tiles_ab, const float *__restrict__ low, T *__restrict__ pair, int64_t values,
-                             int low_blocks, KeptRows kept)
+void adapters_lay_out_kernel(Exchange A, Exchange B, int tiles_a, int tiles_ab, KeptRows kept)
 {
     __shared__ __align__(16) uint16_t s[64][72];
     const int id = blockIdx.x;
     if (id < tiles_a) exchange_tile(A, id, s);
     else if (id < tiles_ab) exchange_tile(B, id - tiles_a, s);
-    else if (id >= tiles_ab + low_blocks) restore_rows(kept.q, kept.e, kept.walk, kept.C, (T *)kept.x, kept.C, id - tiles_ab - low_blocks);
-    else {
-        for (int64_t i = ((int64_t)(id - tiles_ab) * 256 + threadIdx.x) * 8; i < values; i += (int64_t)low_blocks * 2048) {
-            float v[8];
-            *(f32x4 *)v = *(const f32x4 *)(low + i);
-            *(f32x4 *)(v + 4) = *(const f32x4 *)(low + i + 4);
-            typename Half<T>::v8 hi, lo;
-            split8<T>(v, hi, lo);
-            *(typename Half<T>::v8 *)(pair + i) = hi;
-            *(typename Half<T>::v8 *)(pair + values + i) = lo;
-        }
-    }
+    else restore_rows(kept.q, kept.e, kept.walk, kept.C, (T *)kept.x, kept.C, id - tiles_ab);
 }
 
 // Up to so many products (rows x rank x channels) a wave takes four inner products of a row, and the matrices come from L2 again for every row: 512 rows,
@@ -226,7 +200,7 @@ void adapters_lay_out_kernel(Exchange A, Exchange B, int tiles_a, int tiles_ab, 
 constexpr int64_t LOW_FEW_PRODUCTS = (int64_t)64 << 20;
 
 template <class T, int RB, int STAGES>
-int launch_low_tile(int C, const Adapters &ad, const T *down, const T *x, int64_t ldx, int64_t rows, float *low, float *scaled, T *pair, hipStream_t s)
+int launch_low_tile(int C, const Adapters &ad, const T *down, const T *x, int64_t ldx, int64_t rows, float *low, float *scaled, hipStream_t s)
 {
     constexpr size_t LDS = (size_t)4 * STAGES * 4096 * (1 + RB);
     static_assert(LDS >= 4 * 32 * (32 * RB + 1) * sizeof(float) && LDS <= 160 * 1024, "LDS");
@@ -234,38 +208,41 @@ int launch_low_tile(int C, const Adapters &ad, const T *down, const T *x, int64_
     const auto kernel = low_tile_kernel<T, RB, STAGES>;
     const int rc = grant_dynamic_lds((const void *)kernel, LDS, grant);
     if (rc != SNN_OK) return rc;
-    kernel<<<dim3((unsigned)((rows + 31) / 32), (ad.rank + 32 * RB - 1) / (32 * RB)), 256, LDS, s>>>(C, ad, down, x, ldx, (int)rows, low, scaled,
-                                                                                                  pair, rows * ad.rank);
+    kernel<<<dim3((unsigned)((rows + 31) / 32), (ad.rank + 32 * RB - 1) / (32 * RB)), 256, LDS, s>>>(C, ad, down, x, ldx, (int)rows, low, scaled);
     return check_launch();
 }
 
 template <class T>
-int launch_low(int C, const Adapters &ad, const void *down, const void *x, int64_t ldx, int64_t rows, float *low, float *scaled, T *pair, hipStream_t s)
+int launch_low(int C, const Adapters &ad, const void *down, const void *x, int64_t ldx, int64_t rows, float *low, float *scaled, hipStream_t s)
 {
     if (rows <= 64) {
-        low_few_kernel<T, 1><<<dim3((unsigned)rows, ad.rank / 4), 256, 0, s>>>(C, ad, (const T *)down, (const T *)x, ldx, low, scaled, pair, rows * ad.rank);
+        low_few_kernel<T, 1><<<dim3((unsigned)rows, ad.rank / 4), 256, 0, s>>>(C, ad, (const T *)down, (const T *)x, ldx, low, scaled);
         return check_launch();
     }
     if (rows * ad.rank * C <= LOW_FEW_PRODUCTS) {
-        low_few_kernel<T, 4><<<dim3((unsigned)rows, (ad.rank + 15) / 16), 256, 0, s>>>(C, ad, (const T *)down, (const T *)x, ldx, low, scaled, pair, rows * ad.rank);
+        low_few_kernel<T, 4><<<dim3((unsigned)rows, (ad.rank + 15) / 16), 256, 0, s>>>(C, ad, (const T *)down, (const T *)x, ldx, low, scaled);
         return check_launch();
     }
-    if (ad.rank <= 32) return launch_low_tile<T, 1, 4>(C, ad, (const T *)down, (const T *)x, ldx, rows, low, scaled, pair, s);
-    return launch_low_tile<T, 2, 3>(C, ad, (const T *)down, (const T *)x, ldx, rows, low, scaled, pair, s);
+    if (ad.rank <= 32) return launch_low_tile<T, 1, 4>(C, ad, (const T *)down, (const T *)x, ldx, rows, low, scaled, s);
+    return launch_low_tile<T, 2, 3>(C, ad, (const T *)down, (const T *)x, ldx, rows, low, scaled, s);
 }
 
 // Gradients of an adapter: the sum over its rows of x[t][c] low[t][r], for A (x the inputs, low = dlow) and B (x = dy, low as the forward
-// call left it, times scale).  A workgroup takes one adapter, 256 channels (64 a wave) and 32 RB of the rank.
+// call left it, times scale).  A workgroup takes one adapter, 256 channels and 32 RB of the rank, a
+// wave 32 of the rank by as many channels as that leaves it.
 //   - Rows come in chunks of 32.  Lanes look 64 chunks over at once for the adapter's rows, and the chunks that have some are gone through, the loads
 //     of two of them in flight, without registers.  Rows of other adapters inside a chunk are not loaded: zeros in LDS.
-//   - Bound by memory: 8192 rows of rank 64, 4096 -> 4096 (134 MB) 42 - 49 us (less where the inputs are still in the last cache) and 7 for the join; 27 at a copy's
+//   - Bound by memory: 8192 rows of rank 64, 4096 -> 4096 (134 MB) 54 - 60 us (less where the inputs are still in the last cache) and 7 for the join; 27 at a copy's
 //     rate.
-//   - Rows and inner products (in two values of the activations' type) have the contracted axis across memory, and are turned by the reads of their
-//     fragments.
+//   - Both operands have the contracted axis across memory.  Rows are turned by the reads of their fragments; inner products are read as they
+//     are (fp32, one of the rank a lane) and cut into values of the activations' type by the waves: three of bf16 (with two, that
+//     is 16 bits, and cut once in memory, the call above took 44 - 47).  128-byte pieces of rows 8 .. 15 of sixteen are exchanged two by two, so
+//     that both halves of a wave read different banks.
 struct AdapterGradArgs {
     const void *x;
     int64_t ld;
-    const void *pair;                 // the inner products: [2][rows][rank]
+    const float *low;                 // the inner products, by row [rows][rank] or (blocked) as scaled_at says
+    bool blocked;
     int C;
     void *out;                        // A: [n][rank][C]; B: [n][C][rank], times scale
 };
@@ -273,13 +250,10 @@ struct AdapterGradArgs {
 template <int RB>
 struct AdapterGrad {
     static constexpr int CH = 256, WAVES = 4, STAGES = 3;
-    static constexpr int X_BYTES = 32 * CH * 2, P_BYTES = 32 * RB * 64, STAGE = X_BYTES + 2 * P_BYTES;
+    static constexpr int X_BYTES = 32 * CH * 2, STAGE = X_BYTES + 32 * RB * 128;
     static constexpr size_t LDS = STAGES * STAGE;
     static_assert(LDS <= 80 * 1024, "two workgroups a CU");
 };
-
-// How 32-byte pieces of a row of `bytes` bytes are exchanged in LDS, so that those of rows 0 .. 3 lie in different banks.
-__device__ constexpr int piece_turn(int bytes, int row) { return bytes >= 256 ? (row & 3) << 1 : bytes == 128 ? row & 2 : 0; }
 
 template <class T, bool IS_B, int RB>
 __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradArgs &g, int a, int c0, int r0, int rows, int chunk0, int chunks, float *part_out,
@@ -288,12 +262,13 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
     using H = Half<T>;
     using v8 = typename H::v8;
     using S = AdapterGrad<RB>;
-    constexpr int CH = S::CH, STAGES = S::STAGES, THREADS = 64 * S::WAVES, CB = CH / 32 / S::WAVES;
+    constexpr int CH = S::CH, STAGES = S::STAGES, THREADS = 64 * S::WAVES, CB = CH / 32 * RB / S::WAVES;
     constexpr int PX = CH / 8, XL = 32 * PX / THREADS;                      // 16-byte pieces of a row, loads of a thread for a chunk
-    constexpr int PP = RB * 4, PL = 64 * PP / THREADS;                      // the same for the inner products' planes, one after the other
+    constexpr int PL = RB;                                                  // loads for the inner products: 32 rows of 8 RB pieces
     constexpr int LOADS = XL + PL;
-    static_assert(XL * THREADS == 32 * PX && PL * THREADS == 64 * PP, "whole loads");
+    static_assert(XL * THREADS == 32 * PX && THREADS == 32 * 8, "whole loads");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, ln = lane & 31;
+    const int wr = wave % RB, wc = wave / RB;                               // 32 of the rank and CB blocks of channels a wave
     const uint32_t lds0 = lds_address(lds);
 
     uint32_t xo[XL], po[PL];
@@ -302,13 +277,15 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
     for (int i = 0; i < XL; ++i) {
         const int r = (i * THREADS + tid) / PX, c = tid % PX;
         xr[i] = r;
-        xo[i] = (uint32_t)r * (uint32_t)(g.ld * 2) + ((((c >> 1) ^ piece_turn(CH * 2, r)) << 1) | (c & 1)) * 16;
+        xo[i] = (uint32_t)r * (uint32_t)(g.ld * 2) + ((((c >> 1) ^ ((r & 3) << 1)) << 1) | (c & 1)) * 16;
     }
 #pragma unroll
     for (int i = 0; i < PL; ++i) {
-        const int r = (i * THREADS + tid) / PP % 32, c = tid % PP, from = (((c >> 1) ^ piece_turn(RB * 64, r)) << 1) | (c & 1);
-        pr[i] = r;
-        po[i] = r0 + from * 8 < ad.rank ? (uint32_t)(r * ad.rank + from * 8) * 2 : NOWHERE;
+        int piece = (i * THREADS + tid) / 8;                                // of 128 bytes: row piece / RB, 32 of the rank
+        piece ^= (piece / RB >> 3) & 1;
+        const int t = piece / RB, r = r0 + piece % RB * 32 + tid % 8 * 4;
+        pr[i] = t;
+        po[i] = r < ad.rank ? (uint32_t)(g.blocked ? r * 32 + t * 4 : t * ad.rank + r) * 4 : NOWHERE;
     }
     // (a chunk that is none: zeros)
     auto issue = [&](int chunk, uint32_t own, int slot) {
@@ -316,23 +293,18 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
         const int left = min(rows - (int)t, 32);
         const uint32_t at = __builtin_amdgcn_readfirstlane(lds0 + slot * S::STAGE);
         const s32x4 rx = resource((const T *)g.x + t * g.ld + c0, (uint32_t)((left - 1) * (int)g.ld + g.C - c0) * 2);
+        const s32x4 rp = resource(g.low + t * ad.rank, (uint32_t)((g.blocked ? 32 : left) * ad.rank) * 4);
 #pragma unroll
         for (int i = 0; i < XL; ++i) load_lds16(at + i * THREADS * 16 + wave * 1024, (own >> xr[i]) & 1 ? xo[i] : NOWHERE, rx);
 #pragma unroll
-        for (int i = 0; i < PL; ++i) {
-            const int plane = (i * THREADS + wave * 64) / (32 * PP);         // (whole waves load from one)
-            const s32x4 rp = resource((const T *)g.pair + (plane * (int64_t)rows + t) * ad.rank + r0, (uint32_t)(left * ad.rank - r0) * 2);
-            load_lds16(at + S::X_BYTES + i * THREADS * 16 + wave * 1024, (own >> pr[i]) & 1 ? po[i] : NOWHERE, rp);
-        }
+        for (int i = 0; i < PL; ++i) load_lds16(at + S::X_BYTES + i * THREADS * 16 + wave * 1024, (own >> pr[i]) & 1 ? po[i] : NOWHERE, rp);
     };
 
-    f32x16 acc[CB][RB] = {};
+    f32x16 acc[CB] = {};
     const int q = lane >> 4, rr = (lane & 15) >> 2;
-    uint32_t xa[CB], pa[RB];                                   // this lane's place in a tile of rows, and in a plane
+    uint32_t xa[CB];                                           // this lane's place in a tile of rows
 #pragma unroll
-    for (int i = 0; i < CB; ++i) xa[i] = (8 * h + rr) * (CH * 2) + (((2 * (wave * CB + i) + (q & 1)) ^ piece_turn(CH * 2, rr)) * 32) + (lane & 3) * 8;
-#pragma unroll
-    for (int i = 0; i < RB; ++i) pa[i] = (8 * h + rr) * (RB * 64) + (((2 * i + (q & 1)) ^ piece_turn(RB * 64, rr)) * 32) + (lane & 3) * 8;
+    for (int i = 0; i < CB; ++i) xa[i] = (8 * h + rr) * (CH * 2) + (((2 * (wc * CB + i) + (q & 1)) ^ (rr << 1)) * 32) + (lane & 3) * 8;
 
     const __amdgpu_buffer_rsrc_t r_ids = buffer(ad.of_row, (uint32_t)rows * 4);
     bool any = false;
@@ -368,23 +340,24 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
             own2 = next();
             issue(chunk, own2, slot == 0 ? STAGES - 1 : slot - 1);
+            // While the products of 16 rows run, the next sixteen's inner products are cut, in their shadow.
             const char *at = lds + slot * S::STAGE;
+            float v[2][8];
+            v8 x[2][CB];
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                v8 x[CB], z[2][RB];
 #pragma unroll
-                for (int i = 0; i < CB; ++i) x[i] = read_turned<T>(at + xa[i] + s * 16 * (CH * 2), 4 * (CH * 2));
+                for (int e = 0; e < 8; ++e) v[s][e] = *(const float *)(at + S::X_BYTES + (((16 * s + 8 * h + e) * RB + wr) ^ h) * 128 + ln * 4);
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                for (int i = 0; i < CB; ++i) x[s][i] = read_turned<T>(at + xa[i] + s * 16 * (CH * 2), 4 * (CH * 2));
+            }
 #pragma unroll
-                    for (int j = 0; j < RB; ++j)
-                        z[k][j] = read_turned<T>(at + S::X_BYTES + k * S::P_BYTES + pa[j] + s * 16 * (RB * 64), 4 * (RB * 64));
+            for (int s = 0; s < 2; ++s) {
+                const Pieces<T> z = split8<T>(v[s]);
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < Pieces<T>::N; ++k)
 #pragma unroll
-                    for (int i = 0; i < CB; ++i)
-#pragma unroll
-                        for (int j = 0; j < RB; ++j) acc[i][j] = IS_B ? H::mfma(x[i], z[k][j], acc[i][j]) : H::mfma(z[k][j], x[i], acc[i][j]);
+                    for (int i = 0; i < CB; ++i) acc[i] = IS_B ? H::mfma(x[s][i], z.of[k], acc[i]) : H::mfma(z.of[k], x[s][i], acc[i]);
             }
             own0 = own1;
             own1 = own2;
@@ -403,21 +376,19 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
 #pragma unroll
     for (int i = 0; i < CB; ++i)
 #pragma unroll
-        for (int j = 0; j < RB; ++j)
+        for (int m = 0; m < 4; ++m) {
+            const int row = 8 * m + 4 * h, c = c0 + (wc * CB + i) * 32 + (IS_B ? row : ln), r = r0 + wr * 32 + (IS_B ? ln : row);
+            // (C and rank are multiples of 8: the four rows exist together)
+            const uint32_t step = (uint32_t)(IS_B ? ad.rank : g.C) * size;
+            const uint32_t at = c < g.C && r < ad.rank ? (IS_B ? (uint32_t)c * ad.rank + r : (uint32_t)r * g.C + c) * size : NOWHERE;
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                const int row = 8 * m + 4 * h, c = c0 + (wave * CB + i) * 32 + (IS_B ? row : ln), r = r0 + j * 32 + (IS_B ? ln : row);
-                // (C and rank are multiples of 8: the four rows exist together)
-                const uint32_t step = (uint32_t)(IS_B ? ad.rank : g.C) * size;
-                const uint32_t at = c < g.C && r < ad.rank ? (IS_B ? (uint32_t)c * ad.rank + r : (uint32_t)r * g.C + c) * size : NOWHERE;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float v = acc[i][j][4 * m + k];
-                    if (part_out) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), to, at + k * step, 0, 0);
-                    // (an adapter without rows has a gradient of zero, whatever its scale)
-                    else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (T)(v == 0.0f ? 0.0f : v * scale)), to, at + k * step, 0, 0);
-                }
+            for (int k = 0; k < 4; ++k) {
+                const float v = acc[i][4 * m + k];
+                if (part_out) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), to, at + k * step, 0, 0);
+                // (an adapter without rows has a gradient of zero, whatever its scale)
+                else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (T)(v == 0.0f ? 0.0f : v * scale)), to, at + k * step, 0, 0);
             }
+        }
 }
 
 template <class T, int RB>
@@ -489,11 +460,11 @@ int grad_parts(const LinearGeom &g, int n, int64_t rows)
     }
 }
 
-// The backward call's workspace: scaled inner products, also in two values of the activations' type, and low so; A and B with
-// their last two axes exchanged; inputs in 8 bits as the values that they stand for.  (The forward call's: scaled inner products.)
+// The backward call's workspace: scaled inner products; A and B with their last two axes exchanged; inputs in 8 bits as the values that they
+// stand for.  (The forward call's: scaled inner products.)
 struct Scratch {
     float *scaled;
-    char *pair, *low_pair, *At, *Bt, *kept;
+    char *At, *Bt, *kept;
     float *part;                      // sums of parts of the rows, and which parts have some of an adapter's
     uint32_t *flags;
     int parts;
@@ -508,9 +479,8 @@ Scratch scratch(const LinearGeom &g, int n, int rank, int64_t rows, bool kept, v
     const size_t z = scaled_bytes(rows, rank), a = align_up((size_t)n * rank * g.C_in * 2, 256), b = align_up((size_t)n * rank * g.C_out * 2, 256);
     const size_t sums = parts > 1 ? align_up((size_t)parts * n * rank * (g.C_in + g.C_out) * 4, 256) : 0, flags = align_up((size_t)parts * n * 4, 256);
     const size_t x = kept ? align_up((size_t)rows * g.C_in * 2, 256) : 0;
-    char *w = (char *)ws, *e = w + 3 * z + a + b;
-    return {(float *)w, w + z, w + 2 * z, w + 3 * z, w + 3 * z + a, e + sums + flags, (float *)e, (uint32_t *)(e + sums), parts,
-            3 * z + a + b + sums + flags + x};
+    char *w = (char *)ws, *e = w + z + a + b;
+    return {(float *)w, w + z, w + z + a, e + sums + flags, (float *)e, (uint32_t *)(e + sums), parts, z + a + b + sums + flags + x};
 }
 
 template <class T>
@@ -518,7 +488,7 @@ int forward(const LinearGeom &g, const Adapters &ad, const void *x, int64_t ldx,
             float *low, float *scaled, hipStream_t s)
 {
     if (adapters_in_one_launch(g, rows, ad.rank)) return launch_adapters_in_one(g, ad, x, ldx, rows, weights, y, ldy, low, s);
-    const int rc = launch_low<T>(g.C_in, ad, ad.A, x, ldx, rows, low, scaled, nullptr, s);
+    const int rc = launch_low<T>(g.C_in, ad, ad.A, x, ldx, rows, low, scaled, s);
     if (rc != SNN_OK) return rc;
     return launch_linear_rows(g, false, x, ldx, rows, nullptr, weights, y, ldy, &ad, ad.B, scaled, s);
 }
@@ -531,8 +501,7 @@ int backward(const LinearGeom &g, const Adapters &ad, const RowsIn &x, const flo
         const int rt = (ad.rank + 63) / 64, ct = (g.C_in + 63) / 64, ot = (g.C_out + 63) / 64;
         const Exchange A = {(const uint16_t *)ad.A, (uint16_t *)w.At, ad.rank, g.C_in, rt, ct};
         const Exchange B = {(const uint16_t *)ad.B, (uint16_t *)w.Bt, g.C_out, ad.rank, ot, rt};
-        const int64_t values = rows * ad.rank, blocks = (values / 8 + 255) / 256;
-        const int tiles_a = ad.n * rt * ct, tiles_ab = tiles_a + ad.n * rt * ot, low_blocks = (int)(blocks < 512 ? blocks : 512);
+        const int tiles_a = ad.n * rt * ct, tiles_ab = tiles_a + ad.n * rt * ot;
         // (the inputs as 16-bit values once, not bytes widened by every tile: see launch_linear_weight_grad)
         KeptRows kept = {};
         unsigned kept_blocks = 0;
@@ -540,17 +509,16 @@ int backward(const LinearGeom &g, const Adapters &ad, const RowsIn &x, const flo
             kept = {(const int8_t *)x.p, x.e, {}, g.C_in, w.kept};
             kept_blocks = walk_of(rows, g.C_in, kept.walk);
         }
-        adapters_lay_out_kernel<T><<<(unsigned)(tiles_ab + low_blocks) + kept_blocks, 256, 0, s>>>(A, B, tiles_a, tiles_ab, low, (T *)w.low_pair, values,
-                                                                                              low_blocks, kept);
+        adapters_lay_out_kernel<T><<<(unsigned)tiles_ab + kept_blocks, 256, 0, s>>>(A, B, tiles_a, tiles_ab, kept);
         int rc = check_launch();
         if (rc != SNN_OK) return rc;
-        rc = launch_low<T>(g.C_out, ad, w.Bt, dy, lddy, rows, nullptr, w.scaled, (T *)w.pair, s);
+        rc = launch_low<T>(g.C_out, ad, w.Bt, dy, lddy, rows, nullptr, w.scaled, s);
         if (rc != SNN_OK) return rc;
         rc = launch_linear_rows(g, true, dy, lddy, rows, nullptr, weights, dx, lddx, &ad, w.At, w.scaled, s);
         if (rc != SNN_OK) return rc;
     }
-    AdapterGradArgs A = {x.p, x.ld, w.pair, g.C_in, dA};
-    const AdapterGradArgs B = {dy, lddy, w.low_pair, g.C_out, dB};
+    AdapterGradArgs A = {x.p, x.ld, w.scaled, true, g.C_in, dA};
+    const AdapterGradArgs B = {dy, lddy, low, false, g.C_out, dB};
     if (x.e) {
         A.x = w.kept;
         A.ld = g.C_in;

@@ -72,15 +72,40 @@ __device__ inline int64_t scaled_at(int t, int r, int rank) { return ((int64_t)(
 
 constexpr uint32_t NOWHERE = 0x80000000u;                      // an offset past every resource
 
-// Two values of the activations' type that together hold v with twice its mantissa.
+// Eight fp32 values as sums of values of the activations' type, for products that are to have fp32's precision.  Three of bf16 hold all 24 bits: the
+// upper half of an fp32 value is a bf16 value, and what is left after two such cuts fits a third.  Two of f16, rounded, hold 22.
 template <class T>
-__device__ inline void split8(const float *v, typename Half<T>::v8 &hi, typename Half<T>::v8 &lo)
+struct Pieces {
+    static constexpr int N = __is_same(T, __bf16) ? 3 : 2;
+    typename Half<T>::v8 of[N];
+};
+
+template <class T>
+__device__ inline Pieces<T> split8(const float *v)
 {
+    Pieces<T> p;
+    if constexpr (__is_same(T, __bf16)) {
+        uint32_t rest[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        hi[j] = (T)v[j];
-        lo[j] = (T)(v[j] - (float)hi[j]);
+        for (int j = 0; j < 8; ++j) rest[j] = __float_as_uint(v[j]);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            u32x4 half;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) half[j] = __builtin_amdgcn_perm(rest[2 * j + 1], rest[2 * j], 0x07060302u);
+            p.of[k] = __builtin_bit_cast(typename Half<T>::v8, half);
+            if (k < 2)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) rest[j] = __float_as_uint(__uint_as_float(rest[j]) - __uint_as_float(rest[j] & 0xffff0000u));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            p.of[0][j] = (T)v[j];
+            p.of[1][j] = (T)(v[j] - (float)p.of[0][j]);
+        }
     }
+    return p;
 }
 
 // Eight values along the rows (the contracted axis) of a lane's channel, out of a tile of rows in LDS: two reads that exchange the axes

@@ -470,13 +470,11 @@ void linear_rows_kernel(RowsArgs p)
                         float zf[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) zf[i] = __uint_as_float(z[s][i >> 2][i & 3]);
-                        v8 hi, lo;
-                        split8<T>(zf, hi, lo);
+                        const Pieces<T> piece = split8<T>(zf);
 #pragma unroll
-                        for (int i = 0; i < NB; ++i) {
-                            d[i] = H::mfma(__builtin_bit_cast(v8, u[s][i]), hi, d[i]);
-                            d[i] = H::mfma(__builtin_bit_cast(v8, u[s][i]), lo, d[i]);
-                        }
+                        for (int i = 0; i < NB; ++i)
+#pragma unroll
+                            for (int k = 0; k < Pieces<T>::N; ++k) d[i] = H::mfma(__builtin_bit_cast(v8, u[s][i]), piece.of[k], d[i]);
                     }
                 }
                 held = p.ad.rank <= 64 ? a : -1;
