@@ -421,6 +421,8 @@ void linear_rows_kernel(RowsArgs p)
     constexpr int PITCH = WN * 2 + 16;
     char *mine = lds + wave * 32 * PITCH;
     const int nw = n0 + wn * WN;
+    // (With adapters every register counts: what would be kept for the next 32 rows, scales and addresses, would put others into scratch memory, and
+    // waves with scratch start later.  Hence the empty assembly statements, past which nothing is kept.)
     u32x4 u[4][NB] = {};
     int held = -1;
 #pragma unroll
@@ -431,7 +433,8 @@ void linear_rows_kernel(RowsArgs p)
             for (int i = 0; i < NB; ++i)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const int n = min(nw + i * 32 + g * 8, p.N - 8) + 4 * h;
+                    int n = min(nw + i * 32 + g * 8, p.N - 8) + 4 * h;
+                    if constexpr (ADAPT) asm volatile("" : "+v"(n));
                     const typename H::v4 a = *(const typename H::v4 *)(alpha + n);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) acc[i][j][4 * g + k] *= (float)a[k];
@@ -446,10 +449,12 @@ void linear_rows_kernel(RowsArgs p)
                 const int a = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
                 const bool own = id == a;
                 left &= ~__ballot(own);
-                const __amdgpu_buffer_rsrc_t ru = buffer((const T *)p.ad.up + (int64_t)a * p.N * p.ad.rank, (uint32_t)p.N * p.ad.rank * 2);
-                const __amdgpu_buffer_rsrc_t rz = buffer(p.ad.low + scaled_at(tj, 0, p.ad.rank), 32u * p.ad.rank * 4);
-                f32x16 d[NB] = {};
-                for (int r0 = 0; r0 < p.ad.rank; r0 += 64) {
+                int rank = p.ad.rank;
+                asm volatile("" : "+s"(rank));
+                const __amdgpu_buffer_rsrc_t ru = buffer((const T *)p.ad.up + (int64_t)a * p.N * rank, (uint32_t)p.N * rank * 2);
+                const __amdgpu_buffer_rsrc_t rz = buffer(p.ad.low + scaled_at(tj, 0, rank), 32u * rank * 4);
+                const uint32_t zo = own ? (uint32_t)(8 * h * 32 + ln * 4) * 4 : NOWHERE;
+                for (int r0 = 0; r0 < rank; r0 += 64) {
                     // 64 of the rank: all loads before the first product
                     u32x4 z[4][2];
                     const bool load_u = a != held;
@@ -459,14 +464,14 @@ void linear_rows_kernel(RowsArgs p)
                         if (load_u)
 #pragma unroll
                             for (int i = 0; i < NB; ++i)
-                                u[s][i] = __builtin_amdgcn_raw_buffer_load_b128(ru, r < p.ad.rank ? (uint32_t)((nw + i * 32 + ln) * p.ad.rank + r) * 2 : NOWHERE, 0, 0);
+                                u[s][i] = __builtin_amdgcn_raw_buffer_load_b128(ru, r < rank ? (uint32_t)((nw + i * 32 + ln) * rank + r) * 2 : NOWHERE, 0, 0);
 #pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            z[s][i] = __builtin_amdgcn_raw_buffer_load_b128(rz, own && r < p.ad.rank ? (uint32_t)((r + 4 * i) * 32 + ln * 4) * 4 : NOWHERE, 0, 0);
+                        for (int i = 0; i < 2; ++i) z[s][i] = __builtin_amdgcn_raw_buffer_load_b128(rz, zo + (uint32_t)(r0 + 16 * s + 4 * i) * 128, 0, 0);
                     }
+                    f32x16 d[NB] = {};
 #pragma unroll
                     for (int s = 0; s < 4; ++s) {
-                        if (r0 + 16 * s >= p.ad.rank) break;
+                        if (r0 + 16 * s >= rank) break;
                         float zf[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) zf[i] = __uint_as_float(z[s][i >> 2][i & 3]);
@@ -476,12 +481,12 @@ void linear_rows_kernel(RowsArgs p)
 #pragma unroll
                             for (int k = 0; k < Pieces<T>::N; ++k) d[i] = H::mfma(__builtin_bit_cast(v8, u[s][i]), piece.of[k], d[i]);
                     }
+#pragma unroll
+                    for (int i = 0; i < NB; ++i)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) acc[i][j][k] += own ? d[i][k] : 0.0f;
                 }
                 held = p.ad.rank <= 64 ? a : -1;
-#pragma unroll
-                for (int i = 0; i < NB; ++i)
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) acc[i][j][k] += own ? d[i][k] : 0.0f;
             }
         }
 #pragma unroll
