@@ -623,8 +623,8 @@ int snn_linear_weight_grad_checkpoint(const snn_linear_desc *desc, const int8_t 
  *   low      device, float [rows][rank], A[a] x[t] in fp32 (zeros without an adapter): what the backward call takes; NULL: not wanted
  *   workspace  device, >= snn_adapters_workspace_bytes(desc, adapters, rows, call) bytes, `call` the SNN_ADAPTERS_* of the entry point,
  *              256-byte aligned (A and B of *adapters are not looked at)
- * scale[a] A[a] x[t], in fp32, enters the product with B[a] as the sum of three bf16 values (its 24 bits) or of two f16 values: for f16 it has to be in that
- * type's range.
+ * scale[a] A[a] x[t], in fp32, enters the product with B[a] as the sum of three bf16 values (its 24 bits), or of two f16 values times a power of two (22 bits, or
+ * 2^-40 of the row's largest), whatever its size.
  *
  * The backward call, with  dlow[t] = scale[a] * B[a]^T dy[t]:
  *   dx[t] = W^T (alpha * dy[t]) + A[a]^T dlow[t];   dA[a] = sum of dlow[t] x[t]^T;   dB[a] = scale[a] * sum of dy[t] low[t]^T

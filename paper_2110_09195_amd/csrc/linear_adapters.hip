@@ -301,6 +301,7 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
     };
 
     f32x16 acc[CB] = {};
+    float scale = Pieces<T>::SCALED ? power_of_two(126) : 1.0f;               // SCALED: a power of two that the wave's inner products and sums are times
     const int q = lane >> 4, rr = (lane & 15) >> 2;
     uint32_t xa[CB];                                           // this lane's place in a tile of rows
 #pragma unroll
@@ -351,9 +352,31 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
 #pragma unroll
                 for (int i = 0; i < CB; ++i) x[s][i] = read_turned<T>(at + xa[i] + s * 16 * (CH * 2), 4 * (CH * 2));
             }
+            if constexpr (Pieces<T>::SCALED) {
+                float top = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(v[e >> 3][e & 7]));
+                if (__any(top * scale >= 32768.0f)) {
+                    // larger ones than the scale is for: it goes down, and the sums so far with it
+                    top = wave_top(top);
+                    if (top == INFINITY) {                                   // (the others decide)
+                        top = 0.0f;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(v[e >> 3][e & 7]) < INFINITY ? fabsf(v[e >> 3][e & 7]) : 0.0f);
+                        top = wave_top(top);
+                    }
+                    const float next = fminf(power_of_two(piece_exponent(top)), scale);
+                    const int down = (__float_as_int(next) - __float_as_int(scale)) >> 23;
+#pragma unroll
+                    for (int i = 0; i < CB; ++i)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) acc[i][k] = ldexpf(acc[i][k], down);
+                    scale = next;
+                }
+            }
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                const Pieces<T> z = split8<T>(v[s]);
+                const Pieces<T> z = split8<T>(v[s], scale);
 #pragma unroll
                 for (int k = 0; k < Pieces<T>::N; ++k)
 #pragma unroll
@@ -370,7 +393,8 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
         if (!any) return;
     }
     // The lane's column is what is contiguous in the result: the channel of A, the rank of B.  Stores that lie outside are sent past the end.
-    const float scale = IS_B ? ad.scale[a] : 1.0f;
+    const float factor = IS_B ? ad.scale[a] : 1.0f;
+    const float up = power_of_two(127 - (int)(__float_as_uint(scale) >> 23));
     const uint32_t size = part_out ? 4 : 2, whole = (uint32_t)g.C * ad.rank;
     const __amdgpu_buffer_rsrc_t to = part_out ? buffer(part_out, whole * 4) : buffer((T *)g.out + (int64_t)a * whole, whole * 2);
 #pragma unroll
@@ -383,10 +407,10 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
             const uint32_t at = c < g.C && r < ad.rank ? (IS_B ? (uint32_t)c * ad.rank + r : (uint32_t)r * g.C + c) * size : NOWHERE;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float v = acc[i][4 * m + k];
+                const float v = Pieces<T>::SCALED ? acc[i][4 * m + k] * up : acc[i][4 * m + k];
                 if (part_out) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), to, at + k * step, 0, 0);
                 // (an adapter without rows has a gradient of zero, whatever its scale)
-                else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (T)(v == 0.0f ? 0.0f : v * scale)), to, at + k * step, 0, 0);
+                else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (T)(v == 0.0f ? 0.0f : v * factor)), to, at + k * step, 0, 0);
             }
         }
 }

@@ -73,18 +73,21 @@ __device__ inline int64_t scaled_at(int t, int r, int rank) { return ((int64_t)(
 constexpr uint32_t NOWHERE = 0x80000000u;                      // an offset past every resource
 
 // Eight fp32 values as sums of values of the activations' type, for products that are to have fp32's precision.  Three of bf16 hold all 24 bits: the
-// upper half of an fp32 value is a bf16 value, and what is left after two such cuts fits a third.  Two of f16, rounded, hold 22.
+// upper half of an fp32 value is a bf16 value, and what is left after two such cuts fits a third.  Two of f16, rounded, hold 22 where the value is in
+// f16's range, which is why values are first multiplied by a power of two (SCALED) that brings the largest of them to 2^14 .. 2^15; what is
+// smaller than that by more than 2^17 keeps an error of 2^-40 of the largest.
 template <class T>
 struct Pieces {
-    static constexpr int N = __is_same(T, __bf16) ? 3 : 2;
+    static constexpr bool SCALED = !__is_same(T, __bf16);
+    static constexpr int N = SCALED ? 2 : 3;
     typename Half<T>::v8 of[N];
 };
 
 template <class T>
-__device__ inline Pieces<T> split8(const float *v)
+__device__ inline Pieces<T> split8(const float *v, float scale)
 {
     Pieces<T> p;
-    if constexpr (__is_same(T, __bf16)) {
+    if constexpr (!Pieces<T>::SCALED) {
         uint32_t rest[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) rest[j] = __float_as_uint(v[j]);
@@ -101,11 +104,33 @@ __device__ inline Pieces<T> split8(const float *v)
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            p.of[0][j] = (T)v[j];
-            p.of[1][j] = (T)(v[j] - (float)p.of[0][j]);
+            p.of[0][j] = (T)(v[j] * scale);
+            p.of[1][j] = (T)(v[j] * scale - (float)p.of[0][j]);
         }
     }
     return p;
+}
+
+// The exponent of the power of two for values whose largest magnitude is `top` (fp32's range needs -114 .. 141; what is below 2^-112 is brought as near
+// to 2^14 as a power of two whose reciprocal is one, too), and that power.
+__device__ inline int piece_exponent(float top) { return min(141 - (int)(__float_as_uint(top) >> 23), 126); }
+__device__ inline float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+
+// The larger of lanes l and l + 32; and the largest of the wave.  (Magnitudes: as whole numbers they have the same order.)
+__device__ inline float larger_half(float m)
+{
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+    return __uint_as_float(max(both[0], both[1]));
+}
+__device__ inline float wave_top(float m)
+{
+    int v = __float_as_int(m);
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x128, 0xf, 0xf, true));     // sixteen lanes turned by 8, 4, 2, 1
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x124, 0xf, 0xf, true));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x122, 0xf, 0xf, true));
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x121, 0xf, 0xf, true));
+    return __int_as_float(max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
+                              max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48))));
 }
 
 // Eight values along the rows (the contracted axis) of a lane's channel, out of a tile of rows in LDS: two reads that exchange the axes

@@ -468,6 +468,20 @@ void linear_rows_kernel(RowsArgs p)
 #pragma unroll
                         for (int i = 0; i < 2; ++i) z[s][i] = __builtin_amdgcn_raw_buffer_load_b128(rz, zo + (uint32_t)(r0 + 16 * s + 4 * i) * 128, 0, 0);
                     }
+                    // (a power of two a row, whose column of D the lanes ln and ln + 32 hold)
+                    float up = 1.0f, down = 1.0f;
+                    if constexpr (Pieces<T>::SCALED) {
+                        float top = 0.0f;
+#pragma unroll
+                        for (int s = 0; s < 4; ++s) {
+                            if (r0 + 16 * s >= rank) break;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(__uint_as_float(z[s][i >> 2][i & 3])));
+                        }
+                        const int e = piece_exponent(larger_half(top));
+                        up = power_of_two(e);
+                        down = power_of_two(-e);
+                    }
                     f32x16 d[NB] = {};
 #pragma unroll
                     for (int s = 0; s < 4; ++s) {
@@ -475,7 +489,7 @@ void linear_rows_kernel(RowsArgs p)
                         float zf[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) zf[i] = __uint_as_float(z[s][i >> 2][i & 3]);
-                        const Pieces<T> piece = split8<T>(zf);
+                        const Pieces<T> piece = split8<T>(zf, up);
 #pragma unroll
                         for (int i = 0; i < NB; ++i)
 #pragma unroll
@@ -484,7 +498,7 @@ void linear_rows_kernel(RowsArgs p)
 #pragma unroll
                     for (int i = 0; i < NB; ++i)
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) acc[i][j][k] += own ? d[i][k] : 0.0f;
+                        for (int k = 0; k < 16; ++k) acc[i][j][k] += own ? d[i][k] * down : 0.0f;
                 }
                 held = p.ad.rank <= 64 ? a : -1;
             }

@@ -14,7 +14,9 @@ pytestmark = pytest.mark.gpu
 SHAPES = [(20512, 64, 64), (20500, 72, 40), (3000, 64, 1032), (3000, 1032, 64), (304, 64, 4104), (400, 4104, 64), (200, 64, 64)]
 RANKS = [8, 24, 64, 72]
 # type, and the powers of two on vectors, on the matrices that make inner products, and on the factors of +-1
-KINDS = [("bf16", 1.0, 1.0, 1.0)]
+KINDS = [("bf16", 1.0, 1.0, 1.0),
+         ("f16", 1.0, 1.0, 1.0),                             # inner products past the largest f16
+         ("f16", 2.0 ** -17, 2.0 ** -17, 2.0 ** 10)]         # and such as f16 cannot hold, all of whose bits are below its smallest
 TYPES = {"bf16": (torch.bfloat16, B.SNN_DTYPE_BF16), "f16": (torch.float16, B.SNN_DTYPE_F16)}
 N = 3
 
@@ -110,3 +112,49 @@ def test_gradients_of_adapters(T, ci, co, rank, kind):
     want = torch.stack([dy[rows].t() @ low[rows] for _, rows in members])
     _, _, dB = backward(x, low, dy, A, Bm, False)
     assert torch.equal(dB, want.to(dtype))
+
+
+@pytest.mark.parametrize("T", [4096, 20512])
+def test_first_steps_of_an_adapter_in_f16(T):
+    """B just after its start at zero, small gradients: every element of dA is rounded once, to 2^-11 of it or 2^-25, and its sum in fp32 has an error of 2^-21 of the
+    magnitudes' sum."""
+    ci, co, r = 256, 512, 16
+    desc, dtype, w, _, one = setting(T, ci, co, "f16")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, dy = (s * torch.randn(T, c, generator=g, device="cuda", dtype=torch.float64) for s, c in ((1.0, ci), (1e-4, co)))
+    A, Bm = (s * torch.randn(N, *c, generator=g, device="cuda", dtype=torch.float64) for s, c in ((ci ** -0.5, (r, ci)), (1e-3, (co, r))))
+    x, dy, A, Bm = (t.to(dtype) for t in (x, dy, A, Bm))
+    ids = torch.zeros(T, dtype=torch.int32, device="cuda")
+    y, low = B.snn_adapters_forward(desc, x, w, ids, A, Bm, one)
+    dx, dA, dB = B.snn_adapters_backward(desc, x, low, dy, w, ids, A, Bm, one)
+    dlow, S = dy.double() @ Bm[0].double(), dy.double().abs() @ Bm[0].double().abs()
+    want = dlow.t() @ x.double()
+    assert 1e-7 < float(dlow.abs().mean()) < 1e-5
+    bound = 2.0 ** -11 * want.norm() + 2.0 ** -25 * want.numel() ** 0.5 + 2.0 ** -21 * (S.t() @ x.double().abs()).norm()
+    assert float((dA[0].double() - want).norm()) <= float(bound)
+    assert not bool(dA[1:].any()) and not bool(dB[1:].any())
+
+
+@pytest.mark.parametrize("name", sorted(TYPES))
+@pytest.mark.parametrize("rank", [16, 64])
+def test_rows_of_very_different_sizes(rank, name):
+    """Gradients of outputs that grow and shrink by 2^36 from chunk to chunk of an adapter's rows: what the largest contribute is as precise as if they were alone."""
+    T, ci, co = 2000, 136, 264
+    desc, dtype, w, _, one = setting(T, ci, co, name)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    size = torch.exp2(torch.tensor([-18, -6, 2, 9, -15, 0, 12, -18], dtype=torch.float64, device="cuda")).repeat_interleave(250)[:, None]
+    x, dy = (torch.randn(T, c, generator=g, device="cuda", dtype=torch.float64) for c in (ci, co))
+    A, Bm = (torch.randn(N, *c, generator=g, device="cuda", dtype=torch.float64) for c in ((rank, ci), (co, rank)))
+    x, dy, A, Bm = (t.to(dtype) for t in (x, dy * size, A / 2 ** 8, Bm / 2 ** 8))
+    for order in (torch.arange(T, device="cuda"), torch.arange(T - 1, -1, -1, device="cuda")):
+        xo, dyo = x[order].contiguous(), dy[order].contiguous()
+        ids = torch.ones(T, dtype=torch.int32, device="cuda")
+        y, low = B.snn_adapters_forward(desc, xo, w, ids, A, Bm, one)
+        _, dA, dB = B.snn_adapters_backward(desc, xo, low, dyo, w, ids, A, Bm, one)
+        u, tiny = (2.0 ** -8, 0.0) if name == "bf16" else (2.0 ** -11, 2.0 ** -25)
+        dlow, S = dyo.double() @ Bm[1].double(), dyo.double().abs() @ Bm[1].double().abs()
+        want = dlow.t() @ xo.double()
+        assert bool(((dA[1].double() - want).abs() <= u * want.abs() + 2.0 ** -21 * (S.t() @ xo.double().abs()) + tiny).all())
+        lo, S = xo.double() @ A[1].double().t(), xo.double().abs() @ A[1].double().abs().t()
+        want = dyo.double().t() @ lo
+        assert bool(((dB[1].double() - want).abs() <= u * want.abs() + 2.0 ** -21 * (dyo.double().abs().t() @ S) + tiny).all())
