@@ -624,12 +624,14 @@ int snn_linear_weight_grad_checkpoint(const snn_linear_desc *desc, const int8_t 
  *   workspace  device, >= snn_adapters_workspace_bytes(desc, adapters, rows, call) bytes, `call` the SNN_ADAPTERS_* of the entry point,
  *              256-byte aligned (A and B of *adapters are not looked at)
  * scale[a] A[a] x[t], in fp32, enters the product with B[a] as the sum of three bf16 values (its 24 bits), or of two f16 values times a power of two (22 bits, or
- * 2^-40 of the row's largest), whatever its size.
+ * 2^-40 of the row's largest), whatever its size.  An infinite one is an infinity there; an infinite element of B[a], which meets all of
+ * these values, makes NaN in calls of many rows.
  *
  * The backward call, with  dlow[t] = scale[a] * B[a]^T dy[t]:
  *   dx[t] = W^T (alpha * dy[t]) + A[a]^T dlow[t];   dA[a] = sum of dlow[t] x[t]^T;   dB[a] = scale[a] * sum of dy[t] low[t]^T
  *   dA, dB   device, as A and B, 16-byte aligned, fully overwritten (zeros for an adapter without rows); sums in fp32, rounded once
- * The second form reads the inputs from their 8-bit form.  dlow and low enter the products as above.
+ * The second form reads the inputs from their 8-bit form.  dlow and low enter the products as above
+ * (what is infinite on the other side, A, x or dy, makes NaN).
  * Errors: INVALID_ARG (n outside 1 .. 65536, rank not a multiple of 8 in 8 .. 128); UNSUPPORTED (groups != 1); WORKSPACE; LAUNCH.
  */
 typedef struct snn_adapters {

@@ -83,6 +83,9 @@ struct Pieces {
     typename Half<T>::v8 of[N];
 };
 
+// What is left of a value after a piece: nothing of an infinite one.
+__device__ inline float rest_of(float v, float piece) { return fabsf(v) == INFINITY ? 0.0f : v - piece; }
+
 template <class T>
 __device__ inline Pieces<T> split8(const float *v, float scale)
 {
@@ -99,13 +102,16 @@ __device__ inline Pieces<T> split8(const float *v, float scale)
             p.of[k] = __builtin_bit_cast(typename Half<T>::v8, half);
             if (k < 2)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) rest[j] = __float_as_uint(__uint_as_float(rest[j]) - __uint_as_float(rest[j] & 0xffff0000u));
+                for (int j = 0; j < 8; ++j) {
+                    const float all = __uint_as_float(rest[j]), half = __uint_as_float(rest[j] & 0xffff0000u);
+                    rest[j] = __float_as_uint(k == 0 ? rest_of(all, half) : all - half);     // (no rest is infinite)
+                }
         }
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             p.of[0][j] = (T)(v[j] * scale);
-            p.of[1][j] = (T)(v[j] * scale - (float)p.of[0][j]);
+            p.of[1][j] = (T)rest_of(v[j] * scale, (float)p.of[0][j]);
         }
     }
     return p;

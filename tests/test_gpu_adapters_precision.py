@@ -53,13 +53,18 @@ def setting(T, ci, co, name):
     return desc, dtype, weights, torch.from_numpy(ids).cuda(), torch.ones(N, device="cuda")
 
 
-def products(v, down, up, ids):
+def products_of_any_size(v, down, up, ids):
     """(up (down v_t), down v_t) of each row's adapter, in 64 bits: down [n][rank][C], up [n][C'][rank]"""
     low = torch.zeros(v.shape[0], down.shape[1], dtype=torch.float64, device="cuda")
     out = torch.zeros(v.shape[0], up.shape[1], dtype=torch.float64, device="cuda")
     for a in range(N):
         low[ids == a] = v[ids == a] @ down[a].t()
         out[ids == a] = low[ids == a] @ up[a].t()
+    return out, low
+
+
+def products(v, down, up, ids):
+    out, low = products_of_any_size(v, down, up, ids)
     assert float(low.abs().amax()) >= 2 ** 18 * float(v.abs().amax() * down.abs().amax()) / 127 ** 2 / 8     # (of the size that is meant)
     return out, low
 
@@ -158,3 +163,35 @@ def test_rows_of_very_different_sizes(rank, name):
         lo, S = xo.double() @ A[1].double().t(), xo.double().abs() @ A[1].double().abs().t()
         want = dyo.double().t() @ lo
         assert bool(((dB[1].double() - want).abs() <= u * want.abs() + 2.0 ** -21 * (dyo.double().abs().t() @ S) + tiny).all())
+
+
+@pytest.mark.parametrize("name", sorted(TYPES))
+@pytest.mark.parametrize("rank", [8, 72])
+@pytest.mark.parametrize("T, ci, co", SHAPES)
+def test_an_infinite_inner_product_gives_infinities(T, ci, co, rank, name):
+    print("case", T, ci, co, rank, name, flush=True)
+    desc, dtype, w, _, one = setting(T, ci, co, name)
+    ids = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    ids[T // 2], ids[T // 2 + 1:] = 1, 0                     # (one row of the adapter with an infinite weight)
+    x, A, Bm = numbers(1, (T, ci), ci) / 128, near_pairs(2, (N, rank, ci)) / 128, turned(opposites(3, (N, rank, co)))
+    dy = torch.ones(T, co, dtype=torch.float64, device="cuda") * torch.tensor([1.0, -1.0], device="cuda").repeat(co // 2)
+    A[1, 5, 7] = float("inf")
+    want, low = products_of_any_size(x, A, Bm, ids)
+    y, got = B.snn_adapters_forward(desc, x.to(dtype), w, ids, A.to(dtype), Bm.to(dtype), one)
+    row = T // 2
+    assert bool(got[row, 5].isposinf()) and bool(want[row].isinf().all())
+    assert torch.equal(y[row].double(), want[row]) and bool(y[torch.arange(T, device="cuda") != row].isfinite().all())
+    Bm[1, :, 3] *= float("inf")
+    A[1, 5, 7] = 1.0
+    _, low = products_of_any_size(x, A, Bm, ids)
+    low[row, 5] = float("inf")
+    dy = dy * torch.sign(Bm[1, :, 3]) * torch.sign(dy)       # (so that the infinities of the inner product have one sign)
+    dx, dA, dB = B.snn_adapters_backward(desc, x.to(dtype), low.float(), dy.to(dtype), w, ids, A.to(dtype), Bm.to(dtype), one)
+    assert torch.equal(dx[row].isinf(), torch.ones(ci, dtype=torch.bool, device="cuda")) and bool((dx[row] > 0).all())
+    assert bool((dA[1, 3] == float("inf")).all()) and bool(dA[1, [r for r in range(rank) if r != 3]].isfinite().all())
+    assert torch.equal(dB[1, :, 5].double(), dy[row] * float("inf")) and bool(dB[1][:, [r for r in range(rank) if r != 5]].isfinite().all())
+    # the other adapter's gradients are finite where their formula's values are (sums of many rows can be past f16's range)
+    rows = ids == 0
+    _, dlow = products_of_any_size(dy, turned(Bm), turned(A), ids)
+    for got, want in ((dA, dlow[rows].t() @ x[rows]), (dB, dy[rows].t() @ low[rows])):
+        assert torch.equal(got[0].isfinite(), want.to(dtype).isfinite()) and not bool(got[0].isnan().any())
