@@ -64,6 +64,7 @@ void linear_weight_grad_kernel(GradArgs p)
     const int i0 = it * BI, o0 = ot * BO;
     int lo, hi;
     group_rows(p.offsets, grp, p.rows, lo, hi);
+    const bool some = hi > lo;
     if (p.splits > 1) {
         const int run = ((hi - lo + p.splits - 1) / p.splits + 31) & ~31;
         lo = (int)min((int64_t)hi, lo + (int64_t)split * run);
@@ -210,7 +211,8 @@ void linear_weight_grad_kernel(GradArgs p)
 #pragma unroll
     for (int j = 0; j < OB; ++j) {
         const int o = o0 + (wo * OB + j) * 32;
-        const float a = p.splits > 1 ? 1.0f : (float)alpha[min(o + ln, p.C_out - 1)];
+        // (a group without rows has a gradient of zero, whatever its scales)
+        const float a = p.splits > 1 ? 1.0f : some ? (float)alpha[min(o + ln, p.C_out - 1)] : 0.0f;
 #pragma unroll
         for (int i = 0; i < IB; ++i)
 #pragma unroll
@@ -245,7 +247,9 @@ void linear_grad_join_kernel(GradArgs p, float *__restrict__ dw, float *__restri
     const int rows = p.groups * p.C_out;
     if (blockIdx.x < dw_blocks) {
         const int row = blockIdx.x, grp = row / p.C_out;
-        const float a = (float)((const T *)p.alpha)[(size_t)grp * p.alpha_stride + (row - grp * p.C_out)];
+        int lo, hi;
+        group_rows(p.offsets, grp, p.rows, lo, hi);
+        const float a = hi > lo ? (float)((const T *)p.alpha)[(size_t)grp * p.alpha_stride + (row - grp * p.C_out)] : 0.0f;
         const int64_t n = (int64_t)rows * p.C_in;
         for (int i = threadIdx.x * 4; i < p.C_in; i += 1024) {
             const float *from = p.part + (int64_t)row * p.C_in + i;
