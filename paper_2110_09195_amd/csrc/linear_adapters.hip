@@ -393,7 +393,8 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
         if (!any) return;
     }
     // The lane's column is what is contiguous in the result: the channel of A, the rank of B.  Stores that lie outside are sent past the end.
-    const float factor = IS_B ? ad.scale[a] : 1.0f;
+    // (an adapter without rows has a gradient of zero, whatever its scale)
+    const float factor = !any ? 0.0f : IS_B ? ad.scale[a] : 1.0f;
     const float up = power_of_two(127 - (int)(__float_as_uint(scale) >> 23));
     const uint32_t size = part_out ? 4 : 2, whole = (uint32_t)g.C * ad.rank;
     const __amdgpu_buffer_rsrc_t to = part_out ? buffer(part_out, whole * 4) : buffer((T *)g.out + (int64_t)a * whole, whole * 2);
@@ -409,8 +410,7 @@ __device__ inline void adapters_grad_tile(const Adapters &ad, const AdapterGradA
             for (int k = 0; k < 4; ++k) {
                 const float v = Pieces<T>::SCALED ? acc[i][4 * m + k] * up : acc[i][4 * m + k];
                 if (part_out) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), to, at + k * step, 0, 0);
-                // (an adapter without rows has a gradient of zero, whatever its scale)
-                else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (T)(v == 0.0f ? 0.0f : v * factor)), to, at + k * step, 0, 0);
+                else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (T)(v * factor)), to, at + k * step, 0, 0);
             }
         }
 }
@@ -440,13 +440,17 @@ void adapters_join_kernel(Adapters ad, AdapterGradArgs A, AdapterGradArgs B, con
     const int a = blockIdx.y;
     if (i >= per) return;
     f32x4 v = {0, 0, 0, 0};
+    bool any = false;
     for (int s = 0; s < parts; ++s)
-        if (flags[s * ad.n + a]) v += *(const f32x4 *)(part + ((int64_t)s * ad.n + a) * per + i);
+        if (flags[s * ad.n + a]) {
+            v += *(const f32x4 *)(part + ((int64_t)s * ad.n + a) * per + i);
+            any = true;
+        }
     const bool is_b = i >= in_a;
-    const float scale = is_b ? ad.scale[a] : 1.0f;
+    const float scale = !any ? 0.0f : is_b ? ad.scale[a] : 1.0f;
     typename Half<T>::v4 out;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) out[k] = (T)(v[k] == 0.0f ? 0.0f : v[k] * scale);
+    for (int k = 0; k < 4; ++k) out[k] = (T)(v[k] * scale);
     T *to = is_b ? (T *)B.out + (int64_t)a * ad.rank * B.C + (i - in_a) : (T *)A.out + (int64_t)a * in_a + i;
     *(typename Half<T>::v4 *)to = out;
 }

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2110_09195_amd import binding as B
-from test_gpu_linear import Layer, offsets_of
+from test_gpu_linear import Layer, normal, offsets_of
 
 pytestmark = pytest.mark.gpu
 
@@ -23,3 +23,22 @@ def test_gradients_of_a_group_without_rows_are_zero_whatever_its_scales(ci, co, 
     assert torch.equal(dw, want) and torch.equal(da, want_a) and not bool(dw[0].any()) and not bool(da[0].any()) and bool(dw[1].any())
     none = [B.snn_linear_weight_grad(L.desc, x[:0], dy[:0], weights, offsets=offsets_of([0, 0]))[0]]
     assert not bool(none[0].any())
+
+
+# one part of the rows, and several
+@pytest.mark.parametrize("T, n", [(60, 3), (4000, 2)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_scale_that_is_not_finite_shows_in_its_own_gradients(T, n, bad):
+    """dB = scale * sum dy low: where the sum is zero and the scale is infinite or NaN, that is NaN; an adapter without rows has zeros."""
+    L, r = Layer(2, 1, 72, 40, 16, "bf16"), 8
+    x, dy = L.rows(1, T, 72), L.rows(2, T, 40)
+    dy[:, 5] = 0.0
+    A, Bm = normal(3, n + 1, r, 72).to(L.dtype), normal(4, n + 1, 40, r).to(L.dtype)
+    ids = (torch.arange(T, device="cuda") * n // T).int()
+    scale = torch.full((n + 1,), 2.0, device="cuda")
+    y, low = B.snn_adapters_forward(L.desc, x, L.weights, ids, A, Bm, scale)
+    _, _, want = B.snn_adapters_backward(L.desc, x, low, dy, L.weights, ids, A, Bm, scale)
+    scale[1], scale[n] = bad, bad                            # (nobody has the last)
+    _, dA, dB = B.snn_adapters_backward(L.desc, x, low, dy, L.weights, ids, A, Bm, scale)
+    assert bool(dB[1, 5].isnan().all()) and not bool(want[1, 5].any()) and not bool(dB[1].isfinite().any()) and not bool(dA[1].isfinite().any())
+    assert torch.equal(dB[0], want[0]) and not bool(dB[n].any()) and not bool(dA[n].any())
