@@ -816,7 +816,7 @@ def _rows(t, dtype, C, name):
     """Rows of C channels on the GPU, each contiguous, any distance apart -> (pointer, distance)."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape[1] == C and t.stride(1) == 1):
         raise TypeError("%s must be a CUDA tensor of %s, [rows][%d] with contiguous rows" % (name, dtype, C))
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(C, t.stride(0))
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else C     # (what a view says of a single row's distance is of no account)
 
 
 def _rows_out(t, rows, C, like, name):

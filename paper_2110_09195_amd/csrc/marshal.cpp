@@ -259,7 +259,7 @@ const at::Tensor *rows_of(PyObject *o, at::ScalarType type, int64_t C)
     return t && t->is_cuda() && t->scalar_type() == type && t->dim() == 2 && t->size(1) == C && t->stride(1) == 1 ? t : nullptr;
 }
 
-int64_t distance(const at::Tensor &t) { return t.size(0) > 1 ? t.stride(0) : std::max(t.size(1), t.stride(0)); }
+int64_t distance(const at::Tensor &t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
 
 // The output that the caller gave, or a new one; undefined if what was given is not of the right kind.
 at::Tensor rows_out(PyObject *o, const at::Tensor &like, int64_t rows, int64_t C)

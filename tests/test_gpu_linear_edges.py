@@ -42,3 +42,30 @@ def test_a_scale_that_is_not_finite_shows_in_its_own_gradients(T, n, bad):
     _, dA, dB = B.snn_adapters_backward(L.desc, x, low, dy, L.weights, ids, A, Bm, scale)
     assert bool(dB[1, 5].isnan().all()) and not bool(want[1, 5].any()) and not bool(dB[1].isfinite().any()) and not bool(dA[1].isfinite().any())
     assert torch.equal(dB[0], want[0]) and not bool(dB[n].any()) and not bool(dA[n].any())
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_a_single_row_of_any_view(native, monkeypatch):
+    """The last token of a long sequence, a row of an odd distance: the distance of a single row does not count."""
+    if not native:
+        B.lib()
+        monkeypatch.setattr(B, "_fast", None)
+    L, r = Layer(3, 1, 4096, 72, 16, "bf16"), 8
+    A, Bm, scale = normal(3, 2, r, 4096).to(L.dtype), normal(4, 2, 72, r).to(L.dtype), normal(5, 2)
+    ids = torch.zeros(1, dtype=torch.int32, device="cuda")
+    sequence = normal(1, 1, 300, 4096).to(L.dtype)
+    odd, odd_dy = normal(2, 1, 4099).to(L.dtype), normal(6, 1, 75).to(L.dtype)
+    for x, dy in ((sequence[:, -1], odd_dy[:, :72]), (odd[:, :4096], odd_dy[:, :72])):
+        assert x.stride(0) > 4096 and dy.stride(0) == 75
+        own, own_dy = x.clone(), dy.clone()
+        assert torch.equal(B.snn_linear_forward(L.desc, x, L.weights), B.snn_linear_forward(L.desc, own, L.weights))
+        assert torch.equal(B.snn_linear_input_grad(L.desc, dy, L.weights), B.snn_linear_input_grad(L.desc, own_dy, L.weights))
+        kept, want = B.snn_checkpoint_store(x), B.snn_checkpoint_store(own)
+        assert all(torch.equal(a, b) for a, b in zip(kept, want))
+        out = torch.zeros(1, 4099, device="cuda").to(L.dtype)
+        assert torch.equal(B.snn_checkpoint_restore(kept, L.dtype, x=out[:, :4096]), B.snn_checkpoint_restore(want, L.dtype))
+        assert torch.equal(B.snn_linear_weight_grad(L.desc, x, dy, L.weights)[0], B.snn_linear_weight_grad(L.desc, own, own_dy, L.weights)[0])
+        (y, low), (want, _) = (B.snn_adapters_forward(L.desc, v, L.weights, ids, A, Bm, scale) for v in (x, own))
+        assert torch.equal(y, want)
+        got, want = (B.snn_adapters_backward(L.desc, v, low, d, L.weights, ids, A, Bm, scale) for v, d in ((x, dy), (own, own_dy)))
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
