@@ -21,20 +21,21 @@ class _Experts(torch.autograd.Function):
         kept = B.snn_checkpoint_store(x) if keep_8_bits else (x,)
         ctx.save_for_backward(weights, offsets, *kept)
         ctx.desc = desc
-        return B.snn_linear_forward(desc, x, weights, offsets)
+        return B.snn_linear_forward(desc, x, weights, offsets, y=torch.zeros(x.shape[0], c_out, dtype=x.dtype, device=x.device))
 
     @staticmethod
     def backward(ctx, dy):
         weights, offsets, *kept = ctx.saved_tensors
         dy = dy.contiguous()
-        dx = B.snn_linear_input_grad(ctx.desc, dy, weights, offsets)
+        dx = B.snn_linear_input_grad(ctx.desc, dy, weights, offsets, dx=torch.zeros(dy.shape[0], ctx.desc.C_in, dtype=dy.dtype, device=dy.device))
         # (straight through: the gradient of the +-1 weights is that of the real ones)
         dw, dalpha = B.snn_linear_weight_grad(ctx.desc, kept[0] if len(kept) == 1 else tuple(kept), dy, weights, offsets)
         return dx, dw, dalpha, None, None, None
 
 
 def experts(x, w, alpha, codebook8, offsets, keep_8_bits=True):
-    """x [rows][C_in] in 16 bits, rows sorted by expert as offsets (int32 [experts + 1]) says, through projections whose weights are the nearest
+    """x [rows][C_in] in 16 bits, rows sorted by expert as offsets (int32 [experts + 1]) says (rows before the first and behind the last expert's: outputs and
+    gradients of zero), through projections whose weights are the nearest
     members of the experts' subsets codebook8 (int16 [experts][K]) to the vectors of 8 of w (float32 [experts][C_out][C_in]), times
     alpha (float32 [experts][C_out]).  Differentiable in x, w (straight through) and alpha; x is kept in 8 bits or as it is."""
     return _Experts.apply(x, w, alpha, codebook8, offsets, keep_8_bits)
