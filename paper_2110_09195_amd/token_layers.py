@@ -5,6 +5,7 @@
 trains both for some steps towards random teachers of their own kind, and serves the adapted projection token by token.
 """
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -24,6 +25,7 @@ class _Experts(torch.autograd.Function):
         return B.snn_linear_forward(desc, x, weights, offsets, y=torch.zeros(x.shape[0], c_out, dtype=x.dtype, device=x.device))
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         weights, offsets, *kept = ctx.saved_tensors
         dy = dy.contiguous()
@@ -37,7 +39,7 @@ def experts(x, w, alpha, codebook8, offsets, keep_8_bits=True):
     """x [rows][C_in] in 16 bits, rows sorted by expert as offsets (int32 [experts + 1]) says (rows before the first and behind the last expert's: outputs and
     gradients of zero), through projections whose weights are the nearest
     members of the experts' subsets codebook8 (int16 [experts][K]) to the vectors of 8 of w (float32 [experts][C_out][C_in]), times
-    alpha (float32 [experts][C_out]).  Differentiable in x, w (straight through) and alpha; x is kept in 8 bits or as it is."""
+    alpha (float32 [experts][C_out]).  Differentiable (once) in x, w (straight through) and alpha; x is kept in 8 bits or as it is."""
     return _Experts.apply(x, w, alpha, codebook8, offsets, keep_8_bits)
 
 
@@ -51,6 +53,7 @@ class _Adapted(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         A, Bm, scale, adapter, weights, low, *kept = ctx.saved_tensors
         dx, dA, dB = B.snn_adapters_backward(ctx.desc, kept[0] if len(kept) == 1 else tuple(kept), low, dy.contiguous(), weights, adapter, A, Bm, scale)
@@ -60,7 +63,7 @@ class _Adapted(torch.autograd.Function):
 def adapted(x, A, Bm, scale, adapter, desc, weights, keep_8_bits=True):
     """x [rows][C_in] in 16 bits through the projection that snn_linear_prepare laid out as weights and, beside it, each row's adapter
     (int32 [rows], outside 0 .. n - 1: none): A float32 [n][rank][C_in], Bm float32 [n][C_out][rank], scale float32 [n].
-    Differentiable in x, A and Bm."""
+    Differentiable (once) in x, A and Bm."""
     return _Adapted.apply(x, A, Bm, scale, adapter, desc, weights, keep_8_bits)
 
 

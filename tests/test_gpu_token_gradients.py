@@ -23,3 +23,25 @@ def test_rows_of_no_expert_have_zeros(rows):
         y.backward(torch.ones_like(y))
         for t in (y.detach(), x.grad):
             assert not bool(t[:7].any()) and not bool(t[rows - 9:].any()) and bool(t[7:rows - 9].isfinite().all()) and bool(t[7:rows - 9].any(1).all())
+
+
+def _adapted(**change):
+    _, (desc, weights, A, Bm, scale) = TL.train_adapters(steps=0, rows=10, n=4, rank=8, c_in=136, c_out=72)
+    a = dict(x=torch.randn(20, 136, device="cuda").bfloat16().requires_grad_(), A=A.float().requires_grad_(), Bm=Bm.float().requires_grad_(), scale=scale,
+             adapter=torch.arange(20, dtype=torch.int32, device="cuda") % 4, desc=desc, weights=weights)
+    a.update(change)
+    return TL.adapted(**a), a
+
+
+def test_a_second_derivative_is_refused():
+    y, a = _adapted()
+    grad, = torch.autograd.grad(y.float().square().sum(), a["x"], create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        grad.float().square().sum().backward()
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(20, 72, device="cuda").bfloat16().requires_grad_()
+    w = torch.randn(1, 40, 72, device="cuda", requires_grad=True)
+    y = TL.experts(x, w, torch.ones(1, 40, device="cuda"), TL._random_codebook(1, 16, g), torch.tensor([0, 20], dtype=torch.int32, device="cuda"))
+    grad, = torch.autograd.grad(y.float().square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        grad.float().square().sum().backward()
