@@ -63,7 +63,9 @@ class _Adapted(torch.autograd.Function):
 def adapted(x, A, Bm, scale, adapter, desc, weights, keep_8_bits=True):
     """x [rows][C_in] in 16 bits through the projection that snn_linear_prepare laid out as weights and, beside it, each row's adapter
     (int32 [rows], outside 0 .. n - 1: none): A float32 [n][rank][C_in], Bm float32 [n][C_out][rank], scale float32 [n].
-    Differentiable (once) in x, A and Bm."""
+    Differentiable (once) in x, A and Bm; scale is a constant."""
+    if scale.requires_grad:
+        raise ValueError("scale has no gradient here: detach it, or put what is learnt into A or Bm")
     return _Adapted.apply(x, A, Bm, scale, adapter, desc, weights, keep_8_bits)
 
 

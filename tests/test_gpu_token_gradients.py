@@ -45,3 +45,8 @@ def test_a_second_derivative_is_refused():
     grad, = torch.autograd.grad(y.float().square().sum(), x, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         grad.float().square().sum().backward()
+
+
+def test_a_scale_that_asks_for_a_gradient_is_refused():
+    with pytest.raises(ValueError, match="scale has no gradient"):
+        _adapted(scale=torch.full((4,), 2.0, device="cuda", requires_grad=True))
