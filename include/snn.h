@@ -538,8 +538,8 @@ int snn_dense_conv2d_sign_prepared(const snn_conv_desc *desc, const void *x, con
  *   - Rows lie `ld` elements apart (ld >= the row's channels, a multiple of 8, at most 2^20); the base address is a
  *     multiple of 16.  Channels are contiguous.  1 <= rows < 2^28; rows = 0 is allowed, and then only gradients of weights
  *     and adapters are written (zeros).  Outputs must not overlap inputs or each other.
- *   - offsets: device, int32 [groups + 1], non-decreasing.  A group may have no rows.  Values are read as clamped to
- *     0 .. rows; rows before offsets[0] and from offsets[groups] on belong to no group: their outputs are not written.
+ *   - offsets: device, int32 [groups + 1], non-decreasing (else which group's weights a row meets, if any, is not defined).  A group may
+ *     have no rows.  Values are read as clamped to 0 .. rows; rows before offsets[0] and from offsets[groups] on belong to no group: their outputs are not written.
  *     NULL is allowed for groups = 1: all rows.
  *   - A row's infinities and NaN, or those of an adapter, reach no other row and no other group's or adapter's gradient.
  *     Sums are formed in a fixed order: a call repeated gives the same bits.

@@ -138,7 +138,7 @@ struct RowTile {
 };
 
 template <int BT>
-__device__ inline bool find_tile(const int32_t *offsets, int groups, int rows, int col_tiles, const Divisor &col_div, RowTile &tile)
+__device__ inline bool find_tile(const int32_t *offsets, int groups, int rows, int col_tiles, const Divisor &col_div, uint32_t most, RowTile &tile)
 {
     const int lane = threadIdx.x & 63;
     // (groups g0 .. g0 + 63, a lane each: their rows, and the tiles of those up to it)
@@ -153,17 +153,20 @@ __device__ inline bool find_tile(const int32_t *offsets, int groups, int rows, i
         }
         return upto;
     };
-    int total, lo = 0, hi = 0, upto = 0;
-    if (!offsets) total = (rows + BT - 1) / BT;
+    // No more tiles than the grid has workgroups (`most` of rows).  Offsets that do not decrease never name more (see tile_grid); those that go down and up
+    // again can, up to the whole of the rows for every other group: then the surplus is dropped, and which group's result a row gets is not defined.
+    uint32_t total;
+    int lo = 0, hi = 0, upto = 0;
+    if (!offsets) total = (uint32_t)(rows + BT - 1) / BT;
     else {
         upto = look(0, lo, hi);
-        total = __builtin_amdgcn_readlane(upto, 63);
+        total = min((uint32_t)__builtin_amdgcn_readlane(upto, 63), most);
         for (int g0 = 64; g0 < groups; g0 += 64) {
             int l, h;
-            total += __builtin_amdgcn_readlane(look(g0, l, h), 63);
+            total = min(total + (uint32_t)__builtin_amdgcn_readlane(look(g0, l, h), 63), most);
         }
     }
-    const uint32_t tiles = (uint32_t)total * col_tiles;        // (no more than the grid has workgroups, whatever the offsets hold: see tile_grid)
+    const uint32_t tiles = total * (uint32_t)col_tiles;
     const uint32_t share = (tiles + 7) / 8, at = blockIdx.x / 8;
     const uint32_t id = (blockIdx.x % 8) * share + at;
     if (at >= share || id >= tiles) return false;
@@ -220,6 +223,7 @@ struct RowsArgs {
     int64_t ld_out;
     int N, K, col_tiles;
     Divisor col_div;                 // by col_tiles
+    uint32_t most;                   // tiles of rows that the grid has workgroups for
     AdapterShare ad;
 };
 
@@ -249,7 +253,7 @@ void linear_rows_kernel(RowsArgs p)
     extern __shared__ __align__(16) char lds[];
 
     RowTile tile;
-    if (!find_tile<BT>(p.offsets, p.groups, p.rows, p.col_tiles, p.col_div, tile)) return;
+    if (!find_tile<BT>(p.offsets, p.groups, p.rows, p.col_tiles, p.col_div, p.most, tile)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wt = wave % (BT / WT), wn = wave / (BT / WT);
     const int n0 = tile.col * BN, rows = tile.t1 - tile.t0;
@@ -586,7 +590,7 @@ void linear_few_kernel(RowsArgs p)
     float(*const part)[16][16 * NB + 1] = (float(*)[16][16 * NB + 1])lds;
     __shared__ __align__(16) float own[ADAPT == OWN ? OWN_DOTS : 1];         // scaled inner products [rows][rank]
     RowTile tile;
-    if (!find_tile<16>(p.offsets, p.groups, p.rows, p.col_tiles, p.col_div, tile)) return;
+    if (!find_tile<16>(p.offsets, p.groups, p.rows, p.col_tiles, p.col_div, p.most, tile)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int q = lane >> 4, ln = lane & 15, n0 = tile.col * 16 * NB;
     const s32x4 rx = resource((const T *)p.in + (int64_t)tile.t0 * p.ld_in, (uint32_t)(tile.t1 - tile.t0 - 1) * (uint32_t)p.ld_in * 2 + p.K * 2);
@@ -718,6 +722,7 @@ int launch_tiles(RowsArgs p, hipStream_t s)
     p.col_div = make_divisor(p.col_tiles);
     const int64_t grid = tile_grid(p.rows, p.groups, BT, p.col_tiles);
     if (grid >= ((int64_t)1 << 31)) return SNN_ERR_UNSUPPORTED;
+    p.most = (uint32_t)(grid / p.col_tiles);
     kernel<<<dim3((unsigned)grid), 64 * WAVES, LDS, s>>>(p);
     return check_launch();
 }
@@ -729,6 +734,7 @@ int launch_few(RowsArgs p, hipStream_t s)
     p.col_div = make_divisor(p.col_tiles);
     const int64_t grid = tile_grid(p.rows, p.groups, 16, p.col_tiles);
     if (grid >= ((int64_t)1 << 31)) return SNN_ERR_UNSUPPORTED;
+    p.most = (uint32_t)(grid / p.col_tiles);
     // (up to eight blocks of 64 channels a wave has one: 98 rows of 14 groups 512 -> 2800 6.1 us, 7.3 with loads for two)
     if (p.kbs <= 8)
         linear_few_kernel<T, GRAD, ADAPT, NB, 1><<<dim3((unsigned)grid), ADAPT == OWN ? 1024 : 512, 0, s>>>(p);

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from gpu_util import Guarded
 from paper_2110_09195_amd import binding as B
 from test_gpu_linear import Layer, normal, offsets_of
 
@@ -69,3 +70,22 @@ def test_a_single_row_of_any_view(native, monkeypatch):
         assert torch.equal(y, want)
         got, want = (B.snn_adapters_backward(L.desc, v, low, d, L.weights, ids, A, Bm, scale) for v, d in ((x, dy), (own, own_dy)))
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("T, groups", [(90, 64), (5000, 300), (100000, 1024)])
+def test_offsets_that_go_down_and_up_again_stay_inside(T, groups):
+    """Every other group claims all rows: far more tiles than there can be.  What rows get is not defined, but nothing else is written."""
+    L = Layer(4, groups, 16, 24, 4, "bf16")
+    x, dy = L.rows(1, T, 16), L.rows(2, T, 24)
+    off = torch.tensor([0, T] * (groups // 2) + [0] * (1 + groups % 2), dtype=torch.int32, device="cuda")
+    g, y = L.out(T, 24, 8)
+    B.snn_linear_forward(L.desc, x, L.weights, offsets=off, y=y)
+    g.check("y")
+    assert bool(g.t.view(T, 32)[:, 24:].isnan().all())
+    g, dx = L.out(T, 16, 8)
+    B.snn_linear_input_grad(L.desc, dy, L.weights, offsets=off, dx=dx)
+    g.check("dx")
+    assert bool(g.t.view(T, 24)[:, 16:].isnan().all())
+    g = Guarded(groups * 24 * 16, torch.float32)
+    B.snn_linear_weight_grad(L.desc, x, dy, L.weights, offsets=off, dw=g.t.view(groups, 24, 16))
+    g.check("dw")
