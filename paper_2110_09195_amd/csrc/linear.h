@@ -82,17 +82,6 @@ __device__ inline void group_rows(const int32_t *offsets, int g, int rows, int &
     hi = min(max(offsets[g + 1], lo), rows);
 }
 
-// whether W(n, k) of an image is -1
-__device__ inline bool weight_negative(const uint32_t *image, int kbs, int n, int k)
-{
-    const uint32_t w = image[((size_t)(n >> 5) * kbs + (k >> 6)) * 64 + ((k >> 3) & 1) * 32 + (n & 31)];
-    const int j = k & 7;
-    return (w >> (15 - (4 * ((k >> 4) & 3) + (j >> 1)) + 16 * (j & 1))) & 1;
-}
-
-// exponents of a row, in whole words
-__host__ __device__ inline int exponent_words(int C) { return (C + 127) / 128; }
-
 // 2^(e - 127); the stored exponents are 1 .. 254
 __device__ inline float unit_of(uint32_t e) { return __uint_as_float(e << 23); }
 

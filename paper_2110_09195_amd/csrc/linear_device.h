@@ -145,7 +145,6 @@ template <class T>
 __device__ inline typename Half<T>::v8 read_turned(const char *at, int next)
 {
     using v4s = __attribute__((ext_vector_type(4))) short;
-    using v8s = __attribute__((ext_vector_type(8))) short;
     using lds_v4s = __attribute__((address_space(3))) v4s;
     const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(at));
     const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(at + next));
