@@ -89,3 +89,29 @@ def test_offsets_that_go_down_and_up_again_stay_inside(T, groups):
     g = Guarded(groups * 24 * 16, torch.float32)
     B.snn_linear_weight_grad(L.desc, x, dy, L.weights, offsets=off, dw=g.t.view(groups, 24, 16))
     g.check("dw")
+
+
+# few rows, tiles
+@pytest.mark.parametrize("T, ci, co", [(9, 64, 72), (400, 136, 4104), (1500, 264, 520)])
+def test_values_below_the_normal_numbers_of_f16_count(T, ci, co):
+    """Multiples of 2^-24, the smallest f16 value: whole numbers times it, whose sums are exact."""
+    L, r, unit = Layer(6, 1, ci, co, 16, "f16"), 8, 2.0 ** -24
+    L.weights = B.snn_linear_prepare(L.desc, L.codebook, L.idx, torch.ones(1, co, device="cuda").half())
+
+    def whole(seed, *shape):
+        return (normal(seed, *shape) * 3).round().clamp(-9, 9).double()
+    x, dy = whole(1, T, ci), whole(2, T, co)
+    tiny_x, tiny_dy = (x * unit).half(), (dy * unit).half()
+    assert torch.equal(tiny_x.double(), x * unit)
+    assert torch.equal(B.snn_linear_forward(L.desc, tiny_x, L.weights).double(), x @ L.w[0].t() * unit)
+    assert torch.equal(B.snn_linear_input_grad(L.desc, tiny_dy, L.weights).double(), dy @ L.w[0] * unit)
+    dw, _ = B.snn_linear_weight_grad(L.desc, tiny_x, dy.half(), L.weights)
+    assert torch.equal(dw[0].double(), dy.t() @ x * unit)
+    kept = B.snn_checkpoint_restore(B.snn_checkpoint_store(tiny_x), L.dtype)
+    assert torch.equal(kept, tiny_x)
+    A, Bm, one = whole(3, 1, r, ci), torch.zeros(1, co, r, dtype=torch.float64, device="cuda"), torch.ones(1, device="cuda")
+    Bm[0, :, 3] = 1.0
+    ids = torch.zeros(T, dtype=torch.int32, device="cuda")
+    y, low = B.snn_adapters_forward(L.desc, tiny_x, L.weights, ids, A.half(), Bm.half(), one)
+    assert torch.equal(low.double(), x @ A[0].t() * unit)
+    assert torch.equal(y.double(), ((x @ L.w[0].t() + (x @ A[0].t())[:, 3:4]) * unit).half().double())
