@@ -630,8 +630,9 @@ int snn_linear_weight_grad_checkpoint(const snn_linear_desc *desc, const int8_t 
  * The backward call, with  dlow[t] = scale[a] * B[a]^T dy[t]:
  *   dx[t] = W^T (alpha * dy[t]) + A[a]^T dlow[t];   dA[a] = sum of dlow[t] x[t]^T;   dB[a] = scale[a] * sum of dy[t] low[t]^T
  *   dA, dB   device, as A and B, 16-byte aligned, fully overwritten (zeros for an adapter without rows); sums in fp32, rounded once
- * The second form reads the inputs from their 8-bit form.  dlow and low enter the products as above
- * (what is infinite on the other side, A, x or dy, makes NaN).
+ * The second form reads the inputs from their 8-bit form.  dlow and low enter the products as above;
+ * in those of the adapters' gradients the power of two, and the bound of 2^-40, go by the largest of the adapter's rows.  What is infinite on the other side (A,
+ * x or dy) makes NaN.
  * Errors: INVALID_ARG (n outside 1 .. 65536, rank not a multiple of 8 in 8 .. 128); UNSUPPORTED (groups != 1); WORKSPACE; LAUNCH.
  */
 typedef struct snn_adapters {

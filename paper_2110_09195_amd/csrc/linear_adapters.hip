@@ -50,7 +50,7 @@ void low_few_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__r
 // turn (blocks of 64), rows and matrix both by way of LDS, a wave's own part of it, STAGES in flight without registers; then
 // their sums are joined there.  A wave's blocks are consecutive ones: with the waves' blocks in turn every workgroup reads the same columns of all its
 // rows at once, and rows a power of two apart lie in the same few channels of memory (8192 rows of rank 64, 4096 channels 33 us; 29 so).
-// Bound by the rows' way from memory, of which a workgroup has 96 KB in flight: 64 MB, 13 us at a copy's rate, in 25 - 29.
+// Bound by the rows' way from memory, of which a workgroup has 96 KB in flight: 64 MB, 13 us at a copy's rate, in 24 - 29.
 template <class T, int RB, int STAGES>
 __global__ __launch_bounds__(256)
 void low_tile_kernel(int C, Adapters ad, const T *__restrict__ down, const T *__restrict__ x, int64_t ldx, int rows,
@@ -232,7 +232,7 @@ int launch_low(int C, const Adapters &ad, const void *down, const void *x, int64
 // wave 32 of the rank by as many channels as that leaves it.
 //   - Rows come in chunks of 32.  Lanes look 64 chunks over at once for the adapter's rows, and the chunks that have some are gone through, the loads
 //     of two of them in flight, without registers.  Rows of other adapters inside a chunk are not loaded: zeros in LDS.
-//   - Bound by memory: 8192 rows of rank 64, 4096 -> 4096 (134 MB) 54 - 60 us (less where the inputs are still in the last cache) and 7 for the join; 27 at a copy's
+//   - Bound by memory: 8192 rows of rank 64, 4096 -> 4096 (134 MB) 56 - 64 us (less where the inputs are still in the last cache) and 7 for the join; 27 at a copy's
 //     rate.
 //   - Both operands have the contracted axis across memory.  Rows are turned by the reads of their fragments; inner products are read as they
 //     are (fp32, one of the rank a lane) and cut into values of the activations' type by the waves: three of bf16 (with two, that
@@ -474,10 +474,10 @@ int launch_adapters_grad(const Adapters &ad, const AdapterGradArgs &A, const Ada
 }
 
 // Parts of the rows, joined by another launch: an adapter can have nearly all of them, and then its tiles alone would occupy a
-// fraction of the CUs (8192 rows of one adapter of rank 64, 4096 -> 4096: 64 chunks take 45 us, and eight parts of 32 chunks 33 with 5 for the join).  Parts of
+// fraction of the CUs (the call of 8192 rows of one adapter of rank 64, 4096 -> 4096, 452 us whole, 344, 290, 270 and 269 in 2, 4, 8 and 16 parts).  Parts of
 // at least 384 rows, while the workgroups (most of which find no rows of theirs, and end) stay few; of 96, and 75 an adapter, where
-// there are not even as many of them as CUs (the call of 1274 rows of two adapters of rank 32, 1440 -> 608: two parts 36.7 us, eight 32.4; one
-// of 400 rows of eight adapters, 2048 -> 2048, 36.0 whole and 39 in two).
+// there are not even as many of them as CUs (the call of 1274 rows of two adapters of rank 32, 1440 -> 608: two parts 39.9 us, eight 31.2; one
+// of 400 rows of eight adapters, 2048 -> 2048, 34.3 whole and 37.1 in two).
 int grad_parts(const LinearGeom &g, int n, int64_t rows)
 {
     const int64_t tiles = (g.C_in + 255) / 256 + (g.C_out + 255) / 256;

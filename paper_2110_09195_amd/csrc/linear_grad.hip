@@ -29,8 +29,8 @@ struct GradArgs {
 // axis (rows) across memory.  Their tiles go to LDS as they lie, without registers, STAGES in flight, and are turned by the reads that fetch
 // fragments.  32-byte pieces of a row are xor-ed with the row's low two bits, so that the four rows that such a read touches lie in
 // different banks.  alpha's gradient comes from the same sums, with the signs of the tile's own bits.
-// Bound: the matrix pipes at the clock that the chip's power leaves them (16384 rows 4096 -> 4096 426 us = 1.29 PFLOP/s), and for each
-// tile the 256 KB that it writes, with nothing else on the CU (8 groups of as many rows, 512 MB of results: 546 us).  Tiles of 128 x 256
+// Bound: the matrix pipes at the clock that the chip's power leaves them (16384 rows 4096 -> 4096 400 - 426 us by card, 1.29 -
+// 1.37 PFLOP/s), and for each tile the 256 KB that it writes, with nothing else on the CU (8 groups of as many rows, 512 MB of results: 500 - 546 us).  Tiles of 128 x 256
 // two on a CU, which do not hide it either, take 585; groups in another order on each XCD 554, and 8192 rows 2048 -> 2048 107 for 91.
 template <class T, int BI, int BO, int WI, int WO, int STAGES>
 __global__ __launch_bounds__(64 * (BI / WI) * (BO / WO))

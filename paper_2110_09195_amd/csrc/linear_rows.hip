@@ -748,7 +748,7 @@ int launch_few(RowsArgs p, hipStream_t s)
 // 64 contracted channels a tile alone on its CU with most CUs idle, and its share of a CU when all are busy (then the clock is down to
 // 1.8 - 1.9 GHz: such calls are bound by power, and what moves fewer bytes for a product is faster); and once for a tile.  Adapters add 0.9 us for every
 // 32 rows of a tile, whose loads wait for each other, and 0.3 when other tiles fill the wait (rank 64 or less): 1111 rows of rank 24, 1352 ->
-// 2056, 22.8 us in 128 x 128, 20.2 in 32 x 128; 3636 rows, 880 -> 4096, 44 and 46, and 40 in 128 x 256.  The input's gradient also
+// 2056, 22.9 us in 128 x 128, 19.7 in 32 x 128; 3636 rows, 880 -> 4096, 43 and 44, and 39 in 128 x 256.  The input's gradient also
 // scales its weights, which makes small tiles dearer.  A tile is small to spread few rows over the chip and large to be fed with fewer
 // reads; two of 128 x 256 stay on a CU and fill each other's waits (one of 256 x 256 instead: 72 / 69 us, 69 / 69, 100 / 104, 381 / 385).
 // One group, 4096 -> 4096, outputs / input gradients in us:
