@@ -158,7 +158,7 @@ def run(s):
         loss, lse, picked = B.snn_distill_forward(d, s["x"], s["table"], *teacher)
         if path == "distill":
             return loss, lse, picked
-        return loss, lse, picked, *B.snn_distill_backward(d, s["x"], s["table"], *teacher, lse, picked, s["dloss"])
+        return loss, lse, picked, *B.snn_distill_backward(d, s["x"], s["table"], *teacher, lse, s["dloss"])
     if path == "embed":
         return _plain_embed(s)
     if path == "embed_grad":
