@@ -12,7 +12,8 @@
  * Around these: the convolution ending in the next layer's sign (1-bit activations from layer to
  * layer), the training-side lines of Alg. 1 (Eq. 3, Eq. 4, the gradient of the subset), the
  * tau-bit index storage of Sec. 4.4, the extension to 1x1 layers (appendix), the
- * same with 16-bit activations (projections over tokens: by expert, beside low-rank adapters, with their gradients)
+ * same with 16-bit activations (projections over tokens: by expert, beside low-rank adapters, with their gradients),
+ * the first and last layers of such a network (a table's rows for tokens, losses over a vocabulary, with their gradients)
  * and, as a yardstick, the 1-bit layers as dense contractions on the matrix cores.
  *
  * General rules for every entry point
@@ -656,6 +657,85 @@ int snn_adapters_backward_checkpoint(const snn_linear_desc *desc, const snn_adap
                                      const float *low, const void *dy, int64_t lddy, int64_t rows, const int32_t *adapter,
                                      const void *weights, size_t weights_bytes, void *dx, int64_t lddx, void *dA, void *dB,
                                      void *workspace, size_t ws_bytes, void *stream);
+
+/* ---- the ends of a network over tokens -----------------------------------------------------------------------
+ *
+ * The first and last layers, which stay in full precision beside sub-bit ones: a table of V rows of C 16-bit values, a row for each token of a
+ * vocabulary.  At one end a token's row is what the layers get; at the other the inner products with all rows are a token's logits,
+ *   z[t][v] = sum_c table[v][c] x[t][c],
+ * of which losses are made.  Both ends may use one table.
+ *
+ * Rules beside the general ones
+ *   - desc->dtype (SNN_DTYPE_*) is the type of the table, of rows and of their gradients.  Sums are held in fp32 and in a fixed order: a call
+ *     repeated gives the same bits.
+ *   - Rows and the table's rows lie `ld` elements apart, as for the projections above; the table's gradient is contiguous.
+ *     0 <= rows < 2^28.  Outputs must not overlap inputs or each other.
+ *   - A token outside 0 .. V - 1 is none: its row of the output is zeros, its loss is zero, nothing of it reaches a gradient.
+ */
+typedef struct snn_vocab_desc {
+    int32_t V;       /* tokens, 1 .. 2^24                         */
+    int32_t C;       /* channels, a multiple of 8, 8 .. 65536     */
+    int32_t dtype;   /* SNN_DTYPE_*                               */
+} snn_vocab_desc;
+
+/*
+ * Rows of tokens, and the table's gradient (the rows' gradients summed by token):
+ *   y[t] = scale * table[ids[t]];     dtable[v] = scale * sum over the t with ids[t] = v of dy[t]
+ * each rounded once; with accumulate the sum is added to what dtable holds (and rounded again), and rows of tokens that do not occur stay as they are.
+ *   table   device, [V] rows of C;   ids   device, int32 [rows];   y, dy   device, rows of C
+ *   dtable  device, [V][C], 16-byte aligned; without accumulate fully overwritten (zeros for tokens that do not occur)
+ *   workspace  device, >= snn_embedding_grad_workspace_bytes(desc, rows) bytes, 256-byte aligned
+ * Errors: INVALID_ARG; UNSUPPORTED (2^31 workgroups or more); WORKSPACE; LAUNCH.
+ */
+int snn_embedding_forward(const snn_vocab_desc *desc, const void *table, int64_t ldt, const int32_t *ids, int64_t rows, float scale, void *y, int64_t ldy,
+                          void *stream);
+size_t snn_embedding_grad_workspace_bytes(const snn_vocab_desc *desc, int64_t rows);
+int snn_embedding_grad(const snn_vocab_desc *desc, const void *dy, int64_t lddy, const int32_t *ids, int64_t rows, float scale, void *dtable,
+                       int accumulate, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Softmax cross entropy of rows against their target tokens, in pieces of the vocabulary: no logits are kept.
+ *   lse[t] = log(sum_v exp(z[t][v]));     loss[t] = lse[t] - z[t][target[t]]
+ * both zero for a row whose target is none.  The backward call makes the logits again, from which, with the losses' gradients dloss,
+ *   dz[t][v] = dloss[t] (exp(z[t][v] - lse[t]) - (v is target[t]));     dx[t] = sum_v dz[t][v] table[v];     dtable[v] = sum_t dz[t][v] x[t]
+ * A row whose target is none or whose dloss is zero takes no part, whatever x holds there (zeros in dx), and costs next to nothing.
+ *   x, dx    device, rows of C;   table  device, [V] rows of C;   target  device, int32 [rows];   loss, lse, dloss  device, float [rows]
+ *   lse      (backward) as the forward call left it
+ *   dx       NULL: not wanted
+ *   dtable   device, [V][C], 16-byte aligned, fully overwritten, or with accumulate added to; NULL: not wanted (not both NULL)
+ *   workspace  device, >= snn_loss_workspace_bytes(desc, rows, 1, SNN_LOSS_FORWARD or _BACKWARD) bytes, 256-byte aligned.  What it holds
+ *              of probabilities is a piece of the vocabulary, of at most 512 MiB (256 tokens at least).
+ * dz is rounded to desc->dtype before the products (f16: times a power of two that brings the largest |dloss| to 2^14 .. 2^15, so that what is smaller than
+ * 2^-40 of that may be lost); dx and dtable are rounded once.
+ * Errors: INVALID_ARG; UNSUPPORTED (2^30 tiles or more); WORKSPACE; LAUNCH.
+ */
+#define SNN_LOSS_FORWARD  0
+#define SNN_LOSS_BACKWARD 1
+size_t snn_loss_workspace_bytes(const snn_vocab_desc *desc, int64_t rows, int k, int call);
+int snn_cross_entropy_forward(const snn_vocab_desc *desc, const void *x, int64_t ldx, int64_t rows, const void *table, int64_t ldt,
+                              const int32_t *target, float *loss, float *lse, void *workspace, size_t ws_bytes, void *stream);
+int snn_cross_entropy_backward(const snn_vocab_desc *desc, const void *x, int64_t ldx, int64_t rows, const void *table, int64_t ldt,
+                               const int32_t *target, const float *lse, const float *dloss, void *dx, int64_t lddx, void *dtable, int accumulate,
+                               void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Distillation from a teacher of whose logits k a row were kept (1 <= k <= 256): the divergence of the softmax over the whole vocabulary, at a
+ * temperature, from the teacher's over the listed tokens,
+ *   q[t][j] = softmax over the row's listed tokens of logits[t][j] / temperature
+ *   lse[t] = log(sum_v exp(z[t][v] / temperature));     loss[t] = sum_j q[t][j] (log q[t][j] - z[t][ids[t][j]] / temperature + lse[t])
+ *   dz[t][v] = dloss[t] / temperature (exp(z[t][v] / temperature - lse[t]) - sum of q[t][j] over the j with ids[t][j] = v)
+ * and from dz the gradients as above.  A listed token outside 0 .. V - 1 is not listed; one listed twice counts twice; a logit of -infinity has the share
+ * zero.  A row without a listed token that has a logit above -infinity is none, as above.
+ *   ids      device, int32 [rows][k];   logits  device, float [rows][k];   temperature  1/1024 .. 1024
+ *   picked   device, float [rows][k]: z[t][ids[t][j]], zeros where not listed and in rows that are none
+ *   the rest as for the cross entropy (workspace: k in place of 1).
+ */
+int snn_distill_forward(const snn_vocab_desc *desc, const void *x, int64_t ldx, int64_t rows, const void *table, int64_t ldt, const int32_t *ids,
+                        const float *logits, int k, float temperature, float *loss, float *lse, float *picked, void *workspace, size_t ws_bytes,
+                        void *stream);
+int snn_distill_backward(const snn_vocab_desc *desc, const void *x, int64_t ldx, int64_t rows, const void *table, int64_t ldt, const int32_t *ids,
+                         const float *logits, int k, float temperature, const float *lse, const float *dloss, void *dx, int64_t lddx, void *dtable,
+                         int accumulate, void *workspace, size_t ws_bytes, void *stream);
 
 /* Bytes of workspace the given entry point (SNN_WS_*) needs for this layer; 0 if desc is
  * invalid or the combination is unsupported.  Host-only, no device work. */

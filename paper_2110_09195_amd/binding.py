@@ -47,6 +47,8 @@ EXPORTS = ("snn_pack_activations", "snn_pack_activations_many", "snn_project_ker
            "snn_linear_weight_grad_workspace_bytes", "snn_linear_weight_grad", "snn_linear_weight_grad_checkpoint",
            "snn_checkpoint_store", "snn_checkpoint_restore",
            "snn_adapters_workspace_bytes", "snn_adapters_forward", "snn_adapters_backward", "snn_adapters_backward_checkpoint",
+           "snn_embedding_forward", "snn_embedding_grad_workspace_bytes", "snn_embedding_grad", "snn_loss_workspace_bytes",
+           "snn_cross_entropy_forward", "snn_cross_entropy_backward", "snn_distill_forward", "snn_distill_backward",
            "snn_workspace_bytes", "snn_packed_bytes", "snn_status_string", "snn_subbit_slots_per_channel",
            "snn_set_tuning", "snn_get_tuning")
 
@@ -87,6 +89,10 @@ class snn_linear_desc(ctypes.Structure):
 class snn_adapters(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int32), ("rank", ctypes.c_int32), ("A", ctypes.c_void_p), ("B", ctypes.c_void_p),
                 ("scale", ctypes.c_void_p)]
+
+
+class snn_vocab_desc(ctypes.Structure):
+    _fields_ = [("V", ctypes.c_int32), ("C", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 class SnnError(RuntimeError):
@@ -232,6 +238,19 @@ def lib():
         L.snn_set_tuning.restype = i32
         L.snn_get_tuning.argtypes = [i32]
         L.snn_get_tuning.restype = i32
+        ep, f32 = ctypes.POINTER(snn_vocab_desc), ctypes.c_float
+        L.snn_embedding_forward.argtypes = [ep, vp, i64, vp, i64, f32, vp, i64, vp]
+        L.snn_embedding_grad_workspace_bytes.argtypes = [ep, i64]
+        L.snn_embedding_grad.argtypes = [ep, vp, i64, vp, i64, f32, vp, i32, vp, sz, vp]
+        L.snn_loss_workspace_bytes.argtypes = [ep, i64, i32, i32]
+        L.snn_cross_entropy_forward.argtypes = [ep, vp, i64, i64, vp, i64, vp, vp, vp, vp, sz, vp]
+        L.snn_cross_entropy_backward.argtypes = [ep, vp, i64, i64, vp, i64, vp, vp, vp, vp, i64, vp, i32, vp, sz, vp]
+        L.snn_distill_forward.argtypes = [ep, vp, i64, i64, vp, i64, vp, vp, i32, f32, vp, vp, vp, vp, sz, vp]
+        L.snn_distill_backward.argtypes = [ep, vp, i64, i64, vp, i64, vp, vp, i32, f32, vp, vp, vp, i64, vp, i32, vp, sz, vp]
+        for name in ("snn_embedding_forward", "snn_embedding_grad", "snn_cross_entropy_forward", "snn_cross_entropy_backward", "snn_distill_forward",
+                     "snn_distill_backward"):
+            getattr(L, name).restype = i32
+        L.snn_embedding_grad_workspace_bytes.restype = L.snn_loss_workspace_bytes.restype = sz
         _use(L)
     return _lib
 
@@ -1034,3 +1053,147 @@ def snn_adapters_backward(desc, x, low, dy, weights, adapter, A, B, scale, dx=No
         _check(lib().snn_adapters_backward(ctypes.byref(desc), ctypes.byref(ad), *_rows(x, dy.dtype, desc.C_in, "x"), *rest),
                "snn_adapters_backward")
     return dx, dA, dB
+
+
+# ---- the ends of a network over tokens ---------------------------------------------------------------------------
+
+def make_vocab_desc(V, C, dtype=SNN_DTYPE_BF16):
+    return snn_vocab_desc(V, C, dtype)
+
+
+def _here(*tensors):
+    """Tensors of a call lie on the current device, whose stream the call is enqueued on."""
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != torch.cuda.current_device():
+            raise ValueError("a tensor lies on %s, and the current device is cuda:%d" % (t.device, torch.cuda.current_device()))
+
+
+def _table(desc, table):
+    p, ld = _rows(table, _dtype_of(desc), desc.C, "table")
+    if table.shape[0] != desc.V:
+        raise ValueError("table must hold V rows")
+    return p, ld
+
+
+def _one_a_row(t, dtype, rows, name):
+    _dev(t, dtype, name)
+    if t.numel() != rows:
+        raise ValueError("%s must hold one value a row" % name)
+    return t.data_ptr()
+
+
+def _dtable(desc, dtable, accumulate, device):
+    if dtable is None and accumulate:
+        raise ValueError("there is nothing to add to: dtable is not given")
+    return _whole(dtable, (desc.V, desc.C), _dtype_of(desc), "dtable", device)
+
+
+def _teacher(ids, logits, rows):
+    _dev(ids, torch.int32, "ids")
+    _dev(logits, torch.float32, "logits")
+    if ids.dim() != 2 or ids.shape[0] != rows or ids.shape != logits.shape:
+        raise ValueError("ids and logits must both be [rows][k]")
+    return ids.shape[1]
+
+
+def snn_embedding_forward(desc, table, ids, scale=1.0, y=None):
+    """Rows ids (int32 [rows], outside 0 .. V - 1: zeros) of table [V][C] times scale -> y [rows][C]."""
+    _here(table, ids, y)
+    pt, ldt = _table(desc, table)
+    _dev(ids, torch.int32, "ids")
+    y, py, ldy = _rows_out(y, ids.numel(), desc.C, table, "y")
+    _check(lib().snn_embedding_forward(ctypes.byref(desc), pt, ldt, _ptr(ids), ids.numel(), scale, py, ldy, _stream()), "snn_embedding_forward")
+    return y
+
+
+def snn_embedding_grad_workspace_bytes(desc, rows):
+    return int(lib().snn_embedding_grad_workspace_bytes(ctypes.byref(desc), rows))
+
+
+def snn_embedding_grad(desc, dy, ids, scale=1.0, dtable=None, accumulate=False, workspace=None):
+    """dy [rows][C] summed by ids (int32 [rows]) times scale -> dtable [V][C], overwritten or (accumulate) added to."""
+    _here(dy, ids, dtable, workspace)
+    rows = dy.shape[0]
+    pdy, lddy = _rows(dy, _dtype_of(desc), desc.C, "dy")
+    pi = _one_a_row(ids, torch.int32, rows, "ids")
+    dtable = _dtable(desc, dtable, accumulate, dy.device)
+    workspace = _scratch(workspace, snn_embedding_grad_workspace_bytes(desc, rows), dy.device)
+    _check(lib().snn_embedding_grad(ctypes.byref(desc), pdy, lddy, pi, rows, scale, _ptr(dtable), int(accumulate), _ptr(workspace),
+                                    workspace.numel(), _stream()), "snn_embedding_grad")
+    return dtable
+
+
+SNN_LOSS_FORWARD, SNN_LOSS_BACKWARD = range(2)
+
+
+def snn_loss_workspace_bytes(desc, rows, k=1, call=SNN_LOSS_FORWARD):
+    return int(lib().snn_loss_workspace_bytes(ctypes.byref(desc), rows, k, call))
+
+
+def snn_cross_entropy_forward(desc, x, table, target, loss=None, lse=None, workspace=None):
+    """x [rows][C] against target (int32 [rows], outside 0 .. V - 1: none) with the logits x table^T -> loss, lse, float32 [rows]."""
+    _here(x, table, target, loss, lse, workspace)
+    rows = x.shape[0]
+    px, ldx = _rows(x, _dtype_of(desc), desc.C, "x")
+    pt = _one_a_row(target, torch.int32, rows, "target")
+    loss = _whole(loss, (rows,), torch.float32, "loss", x.device)
+    lse = _whole(lse, (rows,), torch.float32, "lse", x.device)
+    workspace = _scratch(workspace, snn_loss_workspace_bytes(desc, rows), x.device)
+    _check(lib().snn_cross_entropy_forward(ctypes.byref(desc), px, ldx, rows, *_table(desc, table), pt, _ptr(loss), _ptr(lse), _ptr(workspace),
+                                           workspace.numel(), _stream()), "snn_cross_entropy_forward")
+    return loss, lse
+
+
+def _loss_grads(desc, x, dx, dtable, accumulate):
+    """dx and dtable, made if not given (False: not wanted, then None) -> (dx, its pointer and distance, dtable)"""
+    pdx, lddx = None, desc.C
+    if dx is False:
+        dx = None
+    else:
+        dx, pdx, lddx = _rows_out(dx, x.shape[0], desc.C, x, "dx")
+    return dx, pdx, lddx, None if dtable is False else _dtable(desc, dtable, accumulate, x.device)
+
+
+def snn_cross_entropy_backward(desc, x, table, target, lse, dloss, dx=None, dtable=None, accumulate=False, workspace=None):
+    """lse as the forward call returned it, dloss float32 [rows] -> dx [rows][C], dtable [V][C] (overwritten, or with accumulate added to).
+    dx=False or dtable=False: not wanted, None is returned."""
+    _here(x, table, target, lse, dloss, dx, dtable, workspace)
+    rows = x.shape[0]
+    px, ldx = _rows(x, _dtype_of(desc), desc.C, "x")
+    given = (_one_a_row(target, torch.int32, rows, "target"), _one_a_row(lse, torch.float32, rows, "lse"),
+             _one_a_row(dloss, torch.float32, rows, "dloss"))
+    dx, pdx, lddx, dtable = _loss_grads(desc, x, dx, dtable, accumulate)
+    workspace = _scratch(workspace, snn_loss_workspace_bytes(desc, rows, 1, SNN_LOSS_BACKWARD), x.device)
+    _check(lib().snn_cross_entropy_backward(ctypes.byref(desc), px, ldx, rows, *_table(desc, table), *given, pdx, lddx, _ptr(dtable), int(accumulate),
+                                            _ptr(workspace), workspace.numel(), _stream()), "snn_cross_entropy_backward")
+    return dx, dtable
+
+
+def snn_distill_forward(desc, x, table, ids, logits, temperature=1.0, loss=None, lse=None, picked=None, workspace=None):
+    """x [rows][C] against a teacher's logits (float32 [rows][k]) of the tokens ids (int32 [rows][k], outside 0 .. V - 1: not listed)
+    -> loss, lse, float32 [rows], and picked, float32 [rows][k]: the rows' own logits of these tokens."""
+    _here(x, table, ids, logits, loss, lse, picked, workspace)
+    rows = x.shape[0]
+    px, ldx = _rows(x, _dtype_of(desc), desc.C, "x")
+    k = _teacher(ids, logits, rows)
+    loss = _whole(loss, (rows,), torch.float32, "loss", x.device)
+    lse = _whole(lse, (rows,), torch.float32, "lse", x.device)
+    picked = _whole(picked, (rows, k), torch.float32, "picked", x.device)
+    workspace = _scratch(workspace, snn_loss_workspace_bytes(desc, rows, k), x.device)
+    _check(lib().snn_distill_forward(ctypes.byref(desc), px, ldx, rows, *_table(desc, table), _ptr(ids), _ptr(logits), k, temperature, _ptr(loss),
+                                     _ptr(lse), _ptr(picked), _ptr(workspace), workspace.numel(), _stream()), "snn_distill_forward")
+    return loss, lse, picked
+
+
+def snn_distill_backward(desc, x, table, ids, logits, temperature, lse, dloss, dx=None, dtable=None, accumulate=False, workspace=None):
+    """As snn_cross_entropy_backward, for snn_distill_forward's loss."""
+    _here(x, table, ids, logits, lse, dloss, dx, dtable, workspace)
+    rows = x.shape[0]
+    px, ldx = _rows(x, _dtype_of(desc), desc.C, "x")
+    k = _teacher(ids, logits, rows)
+    given = _one_a_row(lse, torch.float32, rows, "lse"), _one_a_row(dloss, torch.float32, rows, "dloss")
+    dx, pdx, lddx, dtable = _loss_grads(desc, x, dx, dtable, accumulate)
+    workspace = _scratch(workspace, snn_loss_workspace_bytes(desc, rows, k, SNN_LOSS_BACKWARD), x.device)
+    _check(lib().snn_distill_backward(ctypes.byref(desc), px, ldx, rows, *_table(desc, table), _ptr(ids), _ptr(logits), k, temperature, *given, pdx,
+                                      lddx, _ptr(dtable), int(accumulate), _ptr(workspace), workspace.numel(), _stream()), "snn_distill_backward")
+    return dx, dtable

@@ -22,7 +22,8 @@ PEAKS_SOURCES = ["peaks.hip"]
 MARSHAL_LIB = os.path.join(HERE, "_marshal.so")
 SOURCES = ["snn_api.hip", "pack.hip", "project.hip", "bnn_conv.hip", "subbit_conv.hip", "subbit_f32.hip",
            "subbit_mfma.hip", "subbit_stack.hip", "rows_fp4.hip", "conv1x1_fp4.hip", "train_ops.hip", "dense_fp4.hip",
-           "linear_api.hip", "linear_rows.hip", "linear_grad.hip", "linear_adapters.hip", "checkpoint.hip"]
+           "linear_api.hip", "linear_rows.hip", "linear_grad.hip", "linear_adapters.hip", "checkpoint.hip",
+           "embedding.hip", "vocab_api.hip", "vocab_loss.hip", "vocab_tiles.hip"]
 
 # Packed-fp32 VALU forms are switched off for all device code of this library.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",

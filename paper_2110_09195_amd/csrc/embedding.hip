@@ -1,0 +1,447 @@
+// Tokens to rows of a table, and the table's gradient.
+#include "linear_device.h"
+#include "vocab.h"
+
+namespace snn {
+
+namespace {
+
+// ---- rows of the table -----------------------------------------------------------------------------------------
+
+// Pieces of 8 channels, rows of `pieces` of them; AHEAD of a thread's are on their way at once, a grid apart.
+// Bound by memory, and for a few tokens by two dependent reads (the token, its row).
+constexpr int AHEAD = 4;
+
+template <class T>
+__global__ __launch_bounds__(256)
+void embedding_kernel(const T *__restrict__ table, int64_t ldt, const int32_t *__restrict__ ids, int64_t rows, int V, int pieces, float scale,
+                      T *__restrict__ y, int64_t ldy, int64_t step_rows, int step_pieces)
+{
+    using v8 = typename Half<T>::v8;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    int64_t t = id / pieces;
+    int p = (int)(id - t * pieces);
+    while (t < rows) {
+        int64_t at[AHEAD];
+        int piece[AHEAD], token[AHEAD];
+        v8 v[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            at[i] = t;
+            piece[i] = p;
+            token[i] = t < rows ? ids[t] : -1;
+            t += step_rows;
+            p += step_pieces;
+            if (p >= pieces) {
+                p -= pieces;
+                ++t;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            v[i] = v8{};
+            if ((uint32_t)token[i] < (uint32_t)V) v[i] = *(const v8 *)(table + token[i] * ldt + piece[i] * 8);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            v8 out = {};                                       // (tokens of no row: zeros, whatever the scale)
+            if ((uint32_t)token[i] < (uint32_t)V)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) out[k] = (T)((float)v[i][k] * scale);
+            if (at[i] < rows) *(v8 *)(y + at[i] * ldy + piece[i] * 8) = out;
+        }
+    }
+}
+
+// ---- tokens in order ---------------------------------------------------------------------------------------------
+// The rows by token, rows of one token in their own order, so that sums have a fixed order.  Tokens are compared as unsigned numbers: those
+// of no row of the table come last.
+
+// Up to RANKED rows in one launch: a row's place is the number of tokens below its own, and of its own in earlier rows.  64 rows a workgroup,
+// whose waves share out the tokens that they are compared with; these come by scalar loads, two VALU instructions a comparison.
+constexpr int64_t RANKED = 16384;
+constexpr int RANK_WAVES = 16;
+
+__global__ __launch_bounds__(64 * RANK_WAVES)
+void embedding_rank_kernel(const uint32_t *__restrict__ ids, int rows, uint32_t *__restrict__ sorted, int *__restrict__ order)
+{
+    __shared__ int counts[RANK_WAVES][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i0 = blockIdx.x * 64, i = i0 + lane;
+    const uint32_t mine = i < rows ? ids[i] : 0;
+    const int share = ((rows + RANK_WAVES - 1) / RANK_WAVES + 15) & ~15, lo = min(wave * share, rows), hi = min(lo + share, rows);
+    int below = 0, j = lo;
+    for (; j < min(i0, hi); ++j) below += ids[j] <= mine ? 1 : 0;
+    for (; j < min(i0 + 64, hi); ++j) {
+        const uint32_t other = ids[j];
+        below += other < mine || (other == mine && j < i) ? 1 : 0;
+    }
+    for (; j < hi; ++j) below += ids[j] < mine ? 1 : 0;
+    counts[wave][lane] = below;
+    __syncthreads();
+    if (wave == 0 && i < rows) {
+        int place = 0;
+#pragma unroll
+        for (int w = 0; w < RANK_WAVES; ++w) place += counts[w][lane];
+        sorted[place] = mine;
+        order[place] = i;
+    }
+}
+
+// More rows: by 8 bits of the token at a time, from the lowest.  Workgroups of 2048 rows count their digits; one workgroup turns the counts
+// [digit][workgroup] into places; then rows are put there, in their order.
+constexpr int DIGITS = 256, SORT_ROWS = 2048, SORT_WAVES = 4, SORT_ROUNDS = SORT_ROWS / 64 / SORT_WAVES;
+
+__device__ inline uint32_t sort_key(const uint32_t *keys, int64_t i, uint32_t V) { return min(keys[i], V); }
+
+__global__ __launch_bounds__(256)
+void embedding_count_kernel(const uint32_t *__restrict__ keys, int64_t rows, uint32_t V, int shift, uint32_t *__restrict__ counts, int blocks)
+{
+    __shared__ uint32_t bins[DIGITS];
+    bins[threadIdx.x] = 0;
+    __syncthreads();
+    const int64_t at = (int64_t)blockIdx.x * SORT_ROWS;
+#pragma unroll
+    for (int i = 0; i < SORT_ROWS / 256; ++i) {
+        const int64_t n = at + i * 256 + threadIdx.x;
+        if (n < rows) atomicAdd(&bins[sort_key(keys, n, V) >> shift & (DIGITS - 1)], 1u);
+    }
+    __syncthreads();
+    counts[(int64_t)threadIdx.x * blocks + blockIdx.x] = bins[threadIdx.x];
+}
+
+__global__ __launch_bounds__(1024)
+void embedding_places_kernel(uint32_t *__restrict__ counts, int64_t n)
+{
+    __shared__ uint32_t waves[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t before = 0;
+    for (int64_t at = 0; at < n; at += 4096) {
+        const int64_t i = at + threadIdx.x * 4;
+        uint32_t v[4], sum = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[k] = i + k < n ? counts[i + k] : 0;
+            sum += v[k];
+        }
+        uint32_t upto = sum;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+        }
+        if (lane == 63) waves[wave] = upto;
+        __syncthreads();
+        uint32_t place = before + upto - sum, all = 0;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) place += waves[w];
+            all += waves[w];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (i + k < n) counts[i + k] = place;
+            place += v[k];
+        }
+        before += all;
+        __syncthreads();
+    }
+}
+
+__global__ __launch_bounds__(256)
+void embedding_place_kernel(const uint32_t *__restrict__ keys, const int *__restrict__ order, int64_t rows, uint32_t V, int shift,
+                            const uint32_t *__restrict__ places, int blocks, uint32_t *__restrict__ keys_out, int *__restrict__ order_out)
+{
+    __shared__ uint32_t next[SORT_WAVES][DIGITS];              // where a wave's next row of a digit goes
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    for (int w = 0; w < SORT_WAVES; ++w) next[w][tid] = 0;
+    __syncthreads();
+    const int64_t at = (int64_t)blockIdx.x * SORT_ROWS + wave * (SORT_ROUNDS * 64) + lane;
+    uint32_t key[SORT_ROUNDS];
+#pragma unroll
+    for (int r = 0; r < SORT_ROUNDS; ++r) {
+        key[r] = at + r * 64 < rows ? sort_key(keys, at + r * 64, V) : ~0u;
+        if (at + r * 64 < rows) atomicAdd(&next[wave][key[r] >> shift & (DIGITS - 1)], 1u);
+    }
+    __syncthreads();
+    uint32_t place = places[(int64_t)tid * blocks + blockIdx.x];
+    for (int w = 0; w < SORT_WAVES; ++w) {
+        const uint32_t n = next[w][tid];
+        next[w][tid] = place;
+        place += n;
+    }
+    __syncthreads();
+    volatile uint32_t *const mine = next[wave];
+#pragma unroll
+    for (int r = 0; r < SORT_ROUNDS; ++r) {
+        const bool in = at + r * 64 < rows;
+        const uint32_t digit = key[r] >> shift & (DIGITS - 1);
+        uint64_t same = __ballot(in);
+#pragma unroll
+        for (int b = 0; b < 8; ++b) {
+            const uint64_t set = __ballot(digit >> b & 1);
+            same &= digit >> b & 1 ? set : ~set;
+        }
+        const int earlier = __popcll(same & ((1ull << lane) - 1));
+        const uint32_t base = mine[digit];
+        __builtin_amdgcn_wave_barrier();
+        if (in) {
+            if (earlier == 0) mine[digit] = base + (uint32_t)__popcll(same);
+            keys_out[base + earlier] = key[r];
+            order_out[base + earlier] = order ? order[at + r * 64] : (int)(at + r * 64);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// ---- sums by token -----------------------------------------------------------------------------------------------
+
+struct SumArgs {
+    const void *dy;
+    int64_t lddy, rows;
+    const uint32_t *sorted;
+    const int *order;
+    int V, C, slabs;                  // slabs of 512 channels, a wave's
+    int64_t blocks;                   // of BLOCK rows in the tokens' order
+    float scale;
+    void *dtable;
+    int accumulate;
+    float *part;                      // [block][2][C]: sums of a block's first token, begun in an earlier one, and of its last, which goes on
+};
+constexpr int BLOCK = 32, SUM_AHEAD = 8, FILL_ROWS = 64;
+
+template <class T>
+__device__ inline void write_sum(const SumArgs &p, uint32_t token, int c, const float *sum)
+{
+    using v8 = typename Half<T>::v8;
+    v8 *const at = (v8 *)((T *)p.dtable + (int64_t)token * p.C + c), out = p.accumulate ? *at : v8{};
+    v8 v;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = (T)(p.accumulate ? fmaf(sum[k], p.scale, (float)out[k]) : sum[k] * p.scale);
+    *at = v;
+}
+
+// A wave sums BLOCK rows in the tokens' order, 512 channels.  A token whose rows all lie there is done; the others' sums are joined by the next
+// launch.  Workgroups behind these (when the result is not added to what is there) write zeros for FILL_ROWS tokens each that have no row.
+// Bound by memory: each row is read once, each row of the result written once.
+template <class T>
+__global__ __launch_bounds__(256)
+void embedding_sum_kernel(SumArgs p, unsigned sum_grid)
+{
+    using v8 = typename Half<T>::v8;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (blockIdx.x >= sum_grid) {
+        __shared__ uint64_t absent;
+        const int64_t v0 = (int64_t)(blockIdx.x - sum_grid) * FILL_ROWS;
+        if (wave == 0) {
+            const uint32_t v = (uint32_t)(v0 + lane);
+            int64_t lo = 0, hi = p.rows;                       // the first row of a token >= v
+            while (lo < hi) {
+                const int64_t mid = (lo + hi) >> 1;
+                if (p.sorted[mid] < v) lo = mid + 1;
+                else hi = mid;
+            }
+            const uint64_t none = __ballot(v < (uint32_t)p.V && (lo == p.rows || p.sorted[lo] != v));
+            if (lane == 0) absent = none;
+        }
+        __syncthreads();
+        const uint64_t rows = absent;
+        for (int r = wave; r < FILL_ROWS; r += 4)
+            if (rows >> r & 1)
+                for (int c = lane * 8; c < p.C; c += 512) *(v8 *)((T *)p.dtable + (v0 + r) * p.C + c) = v8{};
+        return;
+    }
+    const int64_t id = (int64_t)blockIdx.x * 4 + wave, block = id / p.slabs;
+    if (block >= p.blocks) return;
+    const int c = (int)(id - block * p.slabs) * 512 + lane * 8;
+    const int64_t first = block * BLOCK;
+    const int n = (int)min((int64_t)BLOCK, p.rows - first);
+    // lane l: row l of the block, and its token; lanes behind them the tokens before and after the block
+    uint32_t token = ~0u;
+    int row = 0;
+    if (lane < n) {
+        token = p.sorted[first + lane];
+        row = p.order[first + lane];
+    } else if (lane == 62 && first > 0) token = p.sorted[first - 1];
+    else if (lane == 63 && first + n < p.rows) token = p.sorted[first + n];
+    const bool in = c < p.C;
+    const T *const dy = (const T *)p.dy;
+    uint32_t now = __builtin_amdgcn_readlane(token, 0);
+    const uint32_t before = __builtin_amdgcn_readlane(token, 62), after = __builtin_amdgcn_readlane(token, 63);
+    bool begun = first > 0 && before == now;                   // the token's rows begin in an earlier block
+    float sum[8] = {};
+    for (int r0 = 0; r0 < n; r0 += SUM_AHEAD) {
+        v8 v[SUM_AHEAD];
+        uint32_t of[SUM_AHEAD];
+#pragma unroll
+        for (int i = 0; i < SUM_AHEAD; ++i) {
+            const int r = r0 + i;
+            of[i] = r < n ? __builtin_amdgcn_readlane(token, min(r, BLOCK - 1)) : ~0u;
+            v[i] = v8{};
+            if (in && of[i] < (uint32_t)p.V) v[i] = *(const v8 *)(dy + (int64_t)__builtin_amdgcn_readlane(row, min(r, BLOCK - 1)) * p.lddy + c);
+        }
+#pragma unroll
+        for (int i = 0; i < SUM_AHEAD; ++i) {
+            if (r0 + i >= n) break;
+            if (of[i] != now) {
+                if (in && now < (uint32_t)p.V) {
+                    if (!begun) write_sum<T>(p, now, c, sum);
+                    else
+#pragma unroll
+                        for (int k = 0; k < 8; k += 4) *(f32x4 *)(p.part + block * 2 * p.C + c + k) = f32x4{sum[k], sum[k + 1], sum[k + 2], sum[k + 3]};
+                }
+                now = of[i];
+                begun = false;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum[k] += (float)v[i][k];
+        }
+    }
+    if (!in || now >= (uint32_t)p.V) return;
+    const bool goes_on = first + n < p.rows && after == now;
+    if (!begun && !goes_on) write_sum<T>(p, now, c, sum);
+    else
+#pragma unroll
+        for (int k = 0; k < 8; k += 4)
+            *(f32x4 *)(p.part + (block * 2 + (begun ? 0 : 1)) * p.C + c + k) = f32x4{sum[k], sum[k + 1], sum[k + 2], sum[k + 3]};
+}
+
+// Tokens whose rows lie in several blocks, from the block in which they begin: the blocks' sums in their order, shared out among the waves
+// in runs.
+constexpr int JOIN_WAVES = 4;
+
+template <class T>
+__global__ __launch_bounds__(64 * JOIN_WAVES)
+void embedding_join_kernel(SumArgs p)
+{
+    __shared__ float sums[JOIN_WAVES][64][9];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t block = blockIdx.x / p.slabs, next = (block + 1) * BLOCK;
+    if (next >= p.rows) return;
+    const uint32_t token = p.sorted[next - 1];
+    if (token >= (uint32_t)p.V || p.sorted[next] != token) return;             // no token goes on,
+    if (block * BLOCK > 0 && p.sorted[block * BLOCK] == token && p.sorted[block * BLOCK - 1] == token) return;          // or none that begins here
+    int64_t lo = block + 1, hi = p.blocks - 1;                 // the last block that begins with it
+    while (lo < hi) {
+        const int64_t mid = (lo + hi + 1) >> 1;
+        if (p.sorted[mid * BLOCK] == token) lo = mid;
+        else hi = mid - 1;
+    }
+    const int64_t n = lo - block + 1, share = (n + JOIN_WAVES - 1) / JOIN_WAVES;
+    const int c = (int)(blockIdx.x - block * p.slabs) * 512 + lane * 8;
+    float sum[8] = {};
+    if (c < p.C)
+#pragma unroll 4
+        for (int64_t i = wave * share; i < min(n, (wave + 1) * share); ++i) {
+            const float *const from = p.part + ((block + i) * 2 + (i ? 0 : 1)) * p.C + c;
+            const f32x4 a = *(const f32x4 *)from, b = *(const f32x4 *)(from + 4);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                sum[k] += a[k];
+                sum[4 + k] += b[k];
+            }
+        }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sums[wave][lane][k] = sum[k];
+    __syncthreads();
+    if (wave != 0 || c >= p.C) return;
+#pragma unroll
+    for (int w = 1; w < JOIN_WAVES; ++w)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[k] += sums[w][lane][k];
+    write_sum<T>(p, token, c, sum);
+}
+
+struct SortPlan {
+    int passes, blocks;
+    size_t keys, counts, part, bytes; // where they lie in the workspace (keys and order twice where there are passes)
+};
+
+SortPlan sort_plan(const Vocab &v, int64_t rows)
+{
+    SortPlan p = {};
+    if (rows > RANKED) {
+        while (((int64_t)1 << (8 * p.passes)) <= v.V) ++p.passes;              // (V itself stands for what is no token)
+        p.blocks = (int)((rows + SORT_ROWS - 1) / SORT_ROWS);
+    }
+    const size_t one = align_up((size_t)rows * 4, 256);
+    p.keys = 0;
+    p.counts = one * (p.passes ? 4 : 2);
+    p.part = p.counts + (p.passes ? align_up((size_t)p.blocks * DIGITS * 4, 256) : 0);
+    p.bytes = p.part + align_up((size_t)((rows + BLOCK - 1) / BLOCK) * 2 * v.C * 4, 256);
+    return p;
+}
+
+template <class T>
+int launch_sums(const SumArgs &p, hipStream_t s)
+{
+    const int64_t sums = (p.blocks * p.slabs + 3) / 4, fill = p.accumulate ? 0 : (p.V + FILL_ROWS - 1) / FILL_ROWS, joins = p.blocks * p.slabs;
+    if (sums + fill >= ((int64_t)1 << 31) || joins >= ((int64_t)1 << 31)) return SNN_ERR_UNSUPPORTED;
+    if (sums + fill > 0) {
+        embedding_sum_kernel<T><<<dim3((unsigned)(sums + fill)), 256, 0, s>>>(p, (unsigned)sums);
+        const int rc = check_launch();
+        if (rc != SNN_OK) return rc;
+    }
+    if (p.blocks < 2) return SNN_OK;
+    embedding_join_kernel<T><<<dim3((unsigned)joins), 64 * JOIN_WAVES, 0, s>>>(p);
+    return check_launch();
+}
+
+}  // namespace
+
+int launch_embedding_forward(const Vocab &v, const Rows16 &table, const int32_t *ids, int64_t rows, float scale, void *y, int64_t ldy, hipStream_t s)
+{
+    const int pieces = v.C / 8;
+    const int64_t blocks = (rows * pieces + 255) / 256, grid = blocks < 8192 ? blocks : 8192;
+    const int64_t step_rows = grid * 256 / pieces;
+    const int step_pieces = (int)(grid * 256 % pieces);
+    if (v.dtype == SNN_DTYPE_BF16)
+        embedding_kernel<__bf16><<<dim3((unsigned)grid), 256, 0, s>>>((const __bf16 *)table.p, table.ld, ids, rows, v.V, pieces, scale, (__bf16 *)y, ldy,
+                                                                      step_rows, step_pieces);
+    else
+        embedding_kernel<_Float16><<<dim3((unsigned)grid), 256, 0, s>>>((const _Float16 *)table.p, table.ld, ids, rows, v.V, pieces, scale, (_Float16 *)y,
+                                                                        ldy, step_rows, step_pieces);
+    return check_launch();
+}
+
+size_t embedding_grad_workspace_bytes(const Vocab &v, int64_t rows) { return sort_plan(v, rows).bytes; }
+
+int launch_embedding_grad(const Vocab &v, const Rows16 &dy, const int32_t *ids, int64_t rows, float scale, void *dtable, bool accumulate, void *ws,
+                          hipStream_t s)
+{
+    const SortPlan plan = sort_plan(v, rows);
+    const size_t one = align_up((size_t)rows * 4, 256);
+    uint32_t *sorted = (uint32_t *)ws, *other = (uint32_t *)((char *)ws + 2 * one);
+    int *order = (int *)((char *)ws + one), *other_order = (int *)((char *)ws + 3 * one);
+    if (rows > 0 && !plan.passes) {
+        embedding_rank_kernel<<<dim3((unsigned)((rows + 63) / 64)), 64 * RANK_WAVES, 0, s>>>((const uint32_t *)ids, (int)rows, sorted, order);
+        const int rc = check_launch();
+        if (rc != SNN_OK) return rc;
+    }
+    const uint32_t *from = (const uint32_t *)ids;
+    const int *from_order = nullptr;
+    uint32_t *const counts = (uint32_t *)((char *)ws + plan.counts);
+    for (int pass = 0; pass < plan.passes; ++pass) {
+        // the last pass ends in the first pair
+        uint32_t *const to = (plan.passes - pass) & 1 ? sorted : other;
+        int *const to_order = (plan.passes - pass) & 1 ? order : other_order;
+        embedding_count_kernel<<<dim3((unsigned)plan.blocks), 256, 0, s>>>(from, rows, (uint32_t)v.V, pass * 8, counts, plan.blocks);
+        embedding_places_kernel<<<1, 1024, 0, s>>>(counts, (int64_t)plan.blocks * DIGITS);
+        embedding_place_kernel<<<dim3((unsigned)plan.blocks), 256, 0, s>>>(from, from_order, rows, (uint32_t)v.V, pass * 8, counts, plan.blocks, to, to_order);
+        const int rc = check_launch();
+        if (rc != SNN_OK) return rc;
+        from = to;
+        from_order = to_order;
+    }
+    SumArgs p = {};
+    p.dy = dy.p; p.lddy = dy.ld; p.rows = rows; p.sorted = sorted; p.order = order;
+    p.V = v.V; p.C = v.C; p.slabs = (v.C + 511) / 512;
+    p.blocks = (rows + BLOCK - 1) / BLOCK;
+    p.scale = scale; p.dtable = dtable; p.accumulate = accumulate;
+    p.part = (float *)((char *)ws + plan.part);
+    return v.dtype == SNN_DTYPE_BF16 ? launch_sums<__bf16>(p, s) : launch_sums<_Float16>(p, s);
+}
+
+}  // namespace snn

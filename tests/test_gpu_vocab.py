@@ -1,0 +1,426 @@
+"""The ends of a network over tokens against their definitions in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from paper_2110_09195_amd import binding as B
+from vocab_reference import F32, TINY, UNIT, Loss, by_token, embedding, within
+
+pytestmark = pytest.mark.gpu
+
+BF, HF = torch.bfloat16, torch.float16
+CODE = {BF: B.SNN_DTYPE_BF16, HF: B.SNN_DTYPE_F16}
+NAN, INF = float("nan"), float("inf")
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def normal(g, *shape):
+    return torch.randn(*shape, generator=g, device="cuda")
+
+
+def apart(t, ld):
+    """The same rows `ld` elements apart, what lies between them not a number."""
+    wide = torch.full((t.shape[0], ld), NAN, dtype=t.dtype, device=t.device)
+    wide[:, :t.shape[1]] = t
+    return wide[:, :t.shape[1]]
+
+
+class Framed:
+    """A contiguous output with known values before and behind it."""
+
+    def __init__(self, shape, dtype, fill=7.0):
+        n = math.prod(shape)
+        self.all = torch.full((n + 512,), fill, dtype=dtype, device="cuda")
+        self.t = self.all[256:256 + n].view(shape)
+        self.fill = fill
+
+    def check(self):
+        n = self.t.numel()
+        assert (self.all[:256] == self.fill).all() and (self.all[256 + n:] == self.fill).all(), "written outside the output"
+
+
+def workspace(n):
+    f = Framed((max(n, 256),), torch.uint8, 113)
+    assert f.t.data_ptr() % 256 == 0
+    return f
+
+
+# ---- tokens to rows ----------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows, V, C", [(1, 1, 8), (1, 50, 4096), (3, 7, 72), (333, 1000, 520), (4097, 301, 2056), (70000, 17, 8)])
+def test_rows_of_tokens(rows, V, C, dtype):
+    g = gen(rows)
+    table = apart(normal(g, V, C).to(dtype), C + 24)
+    ids = torch.randint(-2, V + 2, (rows,), generator=g, device="cuda").int()
+    y = torch.full((rows, C + 8), 7.0, dtype=dtype, device="cuda")
+    B.snn_embedding_forward(B.make_vocab_desc(V, C, CODE[dtype]), table, ids, 1.7, y=y[:, :C])
+    assert torch.equal(y[:, :C], (embedding(table, ids, 1.0).float() * torch.tensor(1.7, device="cuda")).to(dtype))
+    assert (y[:, C:] == 7).all()
+
+
+def test_rows_of_no_token_are_zeros_whatever_the_scale():
+    table = torch.full((4, 8), INF, dtype=BF, device="cuda")
+    ids = torch.tensor([-1, 4, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device="cuda")
+    assert not B.snn_embedding_forward(B.make_vocab_desc(4, 8), table, ids, NAN).any()
+
+
+# (both ways of sorting, on either side of their border; tokens of one row each, of all rows, of none)
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("rows, V, C, dtype, skew", [
+    (1, 1, 8, BF, 1), (1, 300, 520, HF, 1), (31, 5, 72, BF, 1), (32, 1, 1032, HF, 1), (33, 2, 8, BF, 1), (64, 64, 512, HF, 1), (257, 9, 520, BF, 3),
+    (1000, 70000, 136, BF, 1), (5000, 301, 1032, HF, 3), (16384, 1500, 264, BF, 2), (16385, 1500, 264, HF, 2), (40000, 255, 72, BF, 2),
+    (40000, 256, 72, HF, 1), (40001, 70001, 40, BF, 4)])
+def test_gradient_of_the_table(rows, V, C, dtype, skew, accumulate):
+    g = gen(rows + V)
+    ids = (torch.rand(rows, generator=g, device="cuda") ** skew * (V + 3)).long().sub(1).int()             # -1, 0 .. V - 1, V, V + 1
+    ids = torch.where(torch.rand(rows, generator=g, device="cuda") < 0.05, ids - 2 ** 30, ids).int()
+    if rows < 40:
+        ids[0] = V - 1
+    dy = normal(g, rows, C).to(dtype)
+    dy[(ids < 0) | (ids >= V)] = NAN
+    held = normal(g, V, C).to(dtype)
+    out, desc = Framed((V, C), dtype), B.make_vocab_desc(V, C, CODE[dtype])
+    out.t.copy_(held)
+    ws = workspace(B.snn_embedding_grad_workspace_bytes(desc, rows))
+    B.snn_embedding_grad(desc, apart(dy, C + 16), ids, 0.3, dtable=out.t, accumulate=accumulate, workspace=ws.t)
+    out.check(), ws.check()
+    total, magnitude, n = by_token(dy, ids, V)
+    want = total * torch.tensor(0.3).double().item() + (held.double() if accumulate else 0)
+    error = UNIT[dtype] * want.abs() + (n[:, None] + 3) * F32 * (0.3 * magnitude + (held.double().abs() if accumulate else 0)) + TINY[dtype]
+    within(out.t, want, error * (1 + UNIT[dtype]), "dtable")
+    absent = n == 0
+    assert torch.equal(out.t[absent], held[absent] if accumulate else torch.zeros_like(held[absent]))
+    again = held.clone()
+    B.snn_embedding_grad(desc, dy, ids, 0.3, dtable=again, accumulate=accumulate)
+    assert torch.equal(again, out.t), "a call repeated gives other bits"
+
+
+@pytest.mark.parametrize("rows", [20000, 3000])
+def test_all_rows_of_one_token(rows):
+    desc, g = B.make_vocab_desc(7, 1032, CODE[BF]), gen(5)
+    dy = normal(g, rows, 1032).to(BF)
+    got = B.snn_embedding_grad(desc, dy, torch.full((rows,), 3, dtype=torch.int32, device="cuda"))
+    total, magnitude, _ = by_token(dy, torch.full((rows,), 3, device="cuda"), 7)
+    within(got, total, UNIT[BF] * total.abs() + rows * F32 * magnitude, "dtable")
+
+
+def test_no_rows():
+    desc, e = B.make_vocab_desc(40, 72), torch.empty(0, 72, dtype=BF, device="cuda")
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    table = torch.ones(40, 72, dtype=BF, device="cuda")
+    assert B.snn_embedding_forward(desc, table, none).shape == (0, 72)
+    assert not B.snn_embedding_grad(desc, e, none, dtable=table.clone()).any()
+    assert torch.equal(B.snn_embedding_grad(desc, e, none, dtable=table.clone(), accumulate=True), table)
+    f = torch.empty(0, device="cuda")
+    loss, lse = B.snn_cross_entropy_forward(desc, e, table, none)
+    assert loss.shape == lse.shape == (0,)
+    dx, dw = B.snn_cross_entropy_backward(desc, e, table, none, f, f, dtable=table.clone())
+    assert dx.shape == (0, 72) and not dw.any()
+    dx, dw = B.snn_cross_entropy_backward(desc, e, table, none, f, f, dtable=table.clone(), accumulate=True)
+    assert torch.equal(dw, table)
+    n2, f2 = none.view(0, 1).expand(0, 5).contiguous(), f.view(0, 1).expand(0, 5).contiguous()
+    loss, lse, picked = B.snn_distill_forward(desc, e, table, n2, f2, 2.0)
+    assert picked.shape == (0, 5)
+    dx, dw = B.snn_distill_backward(desc, e, table, n2, f2, 2.0, f, f)
+    assert dx.shape == (0, 72) and not dw.any()
+
+
+# ---- losses ------------------------------------------------------------------------------------------------------
+
+def rows_for(g, rows, V, C, dtype, none, k=0):
+    """x leaning towards a token each, a table, the tokens (or k of them a row), and which rows are none"""
+    table = (normal(g, V, C) * C ** -0.5).to(dtype)
+    first = torch.randint(0, V, (rows,), generator=g, device="cuda")
+    lean = torch.rand(rows, 1, generator=g, device="cuda") * 2 * math.log(V + 1)
+    x = (normal(g, rows, C) + lean * table[first].float()).to(dtype)
+    off = torch.rand(rows, generator=g, device="cuda") < none
+    if rows < 3:
+        off[:] = False
+    ids = torch.where(off, torch.where(first % 2 == 0, -1 - first, V + first), first)
+    if k:
+        others = torch.randint(-1, V + 1, (rows, k), generator=g, device="cuda")          # some not listed, some twice
+        others[:, 0] = first
+        ids = torch.where(off[:, None], torch.where(others % 2 == 0, -1 - others.abs(), V + others.abs()), others)
+        ids = ids[:, torch.randperm(k, generator=g, device="cuda")]
+    return x, table, ids.int().contiguous(), off
+
+
+def check_loss(rows, V, C, dtype, none=0.3, k=0, temperature=1.0, seed=0, strided=False, poison=True):
+    g = gen(1000 * rows + V + C + seed)
+    x, table, ids, off = rows_for(g, rows, V, C, dtype, none, k)
+    desc = B.make_vocab_desc(V, C, CODE[dtype])
+    logits = None
+    if k:
+        logits = 4 * normal(g, rows, k)
+        if k > 2:
+            logits[::3, 1] = -INF
+    dloss = (0.2 + torch.rand(rows, generator=g, device="cuda")) * torch.where(torch.rand(rows, generator=g, device="cuda") < 0.3, -1.0, 1.0)
+    if poison and rows > 2:                                            # what does not count may be anything
+        x[off] = torch.tensor([NAN, INF, -INF], dtype=dtype, device="cuda")[torch.arange(C, device="cuda") % 3]
+    idle = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    if rows > 8:
+        dloss[off], idle[5] = NAN, True
+        dloss[5] = 0.0
+    want = Loss(x, table, ids, logits, temperature, torch.where(off | idle, torch.zeros_like(dloss), dloss))
+    xs, ts = (apart(x, C + 40), apart(table, C + 8)) if strided else (x, table)
+    loss, lse = Framed((rows,), torch.float32), Framed((rows,), torch.float32)
+    frames = [loss, lse]
+    ws = workspace(B.snn_loss_workspace_bytes(desc, rows, max(k, 1)))
+    if k:
+        picked = Framed((rows, k), torch.float32)
+        frames.append(picked)
+        B.snn_distill_forward(desc, xs, ts, ids, logits, temperature, loss=loss.t, lse=lse.t, picked=picked.t, workspace=ws.t)
+        within(picked.t, want.picked, want.picked_error, "picked")
+    else:
+        B.snn_cross_entropy_forward(desc, xs, ts, ids, loss=loss.t, lse=lse.t, workspace=ws.t)
+    for f in frames + [ws]:
+        f.check()
+    within(loss.t, want.loss, want.loss_error, "loss")
+    within(lse.t, want.lse, want.lse_error, "lse")
+    ws = workspace(B.snn_loss_workspace_bytes(desc, rows, max(k, 1), B.SNN_LOSS_BACKWARD))
+    wide, dw = torch.full((rows, C + 8), 7.0, dtype=dtype, device="cuda"), Framed((V, C), dtype)
+    if k:
+        B.snn_distill_backward(desc, xs, ts, ids, logits, temperature, lse.t, dloss, dx=wide[:, :C], dtable=dw.t, workspace=ws.t)
+    else:
+        B.snn_cross_entropy_backward(desc, xs, ts, ids, lse.t, dloss, dx=wide[:, :C], dtable=dw.t, workspace=ws.t)
+    dw.check(), ws.check()
+    assert (wide[:, C:] == 7).all()
+    within(wide[:, :C], want.dx, want.dx_error, "dx")
+    within(dw.t, want.dw, want.dw_error, "dtable")
+    return want
+
+
+SIZES = [(1, 1, 8, BF), (1, 2, 8, HF), (1, 129, 72, BF), (2, 1000, 264, HF), (7, 63, 40, BF), (63, 4099, 136, BF), (64, 128, 32, HF), (65, 127, 520, BF),
+         (128, 257, 1032, HF), (129, 300, 72, BF), (200, 2000, 2056, HF), (333, 5003, 264, BF), (700, 1024, 512, HF)]
+
+
+@pytest.mark.parametrize("rows, V, C, dtype", SIZES)
+def test_cross_entropy(rows, V, C, dtype):
+    check_loss(rows, V, C, dtype, strided=rows % 2 == 1)
+
+
+@pytest.mark.parametrize("rows, V, C, dtype, k, temperature", [
+    (1, 1, 8, BF, 1, 1.0), (1, 40, 8, HF, 7, 2.0), (5, 129, 72, BF, 256, 0.5), (64, 1000, 136, HF, 9, 4.0), (65, 257, 264, BF, 64, 1.5),
+    (130, 4099, 520, HF, 100, 2.0), (333, 300, 72, BF, 20, 1.0), (700, 2000, 256, BF, 3, 3.0)])
+def test_distillation(rows, V, C, dtype, k, temperature):
+    check_loss(rows, V, C, dtype, k=k, temperature=temperature, strided=rows % 2 == 1)
+
+
+# large tiles; rows gathered in the forward call; several pieces of the vocabulary
+@pytest.mark.parametrize("rows, V, C, dtype, k", [(700, 60000, 1032, BF, 0), (3001, 12007, 1000, HF, 0), (4133, 70001, 72, BF, 0), (4133, 70001, 40, HF, 5),
+                                                  (600, 50000, 1096, BF, 70)])
+def test_large(rows, V, C, dtype, k):
+    check_loss(rows, V, C, dtype, none=0.6 if rows > 4000 else 0.1, k=k, temperature=2.0 if k else 1.0)
+
+
+@pytest.mark.parametrize("rows", [3, 300])
+@pytest.mark.parametrize("k", [0, 4])
+def test_no_row_counts(rows, k):
+    V, C = 500, 72
+    desc, ids = B.make_vocab_desc(V, C), torch.full((rows, max(k, 1)), -1, dtype=torch.int32, device="cuda")
+    x, table = torch.full((rows, C), NAN, dtype=BF, device="cuda"), torch.ones(V, C, dtype=BF, device="cuda")
+    dloss = torch.ones(rows, device="cuda")
+    if k:
+        ids[0] = 3
+        logits = torch.full((rows, k), -INF, device="cuda")            # (listed, but none has a share)
+        *out, lse = B.snn_distill_forward(desc, x, table, ids, logits, 2.0)[::-1]
+        out += [lse, *B.snn_distill_backward(desc, x, table, ids, logits, 2.0, lse, dloss)]
+    else:
+        loss, lse = B.snn_cross_entropy_forward(desc, x, table, ids.view(-1))
+        out = [loss, lse, *B.snn_cross_entropy_backward(desc, x, table, ids.view(-1), lse, dloss)]
+    for t in out:
+        assert not t.any()
+    held = torch.full((V, C), 3.0, dtype=BF, device="cuda")
+    if not k:
+        B.snn_cross_entropy_backward(desc, x, table, ids.view(-1), lse, dloss, dx=False, dtable=held, accumulate=True)
+        assert (held == 3).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_what_is_wanted_and_what_is_added(dtype):
+    g = gen(3)
+    x, table, ids, _ = rows_for(g, 150, 700, 136, dtype, 0.2)
+    desc, dloss = B.make_vocab_desc(700, 136, CODE[dtype]), torch.rand(150, generator=g, device="cuda")
+    _, lse = B.snn_cross_entropy_forward(desc, x, table, ids)
+    dx, dw = B.snn_cross_entropy_backward(desc, x, table, ids, lse, dloss)
+    only_x, nothing = B.snn_cross_entropy_backward(desc, x, table, ids, lse, dloss, dtable=False)
+    assert nothing is None and torch.equal(only_x, dx)
+    nothing, only_w = B.snn_cross_entropy_backward(desc, x, table, ids, lse, dloss, dx=False)
+    assert nothing is None and torch.equal(only_w, dw)
+    held = normal(g, 700, 136).to(dtype)
+    want = Loss(x, table, ids, None, 1.0, dloss)
+    both = held.double() + want.dw
+    added = held.clone()
+    B.snn_cross_entropy_backward(desc, x, table, ids, lse, dloss, dx=False, dtable=added, accumulate=True)
+    within(added, both, want.dw_error + UNIT[dtype] * both.abs() + F32 * held.double().abs(), "added")
+
+
+def test_a_row_that_is_not_a_number_reaches_no_other_row():
+    g = gen(8)
+    for rows in (40, 300):
+        x, table, ids, _ = rows_for(g, rows, 900, 72, BF, 0.0)
+        desc, dloss = B.make_vocab_desc(900, 72), torch.ones(rows, device="cuda")
+        good = B.snn_cross_entropy_forward(desc, x, table, ids)
+        dx = B.snn_cross_entropy_backward(desc, x, table, ids, good[1], dloss, dtable=False)[0]
+        x[11, 5], x[12, 6] = NAN, INF
+        loss, lse = B.snn_cross_entropy_forward(desc, x, table, ids)
+        others = torch.ones(rows, dtype=torch.bool, device="cuda")
+        others[11:13] = False
+        assert loss[11:13].isnan().all() and torch.equal(loss[others], good[0][others]) and torch.equal(lse[others], good[1][others])
+        bad = B.snn_cross_entropy_backward(desc, x, table, ids, lse, dloss, dtable=False)[0]
+        assert bad[11:13].isnan().any(1).all() and torch.equal(bad[others], dx[others])
+
+
+def test_gradients_of_f16_at_any_scale():
+    """Gradients near the ends of f16's range keep their digits: a power of two brings dloss into the range and back."""
+    g = gen(9)
+    x, table, ids, _ = rows_for(g, 96, 600, 72, HF, 0.0)
+    desc, unit = B.make_vocab_desc(600, 72, CODE[HF]), torch.rand(96, generator=g, device="cuda") + 0.5
+    _, lse = B.snn_cross_entropy_forward(desc, x, table, ids)
+    for factor in (2.0 ** 12, 2.0 ** -6):
+        dloss = unit * factor
+        want = Loss(x, table, ids, None, 1.0, dloss)
+        dx, dw = B.snn_cross_entropy_backward(desc, x, table, ids, lse, dloss)
+        within(dx, want.dx, want.dx_error, "dx")
+        within(dw, want.dw, want.dw_error, "dtable")
+    # a power of two times everything gives the same bits times it
+    a = B.snn_cross_entropy_backward(desc, x, table, ids, lse, unit, dtable=False)[0]
+    b = B.snn_cross_entropy_backward(desc, x, table, ids, lse, unit * 64, dtable=False)[0]
+    normal_ones = a.abs() >= 2.0 ** -14
+    assert torch.equal((a.float() * 64)[normal_ones], b.float()[normal_ones])
+
+
+def test_small_losses_keep_their_digits():
+    """A row whose target is nearly sure: the loss, log(1 + the others' share), is far below a step of the logits."""
+    V, C = 4000, 64
+    table = torch.zeros(V, C, dtype=BF, device="cuda")
+    table[:, 0], table[7, 0] = -1.0, 1.0
+    x = torch.zeros(3, C, dtype=BF, device="cuda")
+    x[:, 0] = torch.tensor([8.0, 10.0, 12.0], device="cuda")
+    ids = torch.full((3,), 7, dtype=torch.int32, device="cuda")
+    loss, _ = B.snn_cross_entropy_forward(B.make_vocab_desc(V, C), x, table, ids)
+    want = torch.log1p((V - 1) * torch.exp(-2 * x[:, 0].double()))
+    # (1 + s in 32 bits: half a step of 1 .. 2; s itself to 2^-20)
+    within(loss, want, 2.0 ** -23 + 2.0 ** -20 * want, "loss")
+
+
+@pytest.mark.parametrize("k", [0, 3])
+def test_gradients_against_differences(k):
+    """Central differences of the losses' sum along a direction of +-1: off by at most h^2 / 6 of a third derivative, which is a third cumulant of
+    values a within the direction's reach, at most their width cubed; and by the losses' own errors over 2 h."""
+    g, rows, V, C, h = gen(4), 6, 50, 32, 2.0 ** -5
+    table = (normal(g, V, C) * 0.2).to(HF)
+    x = (torch.round(normal(g, rows, C) * 64) / 64).clamp(-8, 8).to(HF)               # (x +- h is a value of the type)
+    u = torch.where(torch.rand(rows, C, generator=g, device="cuda") < 0.5, -1.0, 1.0)
+    desc = B.make_vocab_desc(V, C, CODE[HF])
+    ids = torch.randint(0, V, (rows, max(k, 1)), generator=g, device="cuda").int()
+    logits = normal(g, rows, k) if k else None
+    tau = 2.0 if k else 1.0
+
+    def loss(x):
+        return B.snn_distill_forward(desc, x, table, ids, logits, tau)[:2] if k else B.snn_cross_entropy_forward(desc, x, table, ids.view(-1))
+    ones = torch.ones(rows, device="cuda")
+    base = loss(x)
+    dx = B.snn_distill_backward(desc, x, table, ids, logits, tau, base[1], ones)[0] if k else \
+        B.snn_cross_entropy_backward(desc, x, table, ids.view(-1), base[1], ones)[0]
+    plus, minus = (x + h * u).to(HF), (x - h * u).to(HF)
+    assert torch.equal(plus.float() - minus.float(), 2 * h * u)
+    slope = (loss(plus)[0].double() - loss(minus)[0].double()) / (2 * h)
+    reach = (u.double() @ table.double().t()) / tau
+    width = reach.amax(1) - reach.amin(1)
+    want = Loss(x, table, ids, logits, tau, ones)
+    error = h * h / 6 * width ** 3 + want.loss_error / h * 1.5 + want.dx_error.sum(1)
+    within((dx.double() * u.double()).sum(1), slope, error, "slope")
+    # and along the table's rows
+    base_dw = (B.snn_distill_backward(desc, x, table, ids, logits, tau, base[1], ones) if k else
+               B.snn_cross_entropy_backward(desc, x, table, ids.view(-1), base[1], ones))[1]
+    table = (torch.round(table.float() * 64) / 64).to(HF)
+    base = loss(x)
+    dw = (B.snn_distill_backward(desc, x, table, ids, logits, tau, base[1], ones) if k else
+          B.snn_cross_entropy_backward(desc, x, table, ids.view(-1), base[1], ones))[1]
+    assert base_dw.shape == dw.shape
+    want = Loss(x, table, ids, logits, tau, ones)
+    kept = table
+    r = torch.where(torch.rand(V, C, generator=g, device="cuda") < 0.5, -1.0, 1.0)
+    table = (kept.float() + h * r).to(HF)
+    up = loss(x)[0].double().sum()
+    table = (kept.float() - h * r).to(HF)
+    down = loss(x)[0].double().sum()
+    reach = (x.double() @ r.double().t()) / tau
+    width = reach.amax(1) - reach.amin(1)
+    error = (h * h / 6 * width ** 3).sum() + want.loss_error.sum() / h * 1.5 + want.dw_error.sum()
+    assert abs(float((dw.double() * r.double()).sum() - (up - down) / (2 * h))) <= float(error)
+
+
+def test_repeated_calls_give_the_same_bits():
+    g = gen(6)
+    x, table, ids, _ = rows_for(g, 400, 3000, 264, BF, 0.2)
+    desc, dloss = B.make_vocab_desc(3000, 264), torch.rand(400, generator=g, device="cuda")
+    first = None
+    for _ in range(3):
+        loss, lse = B.snn_cross_entropy_forward(desc, x, table, ids)
+        out = loss, lse, *B.snn_cross_entropy_backward(desc, x, table, ids, lse, dloss)
+        first = first or out
+        assert all(torch.equal(a, b) for a, b in zip(first, out))
+
+
+def test_on_another_stream_and_in_a_graph():
+    """Rows of tokens, their loss, and the gradients of one table at both ends, captured and replayed on changing inputs."""
+    g, rows, V, C = gen(7), 300, 2000, 136
+    desc = B.make_vocab_desc(V, C)
+    table = normal(g, V, C).to(BF)
+    ids, target = (torch.randint(-1, V, (rows,), generator=g, device="cuda").int() for _ in range(2))
+    k_ids, logits = torch.randint(0, V, (rows, 6), generator=g, device="cuda").int(), normal(g, rows, 6)
+    dloss = torch.rand(rows, generator=g, device="cuda")
+
+    def step():
+        x = B.snn_embedding_forward(desc, table, ids, 0.5)
+        loss, lse = B.snn_cross_entropy_forward(desc, x, table, target)
+        dx, dw = B.snn_cross_entropy_backward(desc, x, table, target, lse, dloss)
+        far, lse2, picked = B.snn_distill_forward(desc, x, table, k_ids, logits, 2.0)
+        dx2, dw = B.snn_distill_backward(desc, x, table, k_ids, logits, 2.0, lse2, dloss, dtable=dw, accumulate=True)
+        B.snn_embedding_grad(desc, dx + dx2, ids, 0.5, dtable=dw, accumulate=True)
+        return loss, far, picked, dw
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        there = step()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(there, step()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept = step()
+    for n in range(4):
+        ids.copy_(torch.randint(-1, V, (rows,), generator=g, device="cuda"))
+        target.copy_(torch.randint(-1, V, (rows,), generator=g, device="cuda"))
+        logits.copy_(normal(g, rows, 6))
+        graph.replay()
+        got = [t.clone() for t in kept]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, step())), n
+
+
+def test_offsets_past_32_bits():
+    """A table of more than 4 GiB, tokens at its far end."""
+    V, C = 70000, 32776
+    g, desc = gen(2), B.make_vocab_desc(70000, 32776)
+    table = torch.zeros(V, C, dtype=BF, device="cuda")
+    far = torch.tensor([V - 1, 65535, 65536, V - 7], device="cuda")
+    table[far] = normal(g, 4, C).to(BF) * 2.0 ** -7
+    y = B.snn_embedding_forward(desc, table, far.int(), 2.0)
+    assert torch.equal(y, table[far] * 2)
+    x, target = y[[0, 3]].contiguous(), far[[0, 3]].int()
+    loss, lse = B.snn_cross_entropy_forward(desc, x, table, target)
+    z = x.double() @ table[far].double().t()
+    want = torch.logsumexp(torch.cat([z, torch.zeros(2, 1, device="cuda").expand(2, V - 4).double()], 1), 1)
+    magnitude = (x.double().abs() @ table[far].double().abs().t()).amax(1)
+    error = C * F32 * magnitude + (512 + V / 128) * F32 + 2.0 ** -20 * (1 + want.abs())
+    within(lse, want, error, "lse")
+    within(loss, want - z[[0, 1], [0, 3]], 2 * error, "loss")
+    dw = B.snn_embedding_grad(desc, y, far.int(), 1.0, dtable=table)
+    assert torch.equal(dw[far], y) and int((dw != 0).any(1).sum()) == 4

@@ -1,0 +1,98 @@
+"""What the calls on the ends of a network over tokens refuse (CPU only: every call is refused before any device work)."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2110_09195_amd import binding as B
+
+BAD, WS = B.SNN_ERR_INVALID_ARG, B.SNN_ERR_WORKSPACE
+P = 1 << 20            # an address that no refused call looks at
+BIG = 1 << 50
+
+
+def desc(**kw):
+    d = B.make_vocab_desc(1000, 64, B.SNN_DTYPE_BF16)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return ctypes.byref(d)
+
+
+HEAD = dict(desc=desc(), x=P, ldx=64, rows=8, table=P, ldt=64)
+TEACHER = dict(ids=P, logits=P, k=4, temperature=2.0)
+TAIL = dict(lse=P, dloss=P, dx=P, lddx=64, dtable=P, accumulate=0, ws=P, wsb=BIG, stream=None)
+CALLS = {
+    "snn_embedding_forward": dict(desc=desc(), table=P, ldt=64, ids=P, rows=8, scale=1.0, y=P, ldy=64, stream=None),
+    "snn_embedding_grad": dict(desc=desc(), dy=P, lddy=64, ids=P, rows=8, scale=1.0, dtable=P, accumulate=0, ws=P, wsb=BIG, stream=None),
+    "snn_cross_entropy_forward": dict(HEAD, target=P, loss=P, lse=P, ws=P, wsb=BIG, stream=None),
+    "snn_cross_entropy_backward": dict(HEAD, target=P, **TAIL),
+    "snn_distill_forward": dict(HEAD, **TEACHER, loss=P, lse=P, picked=P, ws=P, wsb=BIG, stream=None),
+    "snn_distill_backward": dict(HEAD, **TEACHER, **TAIL),
+}
+
+
+def call(name, **change):
+    return getattr(B.lib(), name)(*dict(CALLS[name], **change).values())
+
+
+@pytest.mark.parametrize("name", sorted(CALLS))
+def test_descriptors(name):
+    assert call(name, desc=None) == BAD
+    for bad in (dict(V=0), dict(V=-1), dict(V=(1 << 24) + 1), dict(C=0), dict(C=60), dict(C=65544), dict(dtype=2), dict(dtype=-1)):
+        assert call(name, desc=desc(**bad)) == BAD, bad
+
+
+@pytest.mark.parametrize("name", sorted(CALLS))
+def test_pointers_distances_and_counts(name):
+    args = CALLS[name]
+    wanted = {"dx", "dtable"} if name.endswith("backward") else set()         # (either may be missing)
+    for key in args:
+        if key in ("x", "table", "ids", "y", "dy", "dx", "dtable", "target", "loss", "lse", "dloss", "picked", "logits") and key not in wanted:
+            assert call(name, **{key: None}) == BAD, key
+        if key in ("x", "table", "y", "dy", "dx", "dtable"):
+            assert call(name, **{key: P + 8}) == BAD, key
+        if key in ("ids", "target", "loss", "lse", "dloss", "picked", "logits"):
+            assert call(name, **{key: P + 2}) == BAD, key
+        if key.startswith("ld"):
+            for v in (56, 68, (1 << 20) + 8, -64, 0):
+                assert call(name, **{key: v}) == BAD, (key, v)
+        if key == "rows":
+            assert call(name, rows=-1) == BAD and call(name, rows=1 << 28) == BAD
+    if wanted:
+        assert call(name, dx=None, dtable=None) == BAD
+
+
+@pytest.mark.parametrize("name", [n for n in sorted(CALLS) if "ws" in CALLS[n]])
+def test_workspaces(name):
+    for change in (dict(ws=None), dict(ws=P + 128), dict(wsb=64), dict(wsb=0)):
+        assert call(name, **change) == WS, change
+
+
+@pytest.mark.parametrize("name", ["snn_distill_forward", "snn_distill_backward"])
+def test_teachers(name):
+    for bad in (dict(k=0), dict(k=257), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("nan")), dict(temperature=float("inf")),
+                dict(temperature=2000.0), dict(temperature=2.0 ** -11)):
+        assert call(name, **bad) == BAD, bad
+
+
+def test_sizes_of_workspaces():
+    L = B.lib()
+    assert L.snn_embedding_grad_workspace_bytes(desc(V=0), 8) == 0 and L.snn_embedding_grad_workspace_bytes(desc(), -1) == 0
+    assert L.snn_embedding_grad_workspace_bytes(desc(), 0) > 0
+    for bad in ((desc(C=60), 8, 1, 0), (desc(), -1, 1, 0), (desc(), 8, 0, 0), (desc(), 8, 257, 1), (desc(), 8, 1, 2), (None, 8, 1, 0)):
+        assert L.snn_loss_workspace_bytes(*bad) == 0, bad
+    # no logits of the whole vocabulary, however many rows
+    rows, V = 65536, 1 << 18
+    assert L.snn_loss_workspace_bytes(desc(V=V), rows, 1, 0) < rows * V // 8
+    assert L.snn_loss_workspace_bytes(desc(V=V), rows, 1, 1) < (1 << 30)
+
+
+def test_binding_checks_its_tensors():
+    d = B.make_vocab_desc(10, 64)
+    x, ids, f = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32), torch.zeros(4)
+    table = torch.zeros(10, 64, dtype=torch.bfloat16)
+    for call in (lambda: B.snn_embedding_forward(d, table, ids), lambda: B.snn_embedding_grad(d, x, ids), lambda: B.snn_cross_entropy_forward(d, x, table, ids),
+                 lambda: B.snn_cross_entropy_backward(d, x, table, ids, f, f), lambda: B.snn_distill_forward(d, x, table, ids, f),
+                 lambda: B.snn_distill_backward(d, x, table, ids, f, 1.0, f, f)):
+        with pytest.raises(TypeError):
+            call()
