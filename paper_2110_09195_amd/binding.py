@@ -121,6 +121,9 @@ def _use(L):
     linear = ("snn_linear_forward", "snn_linear_input_grad", "snn_checkpoint_store", "snn_checkpoint_restore", "snn_adapters_workspace_bytes",
               "snn_adapters_forward")
     _marshal.use_linear(snn_linear_desc, tuple(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in linear))
+    vocab = ("snn_embedding_forward", "snn_embedding_grad_workspace_bytes", "snn_embedding_grad", "snn_loss_workspace_bytes",
+             "snn_cross_entropy_forward", "snn_cross_entropy_backward", "snn_distill_forward", "snn_distill_backward")
+    _marshal.use_vocab(snn_vocab_desc, tuple(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in vocab))
     _lib, _fast = L, _marshal
 
 
@@ -1098,6 +1101,8 @@ def _teacher(ids, logits, rows):
 
 def snn_embedding_forward(desc, table, ids, scale=1.0, y=None):
     """Rows ids (int32 [rows], outside 0 .. V - 1: zeros) of table [V][C] times scale -> y [rows][C]."""
+    if _fast and (r := _fast.embedding_forward(desc, table, ids, scale, y)) is not False:
+        return r
     _here(table, ids, y)
     pt, ldt = _table(desc, table)
     _dev(ids, torch.int32, "ids")
@@ -1112,6 +1117,8 @@ def snn_embedding_grad_workspace_bytes(desc, rows):
 
 def snn_embedding_grad(desc, dy, ids, scale=1.0, dtable=None, accumulate=False, workspace=None):
     """dy [rows][C] summed by ids (int32 [rows]) times scale -> dtable [V][C], overwritten or (accumulate) added to."""
+    if _fast and (r := _fast.embedding_grad(desc, dy, ids, scale, dtable, accumulate, workspace)) is not False:
+        return r
     _here(dy, ids, dtable, workspace)
     rows = dy.shape[0]
     pdy, lddy = _rows(dy, _dtype_of(desc), desc.C, "dy")
@@ -1132,6 +1139,8 @@ def snn_loss_workspace_bytes(desc, rows, k=1, call=SNN_LOSS_FORWARD):
 
 def snn_cross_entropy_forward(desc, x, table, target, loss=None, lse=None, workspace=None):
     """x [rows][C] against target (int32 [rows], outside 0 .. V - 1: none) with the logits x table^T -> loss, lse, float32 [rows]."""
+    if _fast and (r := _fast.cross_entropy_forward(desc, x, table, target, loss, lse, workspace)) is not False:
+        return r
     _here(x, table, target, loss, lse, workspace)
     rows = x.shape[0]
     px, ldx = _rows(x, _dtype_of(desc), desc.C, "x")
@@ -1157,6 +1166,8 @@ def _loss_grads(desc, x, dx, dtable, accumulate):
 def snn_cross_entropy_backward(desc, x, table, target, lse, dloss, dx=None, dtable=None, accumulate=False, workspace=None):
     """lse as the forward call returned it, dloss float32 [rows] -> dx [rows][C], dtable [V][C] (overwritten, or with accumulate added to).
     dx=False or dtable=False: not wanted, None is returned."""
+    if _fast and (r := _fast.cross_entropy_backward(desc, x, table, target, lse, dloss, dx, dtable, accumulate, workspace)) is not False:
+        return r
     _here(x, table, target, lse, dloss, dx, dtable, workspace)
     rows = x.shape[0]
     px, ldx = _rows(x, _dtype_of(desc), desc.C, "x")
@@ -1172,6 +1183,8 @@ def snn_cross_entropy_backward(desc, x, table, target, lse, dloss, dx=None, dtab
 def snn_distill_forward(desc, x, table, ids, logits, temperature=1.0, loss=None, lse=None, picked=None, workspace=None):
     """x [rows][C] against a teacher's logits (float32 [rows][k]) of the tokens ids (int32 [rows][k], outside 0 .. V - 1: not listed)
     -> loss, lse, float32 [rows], and picked, float32 [rows][k]: the rows' own logits of these tokens."""
+    if _fast and (r := _fast.distill_forward(desc, x, table, ids, logits, temperature, loss, lse, picked, workspace)) is not False:
+        return r
     _here(x, table, ids, logits, loss, lse, picked, workspace)
     rows = x.shape[0]
     px, ldx = _rows(x, _dtype_of(desc), desc.C, "x")
@@ -1187,6 +1200,8 @@ def snn_distill_forward(desc, x, table, ids, logits, temperature=1.0, loss=None,
 
 def snn_distill_backward(desc, x, table, ids, logits, temperature, lse, dloss, dx=None, dtable=None, accumulate=False, workspace=None):
     """As snn_cross_entropy_backward, for snn_distill_forward's loss."""
+    if _fast and (r := _fast.distill_backward(desc, x, table, ids, logits, temperature, lse, dloss, dx, dtable, accumulate, workspace)) is not False:
+        return r
     _here(x, table, ids, logits, lse, dloss, dx, dtable, workspace)
     rows = x.shape[0]
     px, ldx = _rows(x, _dtype_of(desc), desc.C, "x")

@@ -57,34 +57,74 @@ void embedding_kernel(const T *__restrict__ table, int64_t ldt, const int32_t *_
 // The rows by token, rows of one token in their own order, so that sums have a fixed order.  Tokens are compared as unsigned numbers: those
 // of no row of the table come last.
 
-// Up to RANKED rows in one launch: a row's place is the number of tokens below its own, and of its own in earlier rows.  64 rows a workgroup,
-// whose waves share out the tokens that they are compared with; these come by scalar loads, two VALU instructions a comparison.
-constexpr int64_t RANKED = 16384;
-constexpr int RANK_WAVES = 16;
+// Up to MERGED rows: blocks of RANK_BLOCK rows are sorted by themselves - a row's place is the number of the block's tokens below its own, and of
+// its own in earlier rows; 64 rows a workgroup, whose waves share out the tokens that they are compared with, by scalar loads - and a row's
+// place among all is its place there and those that a binary search finds for it in the other blocks.
+constexpr int64_t MERGED = 65536;
+constexpr int RANK_BLOCK = 2048, RANK_WAVES = 16;
 
 __global__ __launch_bounds__(64 * RANK_WAVES)
 void embedding_rank_kernel(const uint32_t *__restrict__ ids, int rows, uint32_t *__restrict__ sorted, int *__restrict__ order)
 {
     __shared__ int counts[RANK_WAVES][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int i0 = blockIdx.x * 64, i = i0 + lane;
+    const int i0 = blockIdx.x * 64, i = i0 + lane, first = i0 / RANK_BLOCK * RANK_BLOCK, last = min(first + RANK_BLOCK, rows);
     const uint32_t mine = i < rows ? ids[i] : 0;
-    const int share = ((rows + RANK_WAVES - 1) / RANK_WAVES + 15) & ~15, lo = min(wave * share, rows), hi = min(lo + share, rows);
-    int below = 0, j = lo;
-    for (; j < min(i0, hi); ++j) below += ids[j] <= mine ? 1 : 0;
-    for (; j < min(i0 + 64, hi); ++j) {
-        const uint32_t other = ids[j];
-        below += other < mine || (other == mine && j < i) ? 1 : 0;
+    constexpr int SHARE = RANK_BLOCK / RANK_WAVES;             // a multiple of 64: a wave's tokens are all before, all behind or among the workgroup's
+    const int lo = first + wave * SHARE, hi = min(lo + SHARE, last);
+    int below = 0;
+    if (hi - lo == SHARE && hi <= i0) {
+#pragma unroll 32
+        for (int j = 0; j < SHARE; ++j) below += ids[lo + j] <= mine ? 1 : 0;
+    } else if (hi - lo == SHARE && lo >= i0 + 64) {
+#pragma unroll 32
+        for (int j = 0; j < SHARE; ++j) below += ids[lo + j] < mine ? 1 : 0;
+    } else {
+#pragma unroll 8
+        for (int j = lo; j < hi; ++j) {
+            const uint32_t other = ids[j];
+            below += other < mine || (other == mine && j < i) ? 1 : 0;
+        }
     }
-    for (; j < hi; ++j) below += ids[j] < mine ? 1 : 0;
     counts[wave][lane] = below;
     __syncthreads();
     if (wave == 0 && i < rows) {
-        int place = 0;
+        int place = first;
 #pragma unroll
         for (int w = 0; w < RANK_WAVES; ++w) place += counts[w][lane];
         sorted[place] = mine;
         order[place] = i;
+    }
+}
+
+__global__ __launch_bounds__(64 * RANK_WAVES)
+void embedding_merge_kernel(const uint32_t *__restrict__ keys, const int *__restrict__ rows_of, int rows, uint32_t *__restrict__ sorted,
+                            int *__restrict__ order)
+{
+    __shared__ int counts[RANK_WAVES][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i0 = blockIdx.x * 64, i = i0 + lane, own = i0 / RANK_BLOCK, blocks = (rows + RANK_BLOCK - 1) / RANK_BLOCK;
+    const uint32_t mine = i < rows ? keys[i] : 0;
+    int below = 0;
+    for (int b = wave; b < blocks; b += RANK_WAVES) {
+        if (b == own) continue;
+        const uint32_t *const at = keys + b * RANK_BLOCK;
+        const int n = min(RANK_BLOCK, rows - b * RANK_BLOCK);
+        int found = 0;                                         // tokens below, and in earlier blocks the row's own
+        for (int step = RANK_BLOCK; step; step >>= 1) {
+            const uint32_t other = found + step <= n ? at[found + step - 1] : ~0u;
+            if (found + step <= n && (other < mine || (other == mine && b < own))) found += step;
+        }
+        below += found;
+    }
+    counts[wave][lane] = below;
+    __syncthreads();
+    if (wave == 0 && i < rows) {
+        int place = i - own * RANK_BLOCK;
+#pragma unroll
+        for (int w = 0; w < RANK_WAVES; ++w) place += counts[w][lane];
+        sorted[place] = mine;
+        order[place] = rows_of[i];
     }
 }
 
@@ -323,11 +363,12 @@ void embedding_join_kernel(SumArgs p)
     const uint32_t token = p.sorted[next - 1];
     if (token >= (uint32_t)p.V || p.sorted[next] != token) return;             // no token goes on,
     if (block * BLOCK > 0 && p.sorted[block * BLOCK] == token && p.sorted[block * BLOCK - 1] == token) return;          // or none that begins here
-    int64_t lo = block + 1, hi = p.blocks - 1;                 // the last block that begins with it
-    while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) >> 1;
-        if (p.sorted[mid * BLOCK] == token) lo = mid;
-        else hi = mid - 1;
+    int64_t lo = block + 1, hi = p.blocks;                     // the last block that begins with it: 64 at once
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const int64_t last = lo + step * (__popcll(__ballot(at < hi && p.sorted[min(at, hi - 1) * BLOCK] == token)) - 1);
+        hi = min(hi, last + step);
+        lo = last;
     }
     const int64_t n = lo - block + 1, share = (n + JOIN_WAVES - 1) / JOIN_WAVES;
     const int c = (int)(blockIdx.x - block * p.slabs) * 512 + lane * 8;
@@ -356,19 +397,20 @@ void embedding_join_kernel(SumArgs p)
 
 struct SortPlan {
     int passes, blocks;
-    size_t keys, counts, part, bytes; // where they lie in the workspace (keys and order twice where there are passes)
+    bool twice;                       // sorted in more than one launch: keys and order twice in the workspace
+    size_t counts, part, bytes;       // where these lie there
 };
 
 SortPlan sort_plan(const Vocab &v, int64_t rows)
 {
     SortPlan p = {};
-    if (rows > RANKED) {
+    p.twice = rows > RANK_BLOCK;
+    if (rows > MERGED) {
         while (((int64_t)1 << (8 * p.passes)) <= v.V) ++p.passes;              // (V itself stands for what is no token)
         p.blocks = (int)((rows + SORT_ROWS - 1) / SORT_ROWS);
     }
     const size_t one = align_up((size_t)rows * 4, 256);
-    p.keys = 0;
-    p.counts = one * (p.passes ? 4 : 2);
+    p.counts = one * (p.twice ? 4 : 2);
     p.part = p.counts + (p.passes ? align_up((size_t)p.blocks * DIGITS * 4, 256) : 0);
     p.bytes = p.part + align_up((size_t)((rows + BLOCK - 1) / BLOCK) * 2 * v.C * 4, 256);
     return p;
@@ -416,7 +458,9 @@ int launch_embedding_grad(const Vocab &v, const Rows16 &dy, const int32_t *ids, 
     uint32_t *sorted = (uint32_t *)ws, *other = (uint32_t *)((char *)ws + 2 * one);
     int *order = (int *)((char *)ws + one), *other_order = (int *)((char *)ws + 3 * one);
     if (rows > 0 && !plan.passes) {
-        embedding_rank_kernel<<<dim3((unsigned)((rows + 63) / 64)), 64 * RANK_WAVES, 0, s>>>((const uint32_t *)ids, (int)rows, sorted, order);
+        const dim3 grid((unsigned)((rows + 63) / 64));
+        embedding_rank_kernel<<<grid, 64 * RANK_WAVES, 0, s>>>((const uint32_t *)ids, (int)rows, plan.twice ? other : sorted, plan.twice ? other_order : order);
+        if (plan.twice) embedding_merge_kernel<<<grid, 64 * RANK_WAVES, 0, s>>>(other, other_order, (int)rows, sorted, order);
         const int rc = check_launch();
         if (rc != SNN_OK) return rc;
     }

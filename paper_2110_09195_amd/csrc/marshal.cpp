@@ -42,7 +42,18 @@ struct LinearLibrary {
     decltype(&snn_adapters_forward) adapters_forward;
 };
 LinearLibrary linear;
-PyTypeObject *desc_type = nullptr, *linear_desc_type = nullptr;
+struct VocabLibrary {
+    decltype(&snn_embedding_forward) embedding_forward;
+    decltype(&snn_embedding_grad_workspace_bytes) embedding_grad_workspace_bytes;
+    decltype(&snn_embedding_grad) embedding_grad;
+    decltype(&snn_loss_workspace_bytes) loss_workspace_bytes;
+    decltype(&snn_cross_entropy_forward) cross_entropy_forward;
+    decltype(&snn_cross_entropy_backward) cross_entropy_backward;
+    decltype(&snn_distill_forward) distill_forward;
+    decltype(&snn_distill_backward) distill_backward;
+};
+VocabLibrary vocab;
+PyTypeObject *desc_type = nullptr, *linear_desc_type = nullptr, *vocab_desc_type = nullptr;
 PyObject *error_type = nullptr;              // called with the status and the function's name
 
 // Plain tensors only: subclasses have their own say in Python.
@@ -389,6 +400,223 @@ PyObject *adapters_forward(PyObject *const *a)
     }), std::move(y), std::move(low));
 }
 
+// ---- the ends of a network over tokens: tensors on the current device ----
+
+// What the calls on a vocabulary have in common; `ok` as long as every argument was of the ordinary kind.
+struct VocabCall {
+    snn_vocab_desc d;
+    at::ScalarType type;
+    int64_t device;
+    bool ok;
+
+    explicit VocabCall(PyObject *o) : d{}, type(at::kHalf), device(c10::hip::current_device()), ok(false)
+    {
+        if (Py_TYPE(o) != vocab_desc_type) return;
+        Py_buffer view;
+        if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) {
+            PyErr_Clear();
+            return;
+        }
+        if (view.len == (Py_ssize_t)sizeof d) {
+            std::memcpy(&d, view.buf, sizeof d);
+            ok = d.dtype == SNN_DTYPE_BF16 || d.dtype == SNN_DTYPE_F16;
+            if (ok) type = type_of(d.dtype);
+        }
+        PyBuffer_Release(&view);
+    }
+    const at::Tensor *here(const at::Tensor *t)
+    {
+        if (!t || t->get_device() != device) {
+            ok = false;
+            return nullptr;
+        }
+        return t;
+    }
+    const at::Tensor *rows(PyObject *o) { return ok ? here(rows_of(o, type, d.C)) : nullptr; }
+    const at::Tensor *table(PyObject *o)
+    {
+        const at::Tensor *const t = rows(o);
+        if (t && t->size(0) != d.V) ok = false;
+        return t;
+    }
+    // contiguous values, n of them
+    const at::Tensor *values(PyObject *o, at::ScalarType kind, int64_t n)
+    {
+        const at::Tensor *const t = ok ? here(checked(o, kind)) : nullptr;
+        if (t && n >= 0 && t->numel() != n) ok = false;
+        return t;
+    }
+    // what the caller gave, or new
+    at::Tensor out_rows(PyObject *o, const at::Tensor &like, int64_t n)
+    {
+        at::Tensor t = ok ? rows_out(o, like, n, d.C) : at::Tensor();
+        if (!t.defined() || t.get_device() != device) ok = false;
+        return t;
+    }
+    at::Tensor out(PyObject *o, at::IntArrayRef sizes, at::ScalarType kind, const at::Tensor &like)
+    {
+        at::Tensor t = ok ? whole_out(o, sizes, like.options().dtype(kind).requires_grad(false)) : at::Tensor();
+        if (!t.defined() || t.get_device() != device) ok = false;
+        return t;
+    }
+    at::Tensor workspace(PyObject *o, size_t need, const at::Tensor &like)
+    {
+        if (!ok || !need) ok = false;
+        else if (o == Py_None) return at::empty({(int64_t)need}, like.options().dtype(at::kByte).requires_grad(false));
+        else if (const at::Tensor *const t = here(checked(o, at::kByte)))
+            if ((size_t)t->numel() >= need) return *t;
+        ok = false;
+        return at::Tensor();
+    }
+    // the table's gradient: given (to be added to, perhaps), new, or (False) not wanted
+    at::Tensor dtable(PyObject *o, PyObject *accumulate, const at::Tensor &like, bool &add)
+    {
+        add = accumulate == Py_True;
+        if ((!add && accumulate != Py_False) || (add && o == Py_None)) ok = false;
+        if (!ok || o == Py_False) return at::Tensor();
+        return out(o, {d.V, d.C}, type, like);
+    }
+};
+
+template <class T>
+T *pointer(const at::Tensor &t) { return t.defined() ? (T *)t.data_ptr() : nullptr; }
+
+bool number(PyObject *o, float &v)
+{
+    const double x = PyFloat_CheckExact(o) ? PyFloat_AS_DOUBLE(o) : PyLong_CheckExact(o) ? PyLong_AsDouble(o) : 0.0;
+    if (x == -1.0 && PyErr_Occurred()) {
+        PyErr_Clear();
+        return false;
+    }
+    v = (float)x;
+    return PyFloat_CheckExact(o) || PyLong_CheckExact(o);
+}
+
+// desc, table, ids, scale, y or None
+PyObject *embedding_forward(PyObject *const *a)
+{
+    VocabCall c(a[0]);
+    float scale;
+    const at::Tensor *const table = c.table(a[1]), *const ids = c.values(a[2], at::kInt, -1);
+    if (!c.ok || !number(a[3], scale)) Py_RETURN_FALSE;
+    const int64_t rows = ids->numel();
+    at::Tensor y = c.out_rows(a[4], *table, rows);
+    if (!c.ok) Py_RETURN_FALSE;
+    const void *const pt = table->data_ptr();
+    const int32_t *const pi = (const int32_t *)ids->data_ptr();
+    void *const py = y.data_ptr(), *const s = stream();
+    const int64_t ldt = distance(*table), ldy = distance(y);
+    return outputs(enqueued("snn_embedding_forward", [&] { return vocab.embedding_forward(&c.d, pt, ldt, pi, rows, scale, py, ldy, s); }), std::move(y));
+}
+
+// desc, dy, ids, scale, dtable or None, whether to add, workspace or None
+PyObject *embedding_grad(PyObject *const *a)
+{
+    VocabCall c(a[0]);
+    float scale;
+    bool add;
+    const at::Tensor *const dy = c.rows(a[1]);
+    if (!c.ok || !number(a[3], scale) || a[4] == Py_False) Py_RETURN_FALSE;
+    const int64_t rows = dy->size(0);
+    const at::Tensor *const ids = c.values(a[2], at::kInt, rows);
+    at::Tensor dw = c.dtable(a[4], a[5], *dy, add);
+    const at::Tensor ws = c.workspace(a[6], vocab.embedding_grad_workspace_bytes(&c.d, rows), *dy);
+    if (!c.ok) Py_RETURN_FALSE;
+    const void *const pd = dy->data_ptr();
+    const int32_t *const pi = (const int32_t *)ids->data_ptr();
+    void *const pw = dw.data_ptr(), *const pws = ws.data_ptr(), *const s = stream();
+    const int64_t ld = distance(*dy);
+    const size_t bytes = (size_t)ws.numel();
+    return outputs(enqueued("snn_embedding_grad", [&] { return vocab.embedding_grad(&c.d, pd, ld, pi, rows, scale, pw, add, pws, bytes, s); }), std::move(dw));
+}
+
+// A loss: desc, x, table; target, or (TEACHER) ids, logits, temperature; then loss, lse, (TEACHER) picked and workspace, each or None
+template <bool TEACHER>
+PyObject *loss_forward(PyObject *const *a)
+{
+    VocabCall c(a[0]);
+    const at::Tensor *const x = c.rows(a[1]), *const table = c.table(a[2]);
+    if (!c.ok) Py_RETURN_FALSE;
+    const int64_t rows = x->size(0);
+    const at::Tensor *const ids = c.values(a[3], at::kInt, TEACHER ? -1 : rows), *const logits = TEACHER ? c.values(a[4], at::kFloat, -1) : nullptr;
+    float temperature = 1.0f;
+    if (!c.ok || (TEACHER && (!number(a[5], temperature) || ids->dim() != 2 || ids->size(0) != rows || logits->sizes() != ids->sizes()))) Py_RETURN_FALSE;
+    const int64_t k = TEACHER ? ids->size(1) : 1;
+    if (k > 256) Py_RETURN_FALSE;
+    PyObject *const *const o = a + (TEACHER ? 6 : 4);
+    at::Tensor loss = c.out(o[0], {rows}, at::kFloat, *x), lse = c.out(o[1], {rows}, at::kFloat, *x), picked;
+    if (TEACHER) picked = c.out(o[2], {rows, k}, at::kFloat, *x);
+    const at::Tensor ws = c.workspace(o[TEACHER ? 3 : 2], vocab.loss_workspace_bytes(&c.d, rows, (int)k, SNN_LOSS_FORWARD), *x);
+    if (!c.ok) Py_RETURN_FALSE;
+    const void *const px = x->data_ptr(), *const pt = table->data_ptr();
+    const int32_t *const pi = (const int32_t *)ids->data_ptr();
+    const float *const pl = TEACHER ? (const float *)logits->data_ptr() : nullptr;
+    float *const out = (float *)loss.data_ptr(), *const sums = (float *)lse.data_ptr(), *const pp = pointer<float>(picked);
+    void *const pws = ws.data_ptr(), *const s = stream();
+    const int64_t ldx = distance(*x), ldt = distance(*table);
+    const size_t bytes = (size_t)ws.numel();
+    PyObject *const ok = enqueued(TEACHER ? "snn_distill_forward" : "snn_cross_entropy_forward", [&] {
+        return TEACHER ? vocab.distill_forward(&c.d, px, ldx, rows, pt, ldt, pi, pl, (int)k, temperature, out, sums, pp, pws, bytes, s)
+                       : vocab.cross_entropy_forward(&c.d, px, ldx, rows, pt, ldt, pi, out, sums, pws, bytes, s);
+    });
+    if (!TEACHER || ok != Py_True) return outputs(ok, std::move(loss), std::move(lse));
+    Py_DECREF(ok);
+    PyObject *const t[3] = {THPVariable_Wrap(std::move(loss)), THPVariable_Wrap(std::move(lse)), THPVariable_Wrap(std::move(picked))};
+    PyObject *const all = t[0] && t[1] && t[2] ? PyTuple_Pack(3, t[0], t[1], t[2]) : nullptr;
+    for (PyObject *const p : t) Py_XDECREF(p);
+    return all;
+}
+
+// desc, x, table; target, or ids, logits, temperature; lse, dloss; dx and dtable, each or None or False; whether to add; workspace or None
+template <bool TEACHER>
+PyObject *loss_backward(PyObject *const *a)
+{
+    VocabCall c(a[0]);
+    const at::Tensor *const x = c.rows(a[1]), *const table = c.table(a[2]);
+    if (!c.ok) Py_RETURN_FALSE;
+    const int64_t rows = x->size(0);
+    const at::Tensor *const ids = c.values(a[3], at::kInt, TEACHER ? -1 : rows), *const logits = TEACHER ? c.values(a[4], at::kFloat, -1) : nullptr;
+    float temperature = 1.0f;
+    if (!c.ok || (TEACHER && (!number(a[5], temperature) || ids->dim() != 2 || ids->size(0) != rows || logits->sizes() != ids->sizes()))) Py_RETURN_FALSE;
+    const int64_t k = TEACHER ? ids->size(1) : 1;
+    if (k > 256) Py_RETURN_FALSE;
+    PyObject *const *const o = a + (TEACHER ? 6 : 4);
+    const at::Tensor *const lse = c.values(o[0], at::kFloat, rows), *const dloss = c.values(o[1], at::kFloat, rows);
+    bool add;
+    at::Tensor dx;
+    if (o[2] != Py_False) dx = c.out_rows(o[2], *x, rows);
+    at::Tensor dw = c.dtable(o[3], o[4], *x, add);
+    const at::Tensor ws = c.workspace(o[5], vocab.loss_workspace_bytes(&c.d, rows, (int)k, SNN_LOSS_BACKWARD), *x);
+    if (!c.ok) Py_RETURN_FALSE;
+    const void *const px = x->data_ptr(), *const pt = table->data_ptr();
+    const int32_t *const pi = (const int32_t *)ids->data_ptr();
+    const float *const pl = TEACHER ? (const float *)logits->data_ptr() : nullptr;
+    const float *const sums = (const float *)lse->data_ptr(), *const pg = (const float *)dloss->data_ptr();
+    void *const pdx = pointer<void>(dx), *const pdw = pointer<void>(dw), *const pws = ws.data_ptr(), *const s = stream();
+    const int64_t ldx = distance(*x), ldt = distance(*table), lddx = dx.defined() ? distance(dx) : c.d.C;
+    const size_t bytes = (size_t)ws.numel();
+    PyObject *const ok = enqueued(TEACHER ? "snn_distill_backward" : "snn_cross_entropy_backward", [&] {
+        return TEACHER ? vocab.distill_backward(&c.d, px, ldx, rows, pt, ldt, pi, pl, (int)k, temperature, sums, pg, pdx, lddx, pdw, add, pws, bytes, s)
+                       : vocab.cross_entropy_backward(&c.d, px, ldx, rows, pt, ldt, pi, sums, pg, pdx, lddx, pdw, add, pws, bytes, s);
+    });
+    // (a tensor that is not defined becomes None)
+    return outputs(ok, std::move(dx), std::move(dw));
+}
+
+// use_vocab(descriptor type, addresses of the library's functions in the order of VocabLibrary); after use
+PyObject *use_vocab(PyObject *, PyObject *args)
+{
+    PyObject *type;
+    unsigned long long f[8];
+    if (!PyArg_ParseTuple(args, "O!(KKKKKKKK)", &PyType_Type, &type, f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7)) return nullptr;
+    static_assert(sizeof(VocabLibrary) == sizeof f, "one address each");
+    std::memcpy(&vocab, f, sizeof f);
+    Py_INCREF(type);
+    Py_XDECREF(vocab_desc_type);
+    vocab_desc_type = (PyTypeObject *)type;
+    Py_RETURN_NONE;
+}
+
 // use_linear(descriptor type, addresses of the library's functions in the order of LinearLibrary); after use
 PyObject *use_linear(PyObject *, PyObject *args)
 {
@@ -438,6 +666,13 @@ PyMethodDef methods[] = {
     SNN_FAST(checkpoint_store, 3),
     SNN_FAST(checkpoint_restore, 4),
     SNN_FAST(adapters_forward, 10),
+    {"use_vocab", use_vocab, METH_VARARGS, nullptr},
+    SNN_FAST(embedding_forward, 5),
+    SNN_FAST(embedding_grad, 7),
+    {"cross_entropy_forward", (PyCFunction)(void (*)(void))guarded<loss_forward<false>, 7>, METH_FASTCALL, nullptr},
+    {"cross_entropy_backward", (PyCFunction)(void (*)(void))guarded<loss_backward<false>, 10>, METH_FASTCALL, nullptr},
+    {"distill_forward", (PyCFunction)(void (*)(void))guarded<loss_forward<true>, 10>, METH_FASTCALL, nullptr},
+    {"distill_backward", (PyCFunction)(void (*)(void))guarded<loss_backward<true>, 12>, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -5,11 +5,12 @@
 
 namespace snn {
 
-// What a call finds out about its rows on the device: how many count, and the powers of two that bring their gradients into the type's range
-// and back.
+// What a call finds out about its rows on the device: how many count, the powers of two that bring their gradients into the type's range
+// and back, and how many parts the sums of ROWS and TABLE are cut into.
 struct LossHead {
     int count;
     float up, down;
+    int splits_rows, splits_table;
 };
 
 // The four products.  Rows t are those that count, next to each other; tokens v are all (STATS) or a piece of the vocabulary.
@@ -26,44 +27,43 @@ struct TilesArgs {
     const LossHead *head;             // nullptr: as given
     float c;                          // log2(e) / temperature
     int v0;                           // first token of the piece
-    const int32_t *ids;               // token j of row t at t * id_row + j * id_k
-    const float *q;                   // its share, likewise; nullptr: one
-    int64_t id_row, id_k;
+    const int32_t *ids;               // [t][k] listed tokens; with `start` in rising order
+    const float *q;                   // PROBS: their shares, likewise; nullptr: one
     int k;
+    const uint16_t *start;            // [t][start_ld]: how many of a row's list lie below each LIST_BLOCK tokens; nullptr: not known
+    int64_t start_ld;
+    const int32_t *slot;              // STATS, with start: the tokens' places in the caller's list
     float2 *part;                     // STATS: [tile of tokens][part_ld]
     int64_t part_ld;
-    float *picked;                    // [row of the call][k]
-    const int *list;                  // the rows that count; nullptr: all
+    float *picked;                    // STATS: [row of the call][k]
+    const int *list;                  // with start: the rows that count
     const float *lse2, *g;
     void *probs;
     int64_t ldp;
-    float *out;                       // ROWS: [split][N][M]
+    float *out;                       // ROWS, and TABLE where it is cut: [split][N][M]
     int64_t out_split;
-    int steps, most_splits, add;      // splits go by the first piece's steps; add: to what earlier pieces left
+    int most_splits;
+    int add;                          // ROWS: to what earlier pieces left
     void *dtable;                     // TABLE
     int accumulate;
 };
 
-// How many parts the contracted axis of ROWS is cut into: as many as leave the fewest turns of the chip's 256 workgroups for the work of one.
-__host__ __device__ inline int row_splits(int tiles, int steps, int most)
-{
-    int best = 1;
-    float least = 0.0f;
-    for (int s = 1; s <= most && s <= (steps + 7) / 8; ++s) {
-        const float turns = (float)((tiles * s + 255) / 256);
-        const float cost = turns * ((float)((steps + s - 1) / s) + 6.0f) + 0.5f * (float)s;
-        if (s == 1 || cost < least) {
-            best = s;
-            least = cost;
-        }
-    }
-    return best;
-}
+constexpr int LIST_BLOCK = 128;
 
-// Tile shapes (tile rows x columns)
-enum { TILE_256, TILE_128, TILE_FEW };
-inline int tile_m(int form) { return form == TILE_256 ? 256 : 128; }
-inline int tile_n(int form) { return form == TILE_256 ? 256 : form == TILE_128 ? 128 : 64; }
+// Tile shapes, rows x columns, and how many are on the chip at once (TILE_128_DEEP: with more steps on their way, alone on its CU).  The last three for
+// STATS and PROBS alone.
+enum { TILE_256, TILE_128, TILE_128_DEEP, TILE_128x64, TILE_64, TILE_FORMS };
+inline int tile_m(int form) { return form == TILE_256 ? 256 : form == TILE_64 ? 64 : 128; }
+inline int tile_n(int form) { return form == TILE_256 ? 256 : form <= TILE_128_DEEP ? 128 : 64; }
+inline int tile_slots(int form) { return form == TILE_128 || form == TILE_64 ? 512 : 256; }
+
+// How many parts the contracted axis of ROWS and TABLE is cut into: of 1 .. MOST_SPLITS those that take the least time - turns of the chip's workgroups, each
+// with its steps and what a tile costs beside them, and the joining of the parts.
+constexpr int MOST_SPLITS = 64;
+__host__ __device__ inline float split_cost(int s, int tiles, int slots, int steps)
+{
+    return (float)((tiles * s + slots - 1) / slots) * ((float)((steps + s - 1) / s) + 5.0f) + 0.25f * (float)s;
+}
 
 int launch_vocab_tiles(int kind, int form, int dtype, const TilesArgs &p, hipStream_t s);
 

@@ -38,10 +38,29 @@ void loss_flags_kernel(Targets t, int V, int rows, uint8_t *__restrict__ flags, 
         if (!counts || !listed(t.ids[(int64_t)row * t.k + k], V)) picked[(int64_t)row * t.k + k] = 0.0f;
 }
 
+// A product whose sums are cut into parts: tiles along its other axis, along the rows' (0: it is the rows that are summed over), workgroups at once, steps
+// (0: by the rows), and at most how many parts.
+struct Cut {
+    int tiles, tile_rows, slots, steps, most;
+};
+
+// Which of 1 .. 64 parts costs least, a lane each (of several the smallest).
+__device__ inline int best_cut(const Cut &c, int count, int lane)
+{
+    const int tiles = c.tiles * (c.tile_rows ? (count + c.tile_rows - 1) / c.tile_rows : 1), steps = c.tile_rows ? c.steps : (count + 63) / 64;
+    const int s = lane + 1;
+    const float cost = s == 1 || (s <= c.most && s <= (steps + 3) / 4) ? split_cost(s, tiles, c.slots, steps) : INFINITY;
+    float least = cost;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) least = fminf(least, __shfl_xor(least, d));
+    return __builtin_ctzll(__ballot(cost == least)) + 1;
+}
+
 // The rows that count, in their order, and each row's place among them (-1: none).  One workgroup.  flags = nullptr: by the targets.
 __global__ __launch_bounds__(1024)
 void loss_list_kernel(const int32_t *__restrict__ ids, const uint8_t *__restrict__ flags, const float *__restrict__ g, float temperature, int rows, int V,
-                      bool scaled, LossHead *__restrict__ head, int *__restrict__ list, int *__restrict__ place, float *__restrict__ loss, float *__restrict__ lse)
+                      bool scaled, Cut rows_cut, Cut table_cut, LossHead *__restrict__ head, int *__restrict__ list, int *__restrict__ place,
+                      float *__restrict__ loss, float *__restrict__ lse)
 {
     __shared__ int waves[16];
     __shared__ float tops[16];
@@ -74,6 +93,10 @@ void loss_list_kernel(const int32_t *__restrict__ ids, const uint8_t *__restrict
     top = wave_top(top);
     if (lane == 0) tops[wave] = top;
     __syncthreads();
+    if (wave < 2 && rows_cut.slots) {                          // (the gradients' call, also of no rows at all)
+        const int splits = best_cut(wave ? table_cut : rows_cut, before, lane);
+        if (lane == 0) (wave ? head->splits_table : head->splits_rows) = splits;
+    }
     if (threadIdx.x != 0) return;
     for (int w = 1; w < 16; ++w) top = fmaxf(top, tops[w]);
     // (values of f16 reach from 2^-24 to 2^16: the largest gradient is brought to 2^14 .. 2^15; bf16 has fp32's range)
@@ -83,6 +106,8 @@ void loss_list_kernel(const int32_t *__restrict__ ids, const uint8_t *__restrict
     head->down = power_of_two(-e);
 }
 
+constexpr int MOST_LISTED = 256;
+
 struct GatherArgs {
     Targets t;
     const void *x;
@@ -91,9 +116,11 @@ struct GatherArgs {
     const LossHead *head;
     const int *place;
     void *xc;
-    int32_t *ids;                     // [k][ld]
-    float *q;                         // [k][ld], or nullptr
-    int64_t ld;
+    int32_t *ids;                     // [place][k], a row's in rising order
+    int32_t *slot;                    // likewise, forward: their places in the caller's list;
+    float *q;                         // backward: their shares
+    uint16_t *start;                  // [place][start_ld]
+    int64_t start_ld;
     const float *lse, *g;             // nullptr: forward
     float *lse2, *gc;
     void *dx;                         // rows of zeros for what does not count; nullptr: not wanted
@@ -126,23 +153,58 @@ void loss_gather_kernel(GatherArgs p)
         if (lane == 0) p.ids[at] = p.t.ids[row];
         return;
     }
-    float top = -INFINITY, sum = 0.0f;
-    const int32_t *const ids = p.t.ids + (int64_t)row * p.t.k;
-    const float *const logits = p.t.logits + (int64_t)row * p.t.k;
+    // The list in rising order (those not listed behind): an entry's place is the number of smaller ones, and of equal ones before it.
+    constexpr int E = MOST_LISTED / 64;
+    __shared__ int ordered[4][MOST_LISTED];
+    int *const mine = ordered[threadIdx.x >> 6];
+    const int k = p.t.k;
+    uint32_t id[E];
+    int rank[E] = {};
+    float logit[E], top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int n = lane + 64 * e;
+        const int v = n < k ? p.t.ids[(int64_t)row * k + n] : -1;
+        id[e] = listed(v, p.V) ? (uint32_t)v : 0x7fffffffu;
+        logit[e] = id[e] != 0x7fffffffu && p.q ? p.t.logits[(int64_t)row * k + n] / p.t.temperature : -INFINITY;
+        top = fmaxf(top, logit[e]);
+    }
+#pragma unroll
+    for (int f = 0; f < E; ++f)
+        for (int l = 0; l < min(64, k - 64 * f); ++l) {
+            const uint32_t other = __builtin_amdgcn_readlane(id[f], l);
+#pragma unroll
+            for (int e = 0; e < E; ++e) rank[e] += other < id[e] || (other == id[e] && l + 64 * f < lane + 64 * e) ? 1 : 0;
+        }
     if (p.q) {
-        for (int k = lane; k < p.t.k; k += 64)
-            if (listed(ids[k], p.V)) top = fmaxf(top, logits[k] / p.t.temperature);
 #pragma unroll
         for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-        for (int k = lane; k < p.t.k; k += 64)
-            if (listed(ids[k], p.V)) sum += expf(logits[k] / p.t.temperature - top);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            logit[e] = id[e] != 0x7fffffffu ? expf(logit[e] - top) : 0.0f;
+            sum += logit[e];
+        }
 #pragma unroll
         for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
     }
-    for (int k = lane; k < p.t.k; k += 64) {
-        const bool in = listed(ids[k], p.V);
-        p.ids[k * p.ld + at] = in ? ids[k] : -1;
-        if (p.q) p.q[k * p.ld + at] = in ? expf(logits[k] / p.t.temperature - top) / sum : 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int n = lane + 64 * e;
+        if (n >= k) continue;
+        mine[rank[e]] = (int)id[e];
+        p.ids[(int64_t)at * k + rank[e]] = (int)id[e];
+        if (p.q) p.q[(int64_t)at * k + rank[e]] = logit[e] / sum;
+        else p.slot[(int64_t)at * k + rank[e]] = n;
+    }
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    for (int64_t b = lane; b < p.start_ld; b += 64) {
+        const int64_t first = b * LIST_BLOCK;
+        int lo = 0;
+#pragma unroll
+        for (int step = MOST_LISTED; step; step >>= 1)
+            if (lo + step <= k && mine[lo + step - 1] < first) lo += step;
+        p.start[at * p.start_ld + b] = (uint16_t)lo;
     }
 }
 
@@ -252,34 +314,61 @@ void loss_join_kernel(JoinArgs p)
     }
 }
 
+// The parts of a gradient's eight channels in their order.
+__device__ inline void sum_parts(const float *from, int64_t split, int splits, float *sum)
+{
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+        const f32x4 a = *(const f32x4 *)(from + s * split), b = *(const f32x4 *)(from + s * split + 4);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            sum[k] += a[k];
+            sum[4 + k] += b[k];
+        }
+    }
+}
+
 // Gradients of rows from their parts: a wave a row.
 template <class T>
 __global__ __launch_bounds__(256)
-void loss_rows_kernel(const float *__restrict__ part, int64_t split, int C, int tile_m, int tile_n, int steps, int most, const LossHead *__restrict__ head,
-                      const int *__restrict__ list, T *__restrict__ dx, int64_t lddx)
+void loss_rows_kernel(const float *__restrict__ part, int64_t split, int C, const LossHead *__restrict__ head, const int *__restrict__ list,
+                      T *__restrict__ dx, int64_t lddx)
 {
     using v8 = typename Half<T>::v8;
     const int lane = threadIdx.x & 63, t = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), count = head->count;
     if (t >= count) return;
-    const int splits = row_splits((C + tile_m - 1) / tile_m * ((count + tile_n - 1) / tile_n), steps, most);
+    const int splits = head->splits_rows;
     const float down = head->down;
     T *const to = dx + (int64_t)list[t] * lddx;
     for (int c = lane * 8; c < C; c += 512) {
         float sum[8] = {};
-#pragma unroll 4
-        for (int s = 0; s < splits; ++s) {
-            const float *const from = part + s * split + (int64_t)t * C + c;
-            const f32x4 a = *(const f32x4 *)from, b = *(const f32x4 *)(from + 4);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                sum[k] += a[k];
-                sum[4 + k] += b[k];
-            }
-        }
+        sum_parts(part + (int64_t)t * C + c, split, splits, sum);
         v8 v;
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = (T)(sum[k] * down);
         *(v8 *)(to + c) = v;
+    }
+}
+
+// Rows of the table's gradient from their parts (if there are several): a wave a row.
+template <class T>
+__global__ __launch_bounds__(256)
+void loss_table_kernel(const float *__restrict__ part, int64_t split, int n, int C, const LossHead *__restrict__ head, T *__restrict__ dtable,
+                       bool accumulate)
+{
+    using v8 = typename Half<T>::v8;
+    const int lane = threadIdx.x & 63, v = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int splits = head->splits_table;
+    if (v >= n || splits == 1) return;
+    const float down = head->down;
+    for (int c = lane * 8; c < C; c += 512) {
+        float sum[8] = {};
+        sum_parts(part + (int64_t)v * C + c, split, splits, sum);
+        v8 *const to = (v8 *)(dtable + (int64_t)v * C + c), had = accumulate ? *to : v8{};
+        v8 w;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = (T)(accumulate ? fmaf(sum[k], down, (float)had[k]) : sum[k] * down);
+        *to = w;
     }
 }
 
@@ -295,16 +384,48 @@ struct LossPlan {
     int form, form_rows, form_table;
     int64_t ld;                       // rows, in whole blocks of 64
     int tiles;                        // of the vocabulary (forward)
-    int piece, most_splits;
-    size_t list, place, flags, pick, ids, q, lse2, g, xc, part, probs, out, bytes;
+    int piece, most_splits, most_splits_table;
+    Cut rows_cut, table_cut;
+    int64_t start_ld;
+    size_t list, place, flags, pick, ids, of_ids, start, lse2, g, xc, part, probs, out, out_table, bytes;
 };
 
-int form_of(int64_t m, int64_t n, int64_t enough)
+int64_t tiles_of(int form, int64_t m, int64_t n) { return (m + tile_m(form) - 1) / tile_m(form) * ((n + tile_n(form) - 1) / tile_n(form)); }
+
+// Tiles of logits of `tokens` x `rows`: the form whose turns of the chip cost least, in turns of 256 x 256.
+int logits_form(int64_t tokens, int64_t rows)
 {
-    return (m + 255) / 256 * ((n + 255) / 256) >= enough && n > 128 && m > 128 ? TILE_256 : TILE_128;
+    constexpr float TURN[] = {1.0f, 0.8f, 0.45f, 0.33f, 0.35f}, HALF[] = {1.0f, 0.6f, 0.45f, 0.33f, 0.22f};       // (no CU with two)
+    int best = 0;
+    float least = 0.0f;
+    for (int f = 0; f < TILE_FORMS; ++f) {
+        const int64_t tiles = tiles_of(f, tokens, rows);
+        const float cost = tiles <= 256 ? HALF[f] : TURN[f] * (float)((tiles + tile_slots(f) - 1) / tile_slots(f));
+        if (f == 0 || cost < least) {
+            best = f;
+            least = cost;
+        }
+    }
+    return best;
 }
 
-LossPlan loss_plan(const Vocab &v, int64_t rows, int k, bool backward)
+// Tiles of a gradient [n][m], its sums over `depth` cut into at most `most` parts: likewise.
+int gradient_form(int64_t m, int64_t n, int64_t depth, int most)
+{
+    float cost[2];
+    const int steps = (int)((depth + 63) / 64);
+    for (int f = 0; f < 2; ++f) {
+        const int64_t tiles = tiles_of(f, m, n);
+        const float turn[] = {1.0f, 0.8f}, half[] = {1.0f, 0.6f};
+        for (int s = 1; s == 1 || (tiles < tile_slots(f) && s <= most && s <= (steps + 3) / 4); ++s) {
+            const float c = (tiles * s <= 256 ? half[f] : turn[f]) * split_cost(s, (int)(tiles < (1 << 24) ? tiles : 1 << 24), tile_slots(f), steps);
+            if (s == 1 || c < cost[f]) cost[f] = c;
+        }
+    }
+    return cost[1] < cost[0] ? TILE_128 : TILE_256;
+}
+
+LossPlan loss_plan(const Vocab &v, int64_t rows, int k, bool teacher, bool backward)
 {
     LossPlan p = {};
     p.ld = (rows + 63) / 64 * 64;
@@ -320,11 +441,14 @@ LossPlan loss_plan(const Vocab &v, int64_t rows, int k, bool backward)
         p.list = take(p.ld * 4);
         p.place = take(p.ld * 4);
         p.flags = take(p.ld);
-        p.ids = take((size_t)k * p.ld * 4);
+        p.start_ld = (v.V + LIST_BLOCK - 1) / LIST_BLOCK + 1;
+        p.ids = take((size_t)rows * k * 4);
+        p.of_ids = take(teacher ? (size_t)rows * k * 4 : 0);
+        p.start = take(teacher ? (size_t)rows * p.start_ld * 2 : 0);
         p.xc = take((size_t)rows * v.C * 2);
     }
     if (!backward) {
-        p.form = rows <= 64 ? TILE_FEW : form_of(v.V, rows, 200);
+        p.form = logits_form(v.V, rows);
         p.tiles = (v.V + tile_m(p.form) - 1) / tile_m(p.form);
         p.pick = take(p.ld * 4);
         p.part = take((size_t)p.tiles * p.ld * 8);
@@ -332,16 +456,23 @@ LossPlan loss_plan(const Vocab &v, int64_t rows, int k, bool backward)
         const size_t all = ((size_t)v.V + 255) / 256, most = PIECE_BYTES / 512 / (size_t)(p.ld ? p.ld : 64);
         const size_t pieces = most < 1 ? all : (all + most - 1) / most;
         p.piece = (int)((all + pieces - 1) / pieces * 256);
-        p.form = form_of(p.piece, rows, 200);
-        p.form_rows = form_of(v.C, rows, 1);
-        p.form_table = form_of(v.C, p.piece, 200);
-        const size_t part = (size_t)rows * v.C * 4;
-        p.most_splits = (int)(part * 64 <= PARTS_BYTES ? 64 : part * 2 > PARTS_BYTES ? 1 : PARTS_BYTES / part);
-        p.q = take((size_t)k * p.ld * 4);
+        p.form = logits_form(p.piece, rows);
+        // (as many parts of a gradient as there is room for)
+        auto parts = [&](size_t one) { return (int)(one * MOST_SPLITS <= PARTS_BYTES ? MOST_SPLITS : one * 2 > PARTS_BYTES ? 1 : PARTS_BYTES / one); };
+        const size_t part = (size_t)rows * v.C * 4, part_table = (size_t)p.piece * v.C * 4;
+        p.most_splits = parts(part);
+        p.most_splits_table = parts(part_table);
+        p.form_rows = gradient_form(v.C, rows, p.piece, p.most_splits);
+        p.form_table = gradient_form(v.C, p.piece, rows, p.most_splits_table);
+        if (tiles_of(p.form_table, v.C, p.piece) >= tile_slots(p.form_table)) p.most_splits_table = 1;
+        const int tokens = v.V < p.piece ? v.V : p.piece;
+        p.rows_cut = {(v.C + tile_m(p.form_rows) - 1) / tile_m(p.form_rows), tile_n(p.form_rows), tile_slots(p.form_rows), (tokens + 63) / 64, p.most_splits};
+        p.table_cut = {(int)tiles_of(p.form_table, v.C, tokens), 0, tile_slots(p.form_table), 0, p.most_splits_table};
         p.lse2 = take(p.ld * 4);
         p.g = take(p.ld * 4);
         p.probs = take((size_t)p.ld * p.piece * 2);
         p.out = take(part * p.most_splits);
+        p.out_table = take(p.most_splits_table > 1 ? part_table * p.most_splits_table : 0);
     }
     p.bytes = at;
     return p;
@@ -356,14 +487,16 @@ int launch_rows(const Vocab &v, const LossPlan &plan, const Rows16 &x, int64_t r
     int *const list = (int *)(ws + plan.list), *const place = (int *)(ws + plan.place);
     const unsigned blocks = (unsigned)((rows + 3) / 4);
     if (flags && rows) loss_flags_kernel<<<dim3(blocks), 256, 0, s>>>(t, v.V, (int)rows, flags, loss, lse_out, picked);
-    loss_list_kernel<<<1, 1024, 0, s>>>(t.ids, flags, dloss, t.temperature, (int)rows, v.V, dloss && v.dtype == SNN_DTYPE_F16, head, list, place, loss,
-                                          lse_out);
+    loss_list_kernel<<<1, 1024, 0, s>>>(t.ids, flags, dloss, t.temperature, (int)rows, v.V, dloss && v.dtype == SNN_DTYPE_F16, plan.rows_cut, plan.table_cut,
+                                          head, list, place, loss, lse_out);
     if (rows) {
         GatherArgs g = {};
         g.t = t; g.x = x.p; g.ldx = x.ld; g.rows = (int)rows; g.V = v.V; g.C = v.C; g.head = head; g.place = place;
-        g.xc = ws + plan.xc; g.ids = (int32_t *)(ws + plan.ids); g.ld = plan.ld;
-        if (dloss) {
-            g.q = (float *)(ws + plan.q);
+        g.xc = ws + plan.xc; g.ids = (int32_t *)(ws + plan.ids);
+        g.start = (uint16_t *)(ws + plan.start); g.start_ld = plan.start_ld;
+        if (!dloss) g.slot = (int32_t *)(ws + plan.of_ids);
+        else {
+            g.q = (float *)(ws + plan.of_ids);
             g.lse = lse; g.g = dloss; g.lse2 = (float *)(ws + plan.lse2); g.gc = (float *)(ws + plan.g);
             g.dx = dx; g.lddx = lddx;
         }
@@ -375,30 +508,34 @@ int launch_rows(const Vocab &v, const LossPlan &plan, const Rows16 &x, int64_t r
 
 }  // namespace
 
-size_t loss_workspace_bytes(const Vocab &v, int64_t rows, int k, bool backward) { return loss_plan(v, rows, k, backward).bytes; }
+size_t loss_workspace_bytes(const Vocab &v, int64_t rows, int k, bool backward) { return loss_plan(v, rows, k, true, backward).bytes; }
 
 int launch_loss_forward(const Vocab &v, const Rows16 &x, int64_t rows, const Rows16 &table, const Targets &t, float *loss, float *lse, float *picked,
                         void *workspace, hipStream_t s)
 {
-    const LossPlan plan = loss_plan(v, rows, t.k, false);
+    const LossPlan plan = loss_plan(v, rows, t.k, t.logits != nullptr, false);
     char *const ws = (char *)workspace;
     TilesArgs p = {};
     p.a = table.p; p.lda = table.ld; p.M = v.V;
     p.b = x.p; p.ldb = x.ld; p.N = (int)rows; p.K = v.C;
     p.c = LOG2E / t.temperature;
-    p.ids = t.ids; p.id_row = t.k; p.id_k = 1; p.k = t.k;
+    p.ids = t.ids; p.k = t.k;
     if (plan.gather) {
         const int rc = launch_rows(v, plan, x, rows, t, nullptr, nullptr, nullptr, 0, loss, lse, picked, ws, s);
         if (rc != SNN_OK) return rc;
         p.head = (const LossHead *)ws;
         p.b = ws + plan.xc; p.ldb = v.C;
-        p.ids = (const int32_t *)(ws + plan.ids); p.id_row = 1; p.id_k = plan.ld;
+        p.ids = (const int32_t *)(ws + plan.ids);
+        if (t.logits) {
+            p.start = (const uint16_t *)(ws + plan.start); p.start_ld = plan.start_ld;
+            p.slot = (const int32_t *)(ws + plan.of_ids);
+        }
     }
     const int *const list = plan.gather ? (const int *)(ws + plan.list) : nullptr;
     p.part = (float2 *)(ws + plan.part); p.part_ld = plan.ld;
     // (targets' logits stay in the workspace, by place)
     p.picked = t.logits ? picked : (float *)(ws + plan.pick);
-    p.list = t.logits ? list : nullptr;
+    p.list = list;
     const int rc = launch_vocab_tiles(STATS, plan.form, v.dtype, p, s);
     if (rc != SNN_OK) return rc;
     JoinArgs j = {};
@@ -407,6 +544,7 @@ int launch_loss_forward(const Vocab &v, const Rows16 &x, int64_t rows, const Row
     j.pick = (const float *)(ws + plan.pick);
     j.loss = loss; j.lse = lse; j.picked = picked;
     if (rows <= 256) loss_join_kernel<1><<<dim3((unsigned)rows), 256, 0, s>>>(j);
+    else if (t.logits) loss_join_kernel<8><<<dim3((unsigned)((rows + 7) / 8)), 256, 0, s>>>(j);
     else loss_join_kernel<32><<<dim3((unsigned)((rows + 31) / 32)), 256, 0, s>>>(j);
     return check_launch();
 }
@@ -414,13 +552,11 @@ int launch_loss_forward(const Vocab &v, const Rows16 &x, int64_t rows, const Row
 int launch_loss_backward(const Vocab &v, const Rows16 &x, int64_t rows, const Rows16 &table, const Targets &t, const float *lse, const float *dloss,
                          void *dx, int64_t lddx, void *dtable, bool accumulate, void *workspace, hipStream_t s)
 {
-    const LossPlan plan = loss_plan(v, rows, t.k, true);
+    const LossPlan plan = loss_plan(v, rows, t.k, t.logits != nullptr, true);
     char *const ws = (char *)workspace;
     int rc = launch_rows(v, plan, x, rows, t, lse, dloss, dx, lddx, nullptr, nullptr, nullptr, ws, s);
     if (rc != SNN_OK) return rc;
     const int64_t split = (int64_t)rows * v.C;
-    const int most = plan.most_splits;
-    int steps = 0;
     for (int64_t v0 = 0; v0 < v.V; v0 += plan.piece) {
         const int n = (int)(v.V - v0 < plan.piece ? v.V - v0 : plan.piece);
         const char *const rows_of_piece = (const char *)table.p + v0 * table.ld * 2;
@@ -430,8 +566,11 @@ int launch_loss_backward(const Vocab &v, const Rows16 &x, int64_t rows, const Ro
         p.b = ws + plan.xc; p.ldb = v.C; p.N = (int)rows; p.K = v.C;
         p.c = LOG2E / t.temperature;
         p.v0 = (int)v0;
-        p.ids = (const int32_t *)(ws + plan.ids); p.id_row = 1; p.id_k = plan.ld; p.k = t.k;
-        p.q = t.logits ? (const float *)(ws + plan.q) : nullptr;
+        p.ids = (const int32_t *)(ws + plan.ids); p.k = t.k;
+        if (t.logits) {
+            p.q = (const float *)(ws + plan.of_ids);
+            p.start = (const uint16_t *)(ws + plan.start); p.start_ld = plan.start_ld;
+        }
         p.lse2 = (const float *)(ws + plan.lse2); p.g = (const float *)(ws + plan.g);
         p.probs = ws + plan.probs; p.ldp = plan.piece;
         if ((rc = launch_vocab_tiles(PROBS, plan.form, v.dtype, p, s)) != SNN_OK) return rc;
@@ -440,10 +579,8 @@ int launch_loss_backward(const Vocab &v, const Rows16 &x, int64_t rows, const Ro
             r.head = p.head;
             r.a = rows_of_piece; r.lda = table.ld; r.M = v.C;
             r.b = p.probs; r.ldb = p.ldp; r.N = (int)rows; r.K = n;
-            r.out = (float *)(ws + plan.out); r.out_split = split; r.most_splits = most; r.add = v0 > 0;
-            // (the number of parts is the first piece's in all of them: a shorter last piece leaves some empty)
-            if (v0 == 0) steps = (n + 31) / 32;
-            r.steps = steps;
+            // (the number of parts is the same for all pieces: a shorter last one leaves some empty)
+            r.out = (float *)(ws + plan.out); r.out_split = split; r.most_splits = plan.most_splits; r.add = v0 > 0;
             if ((rc = launch_vocab_tiles(ROWS, plan.form_rows, v.dtype, r, s)) != SNN_OK) return rc;
         }
         if (dtable) {
@@ -452,19 +589,28 @@ int launch_loss_backward(const Vocab &v, const Rows16 &x, int64_t rows, const Ro
             w.a = p.b; w.lda = v.C; w.M = v.C;
             w.b = p.probs; w.ldb = p.ldp; w.N = n; w.K = (int)rows;
             w.v0 = (int)v0; w.dtable = dtable; w.accumulate = accumulate;
+            w.out = (float *)(ws + plan.out_table); w.out_split = (int64_t)n * v.C;
+            w.most_splits = plan.most_splits_table;
             if ((rc = launch_vocab_tiles(TABLE, plan.form_table, v.dtype, w, s)) != SNN_OK) return rc;
+            if (w.most_splits > 1) {
+                const dim3 grid((unsigned)((n + 3) / 4));
+                void *const to = (char *)dtable + v0 * v.C * 2;
+                if (v.dtype == SNN_DTYPE_BF16)
+                    loss_table_kernel<__bf16><<<grid, 256, 0, s>>>(w.out, w.out_split, n, v.C, w.head, (__bf16 *)to, accumulate);
+                else
+                    loss_table_kernel<_Float16><<<grid, 256, 0, s>>>(w.out, w.out_split, n, v.C, w.head, (_Float16 *)to, accumulate);
+                if ((rc = check_launch()) != SNN_OK) return rc;
+            }
         }
     }
     if (!dx || rows == 0) return SNN_OK;
     const unsigned blocks = (unsigned)((rows + 3) / 4);
-    const int tm = tile_m(plan.form_rows), tn = tile_n(plan.form_rows);
     const LossHead *const head = (const LossHead *)ws;
     const int *const list = (const int *)(ws + plan.list);
     if (v.dtype == SNN_DTYPE_BF16)
-        loss_rows_kernel<__bf16><<<dim3(blocks), 256, 0, s>>>((const float *)(ws + plan.out), split, v.C, tm, tn, steps, most, head, list, (__bf16 *)dx, lddx);
+        loss_rows_kernel<__bf16><<<dim3(blocks), 256, 0, s>>>((const float *)(ws + plan.out), split, v.C, head, list, (__bf16 *)dx, lddx);
     else
-        loss_rows_kernel<_Float16><<<dim3(blocks), 256, 0, s>>>((const float *)(ws + plan.out), split, v.C, tm, tn, steps, most, head, list, (_Float16 *)dx,
-                                                                lddx);
+        loss_rows_kernel<_Float16><<<dim3(blocks), 256, 0, s>>>((const float *)(ws + plan.out), split, v.C, head, list, (_Float16 *)dx, lddx);
     return check_launch();
 }
 
