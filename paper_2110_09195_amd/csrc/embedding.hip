@@ -58,33 +58,43 @@ void embedding_kernel(const T *__restrict__ table, int64_t ldt, const int32_t *_
 // of no row of the table come last.
 
 // Up to MERGED rows: blocks of RANK_BLOCK rows are sorted by themselves - a row's place is the number of the block's tokens below its own, and of
-// its own in earlier rows; 64 rows a workgroup, whose waves share out the tokens that they are compared with, by scalar loads - and a row's
+// its own in earlier rows; 64 rows a workgroup, whose waves share out the tokens that they are compared with - and a row's
 // place among all is its place there and those that a binary search finds for it in the other blocks.
 constexpr int64_t MERGED = 65536;
-constexpr int RANK_BLOCK = 2048, RANK_WAVES = 16;
+constexpr int RANK_BLOCK = 1024, RANK_WAVES = 8, MERGE_WAVES = 16;
 
 __global__ __launch_bounds__(64 * RANK_WAVES)
 void embedding_rank_kernel(const uint32_t *__restrict__ ids, int rows, uint32_t *__restrict__ sorted, int *__restrict__ order)
 {
     __shared__ int counts[RANK_WAVES][64];
+    __shared__ __align__(16) uint32_t tokens[RANK_BLOCK];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int i0 = blockIdx.x * 64, i = i0 + lane, first = i0 / RANK_BLOCK * RANK_BLOCK, last = min(first + RANK_BLOCK, rows);
-    const uint32_t mine = i < rows ? ids[i] : 0;
+    const int i0 = blockIdx.x * 64, i = i0 + lane, first = i0 / RANK_BLOCK * RANK_BLOCK, n = min(RANK_BLOCK, rows - first);
+#pragma unroll
+    for (int k = 0; k < RANK_BLOCK; k += 64 * RANK_WAVES) tokens[k + threadIdx.x] = k + (int)threadIdx.x < n ? ids[first + k + threadIdx.x] : ~0u;
+    __syncthreads();
+    const uint32_t mine = i < rows ? tokens[i - first] : 0;
     constexpr int SHARE = RANK_BLOCK / RANK_WAVES;             // a multiple of 64: a wave's tokens are all before, all behind or among the workgroup's
-    const int lo = first + wave * SHARE, hi = min(lo + SHARE, last);
+    const int lo = wave * SHARE, at = i0 - first;
+    const u32x4 *const from = (const u32x4 *)(tokens + lo);
     int below = 0;
-    if (hi - lo == SHARE && hi <= i0) {
-#pragma unroll 32
-        for (int j = 0; j < SHARE; ++j) below += ids[lo + j] <= mine ? 1 : 0;
-    } else if (hi - lo == SHARE && lo >= i0 + 64) {
-#pragma unroll 32
-        for (int j = 0; j < SHARE; ++j) below += ids[lo + j] < mine ? 1 : 0;
-    } else {
+    // (behind the last row: the largest number there is, below none and after all)
+    if (lo + SHARE <= at) {
 #pragma unroll 8
-        for (int j = lo; j < hi; ++j) {
-            const uint32_t other = ids[j];
-            below += other < mine || (other == mine && j < i) ? 1 : 0;
-        }
+        for (int j = 0; j < SHARE / 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) below += from[j][e] <= mine ? 1 : 0;
+    } else if (lo >= at + 64) {
+        if (lo < n)
+#pragma unroll 8
+            for (int j = 0; j < SHARE / 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) below += from[j][e] < mine ? 1 : 0;
+    } else {
+#pragma unroll 4
+        for (int j = 0; j < SHARE / 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) below += from[j][e] < mine || (from[j][e] == mine && lo + 4 * j + e < i - first) ? 1 : 0;
     }
     counts[wave][lane] = below;
     __syncthreads();
@@ -97,16 +107,16 @@ void embedding_rank_kernel(const uint32_t *__restrict__ ids, int rows, uint32_t 
     }
 }
 
-__global__ __launch_bounds__(64 * RANK_WAVES)
+__global__ __launch_bounds__(64 * MERGE_WAVES)
 void embedding_merge_kernel(const uint32_t *__restrict__ keys, const int *__restrict__ rows_of, int rows, uint32_t *__restrict__ sorted,
                             int *__restrict__ order)
 {
-    __shared__ int counts[RANK_WAVES][64];
+    __shared__ int counts[MERGE_WAVES][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i0 = blockIdx.x * 64, i = i0 + lane, own = i0 / RANK_BLOCK, blocks = (rows + RANK_BLOCK - 1) / RANK_BLOCK;
     const uint32_t mine = i < rows ? keys[i] : 0;
     int below = 0;
-    for (int b = wave; b < blocks; b += RANK_WAVES) {
+    for (int b = wave; b < blocks; b += MERGE_WAVES) {
         if (b == own) continue;
         const uint32_t *const at = keys + b * RANK_BLOCK;
         const int n = min(RANK_BLOCK, rows - b * RANK_BLOCK);
@@ -122,7 +132,7 @@ void embedding_merge_kernel(const uint32_t *__restrict__ keys, const int *__rest
     if (wave == 0 && i < rows) {
         int place = i - own * RANK_BLOCK;
 #pragma unroll
-        for (int w = 0; w < RANK_WAVES; ++w) place += counts[w][lane];
+        for (int w = 0; w < MERGE_WAVES; ++w) place += counts[w][lane];
         sorted[place] = mine;
         order[place] = rows_of[i];
     }
@@ -242,13 +252,14 @@ struct SumArgs {
     const uint32_t *sorted;
     const int *order;
     int V, C, slabs;                  // slabs of 512 channels, a wave's
-    int64_t blocks;                   // of BLOCK rows in the tokens' order
+    int block;                        // rows in the tokens' order that a wave sums, at most 32
+    int64_t blocks;
     float scale;
     void *dtable;
     int accumulate;
     float *part;                      // [block][2][C]: sums of a block's first token, begun in an earlier one, and of its last, which goes on
 };
-constexpr int BLOCK = 32, SUM_AHEAD = 8, FILL_ROWS = 64;
+constexpr int SUM_AHEAD = 8, FILL_ROWS = 64;
 
 template <class T>
 __device__ inline void write_sum(const SumArgs &p, uint32_t token, int c, const float *sum)
@@ -261,7 +272,7 @@ __device__ inline void write_sum(const SumArgs &p, uint32_t token, int c, const 
     *at = v;
 }
 
-// A wave sums BLOCK rows in the tokens' order, 512 channels.  A token whose rows all lie there is done; the others' sums are joined by the next
+// A wave sums a block of rows in the tokens' order, 512 channels.  A token whose rows all lie there is done; the others' sums are joined by the next
 // launch.  Workgroups behind these (when the result is not added to what is there) write zeros for FILL_ROWS tokens each that have no row.
 // Bound by memory: each row is read once, each row of the result written once.
 template <class T>
@@ -294,8 +305,8 @@ void embedding_sum_kernel(SumArgs p, unsigned sum_grid)
     const int64_t id = (int64_t)blockIdx.x * 4 + wave, block = id / p.slabs;
     if (block >= p.blocks) return;
     const int c = (int)(id - block * p.slabs) * 512 + lane * 8;
-    const int64_t first = block * BLOCK;
-    const int n = (int)min((int64_t)BLOCK, p.rows - first);
+    const int64_t first = block * p.block;
+    const int n = (int)min((int64_t)p.block, p.rows - first);
     // lane l: row l of the block, and its token; lanes behind them the tokens before and after the block
     uint32_t token = ~0u;
     int row = 0;
@@ -310,34 +321,45 @@ void embedding_sum_kernel(SumArgs p, unsigned sum_grid)
     const uint32_t before = __builtin_amdgcn_readlane(token, 62), after = __builtin_amdgcn_readlane(token, 63);
     bool begun = first > 0 && before == now;                   // the token's rows begin in an earlier block
     float sum[8] = {};
-    for (int r0 = 0; r0 < n; r0 += SUM_AHEAD) {
+    struct Rows {
         v8 v[SUM_AHEAD];
         uint32_t of[SUM_AHEAD];
+    } rows[2];
+    auto load = [&](int r0, Rows &to) {
 #pragma unroll
         for (int i = 0; i < SUM_AHEAD; ++i) {
             const int r = r0 + i;
-            of[i] = r < n ? __builtin_amdgcn_readlane(token, min(r, BLOCK - 1)) : ~0u;
-            v[i] = v8{};
-            if (in && of[i] < (uint32_t)p.V) v[i] = *(const v8 *)(dy + (int64_t)__builtin_amdgcn_readlane(row, min(r, BLOCK - 1)) * p.lddy + c);
+            to.of[i] = r < n ? __builtin_amdgcn_readlane(token, r) : ~0u;
+            to.v[i] = v8{};
+            if (in && to.of[i] < (uint32_t)p.V) to.v[i] = *(const v8 *)(dy + (int64_t)__builtin_amdgcn_readlane(row, r) * p.lddy + c);
         }
+    };
+    auto add = [&](int r0, const Rows &from) {
 #pragma unroll
         for (int i = 0; i < SUM_AHEAD; ++i) {
-            if (r0 + i >= n) break;
-            if (of[i] != now) {
+            if (r0 + i < n && from.of[i] != now) {
                 if (in && now < (uint32_t)p.V) {
                     if (!begun) write_sum<T>(p, now, c, sum);
                     else
 #pragma unroll
                         for (int k = 0; k < 8; k += 4) *(f32x4 *)(p.part + block * 2 * p.C + c + k) = f32x4{sum[k], sum[k + 1], sum[k + 2], sum[k + 3]};
                 }
-                now = of[i];
+                now = from.of[i];
                 begun = false;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] += (float)v[i][k];
+            for (int k = 0; k < 8; ++k) sum[k] += (float)from.v[i][k];
         }
+    };
+    // (the next rows are on their way while these are added)
+    load(0, rows[0]);
+    for (int r0 = 0; r0 < n; r0 += 2 * SUM_AHEAD) {
+        load(r0 + SUM_AHEAD, rows[1]);
+        add(r0, rows[0]);
+        load(r0 + 2 * SUM_AHEAD, rows[0]);
+        add(r0 + SUM_AHEAD, rows[1]);
     }
     if (!in || now >= (uint32_t)p.V) return;
     const bool goes_on = first + n < p.rows && after == now;
@@ -358,15 +380,15 @@ void embedding_join_kernel(SumArgs p)
 {
     __shared__ float sums[JOIN_WAVES][64][9];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t block = blockIdx.x / p.slabs, next = (block + 1) * BLOCK;
+    const int64_t block = blockIdx.x / p.slabs, next = (block + 1) * p.block;
     if (next >= p.rows) return;
     const uint32_t token = p.sorted[next - 1];
     if (token >= (uint32_t)p.V || p.sorted[next] != token) return;             // no token goes on,
-    if (block * BLOCK > 0 && p.sorted[block * BLOCK] == token && p.sorted[block * BLOCK - 1] == token) return;          // or none that begins here
+    if (block > 0 && p.sorted[block * p.block] == token && p.sorted[block * p.block - 1] == token) return;          // or none that begins here
     int64_t lo = block + 1, hi = p.blocks;                     // the last block that begins with it: 64 at once
     while (hi - lo > 1) {
         const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
-        const int64_t last = lo + step * (__popcll(__ballot(at < hi && p.sorted[min(at, hi - 1) * BLOCK] == token)) - 1);
+        const int64_t last = lo + step * (__popcll(__ballot(at < hi && p.sorted[min(at, hi - 1) * p.block] == token)) - 1);
         hi = min(hi, last + step);
         lo = last;
     }
@@ -396,6 +418,8 @@ void embedding_join_kernel(SumArgs p)
 }
 
 struct SortPlan {
+    int block;                        // rows that a wave sums: 32, or 16 where there would be fewer than two waves a SIMD (7001 rows of 1032: 14.8 us for the
+                                      // sums and their joining, 12.7; 16384 rows of 4096 236 and 241)
     int passes, blocks;
     bool twice;                       // sorted in more than one launch: keys and order twice in the workspace
     size_t counts, part, bytes;       // where these lie there
@@ -404,6 +428,7 @@ struct SortPlan {
 SortPlan sort_plan(const Vocab &v, int64_t rows)
 {
     SortPlan p = {};
+    p.block = rows * ((v.C + 511) / 512) < 2048 * 32 ? 16 : 32;
     p.twice = rows > RANK_BLOCK;
     if (rows > MERGED) {
         while (((int64_t)1 << (8 * p.passes)) <= v.V) ++p.passes;              // (V itself stands for what is no token)
@@ -412,7 +437,7 @@ SortPlan sort_plan(const Vocab &v, int64_t rows)
     const size_t one = align_up((size_t)rows * 4, 256);
     p.counts = one * (p.twice ? 4 : 2);
     p.part = p.counts + (p.passes ? align_up((size_t)p.blocks * DIGITS * 4, 256) : 0);
-    p.bytes = p.part + align_up((size_t)((rows + BLOCK - 1) / BLOCK) * 2 * v.C * 4, 256);
+    p.bytes = p.part + align_up((size_t)((rows + p.block - 1) / p.block) * 2 * v.C * 4, 256);
     return p;
 }
 
@@ -460,7 +485,7 @@ int launch_embedding_grad(const Vocab &v, const Rows16 &dy, const int32_t *ids, 
     if (rows > 0 && !plan.passes) {
         const dim3 grid((unsigned)((rows + 63) / 64));
         embedding_rank_kernel<<<grid, 64 * RANK_WAVES, 0, s>>>((const uint32_t *)ids, (int)rows, plan.twice ? other : sorted, plan.twice ? other_order : order);
-        if (plan.twice) embedding_merge_kernel<<<grid, 64 * RANK_WAVES, 0, s>>>(other, other_order, (int)rows, sorted, order);
+        if (plan.twice) embedding_merge_kernel<<<grid, 64 * MERGE_WAVES, 0, s>>>(other, other_order, (int)rows, sorted, order);
         const int rc = check_launch();
         if (rc != SNN_OK) return rc;
     }
@@ -482,7 +507,8 @@ int launch_embedding_grad(const Vocab &v, const Rows16 &dy, const int32_t *ids, 
     SumArgs p = {};
     p.dy = dy.p; p.lddy = dy.ld; p.rows = rows; p.sorted = sorted; p.order = order;
     p.V = v.V; p.C = v.C; p.slabs = (v.C + 511) / 512;
-    p.blocks = (rows + BLOCK - 1) / BLOCK;
+    p.block = plan.block;
+    p.blocks = (rows + p.block - 1) / p.block;
     p.scale = scale; p.dtable = dtable; p.accumulate = accumulate;
     p.part = (float *)((char *)ws + plan.part);
     return v.dtype == SNN_DTYPE_BF16 ? launch_sums<__bf16>(p, s) : launch_sums<_Float16>(p, s);

@@ -24,7 +24,7 @@ __device__ inline bool row_counts(const Targets &t, int V, int64_t row, int lane
     return __any(some);
 }
 
-// Flags of rows with a teacher, a wave each; and the outputs of what does not count.
+// Flags of rows with a teacher, a wave each; and the outputs of what does not count.  (For a few rows the list's kernel finds out itself.)
 __global__ __launch_bounds__(256)
 void loss_flags_kernel(Targets t, int V, int rows, uint8_t *__restrict__ flags, float *__restrict__ loss, float *__restrict__ lse, float *__restrict__ picked)
 {
@@ -56,11 +56,10 @@ __device__ inline int best_cut(const Cut &c, int count, int lane)
     return __builtin_ctzll(__ballot(cost == least)) + 1;
 }
 
-// The rows that count, in their order, and each row's place among them (-1: none).  One workgroup.  flags = nullptr: by the targets.
+// The rows that count, in their order, and each row's place among them (-1: none).  One workgroup.  flags = nullptr: found out here.
 __global__ __launch_bounds__(1024)
-void loss_list_kernel(const int32_t *__restrict__ ids, const uint8_t *__restrict__ flags, const float *__restrict__ g, float temperature, int rows, int V,
-                      bool scaled, Cut rows_cut, Cut table_cut, LossHead *__restrict__ head, int *__restrict__ list, int *__restrict__ place,
-                      float *__restrict__ loss, float *__restrict__ lse)
+void loss_list_kernel(Targets t, const uint8_t *__restrict__ flags, const float *__restrict__ g, int rows, int V, bool scaled, Cut rows_cut, Cut table_cut,
+                      LossHead *__restrict__ head, int *__restrict__ list, int *__restrict__ place, float *__restrict__ loss, float *__restrict__ lse)
 {
     __shared__ int waves[16];
     __shared__ float tops[16];
@@ -69,9 +68,16 @@ void loss_list_kernel(const int32_t *__restrict__ ids, const uint8_t *__restrict
     float top = 0.0f;
     for (int r0 = 0; r0 < rows; r0 += 1024) {
         const int r = r0 + threadIdx.x;
-        bool counts = r < rows && (flags ? flags[r] != 0 : listed(ids[r], V));
+        bool counts = false;
+        if (r < rows) {
+            if (flags) counts = flags[r] != 0;
+            else if (!t.logits) counts = listed(t.ids[r], V);
+            else
+#pragma unroll 4
+                for (int k = 0; k < t.k; ++k) counts |= listed(t.ids[(int64_t)r * t.k + k], V) && !(t.logits[(int64_t)r * t.k + k] == -INFINITY);
+        }
         if (g && counts) {
-            const float v = g[r] / temperature;
+            const float v = g[r] / t.temperature;
             counts = v != 0.0f;
             if (fabsf(v) < INFINITY) top = fmaxf(top, fabsf(v));
         }
@@ -170,12 +176,14 @@ void loss_gather_kernel(GatherArgs p)
         top = fmaxf(top, logit[e]);
     }
 #pragma unroll
-    for (int f = 0; f < E; ++f)
-        for (int l = 0; l < min(64, k - 64 * f); ++l) {
-            const uint32_t other = __builtin_amdgcn_readlane(id[f], l);
+    for (int e = 0; e < E; ++e)
+        if (64 * e < k)
 #pragma unroll
-            for (int e = 0; e < E; ++e) rank[e] += other < id[e] || (other == id[e] && l + 64 * f < lane + 64 * e) ? 1 : 0;
-        }
+            for (int f = 0; f < E; ++f)
+                for (int l = 0; l < min(64, k - 64 * f); ++l) {
+                    const uint32_t other = __builtin_amdgcn_readlane(id[f], l);
+                    rank[e] += other < id[e] || (other == id[e] && l + 64 * f < lane + 64 * e) ? 1 : 0;
+                }
     if (p.q) {
 #pragma unroll
         for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
@@ -198,11 +206,11 @@ void loss_gather_kernel(GatherArgs p)
     }
     __builtin_amdgcn_wave_barrier();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    const int widest = 1 << (31 - __builtin_clz(k));
     for (int64_t b = lane; b < p.start_ld; b += 64) {
         const int64_t first = b * LIST_BLOCK;
         int lo = 0;
-#pragma unroll
-        for (int step = MOST_LISTED; step; step >>= 1)
+        for (int step = widest; step; step >>= 1)
             if (lo + step <= k && mine[lo + step - 1] < first) lo += step;
         p.start[at * p.start_ld + b] = (uint16_t)lo;
     }
@@ -317,7 +325,7 @@ void loss_join_kernel(JoinArgs p)
 // The parts of a gradient's eight channels in their order.
 __device__ inline void sum_parts(const float *from, int64_t split, int splits, float *sum)
 {
-#pragma unroll 4
+#pragma unroll 8
     for (int s = 0; s < splits; ++s) {
         const f32x4 a = *(const f32x4 *)(from + s * split), b = *(const f32x4 *)(from + s * split + 4);
 #pragma unroll
@@ -328,48 +336,42 @@ __device__ inline void sum_parts(const float *from, int64_t split, int splits, f
     }
 }
 
-// Gradients of rows from their parts: a wave a row.
+// Gradients of rows from their parts: a wave 512 channels of a row.
 template <class T>
 __global__ __launch_bounds__(256)
 void loss_rows_kernel(const float *__restrict__ part, int64_t split, int C, const LossHead *__restrict__ head, const int *__restrict__ list,
                       T *__restrict__ dx, int64_t lddx)
 {
     using v8 = typename Half<T>::v8;
-    const int lane = threadIdx.x & 63, t = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), count = head->count;
-    if (t >= count) return;
-    const int splits = head->splits_rows;
+    const int t = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), c = (blockIdx.y * 64 + (threadIdx.x & 63)) * 8;
+    if (t >= head->count || c >= C) return;
     const float down = head->down;
-    T *const to = dx + (int64_t)list[t] * lddx;
-    for (int c = lane * 8; c < C; c += 512) {
-        float sum[8] = {};
-        sum_parts(part + (int64_t)t * C + c, split, splits, sum);
-        v8 v;
+    float sum[8] = {};
+    sum_parts(part + (int64_t)t * C + c, split, head->splits_rows, sum);
+    v8 v;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = (T)(sum[k] * down);
-        *(v8 *)(to + c) = v;
-    }
+    for (int k = 0; k < 8; ++k) v[k] = (T)(sum[k] * down);
+    *(v8 *)(dx + (int64_t)list[t] * lddx + c) = v;
 }
 
-// Rows of the table's gradient from their parts (if there are several): a wave a row.
+// Rows of the table's gradient from their parts (if there are several): likewise.
 template <class T>
 __global__ __launch_bounds__(256)
 void loss_table_kernel(const float *__restrict__ part, int64_t split, int n, int C, const LossHead *__restrict__ head, T *__restrict__ dtable,
                        bool accumulate)
 {
     using v8 = typename Half<T>::v8;
-    const int lane = threadIdx.x & 63, v = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int v = blockIdx.x * 4 + (threadIdx.x >> 6), c = (blockIdx.y * 64 + (threadIdx.x & 63)) * 8;
     const int splits = head->splits_table;
-    if (v >= n || splits == 1) return;
+    if (v >= n || c >= C || splits == 1) return;
     const float down = head->down;
-    for (int c = lane * 8; c < C; c += 512) {
-        float sum[8] = {};
-        sum_parts(part + (int64_t)v * C + c, split, splits, sum);
-        v8 *const to = (v8 *)(dtable + (int64_t)v * C + c), had = accumulate ? *to : v8{};
-        v8 w;
+    float sum[8] = {};
+    sum_parts(part + (int64_t)v * C + c, split, splits, sum);
+    v8 *const to = (v8 *)(dtable + (int64_t)v * C + c), had = accumulate ? *to : v8{};
+    v8 w;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = (T)(accumulate ? fmaf(sum[k], down, (float)had[k]) : sum[k] * down);
-        *to = w;
-    }
+    for (int k = 0; k < 8; ++k) w[k] = (T)(accumulate ? fmaf(sum[k], down, (float)had[k]) : sum[k] * down);
+    *to = w;
 }
 
 // ---- plans -------------------------------------------------------------------------------------------------------
@@ -482,12 +484,13 @@ LossPlan loss_plan(const Vocab &v, int64_t rows, int k, bool teacher, bool backw
 int launch_rows(const Vocab &v, const LossPlan &plan, const Rows16 &x, int64_t rows, const Targets &t, const float *lse, const float *dloss, void *dx,
                 int64_t lddx, float *loss, float *lse_out, float *picked, char *ws, hipStream_t s)
 {
-    uint8_t *const flags = t.logits ? (uint8_t *)(ws + plan.flags) : nullptr;
+    // (333 rows of 11: 7.1 us for the two launches, 5.5 for one)
+    uint8_t *const flags = t.logits && (!dloss || rows * t.k > 16384) ? (uint8_t *)(ws + plan.flags) : nullptr;
     LossHead *const head = (LossHead *)ws;
     int *const list = (int *)(ws + plan.list), *const place = (int *)(ws + plan.place);
     const unsigned blocks = (unsigned)((rows + 3) / 4);
     if (flags && rows) loss_flags_kernel<<<dim3(blocks), 256, 0, s>>>(t, v.V, (int)rows, flags, loss, lse_out, picked);
-    loss_list_kernel<<<1, 1024, 0, s>>>(t.ids, flags, dloss, t.temperature, (int)rows, v.V, dloss && v.dtype == SNN_DTYPE_F16, plan.rows_cut, plan.table_cut,
+    loss_list_kernel<<<1, 1024, 0, s>>>(t, flags, dloss, (int)rows, v.V, dloss && v.dtype == SNN_DTYPE_F16, plan.rows_cut, plan.table_cut,
                                           head, list, place, loss, lse_out);
     if (rows) {
         GatherArgs g = {};
@@ -544,7 +547,7 @@ int launch_loss_forward(const Vocab &v, const Rows16 &x, int64_t rows, const Row
     j.pick = (const float *)(ws + plan.pick);
     j.loss = loss; j.lse = lse; j.picked = picked;
     if (rows <= 256) loss_join_kernel<1><<<dim3((unsigned)rows), 256, 0, s>>>(j);
-    else if (t.logits) loss_join_kernel<8><<<dim3((unsigned)((rows + 7) / 8)), 256, 0, s>>>(j);
+    else if (t.logits) loss_join_kernel<4><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, s>>>(j);
     else loss_join_kernel<32><<<dim3((unsigned)((rows + 31) / 32)), 256, 0, s>>>(j);
     return check_launch();
 }
@@ -593,7 +596,7 @@ int launch_loss_backward(const Vocab &v, const Rows16 &x, int64_t rows, const Ro
             w.most_splits = plan.most_splits_table;
             if ((rc = launch_vocab_tiles(TABLE, plan.form_table, v.dtype, w, s)) != SNN_OK) return rc;
             if (w.most_splits > 1) {
-                const dim3 grid((unsigned)((n + 3) / 4));
+                const dim3 grid((unsigned)((n + 3) / 4), (unsigned)((v.C + 511) / 512));
                 void *const to = (char *)dtable + v0 * v.C * 2;
                 if (v.dtype == SNN_DTYPE_BF16)
                     loss_table_kernel<__bf16><<<grid, 256, 0, s>>>(w.out, w.out_split, n, v.C, w.head, (__bf16 *)to, accumulate);
@@ -604,13 +607,13 @@ int launch_loss_backward(const Vocab &v, const Rows16 &x, int64_t rows, const Ro
         }
     }
     if (!dx || rows == 0) return SNN_OK;
-    const unsigned blocks = (unsigned)((rows + 3) / 4);
+    const dim3 grid((unsigned)((rows + 3) / 4), (unsigned)((v.C + 511) / 512));
     const LossHead *const head = (const LossHead *)ws;
     const int *const list = (const int *)(ws + plan.list);
     if (v.dtype == SNN_DTYPE_BF16)
-        loss_rows_kernel<__bf16><<<dim3(blocks), 256, 0, s>>>((const float *)(ws + plan.out), split, v.C, head, list, (__bf16 *)dx, lddx);
+        loss_rows_kernel<__bf16><<<grid, 256, 0, s>>>((const float *)(ws + plan.out), split, v.C, head, list, (__bf16 *)dx, lddx);
     else
-        loss_rows_kernel<_Float16><<<dim3(blocks), 256, 0, s>>>((const float *)(ws + plan.out), split, v.C, head, list, (_Float16 *)dx, lddx);
+        loss_rows_kernel<_Float16><<<grid, 256, 0, s>>>((const float *)(ws + plan.out), split, v.C, head, list, (_Float16 *)dx, lddx);
     return check_launch();
 }
 
