@@ -681,11 +681,11 @@ typedef struct snn_vocab_desc {
 /*
  * Rows of tokens, and the table's gradient (the rows' gradients summed by token):
  *   y[t] = scale * table[ids[t]];     dtable[v] = scale * sum over the t with ids[t] = v of dy[t]
- * each rounded once; with accumulate the sum is added to what dtable holds (and rounded again), and rows of tokens that do not occur stay as they are.
+ * each rounded once; with accumulate the sum is added to what dtable holds before the rounding, and rows of tokens that do not occur stay as they are.
  *   table   device, [V] rows of C;   ids   device, int32 [rows];   y, dy   device, rows of C
  *   dtable  device, [V][C], 16-byte aligned; without accumulate fully overwritten (zeros for tokens that do not occur)
  *   workspace  device, >= snn_embedding_grad_workspace_bytes(desc, rows) bytes, 256-byte aligned
- * Errors: INVALID_ARG; UNSUPPORTED (2^31 workgroups or more); WORKSPACE; LAUNCH.
+ * Errors: INVALID_ARG; WORKSPACE; LAUNCH.
  */
 int snn_embedding_forward(const snn_vocab_desc *desc, const void *table, int64_t ldt, const int32_t *ids, int64_t rows, float scale, void *y, int64_t ldy,
                           void *stream);
@@ -703,7 +703,7 @@ int snn_embedding_grad(const snn_vocab_desc *desc, const void *dy, int64_t lddy,
  *   lse      (backward) as the forward call left it
  *   dx       NULL: not wanted
  *   dtable   device, [V][C], 16-byte aligned, fully overwritten, or with accumulate added to; NULL: not wanted (not both NULL)
- *   workspace  device, >= snn_loss_workspace_bytes(desc, rows, 1, SNN_LOSS_FORWARD or _BACKWARD) bytes, 256-byte aligned.  What it holds
+ *   workspace  device, >= snn_loss_workspace_bytes(desc, rows, 0, SNN_LOSS_FORWARD or _BACKWARD) bytes, 256-byte aligned.  What it holds
  *              of probabilities is a piece of the vocabulary, of at most 512 MiB (256 tokens at least).
  * dz is rounded to desc->dtype before the products (f16: times a power of two that brings the largest |dloss| to 2^14 .. 2^15, so that what is smaller than
  * 2^-40 of that may be lost); dx and dtable are rounded once.
@@ -728,7 +728,8 @@ int snn_cross_entropy_backward(const snn_vocab_desc *desc, const void *x, int64_
  * zero.  A row without a listed token that has a logit above -infinity is none, as above.
  *   ids      device, int32 [rows][k];   logits  device, float [rows][k];   temperature  1/1024 .. 1024
  *   picked   device, float [rows][k]: z[t][ids[t][j]], zeros where not listed and in rows that are none
- *   the rest as for the cross entropy (workspace: k in place of 1).
+ *   the rest as for the cross entropy (workspace: k in place of 0).
+ * Errors: as above, and INVALID_ARG for k or a temperature outside these.
  */
 int snn_distill_forward(const snn_vocab_desc *desc, const void *x, int64_t ldx, int64_t rows, const void *table, int64_t ldt, const int32_t *ids,
                         const float *logits, int k, float temperature, float *loss, float *lse, float *picked, void *workspace, size_t ws_bytes,

@@ -1133,7 +1133,8 @@ def snn_embedding_grad(desc, dy, ids, scale=1.0, dtable=None, accumulate=False, 
 SNN_LOSS_FORWARD, SNN_LOSS_BACKWARD = range(2)
 
 
-def snn_loss_workspace_bytes(desc, rows, k=1, call=SNN_LOSS_FORWARD):
+def snn_loss_workspace_bytes(desc, rows, k=0, call=SNN_LOSS_FORWARD):
+    """k = 0: of the cross entropy; else of the distillation from k tokens a row."""
     return int(lib().snn_loss_workspace_bytes(ctypes.byref(desc), rows, k, call))
 
 
@@ -1174,7 +1175,7 @@ def snn_cross_entropy_backward(desc, x, table, target, lse, dloss, dx=None, dtab
     given = (_one_a_row(target, torch.int32, rows, "target"), _one_a_row(lse, torch.float32, rows, "lse"),
              _one_a_row(dloss, torch.float32, rows, "dloss"))
     dx, pdx, lddx, dtable = _loss_grads(desc, x, dx, dtable, accumulate)
-    workspace = _scratch(workspace, snn_loss_workspace_bytes(desc, rows, 1, SNN_LOSS_BACKWARD), x.device)
+    workspace = _scratch(workspace, snn_loss_workspace_bytes(desc, rows, 0, SNN_LOSS_BACKWARD), x.device)
     _check(lib().snn_cross_entropy_backward(ctypes.byref(desc), px, ldx, rows, *_table(desc, table), *given, pdx, lddx, _ptr(dtable), int(accumulate),
                                             _ptr(workspace), workspace.numel(), _stream()), "snn_cross_entropy_backward")
     return dx, dtable

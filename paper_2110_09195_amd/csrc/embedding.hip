@@ -445,7 +445,7 @@ template <class T>
 int launch_sums(const SumArgs &p, hipStream_t s)
 {
     const int64_t sums = (p.blocks * p.slabs + 3) / 4, fill = p.accumulate ? 0 : (p.V + FILL_ROWS - 1) / FILL_ROWS, joins = p.blocks * p.slabs;
-    if (sums + fill >= ((int64_t)1 << 31) || joins >= ((int64_t)1 << 31)) return SNN_ERR_UNSUPPORTED;
+    static_assert(((int64_t)1 << 28) / 32 * (65536 / 512) + ((1 << 24) + FILL_ROWS - 1) / FILL_ROWS < ((int64_t)1 << 31), "a grid for every call");
     if (sums + fill > 0) {
         embedding_sum_kernel<T><<<dim3((unsigned)(sums + fill)), 256, 0, s>>>(p, (unsigned)sums);
         const int rc = check_launch();

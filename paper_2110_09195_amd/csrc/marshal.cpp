@@ -541,7 +541,7 @@ PyObject *loss_forward(PyObject *const *a)
     const at::Tensor *const ids = c.values(a[3], at::kInt, TEACHER ? -1 : rows), *const logits = TEACHER ? c.values(a[4], at::kFloat, -1) : nullptr;
     float temperature = 1.0f;
     if (!c.ok || (TEACHER && (!number(a[5], temperature) || ids->dim() != 2 || ids->size(0) != rows || logits->sizes() != ids->sizes()))) Py_RETURN_FALSE;
-    const int64_t k = TEACHER ? ids->size(1) : 1;
+    const int64_t k = TEACHER ? ids->size(1) : 0;
     if (k > 256) Py_RETURN_FALSE;
     PyObject *const *const o = a + (TEACHER ? 6 : 4);
     at::Tensor loss = c.out(o[0], {rows}, at::kFloat, *x), lse = c.out(o[1], {rows}, at::kFloat, *x), picked;
@@ -578,7 +578,7 @@ PyObject *loss_backward(PyObject *const *a)
     const at::Tensor *const ids = c.values(a[3], at::kInt, TEACHER ? -1 : rows), *const logits = TEACHER ? c.values(a[4], at::kFloat, -1) : nullptr;
     float temperature = 1.0f;
     if (!c.ok || (TEACHER && (!number(a[5], temperature) || ids->dim() != 2 || ids->size(0) != rows || logits->sizes() != ids->sizes()))) Py_RETURN_FALSE;
-    const int64_t k = TEACHER ? ids->size(1) : 1;
+    const int64_t k = TEACHER ? ids->size(1) : 0;
     if (k > 256) Py_RETURN_FALSE;
     PyObject *const *const o = a + (TEACHER ? 6 : 4);
     const at::Tensor *const lse = c.values(o[0], at::kFloat, rows), *const dloss = c.values(o[1], at::kFloat, rows);

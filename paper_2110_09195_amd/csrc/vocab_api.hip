@@ -32,8 +32,8 @@ bool temperature_ok(float t) { return t >= 1.0f / 1024 && t <= 1024.0f; }       
 
 bool targets_ok(const Targets &t, int64_t rows)
 {
-    if (t.k < 1 || t.k > 256 || !temperature_ok(t.temperature)) return false;
-    return words_ok(t.ids, rows) && (!t.logits || words_ok(t.logits, rows));
+    if (t.k < 0 || t.k > 256 || !temperature_ok(t.temperature)) return false;
+    return words_ok(t.ids, rows) && (t.k == 0 || words_ok(t.logits, rows));
 }
 
 int forward_call(const snn_vocab_desc *desc, const void *x, int64_t ldx, int64_t rows, const void *table, int64_t ldt, const Targets &t, float *loss,
@@ -41,9 +41,9 @@ int forward_call(const snn_vocab_desc *desc, const void *x, int64_t ldx, int64_t
 {
     if (!desc_ok(desc) || !count_ok(rows) || !rows_ok(x, ldx, desc->C, rows) || !rows_ok(table, ldt, desc->C, 1) || !targets_ok(t, rows))
         return SNN_ERR_INVALID_ARG;
-    if (!words_ok(loss, rows) || !words_ok(lse, rows) || (t.logits && !words_ok(picked, rows))) return SNN_ERR_INVALID_ARG;
+    if (!words_ok(loss, rows) || !words_ok(lse, rows) || (t.k && !words_ok(picked, rows))) return SNN_ERR_INVALID_ARG;
     const Vocab v = vocab(desc);
-    if (!workspace_ok(workspace, ws_bytes, loss_workspace_bytes(v, rows, t.k, false))) return SNN_ERR_WORKSPACE;
+    if (!workspace_ok(workspace, ws_bytes, loss_workspace_bytes(v, rows, t, false))) return SNN_ERR_WORKSPACE;
     if (rows == 0) return SNN_OK;
     return launch_loss_forward(v, {x, ldx}, rows, {table, ldt}, t, loss, lse, picked, workspace, (hipStream_t)stream);
 }
@@ -57,7 +57,7 @@ int backward_call(const snn_vocab_desc *desc, const void *x, int64_t ldx, int64_
     if (!words_ok(lse, rows) || !words_ok(dloss, rows) || (!dx && !dtable) || !aligned(dtable, 16)) return SNN_ERR_INVALID_ARG;
     if (dx && !rows_ok(dx, lddx, desc->C, rows)) return SNN_ERR_INVALID_ARG;
     const Vocab v = vocab(desc);
-    if (!workspace_ok(workspace, ws_bytes, loss_workspace_bytes(v, rows, t.k, true))) return SNN_ERR_WORKSPACE;
+    if (!workspace_ok(workspace, ws_bytes, loss_workspace_bytes(v, rows, t, true))) return SNN_ERR_WORKSPACE;
     if (rows == 0 && (!dtable || accumulate)) return SNN_OK;
     return launch_loss_backward(v, {x, ldx}, rows, {table, ldt}, t, lse, dloss, dx, lddx, dtable, accumulate != 0, workspace, (hipStream_t)stream);
 }
@@ -93,28 +93,28 @@ int snn_embedding_grad(const snn_vocab_desc *desc, const void *dy, int64_t lddy,
 
 size_t snn_loss_workspace_bytes(const snn_vocab_desc *desc, int64_t rows, int k, int call)
 {
-    if (!desc_ok(desc) || !count_ok(rows) || k < 1 || k > 256 || (call != SNN_LOSS_FORWARD && call != SNN_LOSS_BACKWARD)) return 0;
-    return loss_workspace_bytes(vocab(desc), rows, k, call == SNN_LOSS_BACKWARD);
+    if (!desc_ok(desc) || !count_ok(rows) || k < 0 || k > 256 || (call != SNN_LOSS_FORWARD && call != SNN_LOSS_BACKWARD)) return 0;
+    return loss_workspace_bytes(vocab(desc), rows, {nullptr, nullptr, k, 1.0f}, call == SNN_LOSS_BACKWARD);
 }
 
 int snn_cross_entropy_forward(const snn_vocab_desc *desc, const void *x, int64_t ldx, int64_t rows, const void *table, int64_t ldt,
                               const int32_t *target, float *loss, float *lse, void *workspace, size_t ws_bytes, void *stream)
 {
-    return forward_call(desc, x, ldx, rows, table, ldt, {target, nullptr, 1, 1.0f}, loss, lse, nullptr, workspace, ws_bytes, stream);
+    return forward_call(desc, x, ldx, rows, table, ldt, {target, nullptr, 0, 1.0f}, loss, lse, nullptr, workspace, ws_bytes, stream);
 }
 
 int snn_cross_entropy_backward(const snn_vocab_desc *desc, const void *x, int64_t ldx, int64_t rows, const void *table, int64_t ldt,
                                const int32_t *target, const float *lse, const float *dloss, void *dx, int64_t lddx, void *dtable, int accumulate,
                                void *workspace, size_t ws_bytes, void *stream)
 {
-    return backward_call(desc, x, ldx, rows, table, ldt, {target, nullptr, 1, 1.0f}, lse, dloss, dx, lddx, dtable, accumulate, workspace, ws_bytes, stream);
+    return backward_call(desc, x, ldx, rows, table, ldt, {target, nullptr, 0, 1.0f}, lse, dloss, dx, lddx, dtable, accumulate, workspace, ws_bytes, stream);
 }
 
 int snn_distill_forward(const snn_vocab_desc *desc, const void *x, int64_t ldx, int64_t rows, const void *table, int64_t ldt, const int32_t *ids,
                         const float *logits, int k, float temperature, float *loss, float *lse, float *picked, void *workspace, size_t ws_bytes,
                         void *stream)
 {
-    if (!logits && rows != 0) return SNN_ERR_INVALID_ARG;
+    if (k < 1) return SNN_ERR_INVALID_ARG;
     return forward_call(desc, x, ldx, rows, table, ldt, {ids, logits, k, temperature}, loss, lse, picked, workspace, ws_bytes, stream);
 }
 
@@ -122,7 +122,7 @@ int snn_distill_backward(const snn_vocab_desc *desc, const void *x, int64_t ldx,
                          const float *logits, int k, float temperature, const float *lse, const float *dloss, void *dx, int64_t lddx, void *dtable,
                          int accumulate, void *workspace, size_t ws_bytes, void *stream)
 {
-    if (!logits && rows != 0) return SNN_ERR_INVALID_ARG;
+    if (k < 1) return SNN_ERR_INVALID_ARG;
     return backward_call(desc, x, ldx, rows, table, ldt, {ids, logits, k, temperature}, lse, dloss, dx, lddx, dtable, accumulate, workspace, ws_bytes,
                          stream);
 }

@@ -71,7 +71,7 @@ void loss_list_kernel(Targets t, const uint8_t *__restrict__ flags, const float 
         bool counts = false;
         if (r < rows) {
             if (flags) counts = flags[r] != 0;
-            else if (!t.logits) counts = listed(t.ids[r], V);
+            else if (!t.k) counts = listed(t.ids[r], V);
             else
 #pragma unroll 4
                 for (int k = 0; k < t.k; ++k) counts |= listed(t.ids[(int64_t)r * t.k + k], V) && !(t.logits[(int64_t)r * t.k + k] == -INFINITY);
@@ -155,7 +155,7 @@ void loss_gather_kernel(GatherArgs p)
         p.lse2[at] = p.lse[row] * LOG2E;
         p.gc[at] = p.g[row] / p.t.temperature * p.head->up;
     }
-    if (!p.t.logits) {
+    if (!p.t.k) {
         if (lane == 0) p.ids[at] = p.t.ids[row];
         return;
     }
@@ -270,7 +270,7 @@ void loss_join_kernel(JoinArgs p)
         }
     }
     __syncthreads();
-    if (!p.t.logits) {
+    if (!p.t.k) {
         if (tid >= RT || t0 + tid >= rows) return;
         const int t = t0 + tid, row = p.list ? p.list[t] : t;
         m = stat[0][tid].x;
@@ -392,6 +392,8 @@ struct LossPlan {
     size_t list, place, flags, pick, ids, of_ids, start, lse2, g, xc, part, probs, out, out_table, bytes;
 };
 
+// (of the gradients, whose parts are few where tiles are many, there are fewer)
+constexpr int64_t MOST_TILES = (int64_t)1 << 30;
 int64_t tiles_of(int form, int64_t m, int64_t n) { return (m + tile_m(form) - 1) / tile_m(form) * ((n + tile_n(form) - 1) / tile_n(form)); }
 
 // Tiles of logits of `tokens` x `rows`: the form whose turns of the chip cost least, in turns of 256 x 256.
@@ -427,9 +429,11 @@ int gradient_form(int64_t m, int64_t n, int64_t depth, int most)
     return cost[1] < cost[0] ? TILE_128 : TILE_256;
 }
 
-LossPlan loss_plan(const Vocab &v, int64_t rows, int k, bool teacher, bool backward)
+LossPlan loss_plan(const Vocab &v, int64_t rows, const Targets &t, bool backward)
 {
     LossPlan p = {};
+    const bool teacher = t.k > 0;
+    const int k = teacher ? t.k : 1;
     p.ld = (rows + 63) / 64 * 64;
     // (two launches and a copy pay where the product takes longer than some 50 us)
     p.gather = backward || (rows > 256 && (double)rows * v.V * v.C > 3e10);
@@ -485,7 +489,7 @@ int launch_rows(const Vocab &v, const LossPlan &plan, const Rows16 &x, int64_t r
                 int64_t lddx, float *loss, float *lse_out, float *picked, char *ws, hipStream_t s)
 {
     // (333 rows of 11: 7.1 us for the two launches, 5.5 for one)
-    uint8_t *const flags = t.logits && (!dloss || rows * t.k > 16384) ? (uint8_t *)(ws + plan.flags) : nullptr;
+    uint8_t *const flags = t.k && (!dloss || rows * t.k > 16384) ? (uint8_t *)(ws + plan.flags) : nullptr;
     LossHead *const head = (LossHead *)ws;
     int *const list = (int *)(ws + plan.list), *const place = (int *)(ws + plan.place);
     const unsigned blocks = (unsigned)((rows + 3) / 4);
@@ -511,25 +515,26 @@ int launch_rows(const Vocab &v, const LossPlan &plan, const Rows16 &x, int64_t r
 
 }  // namespace
 
-size_t loss_workspace_bytes(const Vocab &v, int64_t rows, int k, bool backward) { return loss_plan(v, rows, k, true, backward).bytes; }
+size_t loss_workspace_bytes(const Vocab &v, int64_t rows, const Targets &t, bool backward) { return loss_plan(v, rows, t, backward).bytes; }
 
 int launch_loss_forward(const Vocab &v, const Rows16 &x, int64_t rows, const Rows16 &table, const Targets &t, float *loss, float *lse, float *picked,
                         void *workspace, hipStream_t s)
 {
-    const LossPlan plan = loss_plan(v, rows, t.k, t.logits != nullptr, false);
+    const LossPlan plan = loss_plan(v, rows, t, false);
+    if (tiles_of(plan.form, v.V, rows) >= MOST_TILES) return SNN_ERR_UNSUPPORTED;
     char *const ws = (char *)workspace;
     TilesArgs p = {};
     p.a = table.p; p.lda = table.ld; p.M = v.V;
     p.b = x.p; p.ldb = x.ld; p.N = (int)rows; p.K = v.C;
     p.c = LOG2E / t.temperature;
-    p.ids = t.ids; p.k = t.k;
+    p.ids = t.ids; p.k = t.k ? t.k : 1;
     if (plan.gather) {
         const int rc = launch_rows(v, plan, x, rows, t, nullptr, nullptr, nullptr, 0, loss, lse, picked, ws, s);
         if (rc != SNN_OK) return rc;
         p.head = (const LossHead *)ws;
         p.b = ws + plan.xc; p.ldb = v.C;
         p.ids = (const int32_t *)(ws + plan.ids);
-        if (t.logits) {
+        if (t.k) {
             p.start = (const uint16_t *)(ws + plan.start); p.start_ld = plan.start_ld;
             p.slot = (const int32_t *)(ws + plan.of_ids);
         }
@@ -537,7 +542,7 @@ int launch_loss_forward(const Vocab &v, const Rows16 &x, int64_t rows, const Row
     const int *const list = plan.gather ? (const int *)(ws + plan.list) : nullptr;
     p.part = (float2 *)(ws + plan.part); p.part_ld = plan.ld;
     // (targets' logits stay in the workspace, by place)
-    p.picked = t.logits ? picked : (float *)(ws + plan.pick);
+    p.picked = t.k ? picked : (float *)(ws + plan.pick);
     p.list = list;
     const int rc = launch_vocab_tiles(STATS, plan.form, v.dtype, p, s);
     if (rc != SNN_OK) return rc;
@@ -547,7 +552,7 @@ int launch_loss_forward(const Vocab &v, const Rows16 &x, int64_t rows, const Row
     j.pick = (const float *)(ws + plan.pick);
     j.loss = loss; j.lse = lse; j.picked = picked;
     if (rows <= 256) loss_join_kernel<1><<<dim3((unsigned)rows), 256, 0, s>>>(j);
-    else if (t.logits) loss_join_kernel<4><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, s>>>(j);
+    else if (t.k) loss_join_kernel<4><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, s>>>(j);
     else loss_join_kernel<32><<<dim3((unsigned)((rows + 31) / 32)), 256, 0, s>>>(j);
     return check_launch();
 }
@@ -555,7 +560,8 @@ int launch_loss_forward(const Vocab &v, const Rows16 &x, int64_t rows, const Row
 int launch_loss_backward(const Vocab &v, const Rows16 &x, int64_t rows, const Rows16 &table, const Targets &t, const float *lse, const float *dloss,
                          void *dx, int64_t lddx, void *dtable, bool accumulate, void *workspace, hipStream_t s)
 {
-    const LossPlan plan = loss_plan(v, rows, t.k, t.logits != nullptr, true);
+    const LossPlan plan = loss_plan(v, rows, t, true);
+    if (tiles_of(plan.form, plan.piece, rows) >= MOST_TILES) return SNN_ERR_UNSUPPORTED;
     char *const ws = (char *)workspace;
     int rc = launch_rows(v, plan, x, rows, t, lse, dloss, dx, lddx, nullptr, nullptr, nullptr, ws, s);
     if (rc != SNN_OK) return rc;
@@ -569,8 +575,8 @@ int launch_loss_backward(const Vocab &v, const Rows16 &x, int64_t rows, const Ro
         p.b = ws + plan.xc; p.ldb = v.C; p.N = (int)rows; p.K = v.C;
         p.c = LOG2E / t.temperature;
         p.v0 = (int)v0;
-        p.ids = (const int32_t *)(ws + plan.ids); p.k = t.k;
-        if (t.logits) {
+        p.ids = (const int32_t *)(ws + plan.ids); p.k = t.k ? t.k : 1;
+        if (t.k) {
             p.q = (const float *)(ws + plan.of_ids);
             p.start = (const uint16_t *)(ws + plan.start); p.start_ld = plan.start_ld;
         }

@@ -437,7 +437,6 @@ int launch_tiles(const TilesArgs &p, hipStream_t s)
     const int rc = grant_dynamic_lds((const void *)kernel, LDS, grant);
     if (rc != SNN_OK) return rc;
     const int64_t tiles = (int64_t)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN) * (KIND == ROWS || KIND == TABLE ? p.most_splits : 1);
-    if (tiles >= ((int64_t)1 << 30)) return SNN_ERR_UNSUPPORTED;
     if (tiles == 0) return SNN_OK;
     kernel<<<dim3((unsigned)((tiles + 7) / 8 * 8)), 64 * WAVES, LDS, s>>>(p);
     return check_launch();

@@ -70,7 +70,7 @@ def test_workspaces(name):
 
 @pytest.mark.parametrize("name", ["snn_distill_forward", "snn_distill_backward"])
 def test_teachers(name):
-    for bad in (dict(k=0), dict(k=257), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("nan")), dict(temperature=float("inf")),
+    for bad in (dict(k=0), dict(k=-1), dict(k=257), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("nan")), dict(temperature=float("inf")),
                 dict(temperature=2000.0), dict(temperature=2.0 ** -11)):
         assert call(name, **bad) == BAD, bad
 
@@ -79,12 +79,15 @@ def test_sizes_of_workspaces():
     L = B.lib()
     assert L.snn_embedding_grad_workspace_bytes(desc(V=0), 8) == 0 and L.snn_embedding_grad_workspace_bytes(desc(), -1) == 0
     assert L.snn_embedding_grad_workspace_bytes(desc(), 0) > 0
-    for bad in ((desc(C=60), 8, 1, 0), (desc(), -1, 1, 0), (desc(), 8, 0, 0), (desc(), 8, 257, 1), (desc(), 8, 1, 2), (None, 8, 1, 0)):
+    for bad in ((desc(C=60), 8, 1, 0), (desc(), -1, 1, 0), (desc(), 8, -1, 0), (desc(), 8, 257, 1), (desc(), 8, 0, 2), (None, 8, 0, 0)):
         assert L.snn_loss_workspace_bytes(*bad) == 0, bad
+    # 2^30 tiles of logits: refused before anything is enqueued (the size is answered, and no such memory exists)
+    for name in ("snn_cross_entropy_forward", "snn_distill_forward"):
+        assert call(name, desc=desc(V=1 << 24), rows=(1 << 28) - 1) == B.SNN_ERR_UNSUPPORTED
     # no logits of the whole vocabulary, however many rows
     rows, V = 65536, 1 << 18
-    assert L.snn_loss_workspace_bytes(desc(V=V), rows, 1, 0) < rows * V // 8
-    assert L.snn_loss_workspace_bytes(desc(V=V), rows, 1, 1) < (1 << 30)
+    assert L.snn_loss_workspace_bytes(desc(V=V), rows, 0, 0) < rows * V // 8
+    assert L.snn_loss_workspace_bytes(desc(V=V), rows, 0, 1) < (1 << 30)
 
 
 def test_binding_checks_its_tensors():
