@@ -379,7 +379,7 @@ void loss_table_kernel(const float *__restrict__ part, int64_t split, int n, int
 // What a piece of the vocabulary may hold of probabilities, in bytes (at least 256 tokens are a piece, at most all)
 constexpr size_t PIECE_BYTES = (size_t)512 << 20;
 // and the parts of the rows' gradients beyond the first
-constexpr size_t PARTS_BYTES = (size_t)64 << 20;
+constexpr size_t PARTS_BYTES = (size_t)256 << 20;
 
 struct LossPlan {
     bool gather;                      // rows that count are copied next to each other
@@ -399,7 +399,7 @@ int64_t tiles_of(int form, int64_t m, int64_t n) { return (m + tile_m(form) - 1)
 // Tiles of logits of `tokens` x `rows`: the form whose turns of the chip cost least, in turns of 256 x 256.
 int logits_form(int64_t tokens, int64_t rows)
 {
-    constexpr float TURN[] = {1.0f, 0.8f, 0.45f, 0.33f, 0.35f}, HALF[] = {1.0f, 0.6f, 0.45f, 0.33f, 0.22f};       // (no CU with two)
+    constexpr float TURN[] = {1.0f, 0.68f, 0.46f, 0.34f, 0.35f}, HALF[] = {1.0f, 0.55f, 0.46f, 0.36f, 0.22f};       // (no CU with two)
     int best = 0;
     float least = 0.0f;
     for (int f = 0; f < TILE_FORMS; ++f) {
@@ -413,20 +413,26 @@ int logits_form(int64_t tokens, int64_t rows)
     return best;
 }
 
-// Tiles of a gradient [n][m], its sums over `depth` cut into at most `most` parts: likewise.
-int gradient_form(int64_t m, int64_t n, int64_t depth, int most)
+// Tiles of a gradient [n][m], its sums over `depth` cut into at most `most` parts: likewise; most: in how many.
+int gradient_form(int64_t m, int64_t n, int64_t depth, int &most)
 {
     float cost[2];
+    int parts[2];
     const int steps = (int)((depth + 63) / 64);
     for (int f = 0; f < 2; ++f) {
         const int64_t tiles = tiles_of(f, m, n);
-        const float turn[] = {1.0f, 0.8f}, half[] = {1.0f, 0.6f};
+        const float turn[] = {1.0f, 0.68f}, half[] = {1.0f, 0.55f};
         for (int s = 1; s == 1 || (tiles < tile_slots(f) && s <= most && s <= (steps + 3) / 4); ++s) {
             const float c = (tiles * s <= 256 ? half[f] : turn[f]) * split_cost(s, (int)(tiles < (1 << 24) ? tiles : 1 << 24), tile_slots(f), steps);
-            if (s == 1 || c < cost[f]) cost[f] = c;
+            if (s == 1 || c < cost[f]) {
+                cost[f] = c;
+                parts[f] = s;
+            }
         }
     }
-    return cost[1] < cost[0] ? TILE_128 : TILE_256;
+    const int form = cost[1] < cost[0] ? TILE_128 : TILE_256;
+    most = parts[form];
+    return form;
 }
 
 LossPlan loss_plan(const Vocab &v, int64_t rows, const Targets &t, bool backward)
@@ -467,10 +473,12 @@ LossPlan loss_plan(const Vocab &v, int64_t rows, const Targets &t, bool backward
         auto parts = [&](size_t one) { return (int)(one * MOST_SPLITS <= PARTS_BYTES ? MOST_SPLITS : one * 2 > PARTS_BYTES ? 1 : PARTS_BYTES / one); };
         const size_t part = (size_t)rows * v.C * 4, part_table = (size_t)p.piece * v.C * 4;
         p.most_splits = parts(part);
+        // (how many rows count is not known here; the fewer, the more parts are worth while)
+        int ignored = p.most_splits;
+        p.form_rows = gradient_form(v.C, rows, p.piece, ignored);
+        // (and here the fewer)
         p.most_splits_table = parts(part_table);
-        p.form_rows = gradient_form(v.C, rows, p.piece, p.most_splits);
         p.form_table = gradient_form(v.C, p.piece, rows, p.most_splits_table);
-        if (tiles_of(p.form_table, v.C, p.piece) >= tile_slots(p.form_table)) p.most_splits_table = 1;
         const int tokens = v.V < p.piece ? v.V : p.piece;
         p.rows_cut = {(v.C + tile_m(p.form_rows) - 1) / tile_m(p.form_rows), tile_n(p.form_rows), tile_slots(p.form_rows), (tokens + 63) / 64, p.most_splits};
         p.table_cut = {(int)tiles_of(p.form_table, v.C, tokens), 0, tile_slots(p.form_table), 0, p.most_splits_table};
