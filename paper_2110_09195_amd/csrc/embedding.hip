@@ -70,8 +70,15 @@ void embedding_rank_kernel(const uint32_t *__restrict__ ids, int rows, uint32_t 
     __shared__ __align__(16) uint32_t tokens[RANK_BLOCK];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i0 = blockIdx.x * 64, i = i0 + lane, first = i0 / RANK_BLOCK * RANK_BLOCK, n = min(RANK_BLOCK, rows - first);
+    constexpr int EACH = RANK_BLOCK / (64 * RANK_WAVES);
+    uint32_t v[EACH];
 #pragma unroll
-    for (int k = 0; k < RANK_BLOCK; k += 64 * RANK_WAVES) tokens[k + threadIdx.x] = k + (int)threadIdx.x < n ? ids[first + k + threadIdx.x] : ~0u;
+    for (int k = 0; k < EACH; ++k) v[k] = ids[first + min(k * 64 * RANK_WAVES + (int)threadIdx.x, n - 1)];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        const int at = k * 64 * RANK_WAVES + threadIdx.x;
+        tokens[at] = at < n ? v[k] : ~0u;
+    }
     __syncthreads();
     const uint32_t mine = i < rows ? tokens[i - first] : 0;
     constexpr int SHARE = RANK_BLOCK / RANK_WAVES;             // a multiple of 64: a wave's tokens are all before, all behind or among the workgroup's
@@ -115,16 +122,26 @@ void embedding_merge_kernel(const uint32_t *__restrict__ keys, const int *__rest
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i0 = blockIdx.x * 64, i = i0 + lane, own = i0 / RANK_BLOCK, blocks = (rows + RANK_BLOCK - 1) / RANK_BLOCK;
     const uint32_t mine = i < rows ? keys[i] : 0;
+    // (a wave's block goes to LDS first: eleven reads there that wait for each other, not eleven from memory)
+    __shared__ __align__(16) uint32_t block[MERGE_WAVES][RANK_BLOCK];
+    uint32_t *const at = block[wave];
     int below = 0;
     for (int b = wave; b < blocks; b += MERGE_WAVES) {
         if (b == own) continue;
-        const uint32_t *const at = keys + b * RANK_BLOCK;
         const int n = min(RANK_BLOCK, rows - b * RANK_BLOCK);
+        uint32_t v[RANK_BLOCK / 64];
+#pragma unroll
+        for (int k = 0; k < RANK_BLOCK / 64; ++k) v[k] = keys[b * RANK_BLOCK + min(k * 64 + lane, n - 1)];
+#pragma unroll
+        for (int k = 0; k < RANK_BLOCK / 64; ++k) at[k * 64 + lane] = v[k];
+        __builtin_amdgcn_wave_barrier();
         int found = 0;                                         // tokens below, and in earlier blocks the row's own
+#pragma unroll
         for (int step = RANK_BLOCK; step; step >>= 1) {
             const uint32_t other = found + step <= n ? at[found + step - 1] : ~0u;
             if (found + step <= n && (other < mine || (other == mine && b < own))) found += step;
         }
+        __builtin_amdgcn_wave_barrier();
         below += found;
     }
     counts[wave][lane] = below;

@@ -56,6 +56,27 @@ __device__ inline int best_cut(const Cut &c, int count, int lane)
     return __builtin_ctzll(__ballot(cost == least)) + 1;
 }
 
+// What is known once the rows are: by one wave (the cuts, if it is the gradients' call) ...
+__device__ inline void write_cuts(LossHead *head, const Cut &rows_cut, const Cut &table_cut, int count, int lane)
+{
+    if (!rows_cut.slots) return;                               // (a call of no rows at all is told by the same)
+    const int r = best_cut(rows_cut, count, lane), t = best_cut(table_cut, count, lane);
+    if (lane == 0) {
+        head->splits_rows = r;
+        head->splits_table = t;
+    }
+}
+
+// ... and by one lane.  Values of f16 reach from 2^-24 to 2^16: the largest gradient is brought to 2^14 .. 2^15; bf16 has fp32's range.
+__device__ inline float write_head(LossHead *head, int count, float top, bool scaled)
+{
+    const int e = scaled ? piece_exponent(top) : 0;
+    head->count = count;
+    head->up = power_of_two(e);
+    head->down = power_of_two(-e);
+    return power_of_two(e);
+}
+
 // The rows that count, in their order, and each row's place among them (-1: none).  One workgroup.  flags = nullptr: found out here.
 __global__ __launch_bounds__(1024)
 void loss_list_kernel(Targets t, const uint8_t *__restrict__ flags, const float *__restrict__ g, int rows, int V, bool scaled, Cut rows_cut, Cut table_cut,
@@ -99,17 +120,10 @@ void loss_list_kernel(Targets t, const uint8_t *__restrict__ flags, const float 
     top = wave_top(top);
     if (lane == 0) tops[wave] = top;
     __syncthreads();
-    if (wave < 2 && rows_cut.slots) {                          // (the gradients' call, also of no rows at all)
-        const int splits = best_cut(wave ? table_cut : rows_cut, before, lane);
-        if (lane == 0) (wave ? head->splits_table : head->splits_rows) = splits;
-    }
+    if (wave == 1) write_cuts(head, rows_cut, table_cut, before, lane);
     if (threadIdx.x != 0) return;
     for (int w = 1; w < 16; ++w) top = fmaxf(top, tops[w]);
-    // (values of f16 reach from 2^-24 to 2^16: the largest gradient is brought to 2^14 .. 2^15; bf16 has fp32's range)
-    const int e = scaled ? piece_exponent(top) : 0;
-    head->count = before;
-    head->up = power_of_two(e);
-    head->down = power_of_two(-e);
+    write_head(head, before, top, scaled);
 }
 
 constexpr int MOST_LISTED = 256;
@@ -119,8 +133,11 @@ struct GatherArgs {
     const void *x;
     int64_t ldx;
     int rows, V, C;
-    const LossHead *head;
-    const int *place;
+    LossHead *head;
+    const int *place;                 // nullptr: found out here, and the head and the list written (few rows, targets)
+    int *list;
+    Cut rows_cut, table_cut;
+    bool scaled;
     void *xc;
     int32_t *ids;                     // [place][k], a row's in rising order
     int32_t *slot;                    // likewise, forward: their places in the caller's list;
@@ -133,7 +150,8 @@ struct GatherArgs {
     int64_t lddx;
 };
 
-// Rows that count next to each other, with what belongs to them.  A wave a row.
+// Rows that count next to each other, with what belongs to them.  A wave a row.  Of a few rows every wave looks at all of them itself, which saves a launch.
+constexpr int64_t FOUND_HERE = 1024;
 template <class T>
 __global__ __launch_bounds__(256)
 void loss_gather_kernel(GatherArgs p)
@@ -141,7 +159,48 @@ void loss_gather_kernel(GatherArgs p)
     using v8 = typename Half<T>::v8;
     const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= p.rows) return;
-    const int at = __builtin_amdgcn_readfirstlane(p.place[row]);
+    int at;
+    float up;
+    if (p.place) {
+        at = __builtin_amdgcn_readfirstlane(p.place[row]);
+        up = p.head->up;
+    } else {
+        int before = 0, count = 0;
+        float top = 0.0f;
+        bool own = false;
+        constexpr int N = (int)FOUND_HERE / 64;
+        float g[N];
+        int token[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (64 * i < p.rows) {
+                const int r = min(64 * i + lane, p.rows - 1);
+                g[i] = p.g[r];
+                token[i] = p.t.ids[r];
+            }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (64 * i < p.rows) {
+                const float v = g[i] / p.t.temperature;
+                const bool counts = 64 * i + lane < p.rows && listed(token[i], p.V) && v != 0.0f;
+                if (counts && fabsf(v) < INFINITY) top = fmaxf(top, fabsf(v));
+                const uint64_t all = __ballot(counts);
+                if (64 * i + 64 <= row) before += __popcll(all);
+                else if (64 * i <= row) {
+                    before += __popcll(all & ((1ull << (row - 64 * i)) - 1));
+                    own = all >> (row - 64 * i) & 1;
+                }
+                count += __popcll(all);
+            }
+        top = wave_top(top);
+        at = own ? before : -1;
+        up = power_of_two(p.scaled ? piece_exponent(top) : 0);
+        if (row == 0) {
+            write_cuts(p.head, p.rows_cut, p.table_cut, count, lane);
+            if (lane == 0) write_head(p.head, count, top, p.scaled);
+        }
+        if (own && lane == 0) p.list[at] = row;
+    }
     if (at < 0) {
         if (p.dx)
             for (int c = lane * 8; c < p.C; c += 512) *(v8 *)((T *)p.dx + (int64_t)row * p.lddx + c) = v8{};
@@ -153,7 +212,7 @@ void loss_gather_kernel(GatherArgs p)
     for (int c = lane * 8; c < p.C; c += 512) *(v8 *)(to + c) = *(const v8 *)(from + c);
     if (p.g && lane == 0) {
         p.lse2[at] = p.lse[row] * LOG2E;
-        p.gc[at] = p.g[row] / p.t.temperature * p.head->up;
+        p.gc[at] = p.g[row] / p.t.temperature * up;
     }
     if (!p.t.k) {
         if (lane == 0) p.ids[at] = p.t.ids[row];
@@ -245,7 +304,7 @@ __global__ __launch_bounds__(256)
 void loss_join_kernel(JoinArgs p)
 {
     constexpr int SLICES = 256 / RT;
-    __shared__ float2 stat[SLICES][RT];
+    __shared__ float2 stat[4][RT];
     const int tid = threadIdx.x, rt = tid % RT, slice = tid / RT;
     const int rows = p.head ? p.head->count : p.rows, t0 = blockIdx.x * RT;
     if (t0 >= rows) return;
@@ -261,13 +320,15 @@ void loss_join_kernel(JoinArgs p)
             for (int n = 0; n < N; ++n) join(m, s, v[n].x, v[n].y);
         }
     }
-    stat[slice][rt] = make_float2(m, s);
-    for (int half = SLICES / 2; half; half >>= 1) {
-        __syncthreads();
-        if (slice < half) {
-            join(m, s, stat[slice + half][rt].x, stat[slice + half][rt].y);
-            stat[slice][rt] = make_float2(m, s);
-        }
+    // (within a wave first, whose lanes hold 64 / RT slices)
+#pragma unroll
+    for (int d = 32; d >= RT; d >>= 1) join(m, s, __shfl_xor(m, d), __shfl_xor(s, d));
+    if ((tid & 63) < RT) stat[tid >> 6][rt] = make_float2(m, s);
+    __syncthreads();
+    if (tid < RT) {
+#pragma unroll
+        for (int w = 1; w < 4; ++w) join(m, s, stat[w][rt].x, stat[w][rt].y);
+        stat[0][rt] = make_float2(m, s);
     }
     __syncthreads();
     if (!p.t.k) {
@@ -501,12 +562,14 @@ int launch_rows(const Vocab &v, const LossPlan &plan, const Rows16 &x, int64_t r
     LossHead *const head = (LossHead *)ws;
     int *const list = (int *)(ws + plan.list), *const place = (int *)(ws + plan.place);
     const unsigned blocks = (unsigned)((rows + 3) / 4);
+    const bool scaled = dloss && v.dtype == SNN_DTYPE_F16, here = dloss && !t.k && rows > 0 && rows <= FOUND_HERE;
     if (flags && rows) loss_flags_kernel<<<dim3(blocks), 256, 0, s>>>(t, v.V, (int)rows, flags, loss, lse_out, picked);
-    loss_list_kernel<<<1, 1024, 0, s>>>(t, flags, dloss, (int)rows, v.V, dloss && v.dtype == SNN_DTYPE_F16, plan.rows_cut, plan.table_cut,
-                                          head, list, place, loss, lse_out);
+    if (!here)
+        loss_list_kernel<<<1, 1024, 0, s>>>(t, flags, dloss, (int)rows, v.V, scaled, plan.rows_cut, plan.table_cut, head, list, place, loss, lse_out);
     if (rows) {
         GatherArgs g = {};
-        g.t = t; g.x = x.p; g.ldx = x.ld; g.rows = (int)rows; g.V = v.V; g.C = v.C; g.head = head; g.place = place;
+        g.t = t; g.x = x.p; g.ldx = x.ld; g.rows = (int)rows; g.V = v.V; g.C = v.C; g.head = head; g.place = here ? nullptr : place;
+        g.list = list; g.rows_cut = plan.rows_cut; g.table_cut = plan.table_cut; g.scaled = scaled;
         g.xc = ws + plan.xc; g.ids = (int32_t *)(ws + plan.ids);
         g.start = (uint16_t *)(ws + plan.start); g.start_ld = plan.start_ld;
         if (!dloss) g.slot = (int32_t *)(ws + plan.of_ids);
