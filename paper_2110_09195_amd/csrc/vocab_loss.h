@@ -50,11 +50,9 @@ struct TilesArgs {
 
 constexpr int LIST_BLOCK = 128;
 
-// Tile shapes, rows x columns, and how many are on the chip at once (TILE_128_DEEP: with more steps on their way, alone on its CU).  The last three for
-// STATS and PROBS alone.
-enum { TILE_256, TILE_128, TILE_128_DEEP, TILE_128x64, TILE_64, TILE_FORMS };
-inline int tile_m(int form) { return form == TILE_256 ? 256 : form == TILE_64 ? 64 : 128; }
-inline int tile_n(int form) { return form == TILE_256 ? 256 : form <= TILE_128_DEEP ? 128 : 64; }
+// Tile shapes, and how many are on the chip at once.  TILE_128_DEEP (with more steps on their way, alone on its CU) and TILE_64 are for STATS and PROBS alone.
+enum { TILE_256, TILE_128, TILE_128_DEEP, TILE_64, TILE_FORMS };
+inline int tile_edge(int form) { return form == TILE_256 ? 256 : form == TILE_64 ? 64 : 128; }
 inline int tile_slots(int form) { return form == TILE_128 || form == TILE_64 ? 512 : 256; }
 
 // How many parts the contracted axis of ROWS and TABLE is cut into: of 1 .. MOST_SPLITS those that take the least time - turns of the chip's workgroups, each

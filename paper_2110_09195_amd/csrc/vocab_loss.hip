@@ -455,12 +455,12 @@ struct LossPlan {
 
 // (of the gradients, whose parts are few where tiles are many, there are fewer)
 constexpr int64_t MOST_TILES = (int64_t)1 << 30;
-int64_t tiles_of(int form, int64_t m, int64_t n) { return (m + tile_m(form) - 1) / tile_m(form) * ((n + tile_n(form) - 1) / tile_n(form)); }
+int64_t tiles_of(int form, int64_t m, int64_t n) { return (m + tile_edge(form) - 1) / tile_edge(form) * ((n + tile_edge(form) - 1) / tile_edge(form)); }
 
 // Tiles of logits of `tokens` x `rows`: the form whose turns of the chip cost least, in turns of 256 x 256.
 int logits_form(int64_t tokens, int64_t rows)
 {
-    constexpr float TURN[] = {1.0f, 0.68f, 0.46f, 0.34f, 0.35f}, HALF[] = {1.0f, 0.55f, 0.46f, 0.36f, 0.22f};       // (no CU with two)
+    constexpr float TURN[] = {1.0f, 0.68f, 0.46f, 0.35f}, HALF[] = {1.0f, 0.55f, 0.46f, 0.22f};       // (no CU with two)
     int best = 0;
     float least = 0.0f;
     for (int f = 0; f < TILE_FORMS; ++f) {
@@ -522,7 +522,7 @@ LossPlan loss_plan(const Vocab &v, int64_t rows, const Targets &t, bool backward
     }
     if (!backward) {
         p.form = logits_form(v.V, rows);
-        p.tiles = (v.V + tile_m(p.form) - 1) / tile_m(p.form);
+        p.tiles = (v.V + tile_edge(p.form) - 1) / tile_edge(p.form);
         p.pick = take(p.ld * 4);
         p.part = take((size_t)p.tiles * p.ld * 8);
     } else {
@@ -541,7 +541,8 @@ LossPlan loss_plan(const Vocab &v, int64_t rows, const Targets &t, bool backward
         p.most_splits_table = parts(part_table);
         p.form_table = gradient_form(v.C, p.piece, rows, p.most_splits_table);
         const int tokens = v.V < p.piece ? v.V : p.piece;
-        p.rows_cut = {(v.C + tile_m(p.form_rows) - 1) / tile_m(p.form_rows), tile_n(p.form_rows), tile_slots(p.form_rows), (tokens + 63) / 64, p.most_splits};
+        const int edge = tile_edge(p.form_rows);
+        p.rows_cut = {(v.C + edge - 1) / edge, edge, tile_slots(p.form_rows), (tokens + 63) / 64, p.most_splits};
         p.table_cut = {(int)tiles_of(p.form_table, v.C, tokens), 0, tile_slots(p.form_table), 0, p.most_splits_table};
         p.lse2 = take(p.ld * 4);
         p.g = take(p.ld * 4);

@@ -274,17 +274,14 @@ void vocab_tiles_kernel(TilesArgs p)
 #pragma unroll
                 for (int i = 0; i < MB; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int v = mw + i * 16 + 4 * h + r;
-                        const float e = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], p.c, -lse2)) * g;
-                        acc[i][j][r] = edge && v >= p.M ? 0.0f : e;
-                    }
-            } else if (edge)
+                    for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], p.c, -lse2)) * g;
+            }
+            if (edge)
 #pragma unroll
                 for (int i = 0; i < MB; ++i)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (mw + i * 16 + 4 * h + r >= p.M) acc[i][j][r] = -INFINITY;
+                        if (mw + i * 16 + 4 * h + r >= p.M) acc[i][j][r] = KIND == PROBS ? 0.0f : -INFINITY;
             // The listed tokens of the row that are among the wave's: a row's place in its list where the wave's tokens begin is known, or all of a
             // short list is looked at.
             const uint32_t most = (uint32_t)max(min(p.M - mw, WM), 0);
@@ -450,7 +447,6 @@ int launch_form(int form, const TilesArgs &p, hipStream_t s)
     if (form == TILE_256) return launch_tiles<T, KIND, 256, 256, 128, 64, 2>(p, s);
     if constexpr (KIND == STATS || KIND == PROBS) {
         if (form == TILE_128_DEEP) return launch_tiles<T, KIND, 128, 128, 64, 64, 4>(p, s);
-        if (form == TILE_128x64) return launch_tiles<T, KIND, 128, 64, 32, 64, 6>(p, s);
         if (form == TILE_64) return launch_tiles<T, KIND, 64, 64, 32, 32, 4>(p, s);
     }
     return launch_tiles<T, KIND, 128, 128, 64, 64, 2>(p, s);
