@@ -202,6 +202,9 @@ void vocab_tiles_kernel(TilesArgs p)
             __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);                // VALU
         }
     };
+    // A wave with nothing but rows or columns behind the last multiplies nothing: it loads its share and keeps the barriers.  (2055 rows of 65536 tokens, whose
+    // ninth tiles have seven rows: 545 -> 518 us)
+    const bool idle = m0 + wm * WM >= p.M || n0 + wn * WN >= N;
     if constexpr (STAGES == 2) {
         // A slot is free once the fragments of its last phase are read, before these are multiplied: from then on the step after the next is loaded
         // there, and has a whole step's time to land.
@@ -209,8 +212,15 @@ void vocab_tiles_kernel(TilesArgs p)
         for (int q = 0; q < 3; ++q) issue(0, q, 3);
         issue(1, 0, 3);
         asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LOADS / 3) : "memory");
-        read(lds, 0);
-        for (int k = 0; k < steps; ++k) {
+        for (int k = 0; k < (idle ? steps : 0); ++k) {
+            const int slot = k & 1;
+            issue(slot ^ 1, 1, 3);
+            issue(slot ^ 1, 2, 3);
+            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+            issue(slot, 0, 3);
+        }
+        if (!idle) read(lds, 0);
+        for (int k = 0; k < (idle ? 0 : steps); ++k) {
             const int slot = k & 1;
 #pragma unroll
             for (int ph = 0; ph < PHASES - 1; ++ph) {
