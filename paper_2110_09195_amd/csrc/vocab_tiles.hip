@@ -174,6 +174,37 @@ void vocab_tiles_kernel(TilesArgs p)
         b.issue(to + A::BYTES, wave, max(first - A::L, 0), max(last - A::L, 0));
     };
 
+    // What belongs to the tile's rows of logits is fetched before the products, in whose time it arrives: of each row what its gradient needs, and its target
+    // or the first of its listed tokens that is among the wave's (a row's place in its list where the wave's tokens begin is known).
+    const int mw = m0 + wm * WM;                               // the wave's first token, of the piece
+    float lse2[NB], g[NB], share[NB];
+    int token[NB], from[NB], to[NB];
+    if constexpr (KIND == STATS || KIND == PROBS) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int t = n0 + wn * WN + j * 16 + (lane & 15);
+            const bool row = t < N;
+            lse2[j] = KIND == PROBS && row ? p.lse2[t] : 0.0f;
+            g[j] = KIND == PROBS && row ? p.g[t] : 0.0f;
+            token[j] = -1;
+            share[j] = 1.0f;
+            from[j] = to[j] = 0;
+            if (p.start) {
+                const uint16_t *const at = p.start + t * p.start_ld + (p.v0 + mw) / LIST_BLOCK;
+                from[j] = row && mw < p.M ? at[0] : 0;
+                to[j] = row && mw < p.M ? at[1] : 0;
+            } else if (p.k == 1) token[j] = row ? p.ids[t] : -1;
+        }
+        if (p.start)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                const int64_t at = (int64_t)(n0 + wn * WN + j * 16 + (lane & 15)) * p.k + from[j];
+                const bool some = from[j] < to[j];
+                token[j] = some ? p.ids[at] : -1;
+                if (KIND == PROBS) share[j] = some ? p.q[at] : 0.0f;
+            }
+    }
+
     f32x4 acc[MB][NB] = {};
     uint32_t am[MB], bn[NB];
 #pragma unroll
@@ -261,30 +292,17 @@ void vocab_tiles_kernel(TilesArgs p)
     // Lane: column ln of a block of 16, rows 4 h .. 4 h + 3.
     const int h = lane >> 4, ln = lane & 15;
     if constexpr (KIND == STATS || KIND == PROBS) {
-        const int mw = m0 + wm * WM;                           // the wave's first token, of the piece
         const bool edge = mw + WM > p.M;
         float top[NB], sum[NB];
-        int from[NB], to[NB];
-        if (p.start)
-#pragma unroll
-            for (int j = 0; j < NB; ++j) {
-                const int t = n0 + wn * WN + j * 16 + ln;
-                const uint16_t *const at = p.start + t * p.start_ld + (p.v0 + mw) / LIST_BLOCK;
-                from[j] = t < N && mw < p.M ? at[0] : 0;
-                to[j] = t < N && mw < p.M ? at[1] : 0;
-            }
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const int t = n0 + wn * WN + j * 16 + ln;
             const bool row = t < N;
-            float g = 0.0f;
             if constexpr (KIND == PROBS) {
-                const float lse2 = row ? p.lse2[t] : 0.0f;
-                g = row ? p.g[t] : 0.0f;
 #pragma unroll
                 for (int i = 0; i < MB; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], p.c, -lse2)) * g;
+                    for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], p.c, -lse2[j])) * g[j];
             }
             if (edge)
 #pragma unroll
@@ -292,12 +310,11 @@ void vocab_tiles_kernel(TilesArgs p)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if (mw + i * 16 + 4 * h + r >= p.M) acc[i][j][r] = KIND == PROBS ? 0.0f : -INFINITY;
-            // The listed tokens of the row that are among the wave's: a row's place in its list where the wave's tokens begin is known, or all of a
-            // short list is looked at.
+            // The listed tokens of the row that are among the wave's
             const uint32_t most = (uint32_t)max(min(p.M - mw, WM), 0);
-            auto take = [&](int token, bool some, int64_t at) {
+            auto take = [&](int token, int64_t at, float share) {
                 const int local = token - p.v0 - mw;
-                const bool hit = some && (uint32_t)local < most && ((local >> 2) & 3) == h;
+                const bool hit = token >= 0 && (uint32_t)local < most && ((local >> 2) & 3) == h;
                 if (!__any(hit)) return;
                 const int mine = hit ? local - 4 * h : -1;
                 if constexpr (KIND == STATS) {
@@ -306,33 +323,35 @@ void vocab_tiles_kernel(TilesArgs p)
                     for (int i = 0; i < MB; ++i)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) z = mine == i * 16 + r ? acc[i][j][r] : z;
-                    if (hit) p.picked[at] = z;
+                    if (hit) p.picked[p.start ? p.list[t] * (int64_t)p.k + p.slot[at] : at] = z;
                 } else {
-                    const float q = hit ? g * (p.q ? p.q[at] : 1.0f) : 0.0f;
+                    const float q = hit ? g[j] * share : 0.0f;
 #pragma unroll
                     for (int i = 0; i < MB; ++i)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) acc[i][j][r] -= mine == i * 16 + r ? q : 0.0f;
                 }
             };
+            const int64_t of_row = (int64_t)t * p.k;
+            if (p.start || p.k == 1) take(token[j], of_row + from[j], share[j]);
             if (p.start) {
-                for (int n = from[j]; __any(n < to[j]); ++n) {
-                    const int64_t at = (int64_t)t * p.k + n;
+                for (int n = from[j] + 1; __any(n < to[j]); ++n) {
                     const bool some = n < to[j];
-                    take(some ? p.ids[at] : -1, some, KIND == STATS ? some ? p.list[t] * (int64_t)p.k + p.slot[at] : 0 : at);
+                    take(some ? p.ids[of_row + n] : -1, of_row + n, KIND == PROBS && some ? p.q[of_row + n] : 0.0f);
                 }
-            } else
+            } else if (KIND == STATS && p.k > 1)
+                // (of few rows lists are as they came, and all of them is looked at)
                 for (int k0 = 0; k0 < p.k; k0 += 8) {
                     int token[8];
                     bool some = false;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        token[e] = row && k0 + e < p.k ? p.ids[t * (int64_t)p.k + k0 + e] : -1;
+                        token[e] = row && k0 + e < p.k ? p.ids[of_row + k0 + e] : -1;
                         some |= token[e] >= 0 && (uint32_t)(token[e] - p.v0 - mw) < most;
                     }
                     if (!__any(some)) continue;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) take(token[e], token[e] >= 0, t * (int64_t)p.k + k0 + e);
+                    for (int e = 0; e < 8; ++e) take(token[e], of_row + k0 + e, 1.0f);
                 }
             if constexpr (KIND == STATS) {
                 float m = -INFINITY, s = 0.0f;
