@@ -705,8 +705,8 @@ int snn_embedding_grad(const snn_vocab_desc *desc, const void *dy, int64_t lddy,
  *   dtable   device, [V][C], 16-byte aligned, fully overwritten, or with accumulate added to; NULL: not wanted (not both NULL)
  *   workspace  device, >= snn_loss_workspace_bytes(desc, rows, 0, SNN_LOSS_FORWARD or _BACKWARD) bytes, 256-byte aligned.  What it holds
  *              of probabilities is a piece of the vocabulary, of at most 256 MiB (256 tokens at least).
- * dz is rounded to desc->dtype before the products (f16: times a power of two that brings the largest |dloss| to 2^14 .. 2^15, so that what is smaller than
- * 2^-40 of that may be lost); dx and dtable are rounded once.
+ * dz is rounded to desc->dtype before the products, relative to the largest |dloss| (f16: and times 2^14, so that what is smaller than 2^-39 of
+ * that may be lost); dx and dtable are rounded once.
  * Errors: INVALID_ARG; UNSUPPORTED (2^30 tiles or more); WORKSPACE; LAUNCH.
  */
 #define SNN_LOSS_FORWARD  0

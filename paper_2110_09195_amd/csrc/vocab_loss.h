@@ -5,11 +5,11 @@
 
 namespace snn {
 
-// What a call finds out about its rows on the device: how many count, the powers of two that bring their gradients into the type's range
-// and back, and how many parts the sums of ROWS and TABLE are cut into.
+// What a call finds out about its rows on the device: how many count, what their gradients are multiplied by and divided by
+// before they are rounded to 16 bits, and what brings the results back, and how many parts the sums of ROWS and TABLE are cut into.
 struct LossHead {
     int count;
-    float up, down;
+    float power, part, down;
     int splits_rows, splits_table;
 };
 

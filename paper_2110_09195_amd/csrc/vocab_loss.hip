@@ -67,14 +67,24 @@ __device__ inline void write_cuts(LossHead *head, const Cut &rows_cut, const Cut
     }
 }
 
-// ... and by one lane.  Values of f16 reach from 2^-24 to 2^16: the largest gradient is brought to 2^14 .. 2^15; bf16 has fp32's range.
-__device__ inline float write_head(LossHead *head, int count, float top, bool scaled)
+// ... and by one lane.  Gradients of the rows' losses are taken relative to the largest, `top`: of rows that count alike (a mean's) the gradients of their
+// targets' logits are then next to -1, which 16 bits hold, and their rounding is no common factor of all results (of up to half a step).  Values of f16
+// reach from 2^-24 to 2^16: there the largest is brought to 2^14; bf16 has fp32's range.
+struct Scale {
+    float power, part;                // times the one, over the other
+};
+__device__ inline Scale scale_of(float top, bool scaled)
 {
-    const int e = scaled ? piece_exponent(top) : 0;
+    const uint32_t bits = __float_as_uint(top);
+    return {power_of_two(scaled ? piece_exponent(top) : 0), bits >> 23 ? __uint_as_float((bits & 0x7fffffu) | 0x3f800000u) : 1.0f};
+}
+
+__device__ inline void write_head(LossHead *head, int count, const Scale &s)
+{
     head->count = count;
-    head->up = power_of_two(e);
-    head->down = power_of_two(-e);
-    return power_of_two(e);
+    head->power = s.power;
+    head->part = s.part;
+    head->down = s.part / s.power;
 }
 
 // The rows that count, in their order, and each row's place among them (-1: none).  One workgroup.  flags = nullptr: found out here.
@@ -123,7 +133,7 @@ void loss_list_kernel(Targets t, const uint8_t *__restrict__ flags, const float 
     if (wave == 1) write_cuts(head, rows_cut, table_cut, before, lane);
     if (threadIdx.x != 0) return;
     for (int w = 1; w < 16; ++w) top = fmaxf(top, tops[w]);
-    write_head(head, before, top, scaled);
+    write_head(head, before, scale_of(top, scaled));
 }
 
 constexpr int MOST_LISTED = 256;
@@ -160,10 +170,10 @@ void loss_gather_kernel(GatherArgs p)
     const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= p.rows) return;
     int at;
-    float up;
+    Scale up;
     if (p.place) {
         at = __builtin_amdgcn_readfirstlane(p.place[row]);
-        up = p.head->up;
+        up = {p.head->power, p.head->part};
     } else {
         int before = 0, count = 0;
         float top = 0.0f;
@@ -194,10 +204,10 @@ void loss_gather_kernel(GatherArgs p)
             }
         top = wave_top(top);
         at = own ? before : -1;
-        up = power_of_two(p.scaled ? piece_exponent(top) : 0);
+        up = scale_of(top, p.scaled);
         if (row == 0) {
             write_cuts(p.head, p.rows_cut, p.table_cut, count, lane);
-            if (lane == 0) write_head(p.head, count, top, p.scaled);
+            if (lane == 0) write_head(p.head, count, up);
         }
         if (own && lane == 0) p.list[at] = row;
     }
@@ -212,7 +222,7 @@ void loss_gather_kernel(GatherArgs p)
     for (int c = lane * 8; c < p.C; c += 512) *(v8 *)(to + c) = *(const v8 *)(from + c);
     if (p.g && lane == 0) {
         p.lse2[at] = p.lse[row] * LOG2E;
-        p.gc[at] = p.g[row] / p.t.temperature * up;
+        p.gc[at] = p.g[row] / p.t.temperature * up.power / up.part;
     }
     if (!p.t.k) {
         if (lane == 0) p.ids[at] = p.t.ids[row];

@@ -301,6 +301,27 @@ def test_gradients_of_f16_at_any_scale():
     assert torch.equal((a.float() * 64)[normal_ones], b.float()[normal_ones])
 
 
+@pytest.mark.parametrize("dtype, step", [(BF, 2.0 ** -8), (HF, 2.0 ** -11)])
+@pytest.mark.parametrize("rows", [300, 1500])
+def test_rows_that_count_alike_share_no_rounding(rows, dtype, step):
+    """Losses of one gradient, as a mean gives: rounded by itself it would be a common factor of all results.  With shares of 1 / V the target's dz is -(1 - 1/V) of it,
+    which rounds by at most 1/V; dz of the other tokens, a half step off at most, is 1 / sqrt(V) of its row's norm.  Roundings of the results are independent: of
+    rows x C values, each off by at most a half step, their mean by eight thousandths of one (with four deviations' room)."""
+    g, V, C = gen(10), 4096, 64
+    table = normal(g, V, C).to(dtype)
+    x = torch.full((rows, C), 2.0 ** -14, device="cuda").to(dtype)
+    ids = torch.randperm(V, generator=g, device="cuda")[:rows].int()
+    desc = B.make_vocab_desc(V, C, CODE[dtype])
+    dloss = torch.full((rows,), (1 + step) / 1024, device="cuda")                # half way between two values of the type
+    _, lse = B.snn_cross_entropy_forward(desc, x, table, ids)
+    dx, _ = B.snn_cross_entropy_backward(desc, x, table, ids, lse, dloss)
+    p = torch.softmax(x.double() @ table.double().t(), 1)
+    p[torch.arange(rows, device="cuda"), ids.long()] -= 1
+    want = dloss.double()[:, None] * (p @ table.double())
+    factor = float((dx.double() * want).sum() / (want * want).sum())
+    assert abs(factor - 1) <= min(1 / V, step) + step / V ** 0.5 + 0.008 * step, factor
+
+
 def test_small_losses_keep_their_digits():
     """A row whose target is nearly sure: the loss, log(1 + the others' share), is far below a step of the logits."""
     V, C = 4000, 64
