@@ -9,7 +9,8 @@ namespace {
 // ---- rows of the table -----------------------------------------------------------------------------------------
 
 // Pieces of 8 channels, rows of `pieces` of them; AHEAD of a thread's are on their way at once, a grid apart.
-// Bound by memory, and for a few tokens by two dependent reads (the token, its row).
+// Bound by memory, and for a few tokens by two dependent reads (the token, its row): 16384 tokens of 4096 channels 54 us (261 MB, 4.8 TB/s, near a copy's 5.3),
+// one token 2.4 us on the GPU and 4.5 with the host's call.  Channels by piece, not rows by wave, so that any number of them fills the lanes.
 constexpr int AHEAD = 4;
 
 template <class T>
@@ -60,6 +61,8 @@ void embedding_kernel(const T *__restrict__ table, int64_t ldt, const int32_t *_
 // Up to MERGED rows: blocks of RANK_BLOCK rows are sorted by themselves - a row's place is the number of the block's tokens below its own, and of
 // its own in earlier rows; 64 rows a workgroup, whose waves share out the tokens that they are compared with - and a row's
 // place among all is its place there and those that a binary search finds for it in the other blocks.
+// Bound by latency: 16384 rows 7.5 and 4 us (every row compared with every other, in one launch: 55).  A whole call of 65536 rows of 64 channels to 50000 tokens
+// takes 49 us, one row more by the passes below 55.
 constexpr int64_t MERGED = 65536;
 constexpr int RANK_BLOCK = 1024, RANK_WAVES = 8, MERGE_WAVES = 16;
 
@@ -156,7 +159,8 @@ void embedding_merge_kernel(const uint32_t *__restrict__ keys, const int *__rest
 }
 
 // More rows: by 8 bits of the token at a time, from the lowest.  Workgroups of 2048 rows count their digits; one workgroup turns the counts
-// [digit][workgroup] into places; then rows are put there, in their order.
+// [digit][workgroup] into places; then rows are put there, in their order.  Bound by latency, three launches a pass: 500000 rows of 64 channels to
+// 50000 tokens, two passes, 169 us with their sums.
 constexpr int DIGITS = 256, SORT_ROWS = 2048, SORT_WAVES = 4, SORT_ROUNDS = SORT_ROWS / 64 / SORT_WAVES;
 
 __device__ inline uint32_t sort_key(const uint32_t *keys, int64_t i, uint32_t V) { return min(keys[i], V); }
@@ -291,7 +295,9 @@ __device__ inline void write_sum(const SumArgs &p, uint32_t token, int c, const 
 
 // A wave sums a block of rows in the tokens' order, 512 channels.  A token whose rows all lie there is done; the others' sums are joined by the next
 // launch.  Workgroups behind these (when the result is not added to what is there) write zeros for FILL_ROWS tokens each that have no row.
-// Bound by memory: each row is read once, each row of the result written once.
+// Bound by memory: each row is read once, each row of the result written once: 16384 rows of 4096 channels to 131072 tokens 190 - 230 us (1.07 GB written and
+// 0.13 read, 5.2 - 6.3 TB/s).  No atomics: sums in the rows' order, the same bits every time.  By blocks of rows, not by token, as a few tokens have most rows
+// of a text: of 7001 rows to 401 tokens a wave sums 16, 6.7 us.
 template <class T>
 __global__ __launch_bounds__(256)
 void embedding_sum_kernel(SumArgs p, unsigned sum_grid)
@@ -388,7 +394,7 @@ void embedding_sum_kernel(SumArgs p, unsigned sum_grid)
 }
 
 // Tokens whose rows lie in several blocks, from the block in which they begin: the blocks' sums in their order, shared out among the waves
-// in runs.
+// in runs.  Bound by latency (the token, its last block, its parts: 6 - 8 us); a token of 16384 rows has 512 blocks.
 constexpr int JOIN_WAVES = 4;
 
 template <class T>

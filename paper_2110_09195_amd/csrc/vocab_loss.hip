@@ -87,7 +87,8 @@ __device__ inline void write_head(LossHead *head, int count, const Scale &s)
     head->down = s.part / s.power;
 }
 
-// The rows that count, in their order, and each row's place among them (-1: none).  One workgroup.  flags = nullptr: found out here.
+// The rows that count, in their order, and each row's place among them (-1: none).  One workgroup, so that places need no second launch: 8192 rows 12 - 16 us of
+// a step of 26 ms, 1501 rows 5.  flags = nullptr: found out here.
 __global__ __launch_bounds__(1024)
 void loss_list_kernel(Targets t, const uint8_t *__restrict__ flags, const float *__restrict__ g, int rows, int V, bool scaled, Cut rows_cut, Cut table_cut,
                       LossHead *__restrict__ head, int *__restrict__ list, int *__restrict__ place, float *__restrict__ loss, float *__restrict__ lse)
@@ -161,6 +162,8 @@ struct GatherArgs {
 };
 
 // Rows that count next to each other, with what belongs to them.  A wave a row.  Of a few rows every wave looks at all of them itself, which saves a launch.
+// Bound by memory for many rows (8192 of 4096 channels 28 us, 128 MB), by latency for few (5 us).  The copy is what makes rows that do not count free: of 4096 rows
+// half of which count, 65536 tokens of 2048 channels 466 us where all of them take 862.
 constexpr int64_t FOUND_HERE = 1024;
 template <class T>
 __global__ __launch_bounds__(256)
@@ -307,7 +310,8 @@ __device__ inline void join(float &m, float &s, float m2, float s2)
     m = top;
 }
 
-// Sums of exponentials of RT rows from those of the tiles, and their losses.  The loss is formed from what the row's logits fall short of the largest
+// Sums of exponentials of RT rows from those of the tiles, and their losses.  RT by the number of rows, so that parts are read in whole lines where there are
+// many (RT x 8 bytes) and a row has a workgroup to itself where there are few: 8192 rows, 512 tiles 13 us, 75 rows, 391 tiles 4.6.  The loss is formed from what the row's logits fall short of the largest
 // one, not from the sum's logarithm as a whole: small losses keep their digits.
 template <int RT>
 __global__ __launch_bounds__(256)
@@ -407,7 +411,7 @@ __device__ inline void sum_parts(const float *from, int64_t split, int splits, f
     }
 }
 
-// Gradients of rows from their parts: a wave 512 channels of a row.
+// Gradients of rows from their parts: a wave 512 channels of a row.  Bound by memory: 8028 rows of 4096 channels from one part 36 us (197 MB, 5.5 TB/s).
 template <class T>
 __global__ __launch_bounds__(256)
 void loss_rows_kernel(const float *__restrict__ part, int64_t split, int C, const LossHead *__restrict__ head, const int *__restrict__ list,
@@ -425,7 +429,7 @@ void loss_rows_kernel(const float *__restrict__ part, int64_t split, int C, cons
     *(v8 *)(dx + (int64_t)list[t] * lddx + c) = v;
 }
 
-// Rows of the table's gradient from their parts (if there are several): likewise.
+// Rows of the table's gradient from their parts (if there are several, for small vocabularies): likewise.
 template <class T>
 __global__ __launch_bounds__(256)
 void loss_table_kernel(const float *__restrict__ part, int64_t split, int n, int C, const LossHead *__restrict__ head, T *__restrict__ dtable,

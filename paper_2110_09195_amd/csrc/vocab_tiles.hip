@@ -124,6 +124,19 @@ __device__ inline bool find_place(int tm, int tn, int splits, Place &at)
 // phases: its two halves of the axis, the two halves of a wave's rows; in each the fragments for the next are read, in the shadow of the matrix instructions.
 // (Two waves a SIMD also where one workgroup fills a CU's LDS: with the registers of both the compiler moves sums between the two kinds of registers, 4000
 // rows of 20000 tokens in tiles of 128 x 128 170 us against 146.)
+//
+// No logit is kept: the backward call makes them again from x and the table, rounds their gradients to 16 bits for a piece of the vocabulary at a time, and two
+// more products turn these into the gradients: 8 T C V operations forward and backward, where 6 would do with T x V logits in memory (2 GB for 8192 rows of
+// 131072 tokens).  In 16 bits because the matrix cores take them at 16 times the rate of fp32; rounded once, they leave errors of the size of one rounding of the
+// results.  Softmax statistics stay fp32: of a tile the largest logit and the sum of exponentials of what the others fall short of it, joined tile by tile.
+//
+// For many rows the matrix cores bound it, at the clock that the chip's power leaves: 8028 rows of 131072 tokens, 4096 channels, bf16: STATS 6.2 - 6.7 ms by card
+// (1.29 - 1.39 PFLOP/s, 65 % of cycles busy at 2.0 GHz), PROBS 6.4 - 7.0, ROWS 6.7 - 7.0, TABLE 6.4 - 6.6; library products of these sizes, which do nothing else, 5.85 for
+// logits, 6.5 and 7.3 for the gradients.  A step of a 256 x 256 tile takes 1.5 us; what comes before a tile's first and after its last, some 6 us (half of them
+// exponentials), nothing hides: with 2048 channels, 32 steps, STATS of 3686 rows of 65536 tokens 0.85 ms, the library's product 0.75.
+// For few rows memory bounds STATS: one row against 131072 tokens of 4096 channels 182 us, 5.9 TB/s.
+// A tile of 256 x 256 reads half of what four of 128 x 128 do, and is the faster where there are enough; smaller ones are for fewer rows (logits_form,
+// gradient_form).
 template <class T, int KIND, int BM, int BN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2)
 void vocab_tiles_kernel(TilesArgs p)
