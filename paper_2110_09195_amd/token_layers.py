@@ -5,6 +5,9 @@ precision at a network's ends, the table of tokens and the losses over the vocab
 
 trains experts and adapters for some steps towards random teachers of their own kind, serves the adapted projection token by token, and trains a small
 network from tokens to tokens, first on targets and then a second one on the first one's top logits.
+
+A step of differentiable functions is captured into a graph forward and backward together, and while no graph of an eager step over the same leaves lives: torch
+adds to a leaf's gradient on the stream on which its oldest living graph was made, and a capture may not wait for that.
 """
 import torch
 from torch.autograd.function import once_differentiable

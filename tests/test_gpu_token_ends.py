@@ -73,6 +73,37 @@ def test_what_is_refused():
         dx.sum().backward()
 
 
+@pytest.mark.parametrize("k", [0, 5])
+def test_a_captured_step(k):
+    """Forward and backward captured together, no graph of an eager step over the same leaves living then, and replayed on changing inputs."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    rows, V, C = 200, 700, 136
+    table = torch.randn(V, C, generator=g, device="cuda").bfloat16().requires_grad_()
+    ids = torch.randint(-1, V, (rows,), generator=g, device="cuda").int()
+    target = torch.randint(-1, V, (rows, k) if k else (rows,), generator=g, device="cuda").int()
+    logits = torch.randn(rows, max(k, 1), generator=g, device="cuda")
+
+    def step():
+        h = TL.embedded(ids, table, 0.1)
+        loss = TL.distilled(h, table, target, logits, 2.0) if k else TL.cross_entropy(h, table, target)
+        return loss.detach(), *torch.autograd.grad(loss.mean(), table)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept = step()
+    for n in range(3):
+        ids.copy_(torch.randint(-1, V, (rows,), generator=g, device="cuda"))
+        target.copy_(torch.randint(-1, V, target.shape, generator=g, device="cuda"))
+        graph.replay()
+        got = [t.clone() for t in kept]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, step())), n
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("k", [0, 9])
 def test_a_network_trains(dtype, k):

@@ -432,6 +432,35 @@ def test_on_another_stream_and_in_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(got, step())), n
 
 
+def test_calls_at_once_on_two_streams():
+    """Calls that run beside each other, of different sizes, give what they give alone."""
+    g, jobs = gen(11), []
+    for rows, V, C, k in ((500, 9000, 264, 0), (90, 2000, 136, 7)):
+        x, table, ids, _ = rows_for(g, rows, V, C, BF, 0.2, k)
+        logits = normal(g, rows, k) if k else None
+        desc, dloss = B.make_vocab_desc(V, C), torch.rand(rows, generator=g, device="cuda")
+
+        def job(desc=desc, x=x, table=table, ids=ids, logits=logits, dloss=dloss):
+            given = (ids,) if logits is None else (ids, logits, 2.0)
+            forward, backward = ((B.snn_cross_entropy_forward, B.snn_cross_entropy_backward) if logits is None else
+                                 (B.snn_distill_forward, B.snn_distill_backward))
+            out = forward(desc, x, table, *given)
+            dx, dw = backward(desc, x, table, *given, out[1], dloss)
+            tokens = ids.flatten()[:x.shape[0]].contiguous()
+            return (*out, dx, B.snn_embedding_grad(desc, dx, tokens, 1.0, dtable=dw, accumulate=True))
+        jobs.append((job, job()))
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = []
+    for _ in range(6):
+        for (job, want), s in zip(jobs, streams):
+            with torch.cuda.stream(s):
+                got.append((job(), want))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for out, want in got for a, b in zip(out, want))
+
+
 def test_offsets_past_32_bits():
     """A table of more than 4 GiB, tokens at its far end."""
     V, C = 70000, 32776
