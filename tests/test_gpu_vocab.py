@@ -200,8 +200,9 @@ def check_loss(rows, V, C, dtype, none=0.3, k=0, temperature=1.0, seed=0, stride
 
 SIZES = [(1, 1, 8, BF), (1, 2, 8, HF), (1, 129, 72, BF), (2, 1000, 264, HF), (7, 63, 40, BF), (63, 4099, 136, BF), (64, 128, 32, HF), (65, 127, 520, BF),
          (128, 257, 1032, HF), (129, 300, 72, BF), (200, 2000, 2056, HF), (333, 5003, 264, BF), (700, 1024, 512, HF),
-         # each form of tiles, sums over rows and over tokens in parts, rows that every wave looks over and those that one workgroup does
-         (100, 20000, 72, BF), (160, 20001, 40, HF), (400, 20000, 72, BF), (2000, 300, 264, HF), (1024, 700, 72, BF), (1025, 700, 72, HF), (64, 9000, 4096, BF)]
+         # each form of tiles, sums over rows and over tokens in parts, rows that every workgroup looks over and those that one does
+         (100, 20000, 72, BF), (160, 20001, 40, HF), (400, 20000, 72, BF), (2000, 300, 264, HF), (1024, 700, 72, BF), (1025, 700, 72, HF), (64, 9000, 4096, BF),
+         (4096, 700, 72, BF), (4097, 700, 72, HF)]
 
 
 @pytest.mark.parametrize("rows, V, C, dtype", SIZES)
@@ -212,14 +213,16 @@ def test_cross_entropy(rows, V, C, dtype):
 @pytest.mark.parametrize("rows, V, C, dtype, k, temperature", [
     (1, 1, 8, BF, 1, 1.0), (1, 40, 8, HF, 7, 2.0), (5, 129, 72, BF, 256, 0.5), (64, 1000, 136, HF, 9, 4.0), (65, 257, 264, BF, 64, 1.5),
     (130, 4099, 520, HF, 100, 2.0), (333, 300, 72, BF, 20, 1.0), (700, 2000, 256, BF, 3, 3.0),
-    (160, 20001, 72, HF, 30, 2.0), (400, 20000, 40, BF, 128, 1.0), (3000, 500, 72, HF, 65, 0.01)])
+    (160, 20001, 72, HF, 30, 2.0), (400, 20000, 40, BF, 128, 1.0), (3000, 500, 72, HF, 65, 0.01),
+    # lists that every workgroup looks over, and more
+    (512, 500, 72, BF, 8, 2.0), (241, 500, 72, HF, 17, 1.0), (4096, 300, 40, BF, 1, 1.0), (4097, 300, 40, HF, 1, 1.0)])
 def test_distillation(rows, V, C, dtype, k, temperature):
     check_loss(rows, V, C, dtype, k=k, temperature=temperature, strided=rows % 2 == 1)
 
 
 # large tiles; rows gathered in the forward call; several pieces of the vocabulary
 @pytest.mark.parametrize("rows, V, C, dtype, k", [(700, 60000, 1032, BF, 0), (3001, 12007, 1000, HF, 0), (4133, 70001, 72, BF, 0), (4133, 70001, 40, HF, 5),
-                                                  (600, 50000, 1096, BF, 70)])
+                                                  (600, 50000, 1096, BF, 70), (4096, 60000, 136, BF, 0), (4097, 60000, 136, HF, 0)])
 def test_large(rows, V, C, dtype, k):
     check_loss(rows, V, C, dtype, none=0.6 if rows > 4000 else 0.1, k=k, temperature=2.0 if k else 1.0)
 
