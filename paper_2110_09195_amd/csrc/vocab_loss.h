@@ -3,6 +3,8 @@
 
 #include "vocab.h"
 
+#include <math.h>
+
 namespace snn {
 
 // What a call finds out about its rows on the device: how many count, what their gradients are multiplied by and divided by
@@ -55,14 +57,43 @@ enum { TILE_256, TILE_128, TILE_128_DEEP, TILE_64, TILE_FORMS };
 inline int tile_edge(int form) { return form == TILE_256 ? 256 : form == TILE_64 ? 64 : 128; }
 inline int tile_slots(int form) { return form == TILE_128 || form == TILE_64 ? 512 : 256; }
 
-// How many parts the contracted axis of ROWS and TABLE is cut into: of 1 .. MOST_SPLITS those that take the least time - turns of the chip's workgroups, each
-// with its steps and what a tile costs beside them, and the joining of the parts.
+// How many parts the contracted axes of ROWS and TABLE are cut into: of 1 .. MOST_SPLITS each those that take the least time, in steps of a tile: the workgroups'
+// steps and what a tile costs beside them, shared out over the chip, and the writing and joining of the parts.
 constexpr int MOST_SPLITS = 64;
-__host__ __device__ inline float split_cost(int s, int tiles, int slots, int steps)
+struct Sums {
+    float tiles;                      // 0: not wanted
+    int steps, most;
+    float join;                       // of a part
+    // (a part has four steps at least, and there is no need for more than two turns of the chip)
+    __host__ __device__ int limit(int slots) const
+    {
+        const int some = most < (steps + 3) / 4 ? most : (steps + 3) / 4, turns = tiles > 0.0f ? (int)((float)(2 * slots) / tiles) : 1;
+        return some < turns ? some : turns;
+    }
+    __host__ __device__ float length(int s) const { return (float)((steps + s - 1) / s) + 5.0f; }
+};
+
+// `first` workgroups of length a, then `second` of length b, each taken up by the first slot that is free.
+__host__ __device__ inline float makespan(float first, float a, float second, float b, float slots)
 {
-    return (float)((tiles * s + slots - 1) / slots) * ((float)((steps + s - 1) / s) + 5.0f) + 0.25f * (float)s;
+    if (first == 0.0f) return ceilf(second / slots) * b;
+    const float turns = floorf(first / slots), rest = first - turns * slots, left = slots - rest;
+    if (second == 0.0f) return ceilf(first / slots) * a;
+    if (rest == 0.0f) return turns * a + ceilf(second / slots) * b;
+    // ending with one of a slot that had none of the first, or with one of a slot that had
+    float k = ceilf(second / left);
+    if (k > ceilf(a / b)) k = ceilf((second + rest * ceilf(a / b)) / slots);
+    const float after = fmaxf(ceilf((second - left * floorf(a / b)) / slots), 0.0f);
+    return turns * a + fminf(fmaxf(k * b, a), a + after * b);
+}
+
+__host__ __device__ inline float cut_cost(const Sums &rows, int r, const Sums &table, int t, float slots)
+{
+    return makespan(rows.tiles * (float)r, rows.length(r), table.tiles * (float)t, table.length(t), slots) + rows.join * (float)r +
+           (t > 1 ? table.join * (float)t : 0.0f);
 }
 
 int launch_vocab_tiles(int kind, int form, int dtype, const TilesArgs &p, hipStream_t s);
+int launch_vocab_gradients(int form, int dtype, const TilesArgs &rows, const TilesArgs &table, hipStream_t s);         // ROWS and TABLE
 
 }  // namespace snn

@@ -38,32 +38,41 @@ void loss_flags_kernel(Targets t, int V, int rows, uint8_t *__restrict__ flags, 
         if (!counts || !listed(t.ids[(int64_t)row * t.k + k], V)) picked[(int64_t)row * t.k + k] = 0.0f;
 }
 
-// A product whose sums are cut into parts: tiles along its other axis, along the rows' (0: it is the rows that are summed over), workgroups at once, steps
-// (0: by the rows), and at most how many parts.
-struct Cut {
-    int tiles, tile_rows, slots, steps, most;
+// The gradients that are wanted, by what is known before the rows are: tiles along the channels, rows a tile, workgroups at once; of the table its tiles.
+struct Cuts {
+    int form, slots, tiles_rows, edge, steps_rows, most_rows, tiles_table, most_table;
+    float join_rows, join_table;      // what a part costs, of a row and of the table's piece
+
+    __host__ __device__ Sums of_rows(int count) const
+    {
+        return {(float)tiles_rows * (float)((count + edge - 1) / edge), steps_rows, most_rows, join_rows * (float)count};
+    }
+    __host__ __device__ Sums of_table(int count) const { return {(float)tiles_table, (count + 63) / 64, most_table, join_table}; }
 };
 
-// Which of 1 .. 64 parts costs least, a lane each (of several the smallest).
-__device__ inline int best_cut(const Cut &c, int count, int lane)
+// What is known once the rows are: by one wave (the parts, if it is the gradients' call: a lane for each number of the rows' parts) ...
+__device__ inline void write_cuts(LossHead *head, const Cuts &cuts, int count, int lane)
 {
-    const int tiles = c.tiles * (c.tile_rows ? (count + c.tile_rows - 1) / c.tile_rows : 1), steps = c.tile_rows ? c.steps : (count + 63) / 64;
-    const int s = lane + 1;
-    const float cost = s == 1 || (s <= c.most && s <= (steps + 3) / 4) ? split_cost(s, tiles, c.slots, steps) : INFINITY;
-    float least = cost;
+    if (!cuts.slots) return;                                   // (a call of no rows at all is told by the same)
+    const Sums rows = cuts.of_rows(count), table = cuts.of_table(count);
+    const int r = lane + 1, last = table.limit(cuts.slots);
+    const bool in = r == 1 || r <= rows.limit(cuts.slots);
+    float least = INFINITY;
+    int parts = 1;
+    for (int t = 1; t == 1 || t <= last; ++t) {
+        const float cost = in ? cut_cost(rows, r, table, t, (float)cuts.slots) : INFINITY;
+        if (cost < least) {
+            least = cost;
+            parts = t;
+        }
+    }
+    float best = least;
 #pragma unroll
-    for (int d = 32; d; d >>= 1) least = fminf(least, __shfl_xor(least, d));
-    return __builtin_ctzll(__ballot(cost == least)) + 1;
-}
-
-// What is known once the rows are: by one wave (the cuts, if it is the gradients' call) ...
-__device__ inline void write_cuts(LossHead *head, const Cut &rows_cut, const Cut &table_cut, int count, int lane)
-{
-    if (!rows_cut.slots) return;                               // (a call of no rows at all is told by the same)
-    const int r = best_cut(rows_cut, count, lane), t = best_cut(table_cut, count, lane);
-    if (lane == 0) {
+    for (int d = 32; d; d >>= 1) best = fminf(best, __shfl_xor(best, d));
+    const int at = __builtin_ctzll(__ballot(least == best));
+    if (lane == at) {
         head->splits_rows = r;
-        head->splits_table = t;
+        head->splits_table = parts;
     }
 }
 
@@ -90,7 +99,7 @@ __device__ inline void write_head(LossHead *head, int count, const Scale &s)
 // The rows that count, in their order, and each row's place among them (-1: none).  One workgroup, so that places need no second launch: 8192 rows 12 - 16 us of
 // a step of 26 ms, 1501 rows 5.  flags = nullptr: found out here.
 __global__ __launch_bounds__(1024)
-void loss_list_kernel(Targets t, const uint8_t *__restrict__ flags, const float *__restrict__ g, int rows, int V, bool scaled, Cut rows_cut, Cut table_cut,
+void loss_list_kernel(Targets t, const uint8_t *__restrict__ flags, const float *__restrict__ g, int rows, int V, bool scaled, Cuts cuts,
                       LossHead *__restrict__ head, int *__restrict__ list, int *__restrict__ place, float *__restrict__ loss, float *__restrict__ lse)
 {
     __shared__ int waves[16];
@@ -131,7 +140,7 @@ void loss_list_kernel(Targets t, const uint8_t *__restrict__ flags, const float 
     top = wave_top(top);
     if (lane == 0) tops[wave] = top;
     __syncthreads();
-    if (wave == 1) write_cuts(head, rows_cut, table_cut, before, lane);
+    if (wave == 1) write_cuts(head, cuts, before, lane);
     if (threadIdx.x != 0) return;
     for (int w = 1; w < 16; ++w) top = fmaxf(top, tops[w]);
     write_head(head, before, scale_of(top, scaled));
@@ -147,7 +156,7 @@ struct GatherArgs {
     LossHead *head;
     const int *place;                 // (FEW: found out here, and the head and the list written)
     int *list;
-    Cut rows_cut, table_cut;
+    Cuts cuts;
     bool scaled;
     void *xc;
     int32_t *ids;                     // [place][k], a row's in rising order
@@ -244,7 +253,7 @@ void loss_gather_kernel(GatherArgs p)
         at = own >> (row & 63) & 1 ? before + __popcll(own & ((1ull << (row & 63)) - 1)) : -1;
         up = scale_of(top, p.scaled);
         if (row == 0) {
-            write_cuts(p.head, p.rows_cut, p.table_cut, count, lane);
+            write_cuts(p.head, p.cuts, count, lane);
             if (lane == 0) write_head(p.head, count, up);
         }
         if (lane == 0) {
@@ -497,11 +506,11 @@ constexpr size_t PARTS_BYTES = (size_t)256 << 20;
 
 struct LossPlan {
     bool gather;                      // rows that count are copied next to each other
-    int form, form_rows, form_table;
+    int form;
     int64_t ld;                       // rows, in whole blocks of 64
     int tiles;                        // of the vocabulary (forward)
-    int piece, most_splits, most_splits_table;
-    Cut rows_cut, table_cut;
+    int piece, most_splits;
+    Cuts both, table_alone, cuts;     // (the last of a call, by what it wants)
     int64_t start_ld;
     size_t list, place, flags, pick, ids, of_ids, start, lse2, g, xc, part, probs, out, out_table, bytes;
 };
@@ -519,9 +528,9 @@ int64_t tiles_of(int form, int64_t m, int64_t n) { return (m + tile_edge(form) -
 //   100 rows,   131072 of 4096          246    187    193    298
 //   4000 rows,  20000 of 640            121    146    197    245
 //   2000 rows,  65536 of 2048           425    524    624    855
+constexpr float TURN[] = {1.0f, 0.68f, 0.46f, 0.35f}, HALF[] = {1.0f, 0.55f, 0.46f, 0.22f};           // (no CU with two)
 int logits_form(int64_t tokens, int64_t rows)
 {
-    constexpr float TURN[] = {1.0f, 0.68f, 0.46f, 0.35f}, HALF[] = {1.0f, 0.55f, 0.46f, 0.22f};       // (no CU with two)
     int best = 0;
     float least = 0.0f;
     for (int f = 0; f < TILE_FORMS; ++f) {
@@ -535,26 +544,45 @@ int logits_form(int64_t tokens, int64_t rows)
     return best;
 }
 
-// Tiles of a gradient [n][m], its sums over `depth` cut into at most `most` parts: likewise; most: in how many.
-int gradient_form(int64_t m, int64_t n, int64_t depth, int &most)
+// The gradients' form and how they may be cut: of those that are wanted, in one launch if it is both.  (A step of a tile of 256 x 256 takes some 1.5 us, in which
+// 6 MB are read; the table's parts are written, too, in place of the result.)  Backward calls in us, in tiles of 256 and 128 of both gradients:
+//   128 rows,   2000 tokens of 512     24.8   21.7
+//   500 rows,   3000 of 2048           69.6   52.4
+//   233 rows,   10007 of 776           43.3   45.2
+//   1500 rows,  30011 of 1032           317    361
+//   100 rows,   65536 of 4096           401    440
+//   2000 rows,  65536 of 2048          1368   1583
+Cuts gradient_cuts(const Vocab &v, int64_t rows, int64_t tokens, int most_rows, int most_table, bool of_rows, bool of_table)
 {
-    float cost[2];
-    int parts[2];
-    const int steps = (int)((depth + 63) / 64);
+    constexpr int PARTS[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};       // (on the device all are looked at)
+    float least = INFINITY;
+    Cuts best = {};
     for (int f = 0; f < 2; ++f) {
-        const int64_t tiles = tiles_of(f, m, n);
-        const float turn[] = {1.0f, 0.68f}, half[] = {1.0f, 0.55f};
-        for (int s = 1; s == 1 || (tiles < tile_slots(f) && s <= most && s <= (steps + 3) / 4); ++s) {
-            const float c = (tiles * s <= 256 ? half[f] : turn[f]) * split_cost(s, (int)(tiles < (1 << 24) ? tiles : 1 << 24), tile_slots(f), steps);
-            if (s == 1 || c < cost[f]) {
-                cost[f] = c;
-                parts[f] = s;
+        const int edge = tile_edge(f);
+        const float part = 4.0f * (float)v.C / 6e6f / TURN[f];
+        Cuts c = {f, tile_slots(f), of_rows ? (v.C + edge - 1) / edge : 0, edge, (int)((tokens + 63) / 64), most_rows,
+                  of_table ? (int)tiles_of(f, v.C, tokens) : 0, most_table, part, 2.0f * part * (float)tokens};
+        const Sums a = c.of_rows((int)rows), b = c.of_table((int)rows);
+        const int last_rows = a.limit(c.slots), last_table = b.limit(c.slots);
+        float cost = INFINITY, groups = 0.0f;
+        for (int r : PARTS) {
+            if (r > 1 && r > last_rows) break;
+            for (int t : PARTS) {
+                if (t > 1 && t > last_table) break;
+                const float here = cut_cost(a, r, b, t, (float)c.slots);
+                if (!(here < cost)) continue;
+                cost = here;
+                groups = a.tiles * (float)r + b.tiles * (float)t;
+                c.most_table = t;              // (the fewer rows count, the fewer parts the table's are cut into)
             }
         }
+        cost *= groups <= 256.0f ? HALF[f] : TURN[f];
+        if (cost < least) {
+            least = cost;
+            best = c;
+        }
     }
-    const int form = cost[1] < cost[0] ? TILE_128 : TILE_256;
-    most = parts[form];
-    return form;
+    return best;
 }
 
 LossPlan loss_plan(const Vocab &v, int64_t rows, const Targets &t, bool backward)
@@ -595,21 +623,15 @@ LossPlan loss_plan(const Vocab &v, int64_t rows, const Targets &t, bool backward
         auto parts = [&](size_t one) { return (int)(one * MOST_SPLITS <= PARTS_BYTES ? MOST_SPLITS : one * 2 > PARTS_BYTES ? 1 : PARTS_BYTES / one); };
         const size_t part = (size_t)rows * v.C * 4, part_table = (size_t)p.piece * v.C * 4;
         p.most_splits = parts(part);
-        // (how many rows count is not known here; the fewer, the more parts are worth while)
-        int ignored = p.most_splits;
-        p.form_rows = gradient_form(v.C, rows, p.piece, ignored);
-        // (and here the fewer)
-        p.most_splits_table = parts(part_table);
-        p.form_table = gradient_form(v.C, p.piece, rows, p.most_splits_table);
-        const int tokens = v.V < p.piece ? v.V : p.piece;
-        const int edge = tile_edge(p.form_rows);
-        p.rows_cut = {(v.C + edge - 1) / edge, edge, tile_slots(p.form_rows), (tokens + 63) / 64, p.most_splits};
-        p.table_cut = {(int)tiles_of(p.form_table, v.C, tokens), 0, tile_slots(p.form_table), 0, p.most_splits_table};
+        const int64_t tokens = v.V < p.piece ? v.V : p.piece;
+        p.both = gradient_cuts(v, rows, tokens, p.most_splits, parts(part_table), true, true);
+        p.table_alone = gradient_cuts(v, rows, tokens, 1, parts(part_table), false, true);
+        const int most_table = p.both.most_table > p.table_alone.most_table ? p.both.most_table : p.table_alone.most_table;
         p.lse2 = take(p.ld * 4);
         p.g = take(p.ld * 4);
         p.probs = take((size_t)p.ld * p.piece * 2);
         p.out = take(part * p.most_splits);
-        p.out_table = take(p.most_splits_table > 1 ? part_table * p.most_splits_table : 0);
+        p.out_table = take(most_table > 1 ? part_table * most_table : 0);
     }
     p.bytes = at;
     return p;
@@ -629,11 +651,11 @@ int launch_rows(const Vocab &v, const LossPlan &plan, const Rows16 &x, int64_t r
     const bool few = rows > 0 && rows <= FOUND_HERE && (!t.k || (dloss && rows * t.k <= FOUND_ENTRIES));
     if (flags && rows) loss_flags_kernel<<<dim3(blocks), 256, 0, s>>>(t, v.V, (int)rows, flags, loss, lse_out, picked);
     if (!few)
-        loss_list_kernel<<<1, 1024, 0, s>>>(t, flags, dloss, (int)rows, v.V, scaled, plan.rows_cut, plan.table_cut, head, list, place, loss, lse_out);
+        loss_list_kernel<<<1, 1024, 0, s>>>(t, flags, dloss, (int)rows, v.V, scaled, plan.cuts, head, list, place, loss, lse_out);
     if (rows) {
         GatherArgs g = {};
         g.t = t; g.x = x.p; g.ldx = x.ld; g.rows = (int)rows; g.V = v.V; g.C = v.C; g.head = head; g.place = place;
-        g.list = list; g.rows_cut = plan.rows_cut; g.table_cut = plan.table_cut; g.scaled = scaled;
+        g.list = list; g.cuts = plan.cuts; g.scaled = scaled;
         g.loss = loss; g.lse_out = lse_out;
         g.xc = ws + plan.xc; g.ids = (int32_t *)(ws + plan.ids);
         g.start = (uint16_t *)(ws + plan.start); g.start_ld = plan.start_ld;
@@ -698,7 +720,10 @@ int launch_loss_forward(const Vocab &v, const Rows16 &x, int64_t rows, const Row
 int launch_loss_backward(const Vocab &v, const Rows16 &x, int64_t rows, const Rows16 &table, const Targets &t, const float *lse, const float *dloss,
                          void *dx, int64_t lddx, void *dtable, bool accumulate, void *workspace, hipStream_t s)
 {
-    const LossPlan plan = loss_plan(v, rows, t, true);
+    LossPlan plan = loss_plan(v, rows, t, true);
+    const bool both = dx && dtable;
+    const int64_t tokens = v.V < plan.piece ? v.V : plan.piece;
+    plan.cuts = both ? plan.both : dtable ? plan.table_alone : gradient_cuts(v, rows, tokens, plan.most_splits, 1, true, false);
     if (tiles_of(plan.form, plan.piece, rows) >= MOST_TILES) return SNN_ERR_UNSUPPORTED;
     char *const ws = (char *)workspace;
     int rc = launch_rows(v, plan, x, rows, t, lse, dloss, dx, lddx, nullptr, nullptr, nullptr, ws, s);
@@ -721,33 +746,28 @@ int launch_loss_backward(const Vocab &v, const Rows16 &x, int64_t rows, const Ro
         p.lse2 = (const float *)(ws + plan.lse2); p.g = (const float *)(ws + plan.g);
         p.probs = ws + plan.probs; p.ldp = plan.piece;
         if ((rc = launch_vocab_tiles(PROBS, plan.form, v.dtype, p, s)) != SNN_OK) return rc;
-        if (dx) {
-            TilesArgs r = {};
-            r.head = p.head;
-            r.a = rows_of_piece; r.lda = table.ld; r.M = v.C;
-            r.b = p.probs; r.ldb = p.ldp; r.N = (int)rows; r.K = n;
-            // (the number of parts is the same for all pieces: a shorter last one leaves some empty)
-            r.out = (float *)(ws + plan.out); r.out_split = split; r.most_splits = plan.most_splits; r.add = v0 > 0;
-            if ((rc = launch_vocab_tiles(ROWS, plan.form_rows, v.dtype, r, s)) != SNN_OK) return rc;
-        }
-        if (dtable) {
-            TilesArgs w = {};
-            w.head = p.head;
-            w.a = p.b; w.lda = v.C; w.M = v.C;
-            w.b = p.probs; w.ldb = p.ldp; w.N = n; w.K = (int)rows;
-            w.v0 = (int)v0; w.dtable = dtable; w.accumulate = accumulate;
-            w.out = (float *)(ws + plan.out_table); w.out_split = (int64_t)n * v.C;
-            w.most_splits = plan.most_splits_table;
-            if ((rc = launch_vocab_tiles(TABLE, plan.form_table, v.dtype, w, s)) != SNN_OK) return rc;
-            if (w.most_splits > 1) {
-                const dim3 grid((unsigned)((n + 3) / 4), (unsigned)((v.C + 511) / 512));
-                void *const to = (char *)dtable + v0 * v.C * 2;
-                if (v.dtype == SNN_DTYPE_BF16)
-                    loss_table_kernel<__bf16><<<grid, 256, 0, s>>>(w.out, w.out_split, n, v.C, w.head, (__bf16 *)to, accumulate);
-                else
-                    loss_table_kernel<_Float16><<<grid, 256, 0, s>>>(w.out, w.out_split, n, v.C, w.head, (_Float16 *)to, accumulate);
-                if ((rc = check_launch()) != SNN_OK) return rc;
-            }
+        TilesArgs r = {}, w = {};
+        r.head = w.head = p.head;
+        r.a = rows_of_piece; r.lda = table.ld; r.M = v.C;
+        r.b = p.probs; r.ldb = p.ldp; r.N = (int)rows; r.K = n;
+        // (the number of parts is the same for all pieces: a shorter last one leaves some empty)
+        r.out = (float *)(ws + plan.out); r.out_split = split; r.most_splits = plan.most_splits; r.add = v0 > 0;
+        w.a = p.b; w.lda = v.C; w.M = v.C;
+        w.b = p.probs; w.ldb = p.ldp; w.N = n; w.K = (int)rows;
+        w.v0 = (int)v0; w.dtable = dtable; w.accumulate = accumulate;
+        w.out = (float *)(ws + plan.out_table); w.out_split = (int64_t)n * v.C;
+        w.most_splits = plan.cuts.most_table;
+        rc = both ? launch_vocab_gradients(plan.cuts.form, v.dtype, r, w, s) :
+             dx ? launch_vocab_tiles(ROWS, plan.cuts.form, v.dtype, r, s) : launch_vocab_tiles(TABLE, plan.cuts.form, v.dtype, w, s);
+        if (rc != SNN_OK) return rc;
+        if (dtable && w.most_splits > 1) {
+            const dim3 grid((unsigned)((n + 3) / 4), (unsigned)((v.C + 511) / 512));
+            void *const to = (char *)dtable + v0 * v.C * 2;
+            if (v.dtype == SNN_DTYPE_BF16)
+                loss_table_kernel<__bf16><<<grid, 256, 0, s>>>(w.out, w.out_split, n, v.C, w.head, (__bf16 *)to, accumulate);
+            else
+                loss_table_kernel<_Float16><<<grid, 256, 0, s>>>(w.out, w.out_split, n, v.C, w.head, (_Float16 *)to, accumulate);
+            if ((rc = check_launch()) != SNN_OK) return rc;
         }
     }
     if (!dx || rows == 0) return SNN_OK;

@@ -107,10 +107,10 @@ struct Place {
     int m, n, split;
 };
 
-__device__ inline bool find_place(int tm, int tn, int splits, Place &at)
+__device__ inline bool find_place(uint32_t block, int tm, int tn, int splits, Place &at)
 {
-    const uint32_t each = (uint32_t)tm * tn, total = each * splits, share = (total + 7) / 8, turn = blockIdx.x >> 3;
-    const uint32_t id = (blockIdx.x & 7) * share + turn;
+    const uint32_t each = (uint32_t)tm * tn, total = each * splits, share = (total + 7) / 8, turn = block >> 3;
+    const uint32_t id = (block & 7) * share + turn;
     if (turn >= share || id >= total) return false;
     at.split = id / each;
     const uint32_t r = id - at.split * each, group = r / (8 * tn), first = group * 8, rest = r - first * tn;
@@ -136,10 +136,9 @@ __device__ inline bool find_place(int tm, int tn, int splits, Place &at)
 // exponentials), nothing hides: with 2048 channels, 32 steps, STATS of 3686 rows of 65536 tokens 0.85 ms, the library's product 0.75.
 // For few rows memory bounds STATS: one row against 131072 tokens of 4096 channels 182 us, 5.9 TB/s.
 // A tile of 256 x 256 reads half of what four of 128 x 128 do, and is the faster where there are enough; smaller ones are for fewer rows (logits_form,
-// gradient_form).
+// gradient_cuts).
 template <class T, int KIND, int BM, int BN, int WM, int WN, int STAGES>
-__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2)
-void vocab_tiles_kernel(TilesArgs p)
+__device__ inline void tile(const TilesArgs &p, const uint32_t block)
 {
     using H = Half<T>;
     using v8 = typename H::v8;
@@ -159,7 +158,7 @@ void vocab_tiles_kernel(TilesArgs p)
     if constexpr (KIND == ROWS || KIND == TABLE)
         splits = __builtin_amdgcn_readfirstlane(min(max(KIND == ROWS ? p.head->splits_rows : p.head->splits_table, 1), p.most_splits));
     Place at;
-    if (!find_place(tm, tn, splits, at)) return;
+    if (!find_place(block, tm, tn, splits, at)) return;
     int first = 0;
     if constexpr (KIND == ROWS || KIND == TABLE) {
         const int run = (steps + splits - 1) / splits;
@@ -466,20 +465,68 @@ void vocab_tiles_kernel(TilesArgs p)
 }
 
 template <class T, int KIND, int BM, int BN, int WM, int WN, int STAGES>
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2)
+void vocab_tiles_kernel(TilesArgs p)
+{
+    tile<T, KIND, BM, BN, WM, WN, STAGES>(p, blockIdx.x);
+}
+
+// ROWS and TABLE, which do not wait for each other, as one launch: one fills what the other leaves of the chip.  (600 rows of 30011 tokens forward and backward
+// 267 -> 250 us, 1000 rows of 5000 tokens of 512 channels backward 59 -> 45; large calls, whose products fill the chip many times, as before)
+template <class T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2)
+void vocab_gradients_kernel(TilesArgs rows, TilesArgs table, uint32_t of_rows)
+{
+    if (blockIdx.x < of_rows) tile<T, ROWS, BM, BN, WM, WN, 2>(rows, blockIdx.x);
+    else tile<T, TABLE, BM, BN, WM, WN, 2>(table, blockIdx.x - of_rows);
+}
+
+template <int KIND, int BM, int BN, int WM, int WN, int STAGES>
+constexpr size_t tiles_lds()
+{
+    constexpr size_t TILES = (size_t)STAGES * (BM + BN) * 128;
+    constexpr size_t OUT = KIND == STATS ? (size_t)(BM / WM) * BN * 8 : (size_t)(BM / WM) * (BN / WN) * 16 * (WM * (KIND == PROBS ? 2 : 4) + 16);
+    return TILES > OUT ? TILES : OUT;
+}
+
+// workgroups: a tile of a part each, in eights (rows that count are fewer than all, perhaps, and then in more parts: of two turns of the chip at most)
+template <int KIND>
+int64_t tiles_grid(const TilesArgs &p, int bm, int bn)
+{
+    const int64_t tiles = (int64_t)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn), turns = bm == 256 ? 2 * tile_slots(TILE_256) : 2 * tile_slots(TILE_128);
+    int64_t groups = tiles;
+    if (KIND == ROWS || KIND == TABLE) groups *= p.most_splits;
+    if (KIND == ROWS && groups > turns) groups = tiles > turns ? tiles : turns;
+    return (groups + 7) / 8 * 8;
+}
+
+template <class T, int KIND, int BM, int BN, int WM, int WN, int STAGES>
 int launch_tiles(const TilesArgs &p, hipStream_t s)
 {
-    constexpr int WAVES = (BM / WM) * (BN / WN);
-    constexpr size_t TILES = (size_t)STAGES * (BM + BN) * 128;
-    constexpr size_t OUT = KIND == STATS ? (size_t)(BM / WM) * BN * 8 : (size_t)WAVES * 16 * (WM * (KIND == PROBS ? 2 : 4) + 16);
-    constexpr size_t LDS = TILES > OUT ? TILES : OUT;
+    constexpr size_t LDS = tiles_lds<KIND, BM, BN, WM, WN, STAGES>();
     static_assert(LDS <= 160 * 1024, "LDS");
     static LdsGrant grant;
     const auto kernel = vocab_tiles_kernel<T, KIND, BM, BN, WM, WN, STAGES>;
     const int rc = grant_dynamic_lds((const void *)kernel, LDS, grant);
     if (rc != SNN_OK) return rc;
-    const int64_t tiles = (int64_t)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN) * (KIND == ROWS || KIND == TABLE ? p.most_splits : 1);
-    if (tiles == 0) return SNN_OK;
-    kernel<<<dim3((unsigned)((tiles + 7) / 8 * 8)), 64 * WAVES, LDS, s>>>(p);
+    const int64_t grid = tiles_grid<KIND>(p, BM, BN);
+    if (grid == 0) return SNN_OK;
+    kernel<<<dim3((unsigned)grid), 64 * (BM / WM) * (BN / WN), LDS, s>>>(p);
+    return check_launch();
+}
+
+template <class T, int BM, int BN, int WM, int WN>
+int launch_gradients(const TilesArgs &rows, const TilesArgs &table, hipStream_t s)
+{
+    constexpr size_t LDS = tiles_lds<ROWS, BM, BN, WM, WN, 2>();
+    static_assert(LDS == tiles_lds<TABLE, BM, BN, WM, WN, 2>(), "of both");
+    static LdsGrant grant;
+    const auto kernel = vocab_gradients_kernel<T, BM, BN, WM, WN>;
+    const int rc = grant_dynamic_lds((const void *)kernel, LDS, grant);
+    if (rc != SNN_OK) return rc;
+    const int64_t of_rows = tiles_grid<ROWS>(rows, BM, BN), of_table = tiles_grid<TABLE>(table, BM, BN);
+    if (of_rows + of_table == 0) return SNN_OK;
+    kernel<<<dim3((unsigned)(of_rows + of_table)), 64 * (BM / WM) * (BN / WN), LDS, s>>>(rows, table, (uint32_t)of_rows);
     return check_launch();
 }
 
@@ -506,6 +553,13 @@ int launch_kind(int kind, int form, const TilesArgs &p, hipStream_t s)
 }
 
 }  // namespace
+
+int launch_vocab_gradients(int form, int dtype, const TilesArgs &rows, const TilesArgs &table, hipStream_t s)
+{
+    if (dtype == SNN_DTYPE_BF16)
+        return form == TILE_256 ? launch_gradients<__bf16, 256, 256, 128, 64>(rows, table, s) : launch_gradients<__bf16, 128, 128, 64, 64>(rows, table, s);
+    return form == TILE_256 ? launch_gradients<_Float16, 256, 256, 128, 64>(rows, table, s) : launch_gradients<_Float16, 128, 128, 64, 64>(rows, table, s);
+}
 
 int launch_vocab_tiles(int kind, int form, int dtype, const TilesArgs &p, hipStream_t s)
 {
