@@ -131,8 +131,8 @@ __device__ inline bool find_place(uint32_t block, int tm, int tn, int splits, Pl
 // results.  Softmax statistics stay fp32: of a tile the largest logit and the sum of exponentials of what the others fall short of it, joined tile by tile.
 //
 // For many rows the matrix cores bound it, at the clock that the chip's power leaves: 8028 rows of 131072 tokens, 4096 channels, bf16: STATS 6.2 - 6.7 ms by card
-// (1.29 - 1.39 PFLOP/s, 65 % of cycles busy at 2.0 GHz), PROBS 6.4 - 7.0, ROWS 6.7 - 7.0, TABLE 6.4 - 6.6; library products of these sizes, which do nothing else, 5.85 for
-// logits, 6.5 and 7.3 for the gradients.  A step of a 256 x 256 tile takes 1.5 us; what comes before a tile's first and after its last, some 6 us (half of them
+// (1.29 - 1.39 PFLOP/s, 65 % of cycles busy at 2.0 GHz), PROBS 6.4 - 7.0, ROWS 6.7 - 7.0, TABLE 6.4 - 6.6, these two together 13.2; library products of these sizes, which
+// do nothing else, 5.85 for logits, 6.5 and 7.3 for the gradients.  A step of a 256 x 256 tile takes 1.5 us; what comes before a tile's first and after its last, some 6 us (half of them
 // exponentials), nothing hides: with 2048 channels, 32 steps, STATS of 3686 rows of 65536 tokens 0.85 ms, the library's product 0.75.
 // For few rows memory bounds STATS: one row against 131072 tokens of 4096 channels 182 us, 5.9 TB/s.
 // A tile of 256 x 256 reads half of what four of 128 x 128 do, and is the faster where there are enough; smaller ones are for fewer rows (logits_form,
