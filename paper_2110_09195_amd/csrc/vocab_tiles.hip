@@ -138,7 +138,8 @@ __device__ inline bool find_place(uint32_t block, int tm, int tn, int splits, Pl
 // A tile of 256 x 256 reads half of what four of 128 x 128 do, and is the faster where there are enough; smaller ones are for fewer rows (logits_form,
 // gradient_cuts).
 template <class T, int KIND, int BM, int BN, int WM, int WN, int STAGES>
-__device__ inline void tile(const TilesArgs &p, const uint32_t block)
+__device__ inline void tile_at(const TilesArgs &p, const Place at, const int N, const int K, const int first, const int steps, const int splits, const int m0,
+                               const int n0)
 {
     using H = Half<T>;
     using v8 = typename H::v8;
@@ -149,23 +150,6 @@ __device__ inline void tile(const TilesArgs &p, const uint32_t block)
     using B = Operand<BN, THREADS, KW, KIND == TABLE>;
     constexpr int STAGE = A::BYTES + B::BYTES, LOADS = A::L + B::L;
     extern __shared__ __align__(16) char lds[];
-
-    const int count = p.head ? __builtin_amdgcn_readfirstlane(p.head->count) : KIND == TABLE ? p.K : p.N;
-    const int N = KIND == TABLE ? p.N : count, K = KIND == TABLE ? count : p.K;
-    const int tm = (p.M + BM - 1) / BM, tn = (N + BN - 1) / BN;
-    int steps = (K + KW - 1) / KW;
-    int splits = 1;
-    if constexpr (KIND == ROWS || KIND == TABLE)
-        splits = __builtin_amdgcn_readfirstlane(min(max(KIND == ROWS ? p.head->splits_rows : p.head->splits_table, 1), p.most_splits));
-    Place at;
-    if (!find_place(block, tm, tn, splits, at)) return;
-    int first = 0;
-    if constexpr (KIND == ROWS || KIND == TABLE) {
-        const int run = (steps + splits - 1) / splits;
-        first = at.split * run;
-        steps = max(min(steps - first, run), 0);
-    }
-    const int m0 = at.m * BM, n0 = at.n * BN;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave % WAVES_M, wn = wave / WAVES_M;
     const uint32_t lds0 = lds_address(lds);
@@ -245,8 +229,8 @@ __device__ inline void tile(const TilesArgs &p, const uint32_t block)
             __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);                // VALU
         }
     };
-    // A wave with nothing but rows or columns behind the last multiplies nothing: it loads its share and keeps the barriers.  (2055 rows of 65536 tokens, whose
-    // ninth tiles have seven rows: 545 -> 518 us)
+    // A wave with nothing but rows or columns behind the last multiplies nothing: it loads its share and keeps the barriers.  (1500 rows of 30011 tokens backward
+    // 365 -> 346 us)
     const bool idle = m0 + wm * WM >= p.M || n0 + wn * WN >= N;
     if constexpr (STAGES == 2) {
         // A slot is free once the fragments of its last phase are read, before these are multiplied: from then on the step after the next is loaded
@@ -464,6 +448,34 @@ __device__ inline void tile(const TilesArgs &p, const uint32_t block)
     }
 }
 
+// Rows that count, tiles and parts as the device knows them; the workgroup's own.  The last 64 rows or fewer in a narrower tile of the same tokens or channels, with
+// four stages, as a step of it is shorter than a load's way (2055 rows of 65536 tokens of 2048 channels, seven of them in the last tile: 493 -> 470 us; tiles of
+// 128 rows, for which there is no room for more than two stages ahead, take what those of 256 do).
+template <class T, int KIND, int BM, int BN, int WM, int WN, int STAGES>
+__device__ inline void tile(const TilesArgs &p, const uint32_t block)
+{
+    const int count = p.head ? __builtin_amdgcn_readfirstlane(p.head->count) : KIND == TABLE ? p.K : p.N;
+    const int N = KIND == TABLE ? p.N : count, K = KIND == TABLE ? count : p.K;
+    const int tm = (p.M + BM - 1) / BM, tn = (N + BN - 1) / BN;
+    int steps = (K + 63) / 64;
+    int splits = 1;
+    if constexpr (KIND == ROWS || KIND == TABLE)
+        splits = __builtin_amdgcn_readfirstlane(min(max(KIND == ROWS ? p.head->splits_rows : p.head->splits_table, 1), p.most_splits));
+    Place at;
+    if (!find_place(block, tm, tn, splits, at)) return;
+    int first = 0;
+    if constexpr (KIND == ROWS || KIND == TABLE) {
+        const int run = (steps + splits - 1) / splits;
+        first = at.split * run;
+        steps = max(min(steps - first, run), 0);
+    }
+    const int m0 = at.m * BM, n0 = at.n * BN;
+    if constexpr (BN == 256 && KIND != TABLE) {
+        if (N - n0 <= 64) return tile_at<T, KIND, BM, 64, 32, 64, 4>(p, at, N, K, first, steps, splits, m0, n0);
+    }
+    tile_at<T, KIND, BM, BN, WM, WN, STAGES>(p, at, N, K, first, steps, splits, m0, n0);
+}
+
 template <class T, int KIND, int BM, int BN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2)
 void vocab_tiles_kernel(TilesArgs p)
@@ -486,6 +498,7 @@ constexpr size_t tiles_lds()
 {
     constexpr size_t TILES = (size_t)STAGES * (BM + BN) * 128;
     constexpr size_t OUT = KIND == STATS ? (size_t)(BM / WM) * BN * 8 : (size_t)(BM / WM) * (BN / WN) * 16 * (WM * (KIND == PROBS ? 2 : 4) + 16);
+    if (BM == 256) return 160 * 1024;                          // (the narrow tile's)
     return TILES > OUT ? TILES : OUT;
 }
 

@@ -227,6 +227,13 @@ def test_large(rows, V, C, dtype, k):
     check_loss(rows, V, C, dtype, none=0.6 if rows > 4000 else 0.1, k=k, temperature=2.0 if k else 1.0)
 
 
+# the last rows of a large tile: one, as many as the narrow one takes, more, and all
+@pytest.mark.parametrize("last", [1, 17, 64, 65, 129, 256])
+@pytest.mark.parametrize("dtype, k", [(BF, 0), (HF, 3)])
+def test_last_rows(last, dtype, k):
+    check_loss(512 + last, 40003, 200, dtype, none=0.0, k=k, temperature=1.5 if k else 1.0)
+
+
 @pytest.mark.parametrize("rows", [3, 300])
 @pytest.mark.parametrize("k", [0, 4])
 def test_no_row_counts(rows, k):
