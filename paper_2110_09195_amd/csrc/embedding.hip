@@ -58,62 +58,65 @@ void embedding_kernel(const T *__restrict__ table, int64_t ldt, const int32_t *_
 // The rows by token, rows of one token in their own order, so that sums have a fixed order.  Tokens are compared as unsigned numbers: those
 // of no row of the table come last.
 
-// Up to MERGED rows: blocks of RANK_BLOCK rows are sorted by themselves - a row's place is the number of the block's tokens below its own, and of
-// its own in earlier rows; 64 rows a workgroup, whose waves share out the tokens that they are compared with - and a row's
-// place among all is its place there and those that a binary search finds for it in the other blocks.
-// Bound by latency: 16384 rows 7.5 and 4 us (every row compared with every other, in one launch: 55).  A whole call of 65536 rows of 64 channels to 50000 tokens
-// takes 49 us, one row more by the passes below 55.
-constexpr int64_t MERGED = 65536;
-constexpr int RANK_BLOCK = 1024, RANK_WAVES = 8, MERGE_WAVES = 16;
+// A row's place is the number of tokens below its own, and of its own in earlier rows.  Up to RANKED rows: found by comparing with all, 32 rows a workgroup, whose
+// half waves share out the tokens that these are compared with.  Up to MERGED rows: blocks of RANK_BLOCK rows are sorted so by themselves, and a row's place
+// among all is its place there and those that a binary search finds for it in the other blocks.
+// Bound by latency: 1024 rows 5 us and blocks of them as many, 4 more for those of 16384 rows; a whole call of 2048 rows of 1032 channels takes 15.1 us, of 2049 16.7
+// (of 7001 in one launch 24.3, in two 18.9).
+constexpr int RANKED = 2048, MERGED = 65536;
+constexpr int RANK_BLOCK = 1024, RANK_WAVES = 16, MERGE_WAVES = 16;
+
+// tokens of no row of the table are one, V
+__device__ inline uint32_t sort_key(const uint32_t *keys, int64_t i, uint32_t V) { return min(keys[i], V); }
 
 __global__ __launch_bounds__(64 * RANK_WAVES)
-void embedding_rank_kernel(const uint32_t *__restrict__ ids, int rows, uint32_t *__restrict__ sorted, int *__restrict__ order)
+void embedding_rank_kernel(const uint32_t *__restrict__ ids, int rows, uint32_t V, int block, uint32_t *__restrict__ sorted, int *__restrict__ order)
 {
     __shared__ int counts[RANK_WAVES][64];
-    __shared__ __align__(16) uint32_t tokens[RANK_BLOCK];
+    __shared__ __align__(16) uint32_t tokens[RANKED];
+    constexpr int THREADS = 64 * RANK_WAVES;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int i0 = blockIdx.x * 64, i = i0 + lane, first = i0 / RANK_BLOCK * RANK_BLOCK, n = min(RANK_BLOCK, rows - first);
-    constexpr int EACH = RANK_BLOCK / (64 * RANK_WAVES);
-    uint32_t v[EACH];
+    const int i0 = blockIdx.x * 32, first = i0 / block * block, n = min(block, rows - first), at = i0 - first;
+    // a half wave's tokens, in whole 32: all are before, all behind or among the workgroup's rows
+    const int share = (n + THREADS - 1) / THREADS * 32;
+    const int lo = (2 * wave + (lane >> 5)) * share, lo_wave = 2 * wave * share;
+    uint32_t v[RANKED / THREADS];
 #pragma unroll
-    for (int k = 0; k < EACH; ++k) v[k] = ids[first + min(k * 64 * RANK_WAVES + (int)threadIdx.x, n - 1)];
+    for (int k = 0; k < RANKED / THREADS; ++k)
+        if (k * THREADS < n) v[k] = sort_key(ids, first + min(k * THREADS + (int)threadIdx.x, n - 1), V);
 #pragma unroll
-    for (int k = 0; k < EACH; ++k) {
-        const int at = k * 64 * RANK_WAVES + threadIdx.x;
-        tokens[at] = at < n ? v[k] : ~0u;
-    }
+    for (int k = 0; k < RANKED / THREADS; ++k)
+        if (k * THREADS < n) tokens[k * THREADS + threadIdx.x] = k * THREADS + (int)threadIdx.x < n ? v[k] : ~0u;
     __syncthreads();
-    const uint32_t mine = i < rows ? tokens[i - first] : 0;
-    constexpr int SHARE = RANK_BLOCK / RANK_WAVES;             // a multiple of 64: a wave's tokens are all before, all behind or among the workgroup's
-    const int lo = wave * SHARE, at = i0 - first;
-    const u32x4 *const from = (const u32x4 *)(tokens + lo);
+    const int i = at + (lane & 31);
+    const uint32_t mine = i < n ? tokens[i] : 0;
     int below = 0;
-    // (behind the last row: the largest number there is, below none and after all)
-    if (lo + SHARE <= at) {
-#pragma unroll 8
-        for (int j = 0; j < SHARE / 4; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) below += from[j][e] <= mine ? 1 : 0;
-    } else if (lo >= at + 64) {
-        if (lo < n)
-#pragma unroll 8
-            for (int j = 0; j < SHARE / 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) below += from[j][e] < mine ? 1 : 0;
-    } else {
+    // (behind the last row: the largest number there is, below none)
+    if (lo_wave < n) {
+        const u32x4 *const from = (const u32x4 *)(tokens + lo);
+        if (at >= lo_wave && at < lo_wave + 2 * share) {
 #pragma unroll 4
-        for (int j = 0; j < SHARE / 4; ++j)
+            for (int j = 0; j < share / 4; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) below += from[j][e] < mine || (from[j][e] == mine && lo + 4 * j + e < i - first) ? 1 : 0;
+                for (int e = 0; e < 4; ++e) below += from[j][e] < mine || (from[j][e] == mine && lo + 4 * j + e < i) ? 1 : 0;
+        } else {
+            const uint32_t least = mine + (lo < at ? 1 : 0);
+#pragma unroll 8
+            for (int j = 0; j < share / 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) below += from[j][e] < least ? 1 : 0;
+        }
     }
     counts[wave][lane] = below;
     __syncthreads();
-    if (wave == 0 && i < rows) {
-        int place = first;
+    if (wave != 0) return;
+    int place = 0;
 #pragma unroll
-        for (int w = 0; w < RANK_WAVES; ++w) place += counts[w][lane];
-        sorted[place] = mine;
-        order[place] = i;
+    for (int w = 0; w < RANK_WAVES; ++w) place += counts[w][lane];
+    place += __shfl_xor(place, 32);
+    if (lane < 32 && i < n) {
+        sorted[first + place] = mine;
+        order[first + place] = first + i;
     }
 }
 
@@ -162,8 +165,6 @@ void embedding_merge_kernel(const uint32_t *__restrict__ keys, const int *__rest
 // [digit][workgroup] into places; then rows are put there, in their order.  Bound by latency, three launches a pass: 500000 rows of 64 channels to
 // 50000 tokens, two passes, 169 us with their sums.
 constexpr int DIGITS = 256, SORT_ROWS = 2048, SORT_WAVES = 4, SORT_ROUNDS = SORT_ROWS / 64 / SORT_WAVES;
-
-__device__ inline uint32_t sort_key(const uint32_t *keys, int64_t i, uint32_t V) { return min(keys[i], V); }
 
 __global__ __launch_bounds__(256)
 void embedding_count_kernel(const uint32_t *__restrict__ keys, int64_t rows, uint32_t V, int shift, uint32_t *__restrict__ counts, int blocks)
@@ -405,16 +406,23 @@ void embedding_join_kernel(SumArgs p)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t block = blockIdx.x / p.slabs, next = (block + 1) * p.block;
     if (next >= p.rows) return;
-    const uint32_t token = p.sorted[next - 1];
-    if (token >= (uint32_t)p.V || p.sorted[next] != token) return;             // no token goes on,
-    if (block > 0 && p.sorted[block * p.block] == token && p.sorted[block * p.block - 1] == token) return;          // or none that begins here
-    int64_t lo = block + 1, hi = p.blocks;                     // the last block that begins with it: 64 at once
-    while (hi - lo > 1) {
-        const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
-        const int64_t last = lo + step * (__popcll(__ballot(at < hi && p.sorted[min(at, hi - 1) * p.block] == token)) - 1);
-        hi = min(hi, last + step);
-        lo = last;
-    }
+    // (all of it fetched at once: the token, whether it goes on, whether it begins here, and the first tokens of the next 64 blocks)
+    const int64_t here = block * p.block, ahead = block + 1 + lane;
+    const uint32_t token = p.sorted[next - 1], follows = p.sorted[next], begins = p.sorted[here], before = p.sorted[here > 0 ? here - 1 : 0];
+    const uint32_t later = p.sorted[ahead < p.blocks ? ahead * p.block : next];
+    if (token >= (uint32_t)p.V || follows != token) return;                    // no token goes on,
+    if (block > 0 && begins == token && before == token) return;               // or none that begins here
+    // the last block that begins with it
+    const uint64_t others = ~__ballot(ahead < p.blocks && later == token);
+    int64_t lo = block + 64;
+    if (others) lo = block + __builtin_ctzll(others);
+    else
+        for (int64_t hi = p.blocks; hi - lo > 1;) {                            // 64 at once
+            const int64_t step = (hi - lo + 63) / 64, at = lo + lane * step;
+            const int64_t last = lo + step * (__popcll(__ballot(at < hi && p.sorted[min(at, hi - 1) * p.block] == token)) - 1);
+            hi = min(hi, last + step);
+            lo = last;
+        }
     const int64_t n = lo - block + 1, share = (n + JOIN_WAVES - 1) / JOIN_WAVES;
     const int c = (int)(blockIdx.x - block * p.slabs) * 512 + lane * 8;
     float sum[8] = {};
@@ -452,7 +460,7 @@ SortPlan sort_plan(const Vocab &v, int64_t rows)
 {
     SortPlan p = {};
     p.block = rows * ((v.C + 511) / 512) < 2048 * 32 ? 16 : 32;
-    p.twice = rows > RANK_BLOCK;
+    p.twice = rows > RANKED;
     if (rows > MERGED) {
         while (((int64_t)1 << (8 * p.passes)) <= v.V) ++p.passes;              // (V itself stands for what is no token)
         p.blocks = (int)((rows + SORT_ROWS - 1) / SORT_ROWS);
@@ -506,9 +514,11 @@ int launch_embedding_grad(const Vocab &v, const Rows16 &dy, const int32_t *ids, 
     uint32_t *sorted = (uint32_t *)ws, *other = (uint32_t *)((char *)ws + 2 * one);
     int *order = (int *)((char *)ws + one), *other_order = (int *)((char *)ws + 3 * one);
     if (rows > 0 && !plan.passes) {
-        const dim3 grid((unsigned)((rows + 63) / 64));
-        embedding_rank_kernel<<<grid, 64 * RANK_WAVES, 0, s>>>((const uint32_t *)ids, (int)rows, plan.twice ? other : sorted, plan.twice ? other_order : order);
-        if (plan.twice) embedding_merge_kernel<<<grid, 64 * MERGE_WAVES, 0, s>>>(other, other_order, (int)rows, sorted, order);
+        embedding_rank_kernel<<<dim3((unsigned)((rows + 31) / 32)), 64 * RANK_WAVES, 0, s>>>((const uint32_t *)ids, (int)rows, (uint32_t)v.V,
+                                                                                             plan.twice ? RANK_BLOCK : RANKED, plan.twice ? other : sorted,
+                                                                                             plan.twice ? other_order : order);
+        if (plan.twice)
+            embedding_merge_kernel<<<dim3((unsigned)((rows + 63) / 64)), 64 * MERGE_WAVES, 0, s>>>(other, other_order, (int)rows, sorted, order);
         const int rc = check_launch();
         if (rc != SNN_OK) return rc;
     }

@@ -69,12 +69,13 @@ def test_rows_of_no_token_are_zeros_whatever_the_scale():
     assert not B.snn_embedding_forward(B.make_vocab_desc(4, 8), table, ids, NAN).any()
 
 
-# (both ways of sorting, on either side of their border; tokens of one row each, of all rows, of none)
+# (each way of sorting, on either side of its border; tokens of one row each, of all rows, of none)
 @pytest.mark.parametrize("accumulate", [False, True])
 @pytest.mark.parametrize("rows, V, C, dtype, skew", [
     (1, 1, 8, BF, 1), (1, 300, 520, HF, 1), (31, 5, 72, BF, 1), (32, 1, 1032, HF, 1), (33, 2, 8, BF, 1), (64, 64, 512, HF, 1), (257, 9, 520, BF, 3),
     (1000, 70000, 136, BF, 1), (5000, 301, 1032, HF, 3), (16384, 1500, 264, BF, 2), (16385, 1500, 264, HF, 2), (40000, 255, 72, BF, 2),
-    (40000, 256, 72, HF, 1), (40001, 70001, 40, BF, 4)])
+    (40000, 256, 72, HF, 1), (40001, 70001, 40, BF, 4), (2048, 300, 72, HF, 2), (2049, 300, 72, BF, 2), (65536, 999, 16, BF, 2),
+    (65537, 999, 16, HF, 2)])
 def test_gradient_of_the_table(rows, V, C, dtype, skew, accumulate):
     g = gen(rows + V)
     ids = (torch.rand(rows, generator=g, device="cuda") ** skew * (V + 3)).long().sub(1).int()             # -1, 0 .. V - 1, V, V + 1
@@ -100,7 +101,7 @@ def test_gradient_of_the_table(rows, V, C, dtype, skew, accumulate):
     assert torch.equal(again, out.t), "a call repeated gives other bits"
 
 
-@pytest.mark.parametrize("rows", [20000, 3000])
+@pytest.mark.parametrize("rows", [20000, 3000, 1024, 1040, 1041, 1057])
 def test_all_rows_of_one_token(rows):
     desc, g = B.make_vocab_desc(7, 1032, CODE[BF]), gen(5)
     dy = normal(g, rows, 1032).to(BF)
