@@ -97,7 +97,7 @@ __device__ inline void write_head(LossHead *head, int count, const Scale &s)
 }
 
 // The rows that count, in their order, and each row's place among them (-1: none).  One workgroup, so that places need no second launch: 8192 rows 12 - 16 us of
-// a step of 26 ms, 1501 rows 5.  flags = nullptr: found out here.
+// a step of 26 ms.  flags = nullptr: found out here.
 __global__ __launch_bounds__(1024)
 void loss_list_kernel(Targets t, const uint8_t *__restrict__ flags, const float *__restrict__ g, int rows, int V, bool scaled, Cuts cuts,
                       LossHead *__restrict__ head, int *__restrict__ list, int *__restrict__ place, float *__restrict__ loss, float *__restrict__ lse)
@@ -358,8 +358,8 @@ __device__ inline void join(float &m, float &s, float m2, float s2)
 }
 
 // Sums of exponentials of RT rows from those of the tiles, and their losses.  RT by the number of rows, so that parts are read in whole lines where there are
-// many (RT x 8 bytes) and a row has a workgroup to itself where there are few: 8192 rows, 512 tiles 13 us, 75 rows, 391 tiles 4.6.  The loss is formed from what the row's logits fall short of the largest
-// one, not from the sum's logarithm as a whole: small losses keep their digits.
+// many (RT x 8 bytes) and a row has a workgroup to itself where there are few: 8192 rows, 512 tiles 13 us, 75 rows, 391 tiles 4.6.  The loss is formed from what
+// the row's logits fall short of the largest one, not from the sum's logarithm as a whole: small losses keep their digits.
 template <int RT>
 __global__ __launch_bounds__(256)
 void loss_join_kernel(JoinArgs p)

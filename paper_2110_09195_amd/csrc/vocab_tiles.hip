@@ -293,7 +293,6 @@ __device__ inline void tile_at(const TilesArgs &p, const Place at, const int N, 
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const int t = n0 + wn * WN + j * 16 + ln;
-            const bool row = t < N;
             if constexpr (KIND == PROBS) {
 #pragma unroll
                 for (int i = 0; i < MB; ++i)
@@ -335,19 +334,29 @@ __device__ inline void tile_at(const TilesArgs &p, const Place at, const int N, 
                     const bool some = n < to[j];
                     take(some ? p.ids[of_row + n] : -1, of_row + n, KIND == PROBS && some ? p.q[of_row + n] : 0.0f);
                 }
-            } else if (KIND == STATS && p.k > 1)
-                // (of few rows lists are as they came, and all of them is looked at)
-                for (int k0 = 0; k0 < p.k; k0 += 8) {
-                    int token[8];
-                    bool some = false;
+            } else if constexpr (KIND == STATS)
+                if (p.k > 1) {
+                    // Lists as they came, of the block's rows: looked over by all lanes, the logits of those among the wave's tokens fetched from LDS.  (Lists of 64 of
+                    // 20000 tokens, 1000 rows of 512 channels 53 us; by a lane's comparisons with all of its row's list 143.  16 rows, lists of 20 of 32768 30 -> 28)
+                    constexpr int PITCH = WM * 4 + 16;
+                    char *const mine = lds + wave * 16 * PITCH;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        token[e] = row && k0 + e < p.k ? p.ids[of_row + k0 + e] : -1;
-                        some |= token[e] >= 0 && (uint32_t)(token[e] - p.v0 - mw) < most;
+                    for (int i = 0; i < MB; ++i) *(f32x4 *)(mine + ln * PITCH + (i * 16 + 4 * h) * 4) = acc[i][j];
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    const int t0 = n0 + wn * WN + j * 16, n = min(16, N - t0) * p.k;
+                    const int64_t base = (int64_t)t0 * p.k;
+                    for (int e0 = 0; e0 < n; e0 += 4 * 64) {
+                        int token[4];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) token[u] = e0 + u * 64 + lane < n ? p.ids[base + e0 + u * 64 + lane] : -1;
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            const int e = e0 + u * 64 + lane, local = token[u] - p.v0 - mw;
+                            if (token[u] >= 0 && (uint32_t)local < most)
+                                p.picked[base + e] = *(const float *)(mine + (uint32_t)e / (uint32_t)p.k * PITCH + local * 4);
+                        }
                     }
-                    if (!__any(some)) continue;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) take(token[e], of_row + k0 + e, 1.0f);
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 }
             if constexpr (KIND == STATS) {
                 float m = -INFINITY, s = 0.0f;
@@ -368,6 +377,7 @@ __device__ inline void tile_at(const TilesArgs &p, const Place at, const int N, 
             }
         }
         if constexpr (KIND == STATS) {
+            if (!p.start && p.k > 1) __syncthreads();
             float2 *const stat = (float2 *)lds;                // [WAVES_M][BN]
             if (h == 0)
 #pragma unroll

@@ -215,6 +215,8 @@ def test_cross_entropy(rows, V, C, dtype):
     (1, 1, 8, BF, 1, 1.0), (1, 40, 8, HF, 7, 2.0), (5, 129, 72, BF, 256, 0.5), (64, 1000, 136, HF, 9, 4.0), (65, 257, 264, BF, 64, 1.5),
     (130, 4099, 520, HF, 100, 2.0), (333, 300, 72, BF, 20, 1.0), (700, 2000, 256, BF, 3, 3.0),
     (160, 20001, 72, HF, 30, 2.0), (400, 20000, 40, BF, 128, 1.0), (3000, 500, 72, HF, 65, 0.01),
+    # long lists in each form of tiles
+    (16, 20000, 72, BF, 256, 1.0), (276, 317, 72, HF, 103, 2.0), (100, 20000, 72, BF, 65, 1.0), (600, 20001, 72, HF, 130, 2.0),
     # lists that every workgroup looks over, and more
     (512, 500, 72, BF, 8, 2.0), (241, 500, 72, HF, 17, 1.0), (4096, 300, 40, BF, 1, 1.0), (4097, 300, 40, HF, 1, 1.0)])
 def test_distillation(rows, V, C, dtype, k, temperature):
