@@ -172,10 +172,10 @@ struct GatherArgs {
 };
 
 // Rows that count next to each other, with what belongs to them.  A wave a row.  Of a few rows every workgroup looks at all of them itself, which saves a launch
-// (FEW; 1501 rows forward and backward 289 -> 282 us, 333 rows with 11 tokens each 85.7 -> 82.1).
+// (FEW; 1501 rows forward and backward 289 -> 282 us, 333 rows with 11 tokens each 85.7 -> 82.1, 216 rows with 49 backward 45.7 -> 35.1).
 // Bound by memory for many rows (8192 of 4096 channels 28 us, 128 MB), by latency for few (5 us).  The copy is what makes rows that do not count free: of 4096 rows
 // half of which count, 65536 tokens of 2048 channels 466 us where all of them take 862.
-constexpr int FOUND_HERE = 4096, FOUND_ENTRIES = 4096;
+constexpr int FOUND_HERE = 4096, FOUND_ENTRIES = 12288;
 template <class T, bool FEW>
 __global__ __launch_bounds__(256)
 void loss_gather_kernel(GatherArgs p)
@@ -197,19 +197,22 @@ void loss_gather_kernel(GatherArgs p)
             ((u32x4 *)some)[threadIdx.x] = u32x4{};            // (16 rows a thread)
             __syncthreads();
             const int n = p.rows * p.t.k;
-            int id[FOUND_ENTRIES / 256];
-            float logit[FOUND_ENTRIES / 256];
+            constexpr int EACH = 16;
+            for (int e0 = 0; e0 < n; e0 += 256 * EACH) {
+                int id[EACH];
+                float logit[EACH];
 #pragma unroll
-            for (int i = 0; i < FOUND_ENTRIES / 256; ++i) {
-                if (256 * i >= n) continue;
-                const int e = min(256 * i + (int)threadIdx.x, n - 1);
-                id[i] = p.t.ids[e];
-                logit[i] = p.t.logits[e];
-            }
+                for (int i = 0; i < EACH; ++i) {
+                    if (e0 + 256 * i >= n) continue;
+                    const int e = min(e0 + 256 * i + (int)threadIdx.x, n - 1);
+                    id[i] = p.t.ids[e];
+                    logit[i] = p.t.logits[e];
+                }
 #pragma unroll
-            for (int i = 0; i < FOUND_ENTRIES / 256; ++i) {
-                const int e = 256 * i + threadIdx.x;
-                if (e < n && listed(id[i], p.V) && !(logit[i] == -INFINITY)) some[(uint32_t)e / (uint32_t)p.t.k] = 1;
+                for (int i = 0; i < EACH; ++i) {
+                    const int e = e0 + 256 * i + threadIdx.x;
+                    if (e < n && listed(id[i], p.V) && !(logit[i] == -INFINITY)) some[(uint32_t)e / (uint32_t)p.t.k] = 1;
+                }
             }
             __syncthreads();
         }
@@ -642,7 +645,7 @@ int launch_rows(const Vocab &v, const LossPlan &plan, const Rows16 &x, int64_t r
                 int64_t lddx, float *loss, float *lse_out, float *picked, char *ws, hipStream_t s)
 {
     // (a launch costs some 4.5 us in a row of dependent ones, a list of 11 tokens 2 us more in the other)
-    uint8_t *const flags = t.k && (!dloss || rows * t.k > 16384) ? (uint8_t *)(ws + plan.flags) : nullptr;
+    uint8_t *const flags = t.k && (!dloss || rows * t.k > FOUND_ENTRIES) ? (uint8_t *)(ws + plan.flags) : nullptr;
     LossHead *const head = (LossHead *)ws;
     int *const list = (int *)(ws + plan.list), *const place = (int *)(ws + plan.place);
     const unsigned blocks = (unsigned)((rows + 3) / 4);

@@ -330,9 +330,17 @@ __device__ inline void tile_at(const TilesArgs &p, const Place at, const int N, 
             const int64_t of_row = (int64_t)t * p.k;
             if (p.start || p.k == 1) take(token[j], of_row + from[j], share[j]);
             if (p.start) {
-                for (int n = from[j] + 1; __any(n < to[j]); ++n) {
-                    const bool some = n < to[j];
-                    take(some ? p.ids[of_row + n] : -1, of_row + n, KIND == PROBS && some ? p.q[of_row + n] : 0.0f);
+                for (int n0 = from[j] + 1; __any(n0 < to[j]); n0 += 4) {
+                    int next[4];
+                    float shares[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const bool some = n0 + u < to[j];
+                        next[u] = some ? p.ids[of_row + n0 + u] : -1;
+                        shares[u] = KIND == PROBS && some ? p.q[of_row + n0 + u] : 0.0f;
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) take(next[u], of_row + n0 + u, shares[u]);
                 }
             } else if constexpr (KIND == STATS)
                 if (p.k > 1) {

@@ -218,7 +218,7 @@ def test_cross_entropy(rows, V, C, dtype):
     # long lists in each form of tiles
     (16, 20000, 72, BF, 256, 1.0), (276, 317, 72, HF, 103, 2.0), (100, 20000, 72, BF, 65, 1.0), (600, 20001, 72, HF, 130, 2.0),
     # lists that every workgroup looks over, and more
-    (512, 500, 72, BF, 8, 2.0), (241, 500, 72, HF, 17, 1.0), (4096, 300, 40, BF, 1, 1.0), (4097, 300, 40, HF, 1, 1.0)])
+    (512, 500, 72, BF, 24, 2.0), (513, 500, 72, HF, 24, 1.0), (241, 500, 72, HF, 17, 1.0), (4096, 300, 40, BF, 1, 1.0), (4097, 300, 40, HF, 1, 1.0)])
 def test_distillation(rows, V, C, dtype, k, temperature):
     check_loss(rows, V, C, dtype, k=k, temperature=temperature, strided=rows % 2 == 1)
 
