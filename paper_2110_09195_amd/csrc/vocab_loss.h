@@ -57,6 +57,9 @@ enum { TILE_256, TILE_128, TILE_128_DEEP, TILE_64, TILE_FORMS };
 inline int tile_edge(int form) { return form == TILE_256 ? 256 : form == TILE_64 ? 64 : 128; }
 inline int tile_slots(int form) { return form == TILE_128 || form == TILE_64 ? 512 : 256; }
 
+// The last rows in a tile of 256, if they are no more than these, are taken in a narrow one.
+constexpr int NARROW_ROWS = 64;
+
 // How many parts the contracted axes of ROWS and TABLE are cut into: of 1 .. MOST_SPLITS each those that take the least time, in steps of a tile: the workgroups'
 // steps and what a tile costs beside them, shared out over the chip, and the writing and joining of the parts.
 constexpr int MOST_SPLITS = 64;

@@ -531,6 +531,11 @@ int64_t tiles_of(int form, int64_t m, int64_t n) { return (m + tile_edge(form) -
 //   100 rows,   131072 of 4096          246    187    193    298
 //   4000 rows,  20000 of 640            121    146    197    245
 //   2000 rows,  65536 of 2048           425    524    624    855
+// and where all rows lie in the narrow tile (from memory, tables in turn):
+//   1 row,      32768 of 2048          39.6   41.6   39.1   37.4
+//   1 row,      131072 of 4096          178    187    182    180
+//   64 rows,    50021 of 2056          57.1   66.1   65.4   73.9
+//   33 rows,    131072 of 2048          126    136    129    125
 constexpr float TURN[] = {1.0f, 0.68f, 0.46f, 0.35f}, HALF[] = {1.0f, 0.55f, 0.46f, 0.22f};           // (no CU with two)
 int logits_form(int64_t tokens, int64_t rows)
 {
@@ -538,7 +543,8 @@ int logits_form(int64_t tokens, int64_t rows)
     float least = 0.0f;
     for (int f = 0; f < TILE_FORMS; ++f) {
         const int64_t tiles = tiles_of(f, tokens, rows);
-        const float cost = tiles <= 256 ? HALF[f] : TURN[f] * (float)((tiles + tile_slots(f) - 1) / tile_slots(f));
+        float cost = tiles <= 256 ? HALF[f] : TURN[f] * (float)((tiles + tile_slots(f) - 1) / tile_slots(f));
+        if (f == TILE_256 && rows <= NARROW_ROWS) cost *= 0.66f;
         if (f == 0 || cost < least) {
             best = f;
             least = cost;

@@ -134,7 +134,7 @@ __device__ inline bool find_place(uint32_t block, int tm, int tn, int splits, Pl
 // (1.29 - 1.39 PFLOP/s, 65 % of cycles busy at 2.0 GHz), PROBS 6.4 - 7.0, ROWS 6.7 - 7.0, TABLE 6.4 - 6.6, these two together 13.2; library products of these sizes, which
 // do nothing else, 5.85 for logits, 6.5 and 7.3 for the gradients.  A step of a 256 x 256 tile takes 1.5 us; what comes before a tile's first and after its last, some 6 us (half of them
 // exponentials), nothing hides: with 2048 channels, 32 steps, STATS of 3686 rows of 65536 tokens 0.85 ms, the library's product 0.75.
-// For few rows memory bounds STATS: one row against 131072 tokens of 4096 channels 182 us, 5.9 TB/s.
+// For few rows memory bounds STATS: one row against 131072 tokens of 4096 channels 178 us, 6.0 TB/s.
 // A tile of 256 x 256 reads half of what four of 128 x 128 do, and is the faster where there are enough; smaller ones are for fewer rows (logits_form,
 // gradient_cuts).
 template <class T, int KIND, int BM, int BN, int WM, int WN, int STAGES>
@@ -489,7 +489,7 @@ __device__ inline void tile(const TilesArgs &p, const uint32_t block)
     }
     const int m0 = at.m * BM, n0 = at.n * BN;
     if constexpr (BN == 256 && KIND != TABLE) {
-        if (N - n0 <= 64) return tile_at<T, KIND, BM, 64, 32, 64, 4>(p, at, N, K, first, steps, splits, m0, n0);
+        if (N - n0 <= NARROW_ROWS) return tile_at<T, KIND, BM, NARROW_ROWS, 32, 64, 4>(p, at, N, K, first, steps, splits, m0, n0);
     }
     tile_at<T, KIND, BM, BN, WM, WN, STAGES>(p, at, N, K, first, steps, splits, m0, n0);
 }
