@@ -75,7 +75,7 @@ def test_rows_of_no_token_are_zeros_whatever_the_scale():
     (1, 1, 8, BF, 1), (1, 300, 520, HF, 1), (31, 5, 72, BF, 1), (32, 1, 1032, HF, 1), (33, 2, 8, BF, 1), (64, 64, 512, HF, 1), (257, 9, 520, BF, 3),
     (1000, 70000, 136, BF, 1), (5000, 301, 1032, HF, 3), (16384, 1500, 264, BF, 2), (16385, 1500, 264, HF, 2), (40000, 255, 72, BF, 2),
     (40000, 256, 72, HF, 1), (40001, 70001, 40, BF, 4), (2048, 300, 72, HF, 2), (2049, 300, 72, BF, 2), (65536, 999, 16, BF, 2),
-    (65537, 999, 16, HF, 2)])
+    (65537, 999, 16, HF, 2), (70, 9, 65536, BF, 1)])
 def test_gradient_of_the_table(rows, V, C, dtype, skew, accumulate):
     g = gen(rows + V)
     ids = (torch.rand(rows, generator=g, device="cuda") ** skew * (V + 3)).long().sub(1).int()             # -1, 0 .. V - 1, V, V + 1
@@ -203,7 +203,7 @@ SIZES = [(1, 1, 8, BF), (1, 2, 8, HF), (1, 129, 72, BF), (2, 1000, 264, HF), (7,
          (128, 257, 1032, HF), (129, 300, 72, BF), (200, 2000, 2056, HF), (333, 5003, 264, BF), (700, 1024, 512, HF),
          # each form of tiles, sums over rows and over tokens in parts, rows that every workgroup looks over and those that one does
          (100, 20000, 72, BF), (160, 20001, 40, HF), (400, 20000, 72, BF), (2000, 300, 264, HF), (1024, 700, 72, BF), (1025, 700, 72, HF), (64, 9000, 4096, BF),
-         (4096, 700, 72, BF), (4097, 700, 72, HF)]
+         (4096, 700, 72, BF), (4097, 700, 72, HF), (5, 300, 65536, BF)]
 
 
 @pytest.mark.parametrize("rows, V, C, dtype", SIZES)
@@ -472,6 +472,37 @@ def test_calls_at_once_on_two_streams():
                 got.append((job(), want))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for out, want in got for a, b in zip(out, want))
+
+
+def test_many_rows_and_many_tokens():
+    """Hundreds of thousands of rows, of which few count, against a small vocabulary; a vocabulary of the largest size, and its gradient from more rows than are
+    merged."""
+    g, rows, V, C = gen(13), 300001, 501, 40
+    x, table = normal(g, rows, C).to(BF), (normal(g, V, C) * 0.3).to(BF)
+    target = torch.randint(0, V, (rows,), generator=g, device="cuda")
+    target = torch.where(torch.rand(rows, generator=g, device="cuda") < 0.9, -1, target)
+    desc, dloss = B.make_vocab_desc(V, C), torch.rand(rows, generator=g, device="cuda")
+    some = target >= 0
+    want = Loss(x[some], table, target[some].int(), None, 1.0, dloss[some])
+    loss, lse = B.snn_cross_entropy_forward(desc, x, table, target.int())
+    within(loss[some], want.loss, want.loss_error, "loss")
+    assert not loss[~some].any()
+    dx, dw = B.snn_cross_entropy_backward(desc, x, table, target.int(), lse, dloss)
+    within(dx[some], want.dx, want.dx_error, "dx")
+    assert not dx[~some].any()
+    within(dw, want.dw, want.dw_error, "dtable")
+
+    V, C, rows = 1 << 24, 8, 70001
+    desc, ids = B.make_vocab_desc(V, C, CODE[HF]), torch.randint(0, V, (rows,), generator=g, device="cuda")
+    ids[:2000], ids[2000], ids[2001] = V - 1, 0, V - 2
+    dy = normal(g, rows, C).to(HF)
+    got = B.snn_embedding_grad(desc, dy, ids.int())
+    tokens, inverse = torch.unique(ids, return_inverse=True)
+    total, magnitude, n = by_token(dy, inverse, len(tokens))
+    within(got[tokens], total, UNIT[HF] * total.abs() + (n[:, None] + 3) * F32 * magnitude + TINY[HF], "dtable")
+    got[tokens] = 0
+    assert not got.any()
+    assert torch.equal(B.snn_embedding_forward(desc, got, ids.int()), torch.zeros_like(dy))
 
 
 def test_offsets_past_32_bits():
